@@ -1,0 +1,213 @@
+// C ABI of the attention operators: argument checks on the host, then launches.
+#include "fc_attn_internal.hpp"
+#include <math.h>
+
+using namespace fc;
+
+namespace {
+
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// Fields that describe the cache.
+int32_t check_cache(const fc_attention_desc *d)
+{
+    if (!d) return FC_ERR_NULL;
+    if (d->blocks <= 0 || d->kv_heads <= 0 || d->head_dim <= 0 || d->head_dim > FC_KV_MAX_HEAD_DIM) return FC_ERR_SHAPE;
+    if ((int64_t)d->blocks * d->kv_heads >= INT32_MAX) return FC_ERR_RANGE;
+    return FC_OK;
+}
+
+// Those and the sequences.
+int32_t make_kv_geom(const fc_attention_desc *d, const void *cache, const int32_t *table, const int32_t *lengths, const int32_t *starts, KvGeom *g)
+{
+    const int32_t rc = check_cache(d);
+    if (rc != FC_OK) return rc;
+    if (d->batch <= 0 || d->tokens < 0 || d->max_new <= 0 || d->max_len <= 0 || d->table_width <= 0) return FC_ERR_SHAPE;
+    if (d->flags & ~(uint32_t)FC_CAUSAL || d->reserved) return FC_ERR_DTYPE;
+    // (one dimension of a grid)
+    if (d->batch > 65535 || d->kv_heads > 65535) return FC_ERR_RANGE;
+    if (!starts && (int64_t)d->batch * d->max_new != d->tokens) return FC_ERR_SHAPE;
+    const KvLayout l = kv_layout(d->blocks, d->kv_heads, d->head_dim);
+    uint8_t *const base = static_cast<uint8_t *>(const_cast<void *>(cache));
+    g->blocks = d->blocks; g->kv_heads = d->kv_heads; g->d = d->head_dim; g->dp = padded_dim(d->head_dim);
+    g->batch = d->batch; g->tokens = d->tokens; g->max_new = d->max_new; g->width = d->table_width;
+    const int64_t held = (int64_t)d->table_width * kBlock;
+    g->max_len = held < d->max_len ? (int32_t)held : d->max_len;
+    g->codes = base;
+    g->scales = reinterpret_cast<float2 *>(base + l.scales);
+    g->sketches = reinterpret_cast<int8_t *>(base + l.sketches);
+    g->weights = reinterpret_cast<float *>(base + l.weights);
+    g->table = table; g->lengths = lengths; g->starts = starts;
+    return FC_OK;
+}
+
+int32_t check_pointers(const void *cache, const int32_t *table, const int32_t *lengths, const int32_t *starts)
+{
+    if (!cache || !table || !lengths) return FC_ERR_NULL;
+    if (!aligned(cache, 16) || !aligned(table, 16) || !aligned(lengths, 16) || (starts && !aligned(starts, 16))) return FC_ERR_ALIGN;
+    return FC_OK;
+}
+
+// Are rows of `d` channels with these strides whole 16-byte pieces?
+bool wide_rows(const void *p, int64_t row, int64_t head, int32_t d) { return aligned(p, 16) && row % 8 == 0 && head % 8 == 0 && d % 8 == 0; }
+
+bool known_type(int32_t dtype) { return dtype == FC_BF16 || dtype == FC_F16; }
+
+// How a call's rows and blocks are cut.
+struct Plan {
+    int32_t rows_tile, tiles, splits, per_split;
+    size_t workspace;
+};
+
+// Pieces of the long axis: enough workgroups to fill the chip, no fewer than four blocks a piece (one a wave).
+constexpr int64_t kWorkgroups = 1024;
+
+int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *p)
+{
+    if (d->heads <= 0 || d->heads % d->kv_heads) return FC_ERR_SHAPE;
+    if (!known_type(d->dtype)) return FC_ERR_DTYPE;
+    if (!isfinite(d->scale) || d->q_row < 0 || d->q_head < 0) return FC_ERR_SHAPE;
+    const int32_t group = d->heads / d->kv_heads;
+    if ((int64_t)d->tokens * d->heads >= INT32_MAX || (int64_t)d->max_new * group >= INT32_MAX / 2) return FC_ERR_RANGE;
+    const int64_t rows = (int64_t)d->max_new * group;
+    int32_t blocks = (g.max_len + kBlock - 1) / kBlock;
+    if (list) {
+        if (d->first < 0 || d->last < 1 || d->top < 0 || d->first > FC_MAX_SELECTED || d->last > FC_MAX_SELECTED || d->top > FC_MAX_SELECTED ||
+            d->first + d->last + d->top > FC_MAX_SELECTED)
+            return FC_ERR_SHAPE;
+        if (blocks > kSelectMaxBlocks) return FC_ERR_RANGE;
+        blocks = blocks < d->first + d->last + d->top ? blocks : d->first + d->last + d->top;
+        p->rows_tile = 16;
+        p->tiles = d->max_new * ((group + 15) / 16);
+        if ((int64_t)d->max_new * ((group + 15) / 16) >= INT32_MAX) return FC_ERR_RANGE;
+    } else {
+        p->rows_tile = rows <= 16 || g.dp > 128 ? 16 : 32;      // (32 rows of more channels do not fit the registers)
+        p->tiles = (int32_t)((rows + p->rows_tile - 1) / p->rows_tile);
+    }
+    const int64_t units = (int64_t)d->batch * d->kv_heads * p->tiles;
+    int64_t splits = (kWorkgroups + units - 1) / units;
+    const int64_t most = (blocks + 3) / 4;
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    const int64_t per = ((blocks + splits - 1) / splits + 3) / 4 * 4;
+    p->per_split = (int32_t)per;
+    p->splits = (int32_t)((blocks + per - 1) / per);
+    if (units * p->splits >= INT32_MAX || units * p->rows_tile >= INT32_MAX) return FC_ERR_RANGE;
+    p->workspace = p->splits == 1 ? 0 : (size_t)units * p->splits * p->rows_tile * (g.dp * sizeof(float) + sizeof(float2));
+    return FC_OK;
+}
+
+int32_t workspace_bytes(const fc_attention_desc *d, bool list, size_t *bytes)
+{
+    KvGeom g;
+    Plan p;
+    if (!bytes) return FC_ERR_NULL;
+    // (whether rows are counted by starts does not matter here)
+    const int32_t dummy = 0;
+    int32_t rc = make_kv_geom(d, nullptr, nullptr, nullptr, &dummy, &g);
+    if (rc == FC_OK) rc = make_plan(d, g, list, &p);
+    if (rc == FC_OK) *bytes = p.workspace;
+    return rc;
+}
+
+int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, const int32_t *table, const int32_t *lengths, const int32_t *starts,
+               void *out, float *lse, int32_t *selected, bool list, void *workspace, size_t workspace_bytes, void *stream)
+{
+    KvGeom g;
+    Plan p;
+    int32_t rc = make_kv_geom(d, cache, table, lengths, starts, &g);
+    if (rc == FC_OK) rc = make_plan(d, g, list, &p);
+    if (rc != FC_OK) return rc;
+    if (d->tokens == 0) return FC_OK;
+    rc = check_pointers(cache, table, lengths, starts);
+    if (rc != FC_OK) return rc;
+    if (!q || !out || (list && !selected)) return FC_ERR_NULL;
+    if (!aligned(q, 2) || !aligned(out, 16) || (lse && !aligned(lse, 16)) || (list && !aligned(selected, 16))) return FC_ERR_ALIGN;
+    if (p.workspace) {
+        if (!workspace || workspace_bytes < p.workspace) return FC_ERR_WORKSPACE;
+        if (!aligned(workspace, 16)) return FC_ERR_ALIGN;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    AttnArgs a;
+    a.kv = g;
+    a.q = static_cast<const uint16_t *>(q);
+    a.q_row = d->q_row; a.q_head = d->q_head;
+    a.out = static_cast<uint16_t *>(out);
+    a.lse = lse;
+    a.heads = d->heads; a.group = d->heads / d->kv_heads;
+    a.causal = list || (d->flags & FC_CAUSAL);
+    a.wide = wide_rows(q, d->q_row, d->q_head, d->head_dim);
+    a.scale_log2 = d->scale * 1.44269504088896f;
+    a.div_group = make_fastdiv((uint32_t)a.group);
+    a.selected = list ? selected : nullptr;
+    a.selected_width = d->first + d->last + d->top;
+    a.tiles = p.tiles; a.splits = p.splits; a.per_split = p.per_split;
+    a.part_out = static_cast<float *>(workspace);
+    a.part_ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) +
+                                           (size_t)d->batch * d->kv_heads * p.tiles * p.splits * p.rows_tile * g.dp * sizeof(float));
+    if (list && launch_select(g, d->dtype, a.q, d->q_row, d->q_head, d->heads, a.wide, d->first, d->last, d->top, selected, s) != hipSuccess)
+        return FC_ERR_HIP;
+    return launch_attend_rows(a, d->dtype, p.rows_tile, s) == hipSuccess ? FC_OK : FC_ERR_HIP;
+}
+
+} // namespace
+
+extern "C" {
+
+int32_t fc_kv_cache_bytes(const fc_attention_desc *d, size_t *bytes)
+{
+    const int32_t rc = check_cache(d);
+    if (rc != FC_OK) return rc;
+    if (!bytes) return FC_ERR_NULL;
+    *bytes = kv_layout(d->blocks, d->kv_heads, d->head_dim).bytes;
+    return FC_OK;
+}
+
+int32_t fc_kv_append(const fc_attention_desc *d, void *cache, const void *k, const void *v, const int32_t *table, const int32_t *lengths,
+                     const int32_t *starts, void *stream)
+{
+    KvGeom g;
+    int32_t rc = make_kv_geom(d, cache, table, lengths, starts, &g);
+    if (rc != FC_OK) return rc;
+    if (!known_type(d->dtype)) return FC_ERR_DTYPE;
+    if (d->k_row < 0 || d->k_head < 0 || d->v_row < 0 || d->v_head < 0) return FC_ERR_SHAPE;
+    if (d->tokens == 0) return FC_OK;
+    rc = check_pointers(cache, table, lengths, starts);
+    if (rc != FC_OK) return rc;
+    if (!k || !v) return FC_ERR_NULL;
+    if (!aligned(k, 2) || !aligned(v, 2)) return FC_ERR_ALIGN;
+    return launch_kv_append(g, d->dtype, static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), d->k_row, d->k_head, d->v_row, d->v_head,
+                            wide_rows(k, d->k_row, d->k_head, d->head_dim), wide_rows(v, d->v_row, d->v_head, d->head_dim),
+                            static_cast<hipStream_t>(stream)) == hipSuccess ? FC_OK : FC_ERR_HIP;
+}
+
+int32_t fc_kv_read(const fc_attention_desc *d, const void *cache, const int32_t *table, const int32_t *lengths, const int32_t *starts, float *k,
+                   float *v, void *stream)
+{
+    KvGeom g;
+    int32_t rc = make_kv_geom(d, cache, table, lengths, starts, &g);
+    if (rc != FC_OK) return rc;
+    if (d->tokens == 0) return FC_OK;
+    rc = check_pointers(cache, table, lengths, starts);
+    if (rc != FC_OK) return rc;
+    if (!k && !v) return FC_ERR_NULL;
+    if (!aligned(k, 16) || !aligned(v, 16)) return FC_ERR_ALIGN;
+    return launch_kv_read(g, k, v, static_cast<hipStream_t>(stream)) == hipSuccess ? FC_OK : FC_ERR_HIP;
+}
+
+int32_t fc_cache_attention_workspace_bytes(const fc_attention_desc *d, size_t *bytes) { return workspace_bytes(d, false, bytes); }
+int32_t fc_focused_attention_workspace_bytes(const fc_attention_desc *d, size_t *bytes) { return workspace_bytes(d, true, bytes); }
+
+int32_t fc_cache_attention(const fc_attention_desc *d, const void *cache, const void *q, const int32_t *table, const int32_t *lengths,
+                           const int32_t *starts, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return attend(d, cache, q, table, lengths, starts, out, lse, nullptr, false, workspace, workspace_bytes, stream);
+}
+
+int32_t fc_focused_attention(const fc_attention_desc *d, const void *cache, const void *q, const int32_t *table, const int32_t *lengths,
+                             const int32_t *starts, void *out, float *lse, int32_t *selected, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return attend(d, cache, q, table, lengths, starts, out, lse, selected, true, workspace, workspace_bytes, stream);
+}
+
+} // extern "C"

@@ -1,0 +1,216 @@
+// Declarations shared by the attention operators' translation units: the cache's layout, what a sequence's arrays say, conversions.
+//
+// Layout of the cache.  A unit is one block of one key/value head: unit = pool block * kv_heads + head.
+//   codes    [unit][128 * dp] bytes: keys [64 tokens][dp], then values [dp][64 places]; dp = head_dim rounded up to a multiple of 64, zeros behind
+//   scales   [unit] of two floats: the keys' scale; the values', negative where a value of the block is NaN
+//   sketches [unit][dp] signed bytes, weights [unit] floats
+// Everything that a wave reads of a unit is then in one piece: the matrix instructions' own order.  A lane of the 16x16 instructions
+// holds eight consecutive places of the reduction, lanes 16 apart the next eight (g = lane / 16):
+//   scores S^T = K q^T: a lane's rows are tokens, and sixteen channels 64 c + 16 g .. + 15 of one token make its share of two
+//     instructions; a load of 16 bytes a lane reads 64-byte pieces of 16 tokens.
+//   out^T = V^T P^T: P^T comes out of the first product with tokens 4 g + i of each 16 (i = 0 .. 3) in the lane that needs them as
+//     operand, so no weight moves between lanes if V's rows are held in that order too: token 32 h + 16 k + 4 g + i is at place
+//     16 g + 8 h + 4 k + i of its row, and 16 bytes a lane, 1 KB a wave in one piece, are its share for a whole block.
+#pragma once
+#include <atomic>
+#include "fc_mfma_util.hpp"
+#include "focused_attention.h"
+
+namespace fc {
+
+constexpr int kBlock = FC_KV_BLOCK;
+
+struct KvGeom {
+    int32_t blocks, kv_heads, d, dp;
+    int32_t batch, tokens, max_new, max_len, width;
+    uint8_t *codes;
+    float2 *scales;
+    int8_t *sketches;
+    float *weights;
+    const int32_t *table, *lengths, *starts;
+};
+
+static inline int32_t padded_dim(int32_t d) { return (d + 63) / 64 * 64; }
+
+// Byte offsets of the cache's sections and its size.
+struct KvLayout {
+    size_t scales, sketches, weights, bytes;
+};
+static inline KvLayout kv_layout(int32_t blocks, int32_t kv_heads, int32_t head_dim)
+{
+    const size_t units = (size_t)blocks * (size_t)kv_heads, dp = (size_t)padded_dim(head_dim);
+    KvLayout l;
+    l.scales = units * 2 * kBlock * dp;
+    l.sketches = l.scales + align_up(units * sizeof(float2), 256);
+    l.weights = l.sketches + align_up(units * dp, 256);
+    l.bytes = l.weights + align_up(units * sizeof(float), 256);
+    return l;
+}
+
+// A sequence as its arrays describe it, cut to the call's bounds: rows row0 .. row0 + n - 1 are its new tokens, row0 has position pos0
+// (negative: rows without a position come first).
+struct Sequence {
+    int32_t len, n, row0, pos0;
+};
+__device__ __forceinline__ Sequence sequence_of(const KvGeom &g, int b)
+{
+    Sequence s;
+    s.len = min(max(g.lengths[b], 0), g.max_len);
+    if (g.starts) {
+        const int32_t from = min(max(g.starts[b], 0), g.tokens), to = min(max(g.starts[b + 1], from), g.tokens);
+        s.row0 = from;
+        s.n = min(to - from, g.max_new);
+    } else {
+        s.row0 = b * g.max_new;
+        s.n = g.max_new;
+    }
+    s.pos0 = s.len - s.n;
+    return s;
+}
+
+// The pool's number of a sequence's block, -1: not there.  (block < width: lengths are cut to the table on the host.)
+__device__ __forceinline__ int32_t pool_block(const KvGeom &g, int b, int block)
+{
+    const int32_t p = g.table[(int64_t)b * g.width + block];
+    return (uint32_t)p < (uint32_t)g.blocks ? p : -1;
+}
+
+__device__ __forceinline__ int64_t unit_of(const KvGeom &g, int32_t pool, int head) { return (int64_t)pool * g.kv_heads + head; }
+
+// Where a token of its block is in a row of values.
+__host__ __device__ __forceinline__ int value_place(int token)
+{
+    return (token >> 2 & 3) << 4 | (token >> 5) << 3 | (token >> 4 & 1) << 2 | (token & 3);
+}
+
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4_t;
+
+// Eight codes -> eight 16-bit floats, exact in both types (3 bits behind the point, 2^-9 .. 448).
+template <int DT> __device__ __forceinline__ uint4 codes_to_16(uint32_t lo, uint32_t hi)
+{
+    uint4 r;
+    if constexpr (DT == FC_BF16) {
+        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
+        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
+        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
+        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
+    } else {
+        r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false));
+        r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true));
+        r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false));
+        r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
+    }
+    return r;
+}
+
+template <int DT> __device__ __forceinline__ f32x4_t mfma16(const uint4 &a, const uint4 &b, const f32x4_t &c)
+{
+    if constexpr (DT == FC_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
+template <int DT> __device__ __forceinline__ float bits_to_float(uint16_t v)
+{
+    if constexpr (DT == FC_BF16) return to_float(bf16_t{v});
+    else return to_float(f16_t{v});
+}
+template <int DT> __device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    const f32x2_t v = {a, b};
+    if constexpr (DT == FC_BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
+}
+
+// Eight elements c .. c + 7 of a row of d, zeros behind its end.  wide: 16 bytes lie together (d a multiple of 8, the row 16-byte aligned).
+__device__ __forceinline__ uint4 load8(const uint16_t *__restrict__ row, int c, int d, bool wide)
+{
+    if (wide) return c < d ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0, 0, 0, 0);
+    uint32_t v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = c + 2 * j < d ? row[c + 2 * j] : 0, hi = c + 2 * j + 1 < d ? row[c + 2 * j + 1] : 0;
+        v[j] = lo | hi << 16;
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+__device__ __forceinline__ float pow2_of(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // -126 <= e <= 127
+
+// The least e with a <= limit * 2^e for a >= 0 that is not infinite; limit_bits: the fraction of the limit, limit_e its exponent.
+// (a = 1.f 2^x: x - limit_e, one more where a's fraction is above the limit's.  Subnormals count as zero: far below every bound on e.)
+__device__ __forceinline__ int least_exponent(float a, uint32_t limit_fraction, int limit_e)
+{
+    const uint32_t u = __float_as_uint(a);
+    return (int)(u >> 23) - 127 - limit_e + ((u & 0x7fffffu) > limit_fraction ? 1 : 0);
+}
+// 448 = 1.75 * 2^8, 127 = 1.984375 * 2^6
+__device__ __forceinline__ int scale_exponent(float amax) { return min(max(least_exponent(amax, 0x600000u, 8), -64), 120); }
+__device__ __forceinline__ int unit_exponent(float amax) { return min(max(least_exponent(amax, 0x7e0000u, 6), -126), 120); }
+
+struct AttnArgs {
+    KvGeom kv;
+    const uint16_t *q;
+    int64_t q_row, q_head;
+    uint16_t *out;
+    float *lse;
+    const int32_t *selected;    // (list form)
+    int32_t selected_width;
+    int32_t heads, group, causal;
+    int32_t wide;               // q's rows are 16-byte pieces
+    float scale_log2;           // scale * log2(e)
+    FastDiv div_group;
+    int32_t tiles;              // row tiles of a sequence and key head
+    int32_t splits, per_split;  // pieces of the long axis and a piece's blocks
+    float *part_out;            // [unit of rows][split][rows][dp], not yet divided
+    float2 *part_ml;            // [unit of rows][split][rows]: running maximum (base 2) and sum
+};
+
+// Four channels c .. c + 3 of a finished row (head `row` of the output's tokens x heads), not yet divided by the sum of the weights.
+template <int DT> __device__ __forceinline__ void finish_row(const AttnArgs &a, int64_t row, int c, f32x4_t sum, float most, float total)
+{
+    if (a.lse && c == 0) a.lse[row] = total == 0.f ? -__builtin_inff() : (most + __builtin_amdgcn_logf(total)) * 0.693147180559945f;
+    const int d = a.kv.d;
+    if (c >= d) return;
+    const float inverse = total == 0.f ? 0.f : 1.f / total;     // (nothing to attend to: the sum is zero)
+    const uint32_t lo = pack2<DT>(sum[0] * inverse, sum[1] * inverse), hi = pack2<DT>(sum[2] * inverse, sum[3] * inverse);
+    uint16_t *const to = a.out + row * d + c;
+    if ((d & 3) == 0) {
+        *reinterpret_cast<uint2 *>(to) = make_uint2(lo, hi);
+    } else {
+        const uint16_t v[4] = {(uint16_t)lo, (uint16_t)(lo >> 16), (uint16_t)hi, (uint16_t)(hi >> 16)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < d) to[i] = v[i];
+    }
+}
+
+// Raises a kernel's limit of dynamic LDS, once per device.
+template <auto KERNEL> hipError_t raise_lds(size_t bytes)
+{
+    static std::atomic<uint64_t> raised{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (raised.load(std::memory_order_acquire) & bit) return hipSuccess;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess) raised.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
+hipError_t launch_kv_append(const KvGeom &g, int dtype, const uint16_t *k, const uint16_t *v, int64_t k_row, int64_t k_head, int64_t v_row,
+                            int64_t v_head, bool wide_k, bool wide_v, hipStream_t s);
+hipError_t launch_kv_read(const KvGeom &g, float *k, float *v, hipStream_t s);
+
+// Few rows or a list of blocks (see fc_attn_rows.hip); rows_tile: rows a workgroup holds.
+hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s);
+
+// The selection (see fc_attn_select.hip).
+constexpr int kSelectMaxBlocks = 32768;     // blocks of a sequence whose scores fit LDS
+hipError_t launch_select(const KvGeom &g, int dtype, const uint16_t *q, int64_t q_row, int64_t q_head, int heads, bool wide, int first, int last,
+                         int top, int32_t *selected, hipStream_t s);
+
+} // namespace fc

@@ -1,0 +1,298 @@
+// The key/value cache in 8 bits: appending tokens and reading them back.
+//
+// A workgroup takes one block of one head that new tokens of a sequence fall into: it reads their rows, finds the largest magnitude,
+// makes the scale, and writes codes.  Both are bound by memory: 4 bytes read and 2 written a channel of a token.
+#include "fc_attn_internal.hpp"
+
+namespace fc {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct AppendArgs {
+    KvGeom kv;
+    const uint16_t *k, *v;
+    int64_t k_row, k_head, v_row, v_head;
+    int32_t wide_k, wide_v;
+};
+
+// Four codes under another scale; ratio = old scale / new scale, a power of two.
+__device__ __forceinline__ uint32_t rescale4(uint32_t c, float ratio)
+{
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(c, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8(c, 1) * ratio, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(c, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8(c, 3) * ratio, r, true);
+}
+
+// A value in units of its scale; what is not finite becomes NaN.
+__device__ __forceinline__ float code_of(float v, float inverse)
+{
+    v *= inverse;
+    return __builtin_fabsf(v) <= 448.f ? v : __builtin_nanf("");
+}
+
+__device__ __forceinline__ float max_over_workgroup(float v, float *scratch)
+{
+#pragma unroll
+    for (int m = 32; m; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = fmaxf(fmaxf(scratch[0], scratch[1]), fmaxf(scratch[2], scratch[3]));
+    __syncthreads();
+    return v;
+}
+
+// Largest finite magnitude of eight 16-bit floats.
+template <int DT> __device__ __forceinline__ float finite_amax(const uint4 &x, float so_far)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float a = __builtin_fabsf(bits_to_float<DT>((uint16_t)(w[j >> 1] >> (16 * (j & 1)))));
+        so_far = a < __builtin_inff() ? fmaxf(so_far, a) : so_far;
+    }
+    return so_far;
+}
+
+// A thread holds channels 8 c .. 8 c + 7 of four consecutive tokens 4 r .. 4 r + 3 at a time: four tokens are one word of a row of values.
+template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a)
+{
+    constexpr int kChunks = DP / 8, kRows = kThreads / kChunks * 4, kRounds = (kBlock + kRows - 1) / kRows;
+    constexpr int kPitch = 17;      // words of a row of values in LDS
+    __shared__ float scratch[4];
+    __shared__ uint32_t turned[DP * kPitch];
+    __shared__ int sums[DP];
+    const KvGeom &g = a.kv;
+    const int b = blockIdx.z, h = blockIdx.y;
+    const Sequence s = sequence_of(g, b);
+    const int from = max(s.pos0, 0);                        // first new position
+    const int block = from / kBlock + (int)blockIdx.x;
+    const int at = block * kBlock;
+    if (at >= s.len || from >= s.len) return;
+    const int32_t pool = pool_block(g, b, block);
+    if (pool < 0) return;
+    const int old = min(max(from - at, 0), kBlock), end = min(s.len - at, kBlock);    // new tokens of the block: old .. end - 1
+    const int64_t unit = unit_of(g, pool, h);
+    uint8_t *const kc = g.codes + unit * (2 * kBlock * DP), *const vc = kc + kBlock * DP;
+    const int c = threadIdx.x % kChunks, r = threadIdx.x / kChunks;
+
+    uint4 kx[kRounds][4], vx[kRounds][4];
+    float ka = 0.f, va = 0.f;
+    bool strange = false;
+#pragma unroll
+    for (int round = 0; round < kRounds; ++round)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = round * kRows + 4 * r + j;
+            kx[round][j] = vx[round][j] = make_uint4(0, 0, 0, 0);
+            if (4 * r < kRows && t >= old && t < end) {
+                const int64_t row = s.row0 + (at + t - s.pos0);
+                kx[round][j] = load8(a.k + row * a.k_row + h * a.k_head, 8 * c, g.d, a.wide_k);
+                vx[round][j] = load8(a.v + row * a.v_row + h * a.v_head, 8 * c, g.d, a.wide_v);
+            }
+        }
+#pragma unroll
+    for (int round = 0; round < kRounds; ++round)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            ka = finite_amax<DT>(kx[round][j], ka);
+            va = finite_amax<DT>(vx[round][j], va);
+            const uint32_t w[4] = {vx[round][j].x, vx[round][j].y, vx[round][j].z, vx[round][j].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t bits = w[i >> 1] >> (16 * (i & 1)) & 0x7fffu;
+                strange |= bits >= (DT == FC_BF16 ? 0x7f80u : 0x7c00u);
+            }
+        }
+    ka = max_over_workgroup(ka, scratch);
+    va = max_over_workgroup(va, scratch);
+    strange = __syncthreads_or(strange);
+    float ks = pow2_of(scale_exponent(ka)), vs = pow2_of(scale_exponent(va));
+    if (old) {
+        const float2 was = g.scales[unit];
+        const float was_v = __builtin_fabsf(was.y);
+        strange |= was.y < 0.f;
+        ks = fmaxf(ks, was.x);
+        vs = fmaxf(vs, was_v);
+        if (ks != was.x)
+            for (int i = threadIdx.x; i < old * (DP / 4); i += kThreads) {
+                uint32_t *p = reinterpret_cast<uint32_t *>(kc) + i;
+                *p = rescale4(*p, was.x / ks);
+            }
+        if (vs != was_v)        // (places behind the old tokens hold nothing yet)
+            for (int i = threadIdx.x; i < kBlock * (DP / 4); i += kThreads) {
+                uint32_t *p = reinterpret_cast<uint32_t *>(vc) + i;
+                *p = rescale4(*p, was_v / vs);
+            }
+        __syncthreads();        // (the scales have been read, and values' words are rewritten by other threads below)
+    }
+    if (threadIdx.x == 0) g.scales[unit] = make_float2(ks, strange ? -vs : vs);
+
+    const float ki = 1.f / ks, vi = 1.f / vs;
+#pragma unroll
+    for (int round = 0; round < kRounds; ++round) {
+        uint32_t column[8] = {};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = round * kRows + 4 * r + j;
+            const uint32_t kw[4] = {kx[round][j].x, kx[round][j].y, kx[round][j].z, kx[round][j].w};
+            const uint32_t vw[4] = {vx[round][j].x, vx[round][j].y, vx[round][j].z, vx[round][j].w};
+            uint32_t codes[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float k0 = code_of(bits_to_float<DT>((uint16_t)kw[i]), ki), k1 = code_of(bits_to_float<DT>((uint16_t)(kw[i] >> 16)), ki);
+                const float v0 = code_of(bits_to_float<DT>((uint16_t)vw[i]), vi), v1 = code_of(bits_to_float<DT>((uint16_t)(vw[i] >> 16)), vi);
+                const uint32_t two = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(k0, k1, 0, false) & 0xffffu;
+                codes[i >> 1] |= two << (16 * (i & 1));
+                const uint32_t v2 = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v0, v1, 0, false);
+                column[2 * i] |= (v2 & 0xffu) << (8 * j);
+                column[2 * i + 1] |= (v2 >> 8 & 0xffu) << (8 * j);
+            }
+            // a block that is begun is written whole, so that what lies behind its tokens is zero
+            if (4 * r < kRows && t < kBlock && t >= old && (old == 0 || t < end))
+                *reinterpret_cast<uint2 *>(kc + t * DP + 8 * c) = make_uint2(codes[0], codes[1]);
+        }
+        const int t0 = round * kRows + 4 * r;
+        if (4 * r < kRows && t0 < kBlock)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) turned[(8 * c + i) * kPitch + value_place(t0) / 4] = column[i];
+    }
+    __syncthreads();
+    // words of four tokens; a word with old or absent tokens keeps their bytes
+    for (int i = threadIdx.x; i < DP * 16; i += kThreads) {
+        const int channel = i >> 4, word = i & 15;
+        const int t0 = (word >> 1 & 1) << 5 | (word & 1) << 4 | word >> 2 << 2;
+        uint32_t *p = reinterpret_cast<uint32_t *>(vc) + i;
+        const uint32_t fresh = turned[channel * kPitch + word];
+        if (old == 0) {
+            *p = fresh;
+        } else if (t0 + 3 >= old && t0 < end) {
+            uint32_t take = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) take |= t0 + j >= old && t0 + j < end ? 0xffu << (8 * j) : 0u;
+            *p = (*p & ~take) | (fresh & take);
+        }
+    }
+
+    if (end < kBlock) return;
+    // The block is full: its sketch.  Codes are multiples of 2^-9 below 2^9, so their sums over 64 tokens are whole numbers below 2^24 in those units.
+    for (int i = threadIdx.x; i < DP; i += kThreads) sums[i] = 0;
+    __syncthreads();
+    {
+        constexpr int kWords = DP / 4, kParts = kThreads / kWords;
+        const int w = threadIdx.x % kWords, part = threadIdx.x / kWords;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if (part < kParts)
+            for (int t = part; t < kBlock; t += kParts) {
+                const uint32_t x = *reinterpret_cast<const uint32_t *>(kc + t * DP + 4 * w);
+                const float f[4] = {__builtin_amdgcn_cvt_f32_fp8(x, 0), __builtin_amdgcn_cvt_f32_fp8(x, 1), __builtin_amdgcn_cvt_f32_fp8(x, 2),
+                                    __builtin_amdgcn_cvt_f32_fp8(x, 3)};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) sum[j] += f[j] == f[j] ? f[j] : 0.f;
+            }
+        if (part < kParts)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) atomicAdd(&sums[4 * w + j], (int)(sum[j] * 512.f));
+    }
+    __syncthreads();
+    float most = 0.f;
+    for (int i = threadIdx.x; i < DP; i += kThreads) most = fmaxf(most, __builtin_fabsf((float)sums[i]));
+    most = max_over_workgroup(most, scratch);
+    const int e = unit_exponent(most * (1.f / 512.f));
+    const float inverse = pow2_of(-e) * (1.f / 512.f);
+    for (int i = threadIdx.x; i < DP; i += kThreads) g.sketches[unit * DP + i] = (int8_t)(int)__builtin_rintf((float)sums[i] * inverse);
+    if (threadIdx.x == 0) g.weights[unit] = ks * pow2_of(e) * (1.f / kBlock);
+}
+
+struct ReadArgs {
+    KvGeom kv;
+    float *k, *v;
+};
+
+template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs a)
+{
+    __shared__ uint32_t turned[DP * 17];
+    const KvGeom &g = a.kv;
+    const int b = blockIdx.z, h = blockIdx.y;
+    const Sequence s = sequence_of(g, b);
+    // block -1: the rows without a position
+    const int from = max(s.pos0, 0), first = s.pos0 < 0 ? -1 : 0;
+    const int block = (int)blockIdx.x + first < 0 ? -1 : from / kBlock + (int)blockIdx.x + first;
+    if (block < 0) {
+        const int none = min(-s.pos0, s.n);
+        for (int64_t i = threadIdx.x; i < (int64_t)none * g.d; i += kThreads) {
+            const int64_t to = ((s.row0 + i / g.d) * g.kv_heads + h) * g.d + i % g.d;
+            if (a.k) a.k[to] = 0.f;
+            if (a.v) a.v[to] = 0.f;
+        }
+        return;
+    }
+    const int at = block * kBlock;
+    if (at >= s.len || from >= s.len) return;
+    const int begin = max(from - at, 0), end = min(s.len - at, kBlock);
+    const int32_t pool = pool_block(g, b, block);
+    const bool there = pool >= 0;
+    const int64_t unit = unit_of(g, max(pool, 0), h);
+    const uint8_t *const kc = g.codes + unit * (2 * kBlock * DP), *const vc = kc + kBlock * DP;
+    const float2 scale = there ? g.scales[unit] : make_float2(0.f, 0.f);
+    const float vs = __builtin_fabsf(scale.y);
+    if (a.v && there)
+        for (int i = threadIdx.x; i < DP * 16; i += kThreads) turned[(i >> 4) * 17 + (i & 15)] = reinterpret_cast<const uint32_t *>(vc)[i];
+    __syncthreads();
+    const int64_t row0 = s.row0 + (int64_t)(at - s.pos0);
+    for (int i = threadIdx.x; i < kBlock * DP; i += kThreads) {
+        const int t = i / DP, c = i % DP;
+        if (t < begin || t >= end || c >= g.d) continue;
+        const int64_t to = ((row0 + t) * g.kv_heads + h) * g.d + c;
+        if (a.k) a.k[to] = there ? __builtin_amdgcn_cvt_f32_fp8(kc[t * DP + c], 0) * scale.x : 0.f;
+        if (a.v) {
+            const int place = value_place(t);
+            a.v[to] = there ? __builtin_amdgcn_cvt_f32_fp8(turned[c * 17 + place / 4] >> (8 * (place & 3)) & 0xffu, 0) * vs : 0.f;
+        }
+    }
+}
+
+// Blocks that n new tokens can touch, at most.
+int touched_blocks(const KvGeom &g) { return (int)((int64_t)g.max_new + kBlock - 2) / kBlock + 1; }
+
+template <int DT, int DP> hipError_t run_append(const AppendArgs &a, hipStream_t s)
+{
+    const int blocks = min(touched_blocks(a.kv), (a.kv.max_len + kBlock - 1) / kBlock);
+    k_kv_append<DT, DP><<<dim3(blocks, a.kv.kv_heads, a.kv.batch), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int DP> hipError_t run_read(const ReadArgs &a, hipStream_t s)
+{
+    const int blocks = min(touched_blocks(a.kv), (a.kv.max_len + kBlock - 1) / kBlock) + 1;
+    k_kv_read<DP><<<dim3(blocks, a.kv.kv_heads, a.kv.batch), kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+} // namespace
+
+hipError_t launch_kv_append(const KvGeom &g, int dtype, const uint16_t *k, const uint16_t *v, int64_t k_row, int64_t k_head, int64_t v_row,
+                            int64_t v_head, bool wide_k, bool wide_v, hipStream_t s)
+{
+    const AppendArgs a = {g, k, v, k_row, k_head, v_row, v_head, wide_k, wide_v};
+    const bool b = dtype == FC_BF16;
+    switch (g.dp) {
+    case 64: return b ? run_append<FC_BF16, 64>(a, s) : run_append<FC_F16, 64>(a, s);
+    case 128: return b ? run_append<FC_BF16, 128>(a, s) : run_append<FC_F16, 128>(a, s);
+    case 192: return b ? run_append<FC_BF16, 192>(a, s) : run_append<FC_F16, 192>(a, s);
+    default: return b ? run_append<FC_BF16, 256>(a, s) : run_append<FC_F16, 256>(a, s);
+    }
+}
+
+hipError_t launch_kv_read(const KvGeom &g, float *k, float *v, hipStream_t s)
+{
+    const ReadArgs a = {g, k, v};
+    switch (g.dp) {
+    case 64: return run_read<64>(a, s);
+    case 128: return run_read<128>(a, s);
+    case 192: return run_read<192>(a, s);
+    default: return run_read<256>(a, s);
+    }
+}
+
+} // namespace fc

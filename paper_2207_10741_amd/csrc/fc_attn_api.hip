@@ -81,7 +81,7 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
         p->tiles = d->max_new * ((group + 15) / 16);
         if ((int64_t)d->max_new * ((group + 15) / 16) >= INT32_MAX) return FC_ERR_RANGE;
     } else {
-        p->rows_tile = rows <= 16 || g.dp > 128 ? 16 : 32;      // (32 rows of more channels do not fit the registers)
+        p->rows_tile = rows <= 16 ? 16 : rows <= 32 && g.dp <= 128 ? 32 : kTileRows;
         p->tiles = (int32_t)((rows + p->rows_tile - 1) / p->rows_tile);
     }
     const int64_t units = (int64_t)d->batch * d->kv_heads * p->tiles;
@@ -137,7 +137,8 @@ int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, con
     a.heads = d->heads; a.group = d->heads / d->kv_heads;
     a.causal = list || (d->flags & FC_CAUSAL);
     a.wide = wide_rows(q, d->q_row, d->q_head, d->head_dim);
-    a.scale_log2 = d->scale * 1.44269504088896f;
+    a.scale_log2 = fabsf(d->scale) * 1.44269504088896f;
+    a.signs = d->scale < 0.f ? 0x80008000u : 0u;
     a.div_group = make_fastdiv((uint32_t)a.group);
     a.selected = list ? selected : nullptr;
     a.selected_width = d->first + d->last + d->top;
@@ -147,7 +148,8 @@ int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, con
                                            (size_t)d->batch * d->kv_heads * p.tiles * p.splits * p.rows_tile * g.dp * sizeof(float));
     if (list && launch_select(g, d->dtype, a.q, d->q_row, d->q_head, d->heads, a.wide, d->first, d->last, d->top, selected, s) != hipSuccess)
         return FC_ERR_HIP;
-    return launch_attend_rows(a, d->dtype, p.rows_tile, s) == hipSuccess ? FC_OK : FC_ERR_HIP;
+    return (p.rows_tile <= 32 ? launch_attend_rows(a, d->dtype, p.rows_tile, s) : launch_attend_tile(a, d->dtype, s)) == hipSuccess
+               ? FC_OK : FC_ERR_HIP;
 }
 
 } // namespace

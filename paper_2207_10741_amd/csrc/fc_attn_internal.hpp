@@ -150,6 +150,23 @@ __device__ __forceinline__ int least_exponent(float a, uint32_t limit_fraction, 
 __device__ __forceinline__ int scale_exponent(float amax) { return min(max(least_exponent(amax, 0x600000u, 8), -64), 120); }
 __device__ __forceinline__ int unit_exponent(float amax) { return min(max(least_exponent(amax, 0x7e0000u, 6), -126), 120); }
 
+// Eight f16 values: NaN replaced by zero, and ones where they were.
+__device__ __forceinline__ void split_nan(const uint4 &x, uint4 &clean, uint4 &marks)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    uint32_t c[4], m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = (w[i] & 0x7fffu) > 0x7c00u ? 0xffffu : 0u, hi = (w[i] & 0x7fff0000u) > 0x7c000000u ? 0xffff0000u : 0u;
+        c[i] = w[i] & ~(lo | hi);
+        m[i] = (lo | hi) & 0x3c003c00u;
+    }
+    clean = make_uint4(c[0], c[1], c[2], c[3]);
+    marks = make_uint4(m[0], m[1], m[2], m[3]);
+}
+
+__device__ __forceinline__ uint4 flip_signs(uint4 x, uint32_t signs) { return make_uint4(x.x ^ signs, x.y ^ signs, x.z ^ signs, x.w ^ signs); }
+
 struct AttnArgs {
     KvGeom kv;
     const uint16_t *q;
@@ -160,7 +177,8 @@ struct AttnArgs {
     int32_t selected_width;
     int32_t heads, group, causal;
     int32_t wide;               // q's rows are 16-byte pieces
-    float scale_log2;           // scale * log2(e)
+    float scale_log2;           // |scale| * log2(e); a negative scale changes the queries' signs
+    uint32_t signs;             // of two 16-bit queries
     FastDiv div_group;
     int32_t tiles;              // row tiles of a sequence and key head
     int32_t splits, per_split;  // pieces of the long axis and a piece's blocks
@@ -207,6 +225,13 @@ hipError_t launch_kv_read(const KvGeom &g, float *k, float *v, hipStream_t s);
 
 // Few rows or a list of blocks (see fc_attn_rows.hip); rows_tile: rows a workgroup holds.
 hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s);
+
+// Many rows (see fc_attn_tile.hip): kTileRows a workgroup.
+constexpr int kTileRows = 128;
+hipError_t launch_attend_tile(const AttnArgs &a, int dtype, hipStream_t s);
+
+// The pieces of the long axis.
+hipError_t launch_attend_join(const AttnArgs &a, int dtype, int rows_tile, bool list, hipStream_t s);
 
 // The selection (see fc_attn_select.hip).
 constexpr int kSelectMaxBlocks = 32768;     // blocks of a sequence whose scores fit LDS

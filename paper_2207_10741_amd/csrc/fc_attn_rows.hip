@@ -24,21 +24,6 @@ __device__ __forceinline__ float row_sum(float v)
     return v + __shfl_xor(v, 32);
 }
 
-// Eight f16 values: NaN replaced by zero, and ones where they were.
-__device__ __forceinline__ void split_nan(const uint4 &x, uint4 &clean, uint4 &marks)
-{
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t c[4], m[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = (w[i] & 0x7fffu) > 0x7c00u ? 0xffffu : 0u, hi = (w[i] & 0x7fff0000u) > 0x7c000000u ? 0xffff0000u : 0u;
-        c[i] = w[i] & ~(lo | hi);
-        m[i] = (lo | hi) & 0x3c003c00u;
-    }
-    clean = make_uint4(c[0], c[1], c[2], c[3]);
-    marks = make_uint4(m[0], m[1], m[2], m[3]);
-}
-
 template <int DT, int DP, int MT, bool LIST> __global__ __launch_bounds__(kThreads) void k_attend_rows(AttnArgs a)
 {
     constexpr int kChunks = DP / 64, kTiles = DP / 16, kRows = 16 * MT, kPitch = DP + 4;
@@ -96,8 +81,8 @@ template <int DT, int DP, int MT, bool LIST> __global__ __launch_bounds__(kThrea
         for (int c = 0; c < 2 * kChunks; ++c) {
             q[mt][c] = make_uint4(0, 0, 0, 0);
             if (16 * mt + col < rows)
-                q[mt][c] = load8(a.q + (s.row0 + token[mt]) * a.q_row + (int64_t)(h * a.group + head[mt]) * a.q_head,
-                                 (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, g.d, a.wide);
+                q[mt][c] = flip_signs(load8(a.q + (s.row0 + token[mt]) * a.q_row + (int64_t)(h * a.group + head[mt]) * a.q_head,
+                                            (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, g.d, a.wide), a.signs);
         }
 
     f32x4_t o[MT][kTiles];
@@ -325,6 +310,13 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_attend_j
     finish_row<DT>(a, (int64_t)(s.row0 + token) * a.heads + h * a.group + head, 4 * c, sum, most, total);
 }
 
+template <int DT, int DP> hipError_t run_join(const AttnArgs &a, int rows_tile, bool list, hipStream_t s)
+{
+    const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
+    k_attend_join<DT, DP><<<dim3((uint32_t)(units * rows_tile)), kThreads, 0, s>>>(a, rows_tile, list);
+    return hipGetLastError();
+}
+
 template <int DT, int DP, int MT, bool LIST> hipError_t run_rows(const AttnArgs &a, hipStream_t s)
 {
     constexpr size_t lds = (size_t)kWaves * 16 * MT * (DP + 4 + 2) * sizeof(float);
@@ -334,10 +326,8 @@ template <int DT, int DP, int MT, bool LIST> hipError_t run_rows(const AttnArgs 
     }
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
     k_attend_rows<DT, DP, MT, LIST><<<dim3((uint32_t)(units * a.splits)), kThreads, lds, s>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    k_attend_join<DT, DP><<<dim3((uint32_t)(units * 16 * MT)), kThreads, 0, s>>>(a, 16 * MT, LIST);
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || a.splits == 1 ? e : run_join<DT, DP>(a, 16 * MT, LIST, s);
 }
 
 template <int DT, int DP> hipError_t run_dim(const AttnArgs &a, int rows_tile, hipStream_t s)
@@ -358,7 +348,22 @@ template <int DT> hipError_t run_type(const AttnArgs &a, int rows_tile, hipStrea
     }
 }
 
+template <int DT> hipError_t join_type(const AttnArgs &a, int rows_tile, bool list, hipStream_t s)
+{
+    switch (a.kv.dp) {
+    case 64: return run_join<DT, 64>(a, rows_tile, list, s);
+    case 128: return run_join<DT, 128>(a, rows_tile, list, s);
+    case 192: return run_join<DT, 192>(a, rows_tile, list, s);
+    default: return run_join<DT, 256>(a, rows_tile, list, s);
+    }
+}
+
 } // namespace
+
+hipError_t launch_attend_join(const AttnArgs &a, int dtype, int rows_tile, bool list, hipStream_t s)
+{
+    return dtype == FC_BF16 ? join_type<FC_BF16>(a, rows_tile, list, s) : join_type<FC_F16>(a, rows_tile, list, s);
+}
 
 hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s)
 {

@@ -1,0 +1,264 @@
+// Attention of many rows: prompts and pieces of them.
+//
+// A workgroup holds 32 rows a wave (new tokens x the heads of one key head's group) and goes over the sequence's blocks.  A block's codes
+// become 16-bit floats once, on their way into LDS, where all waves read them as operands; the next block's codes are in
+// registers meanwhile.  S^T = K q^T with v_mfma_f32_32x32x16: a lane holds 32 scores of one row, so the softmax is the lane's own but for one
+// exchange between the halves of the wave, and its weights are the other product's operand as they are (fc_attn_internal.hpp).
+// The vector unit's work for a score is a multiply-add, an exponential, half a maximum, an addition and half a conversion.
+#include "fc_attn_internal.hpp"
+
+namespace fc {
+
+namespace {
+
+constexpr int kThreads = 2 * kTileRows;
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+// the value of the lane 32 away
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+template <int DT> __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, const f32x16_t &c) { return mfma32<DT>(a, b, c); }
+
+// Rows of 16-byte pieces in LDS; a row's pieces are exchanged by its number, so that rows read together lie in different banks.
+__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t row_bytes, uint32_t piece) { return row * row_bytes + ((piece ^ (row & 7u)) << 4); }
+
+constexpr float kSlack = 8.f;   // a row's weights are at most 2^kSlack before its maximum is brought up to date
+
+template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
+{
+    constexpr int kRows = kTileRows, kSteps = DP / 16, kOut = DP / 32;
+    constexpr int kShare = 4 * DP / kThreads;       // 16-byte pieces of the codes of keys (values) a thread brings
+    constexpr uint32_t kKeyRow = 2 * DP, kKeys = kBlock * kKeyRow, kValueRow = 2 * kBlock, kBuffer = kKeys + DP * kValueRow;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const KvGeom &g = a.kv;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+
+    // key heads of sequences first, so that a head's tiles run on one XCD where their number is a multiple of eight; long tiles first
+    const int units = g.batch * g.kv_heads;
+    uint32_t at = blockIdx.x;
+    const int unit_rows = at % units;
+    at /= units;
+    const int split = at % a.splits, tile = a.tiles - 1 - (int)(at / a.splits);
+    const int h = unit_rows % g.kv_heads, b = unit_rows / g.kv_heads;
+    const Sequence s = sequence_of(g, b);
+    const int rows = min(max(s.n * a.group - tile * kRows, 0), kRows);
+    if (rows == 0) return;
+    const int r = tile * kRows + wave * 32 + col;
+    const bool valid = wave * 32 + col < rows;
+    const int token = (int)fast_div((uint32_t)r, a.div_group), head = r - token * a.group;
+    const int last = valid ? (a.causal ? s.pos0 + token : s.len - 1) : -1;
+    const int token_last = (int)fast_div((uint32_t)(tile * kRows + rows - 1), a.div_group);
+    const int last_most = a.causal ? s.pos0 + token_last : s.len - 1;
+    // the wave's own bounds
+    const int wave_rows = min(max(rows - wave * 32, 0), 32);
+    const int wave_first = a.causal ? s.pos0 + (int)fast_div((uint32_t)(tile * kRows + wave * 32), a.div_group) : s.len - 1;
+    const int wave_last = wave_rows == 0 ? -1 : a.causal ? s.pos0 + (int)fast_div((uint32_t)(tile * kRows + wave * 32 + wave_rows - 1), a.div_group) : s.len - 1;
+    const int blocks = last_most < 0 ? 0 : last_most / kBlock + 1;
+    const int active = max((blocks + a.per_split - 1) / a.per_split, 1);
+    if (split >= active) return;
+    const int begin = split * a.per_split, end = min(blocks, begin + a.per_split);
+
+    uint4 q[kSteps];
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) {
+        q[c] = make_uint4(0, 0, 0, 0);
+        if (valid)
+            q[c] = flip_signs(load8(a.q + (s.row0 + token) * a.q_row + (int64_t)(h * a.group + head) * a.q_head, 16 * c + 8 * half, g.d, a.wide), a.signs);
+    }
+
+    f32x16_t o[kOut];
+#pragma unroll
+    for (int t = 0; t < kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = -__builtin_inff(), l = 0.f, unit_v = 1.f;     // m: the row's weights are 2^(z - m)
+
+    uint4 kx[kShare], vx[kShare];
+    float2 scales;
+    bool there;
+    auto bring = [&](int block) {
+        const int32_t pool = pool_block(g, b, block);
+        there = pool >= 0;
+        const int64_t unit = unit_of(g, max(pool, 0), h);
+        const uint4 *const from = reinterpret_cast<const uint4 *>(g.codes + unit * (2 * kBlock * DP));
+        scales = g.scales[unit];
+#pragma unroll
+        for (int i = 0; i < kShare; ++i) {
+            kx[i] = from[threadIdx.x + i * kThreads];
+            vx[i] = from[4 * DP + threadIdx.x + i * kThreads];
+        }
+    };
+    if (begin < end) bring(begin);
+    uint32_t buffer = 0;
+    for (int block = begin; block < end; ++block, buffer ^= kBuffer) {
+        // Values keep the unit they have in LDS as long as a code is exact there (multiples of 2^-9, at most 448: 16 times more or less)
+        const bool here = there;
+        const float scale_k = here ? scales.x : 1.f, scale_v = here ? __builtin_fabsf(scales.y) : unit_v;
+        const bool strange = here && scales.y < 0.f;
+        const float ratio = scale_v / unit_v;
+        float to_unit = ratio;
+        if (!(ratio <= 16.f && ratio >= 0.0625f)) {
+            const float factor = fminf(unit_v / scale_v, 0x1p127f);
+#pragma unroll
+            for (int t = 0; t < kOut; ++t) o[t] *= factor;
+            unit_v = scale_v;
+            to_unit = 1.f;
+        }
+        unsigned char *const keys = lds + buffer, *const values = keys + kKeys;
+#pragma unroll
+        for (int i = 0; i < kShare; ++i) {
+            const uint32_t piece = threadIdx.x + i * kThreads;
+            const uint32_t row = piece / (DP / 16), c = piece % (DP / 16);
+            *reinterpret_cast<uint4 *>(keys + piece_at(row, kKeyRow, 2 * c)) = codes_to_16<DT>(kx[i].x, kx[i].y);
+            *reinterpret_cast<uint4 *>(keys + piece_at(row, kKeyRow, 2 * c + 1)) = codes_to_16<DT>(kx[i].z, kx[i].w);
+            // four words of four tokens 16 s + 4 quarter .. + 3: as the scores' lanes hold them, half `quarter & 1`
+            const uint32_t channel = piece >> 2, quarter = piece & 3;
+            const uint32_t words[4] = {vx[i].x, vx[i].y, vx[i].z, vx[i].w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                u32x2_t two;
+                two.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(words[w], to_unit, false));
+                two.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(words[w], to_unit, true));
+                *reinterpret_cast<u32x2_t *>(values + piece_at(channel, kValueRow, 2 * w + (quarter & 1)) + 8 * (quarter >> 1)) = two;
+            }
+        }
+        __syncthreads();
+        if (block + 1 < end) bring(block + 1);
+        if (!here || block * kBlock > wave_last) continue;
+
+        f32x16_t z[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c)
+                z[t] = mfma_32<DT>(*reinterpret_cast<const uint4 *>(keys + piece_at(32 * t + col, kKeyRow, 2 * c + half)), q[c], z[t]);
+        }
+
+        const float to_log2 = a.scale_log2 * scale_k;
+        const bool partly = block * kBlock + kBlock - 1 > wave_first;
+        const int left = last - block * kBlock - 4 * half;      // scores i of tile t whose token 32 t + 8 (i / 4) + i % 4 is at most this are seen
+        if (partly) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[t][i] = 32 * t + 8 * (i >> 2) + (i & 3) <= left ? z[t][i] : -__builtin_inff();
+        }
+        float most = z[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) most = fmaxf(most, z[i >> 4][i & 15]);
+        most = fmaxf(most, other_half(most)) * to_log2;
+        if (to_log2 == 0.f) most = most == most ? most : -__builtin_inff();             // (all masked)
+        if (__any(most - m > kSlack)) {
+            const float m_new = fmaxf(m, most);
+            const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+            m = m_new;
+            l *= factor;
+#pragma unroll
+            for (int t = 0; t < kOut; ++t) o[t] *= factor;
+        }
+        const float base = m == -__builtin_inff() ? 0.f : -m;
+        float sum = 0.f;
+        uint4 p[4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i], to_log2, base)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i + 1], to_log2, base));
+                if (partly) {   // (a factor of zero makes NaN of what is masked)
+                    e0 = 32 * t + 8 * (i >> 2) + (i & 3) <= left ? e0 : 0.f;
+                    e1 = 32 * t + 8 * (i >> 2) + (i & 3) + 1 <= left ? e1 : 0.f;
+                }
+                sum += e0;
+                sum += e1;
+                w[i >> 1] = pack2<FC_F16>(e0, e1);
+            }
+            p[2 * t] = make_uint4(w[0], w[1], w[2], w[3]);
+            p[2 * t + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+        l += sum;
+
+        if (partly && strange) {
+            // NaN among values that some rows do not see: see k_attend_rows
+            uint4 seen[4];
+#pragma unroll
+            for (int step = 0; step < 4; ++step) {
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int first = 16 * step + 8 * (j >> 1) + 2 * (j & 1);
+                    w[j] = (first <= left ? 0x3c00u : 0u) | (first + 1 <= left ? 0x3c000000u : 0u);
+                }
+                seen[step] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+#pragma unroll
+            for (int t = 0; t < kOut; ++t) {
+                f32x16_t count;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) count[i] = 0.f;
+#pragma unroll
+                for (int step = 0; step < 4; ++step) {
+                    uint4 clean, marks;
+                    split_nan(*reinterpret_cast<const uint4 *>(values + piece_at(32 * t + col, kValueRow, 2 * step + half)), clean, marks);
+                    o[t] = mfma_32<FC_F16>(clean, p[step], o[t]);
+                    count = mfma_32<FC_F16>(marks, seen[step], count);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[t][i] = count[i] > 0.f ? __builtin_nanf("") : o[t][i];
+            }
+            continue;
+        }
+#pragma unroll
+        for (int t = 0; t < kOut; ++t)
+#pragma unroll
+            for (int step = 0; step < 4; ++step)
+                o[t] = mfma_32<FC_F16>(*reinterpret_cast<const uint4 *>(values + piece_at(32 * t + col, kValueRow, 2 * step + half)), p[step], o[t]);
+    }
+
+    l += other_half(l);
+    if (!valid) return;
+    const int64_t part = ((((int64_t)b * g.kv_heads + h) * a.tiles + tile) * a.splits + split) * kRows + wave * 32 + col;
+    const int64_t row = (int64_t)(s.row0 + token) * a.heads + h * a.group + head;
+    if (active > 1 && half == 0) a.part_ml[part] = make_float2(m, l);
+#pragma unroll
+    for (int t = 0; t < kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int c = 32 * t + 2 * i + 4 * half;
+            const f32x4_t v = {o[t][i] * unit_v, o[t][i + 1] * unit_v, o[t][i + 2] * unit_v, o[t][i + 3] * unit_v};
+            if (active > 1) *reinterpret_cast<f32x4_t *>(a.part_out + part * DP + c) = v;
+            else finish_row<DT>(a, row, c, v, m, l);
+        }
+}
+
+template <int DT, int DP> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
+{
+    constexpr size_t lds = 2 * (size_t)(kBlock * 2 * DP + DP * 2 * kBlock);
+    const hipError_t raised = raise_lds<k_attend_tile<DT, DP>>(lds);
+    if (raised != hipSuccess) return raised;
+    const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
+    k_attend_tile<DT, DP><<<dim3((uint32_t)(units * a.splits)), kThreads, lds, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || a.splits == 1 ? e : launch_attend_join(a, DT, kTileRows, false, s);
+}
+
+template <int DT> hipError_t run_type(const AttnArgs &a, hipStream_t s)
+{
+    switch (a.kv.dp) {
+    case 64: return run_tile<DT, 64>(a, s);
+    case 128: return run_tile<DT, 128>(a, s);
+    case 192: return run_tile<DT, 192>(a, s);
+    default: return run_tile<DT, 256>(a, s);
+    }
+}
+
+} // namespace
+
+hipError_t launch_attend_tile(const AttnArgs &a, int dtype, hipStream_t s)
+{
+    return dtype == FC_BF16 ? run_type<FC_BF16>(a, s) : run_type<FC_F16>(a, s);
+}
+
+} // namespace fc

@@ -59,7 +59,7 @@ extern "C" {
 #endif
 
 enum {
-    FC_CAUSAL = 1u /* a row attends to no position after its own */
+    FC_CAUSAL = 1u /* a row attends to no position after its own; FC_WORKSPACE_READY (4) as for convolutions */
 };
 
 enum { FC_KV_BLOCK = 64 };        /* tokens of a block */
@@ -71,7 +71,7 @@ typedef struct {
     int32_t batch, tokens, max_new, max_len, table_width; /* sequences, rows of q / k / v, bounds, entries of a table row */
     int32_t heads;                                      /* query heads, a multiple of kv_heads */
     int32_t dtype;                                      /* of q, k, v and out: FC_BF16 or FC_F16 */
-    uint32_t flags;                                     /* FC_CAUSAL */
+    uint32_t flags;                                     /* FC_CAUSAL, FC_WORKSPACE_READY */
     int32_t first, last, top;                           /* selection */
     float scale;                                        /* of the products q.k, finite */
     int32_t reserved;                                   /* zero */
@@ -91,7 +91,9 @@ int32_t fc_kv_append(const fc_attention_desc *d, void *cache, const void *k, con
 int32_t fc_kv_read(const fc_attention_desc *d, const void *cache, const int32_t *table, const int32_t *lengths, const int32_t *starts,
                    float *k, float *v, void *stream);
 
-/* Bytes of workspace for the two calls below (zero: none is needed).  Its contents do not matter. */
+/* Bytes of workspace for the two calls below (zero: none is needed).  With FC_WORKSPACE_READY in flags the caller vouches that the workspace's
+ * counters are zero, as a workspace that was zeroed once has them, and from then on after every completed call of one of these functions with
+ * this descriptor: it saves the launch that clears them (fc_cache_attention; the selection of fc_focused_attention clears them beside its work). */
 int32_t fc_cache_attention_workspace_bytes(const fc_attention_desc *d, size_t *bytes);
 int32_t fc_focused_attention_workspace_bytes(const fc_attention_desc *d, size_t *bytes);
 

@@ -192,7 +192,7 @@ class _PreparedAttend(_Prepared):
             raise ValueError("lse is float32 [tokens, heads]")
         need = _bytes(name + "_workspace_bytes", desc)
         if workspace is None and need:
-            workspace = self._workspace(need, q.device, stream)
+            workspace = self._workspace(need, q.device, stream, desc)
         self._keep = (desc, cache.data, q, table, lengths, starts, out, lse, selected, workspace)
         self._fn = getattr(lib(), name)
         outputs = (out.data_ptr(), B._ptr(lse)) + (() if selected is None else (selected.data_ptr(),))
@@ -200,8 +200,15 @@ class _PreparedAttend(_Prepared):
                       B._ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
         self._result = out if selected is None else (out, selected)
 
-    def _workspace(self, need, device, stream):
-        return B._scratch(need, device, stream)
+    def _workspace(self, need, device, stream, desc):
+        """A workspace of the call's own, cleared here once: the calls leave its counters zero."""
+        torch = B._torch()
+        desc.flags |= B.WORKSPACE_READY
+        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
+            workspace = torch.zeros((need,), dtype=torch.uint8, device=device)
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream(device).synchronize()     # (a call may come on any stream)
+        return workspace
 
 
 class PreparedAttention(_PreparedAttend):
@@ -232,7 +239,7 @@ class PreparedFocusedAttention(_PreparedAttend):
         self._prepare("fc_focused_attention", desc, cache, q, table, lengths, starts, scale, out, lse, selected, workspace, stream)
 
 
-def _kept_workspace(self, need, device, stream):
+def _kept_workspace(self, need, device, stream, desc):
     return B._own_workspace(need, device, B._stream(stream), stream)
 
 

@@ -23,7 +23,7 @@ int32_t make_kv_geom(const fc_attention_desc *d, const void *cache, const int32_
     const int32_t rc = check_cache(d);
     if (rc != FC_OK) return rc;
     if (d->batch <= 0 || d->tokens < 0 || d->max_new <= 0 || d->max_len <= 0 || d->table_width <= 0) return FC_ERR_SHAPE;
-    if (d->flags & ~(uint32_t)FC_CAUSAL || d->reserved) return FC_ERR_DTYPE;
+    if (d->flags & ~(uint32_t)(FC_CAUSAL | FC_WORKSPACE_READY) || d->reserved) return FC_ERR_DTYPE;
     // (one dimension of a grid)
     if (d->batch > 65535 || d->kv_heads > 65535) return FC_ERR_RANGE;
     if (!starts && (int64_t)d->batch * d->max_new != d->tokens) return FC_ERR_SHAPE;
@@ -56,11 +56,15 @@ bool known_type(int32_t dtype) { return dtype == FC_BF16 || dtype == FC_F16; }
 // How a call's rows and blocks are cut.
 struct Plan {
     int32_t rows_tile, tiles, splits, per_split;
-    size_t workspace;
+    int64_t units;              // of rows: sequences x key heads x tiles
+    bool whole;                 // a wave takes a token's whole list
+    size_t counters, workspace; // bytes; none where nothing is split
 };
 
 // Pieces of the long axis: enough workgroups to fill the chip, no fewer than four blocks a piece (one a wave).
 constexpr int64_t kWorkgroups = 1024;
+// Lists: from this many on there are enough to fill the chip with a wave each.
+constexpr int64_t kWholeLists = 4096;
 
 int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *p)
 {
@@ -79,21 +83,22 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
         blocks = blocks < d->first + d->last + d->top ? blocks : d->first + d->last + d->top;
         p->rows_tile = 16;
         p->tiles = d->max_new * ((group + 15) / 16);
-        if ((int64_t)d->max_new * ((group + 15) / 16) >= INT32_MAX) return FC_ERR_RANGE;
     } else {
         p->rows_tile = rows <= 16 ? 16 : rows <= 32 && g.dp <= 128 ? 32 : kTileRows;
         p->tiles = (int32_t)((rows + p->rows_tile - 1) / p->rows_tile);
     }
-    const int64_t units = (int64_t)d->batch * d->kv_heads * p->tiles;
-    int64_t splits = (kWorkgroups + units - 1) / units;
+    const int64_t units = p->units = (int64_t)d->batch * d->kv_heads * p->tiles;
+    p->whole = list && units >= kWholeLists;
+    int64_t splits = p->whole ? 1 : (kWorkgroups + units - 1) / units;
     const int64_t most = (blocks + 3) / 4;
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
     const int64_t per = ((blocks + splits - 1) / splits + 3) / 4 * 4;
     p->per_split = (int32_t)per;
-    p->splits = (int32_t)((blocks + per - 1) / per);
-    if (units * p->splits >= INT32_MAX || units * p->rows_tile >= INT32_MAX) return FC_ERR_RANGE;
-    p->workspace = p->splits == 1 ? 0 : (size_t)units * p->splits * p->rows_tile * (g.dp * sizeof(float) + sizeof(float2));
+    p->splits = p->whole ? 1 : (int32_t)((blocks + per - 1) / per);
+    if (units * p->splits >= INT32_MAX || (int64_t)p->splits * p->rows_tile * g.dp * 4 >= INT32_MAX) return FC_ERR_RANGE;
+    p->counters = p->splits == 1 ? 0 : align_up((size_t)units * sizeof(int32_t), 256);
+    p->workspace = p->counters + (p->splits == 1 ? 0 : (size_t)units * p->splits * p->rows_tile * (g.dp * sizeof(float) + sizeof(float2)));
     return FC_OK;
 }
 
@@ -143,13 +148,19 @@ int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, con
     a.selected = list ? selected : nullptr;
     a.selected_width = d->first + d->last + d->top;
     a.tiles = p.tiles; a.splits = p.splits; a.per_split = p.per_split;
-    a.part_out = static_cast<float *>(workspace);
-    a.part_ml = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) +
-                                           (size_t)d->batch * d->kv_heads * p.tiles * p.splits * p.rows_tile * g.dp * sizeof(float));
-    if (list && launch_select(g, d->dtype, a.q, d->q_row, d->q_head, d->heads, a.wide, d->first, d->last, d->top, selected, s) != hipSuccess)
-        return FC_ERR_HIP;
-    return (p.rows_tile <= 32 ? launch_attend_rows(a, d->dtype, p.rows_tile, s) : launch_attend_tile(a, d->dtype, s)) == hipSuccess
-               ? FC_OK : FC_ERR_HIP;
+    a.arrived = static_cast<int32_t *>(workspace);
+    a.part_out = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.counters);
+    a.part_ml = reinterpret_cast<float2 *>(a.part_out + (size_t)p.units * p.splits * p.rows_tile * g.dp);
+    const int32_t counters = p.counters && !(d->flags & FC_WORKSPACE_READY) ? (int32_t)p.units : 0;     // to be cleared
+    hipError_t e;
+    if (list) {
+        e = launch_select(g, d->dtype, a.q, d->q_row, d->q_head, d->heads, a.wide, d->first, d->last, d->top, selected, a.arrived, counters, s);
+        if (e == hipSuccess) e = launch_attend_lists(a, d->dtype, p.whole, s);
+    } else {
+        e = counters ? launch_zero_i32(a.arrived, counters, s) : hipSuccess;
+        if (e == hipSuccess) e = p.rows_tile <= 32 ? launch_attend_rows(a, d->dtype, p.rows_tile, s) : launch_attend_tile(a, d->dtype, s);
+    }
+    return e == hipSuccess ? FC_OK : FC_ERR_HIP;
 }
 
 } // namespace

@@ -83,6 +83,7 @@ __host__ __device__ __forceinline__ int value_place(int token)
     return (token >> 2 & 3) << 4 | (token >> 5) << 3 | (token >> 4 & 1) << 2 | (token & 3);
 }
 
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4_t;
 
@@ -182,9 +183,20 @@ struct AttnArgs {
     FastDiv div_group;
     int32_t tiles;              // row tiles of a sequence and key head
     int32_t splits, per_split;  // pieces of the long axis and a piece's blocks
-    float *part_out;            // [unit of rows][split][rows][dp], not yet divided
-    float2 *part_ml;            // [unit of rows][split][rows]: running maximum (base 2) and sum
+    float *part_out;            // [unit of rows][split][rows][dp], not yet divided by the sum of the weights
+    float2 *part_ml;            // [unit of rows][split][rows]: the weights' reference (base 2) and their sum
+    int32_t *arrived;           // [unit of rows]: pieces that are done; zero before and after every call
 };
+
+// Where row r of a tile is: its token among the sequence's new ones, its head among the group's.
+struct RowPlace {
+    int32_t token, head;
+};
+__device__ __forceinline__ RowPlace row_place(const AttnArgs &a, int row)
+{
+    const int32_t token = (int32_t)fast_div((uint32_t)row, a.div_group);
+    return {token, row - token * a.group};
+}
 
 // Four channels c .. c + 3 of a finished row (head `row` of the output's tokens x heads), not yet divided by the sum of the weights.
 template <int DT> __device__ __forceinline__ void finish_row(const AttnArgs &a, int64_t row, int c, f32x4_t sum, float most, float total)
@@ -219,23 +231,150 @@ template <auto KERNEL> hipError_t raise_lds(size_t bytes)
     return e;
 }
 
+constexpr float kSlack = 8.f;   // a row's weights are at most 2^kSlack before its reference is brought up to date
+
+// Joining the pieces of a unit of rows.  A workgroup that has written its piece counts itself; the one that comes last reads all pieces (in
+// their order, whoever is last) and finishes the rows.  What workgroups of other XCDs wrote is read past the caches (kDeviceScope both ways).
+constexpr int kPastCaches = 16;
+template <int DP> struct Pieces {
+    __amdgpu_buffer_rsrc_t out, ml;
+    __device__ __forceinline__ Pieces(const AttnArgs &a, int64_t unit, int rows_tile)
+    {
+        const uint32_t rows = (uint32_t)(a.splits * rows_tile);
+        out = __builtin_amdgcn_make_buffer_rsrc(a.part_out + unit * rows * DP, 0, rows * DP * (uint32_t)sizeof(float), 0x00020000);
+        ml = __builtin_amdgcn_make_buffer_rsrc(a.part_ml + unit * rows, 0, rows * (uint32_t)sizeof(float2), 0x00020000);
+    }
+    // row: split * rows_tile + row of the tile
+    __device__ __forceinline__ void put(uint32_t row, int c, f32x4_t v) const
+    {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), out, (row * DP + (uint32_t)c) * 4u, 0, kPastCaches);
+    }
+    __device__ __forceinline__ void put_ml(uint32_t row, float m, float l) const
+    {
+        const u32x2_t v = {__float_as_uint(m), __float_as_uint(l)};
+        __builtin_amdgcn_raw_buffer_store_b64(v, ml, row * 8u, 0, kPastCaches);
+    }
+    __device__ __forceinline__ f32x4_t get(uint32_t row, int c) const
+    {
+        return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(out, (row * DP + (uint32_t)c) * 4u, 0, kPastCaches));
+    }
+    __device__ __forceinline__ float2 get_ml(uint32_t row) const
+    {
+        const u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(ml, row * 8u, 0, kPastCaches);
+        return make_float2(__uint_as_float(v[0]), __uint_as_float(v[1]));
+    }
+};
+
+// Every thread of the workgroup, after its stores of pieces: is this the unit's last workgroup?
+__device__ __forceinline__ bool last_to_arrive(const AttnArgs &a, int64_t unit, int active, int32_t *lds_flag)
+{
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wave's pieces have been acknowledged ...
+    __syncthreads();                                        // ... and the others'
+    if (threadIdx.x == 0) {
+        const int32_t before = __hip_atomic_fetch_add(a.arrived + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == active - 1) __hip_atomic_store(a.arrived + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *lds_flag = before == active - 1;
+    }
+    __syncthreads();
+    return *lds_flag;
+}
+
+// The last workgroup's part: rows `first` .. of the tile, out_row(r) is row r's place in the output.  A thread takes four channels of a row and,
+// where there are threads to spare, every so-manyth piece.
+template <int DT, int DP, int THREADS, typename F>
+__device__ __forceinline__ void join_pieces(const AttnArgs &a, const Pieces<DP> &pieces, int rows, int rows_tile, int active, float *lds, F out_row)
+{
+    constexpr int kPieces = DP / 4, kUnroll = 4;
+    const int items = rows * kPieces, sets = items < THREADS ? THREADS / items : 1;
+    for (int first = 0; first < items; first += THREADS) {
+        const int item = sets > 1 ? (int)threadIdx.x % items : first + (int)threadIdx.x, set = sets > 1 ? (int)threadIdx.x / items : 0;
+        const bool mine = item < items && set < sets;
+        const int r = item / kPieces, c = item % kPieces * 4;
+        float m = -__builtin_inff(), l = 0.f;
+        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+        auto add = [&](float2 ml, f32x4_t v) {
+            const float most = fmaxf(m, ml.x), base = most == -__builtin_inff() ? 0.f : most;
+            const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(ml.x - base);
+            l = l * f0 + ml.y * f1;
+            o = o * f0 + v * f1;
+            m = most;
+        };
+        if (mine)
+            for (int i = set; i < active; i += sets * kUnroll) {
+                float2 ml[kUnroll];
+                f32x4_t v[kUnroll];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    const uint32_t row = (uint32_t)(min(i + u * sets, active - 1) * rows_tile + r);
+                    ml[u] = pieces.get_ml(row);
+                    v[u] = pieces.get(row, c);
+                }
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u)
+                    if (i + u * sets < active) add(ml[u], v[u]);
+            }
+        if (sets > 1) {
+            __syncthreads();
+            float *const at = lds + threadIdx.x * 8;
+            if (mine && set) {
+                at[0] = m, at[1] = l;
+                *reinterpret_cast<f32x4_t *>(at + 4) = o;
+            }
+            __syncthreads();
+            if (mine && !set)
+                for (int i = 1; i < sets; ++i) {
+                    const float *const other = lds + (i * items + item) * 8;
+                    add(make_float2(other[0], other[1]), *reinterpret_cast<const f32x4_t *>(other + 4));
+                }
+        }
+        if (mine && !set) finish_row<DT>(a, out_row(r), c, o, m, l);
+    }
+}
+
+// max over the lanes 16 and 32 apart
+__device__ __forceinline__ float max_over_32(float v)
+{
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float max_over_16(float v)
+{
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+
+// Eight codes -> eight f16 values in units of `scale` of them (exact for 2^-4 .. 2^4).
+__device__ __forceinline__ uint4 codes_to_f16(uint32_t lo, uint32_t hi, float scale)
+{
+    uint4 r;
+    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, false));
+    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, scale, true));
+    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, false));
+    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, scale, true));
+    return r;
+}
+
+// The unit that values are held in while it stays within 16 times the blocks' scales, either way, where every code times their ratio is exact in
+// f16 (multiples of 2^-13 up to 7168); else the block's own scale.  Returns the ratio; factor: what sums in the old unit are multiplied by.
+__device__ __forceinline__ bool keeps_unit(float scale, float unit) { return scale <= unit * 16.f && scale * 16.f >= unit; }
+
 hipError_t launch_kv_append(const KvGeom &g, int dtype, const uint16_t *k, const uint16_t *v, int64_t k_row, int64_t k_head, int64_t v_row,
                             int64_t v_head, bool wide_k, bool wide_v, hipStream_t s);
 hipError_t launch_kv_read(const KvGeom &g, float *k, float *v, hipStream_t s);
 
-// Few rows or a list of blocks (see fc_attn_rows.hip); rows_tile: rows a workgroup holds.
+// Few rows (see fc_attn_rows.hip); rows_tile: rows a workgroup holds, 16 or 32.
 hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s);
+// 16 rows of one token, over its list of blocks; a wave's, or (a.splits counts the pieces) a workgroup's.
+hipError_t launch_attend_lists(const AttnArgs &a, int dtype, bool whole, hipStream_t s);
 
 // Many rows (see fc_attn_tile.hip): kTileRows a workgroup.
 constexpr int kTileRows = 128;
 hipError_t launch_attend_tile(const AttnArgs &a, int dtype, hipStream_t s);
 
-// The pieces of the long axis.
-hipError_t launch_attend_join(const AttnArgs &a, int dtype, int rows_tile, bool list, hipStream_t s);
-
 // The selection (see fc_attn_select.hip).
 constexpr int kSelectMaxBlocks = 32768;     // blocks of a sequence whose scores fit LDS
+// clear, n_clear: counters that the attention behind it wants zero.
 hipError_t launch_select(const KvGeom &g, int dtype, const uint16_t *q, int64_t q_row, int64_t q_head, int heads, bool wide, int first, int last,
-                         int top, int32_t *selected, hipStream_t s);
+                         int top, int32_t *selected, int32_t *clear, int32_t n_clear, hipStream_t s);
 
 } // namespace fc

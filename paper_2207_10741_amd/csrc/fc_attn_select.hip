@@ -1,16 +1,19 @@
 // Which blocks a token attends to: every block's sketch against the token's queries, then the best ones in order.
 //
-// A workgroup takes up to 16 tokens of one sequence and one key head.  The scores are products of 8-bit whole numbers on the matrix
-// cores (v_mfma_i32_16x16x64_i8: 16 blocks x 16 tokens; the group's queries are summed first and taken apart again into 128 hi + lo),
-// so they do not depend on an order of summation; they stay in LDS.  A wave then picks one token's blocks: the threshold bit by
-// bit, and the list in order by ballots, as the kept lists of masks are made.
+// The scores are products of 8-bit whole numbers on the matrix cores (v_mfma_i32_16x16x64_i8: 16 blocks x 16 tokens; the group's queries are
+// summed first and taken apart again into 128 hi + lo), so they do not depend on an order of summation; they stay in LDS.  The `top` best are
+// those at or above a threshold, which is found from its highest bit on by counting (ballots), and the list comes out in order by ballots, as the
+// kept lists of masks are made.
+//   k_select: 16 (4) tokens a workgroup; a wave finds one token's threshold.  Prompts.
+//   k_select_one: one token a workgroup of 16 waves, which each count for one of 15 thresholds: four bits a round.  Single tokens, where the
+//     chain of dependent steps is all that counts, and sequences so long that more tokens' scores do not fit LDS.
 #include "fc_attn_internal.hpp"
 
 namespace fc {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kThreadsOne = 1024;
 
 struct SelectArgs {
     KvGeom kv;
@@ -18,6 +21,8 @@ struct SelectArgs {
     int64_t q_row, q_head;
     int32_t group, wide, first, last, top, tiles, stride;   // stride: scores of a token in LDS
     int32_t *selected;
+    int32_t *clear;
+    int32_t n_clear;
 };
 
 // Larger floats have larger keys (no NaN).
@@ -27,12 +32,119 @@ __device__ __forceinline__ uint32_t key_of(float v)
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+template <int DT> __device__ __forceinline__ float element(const uint4 &x, int j)
+{
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    return bits_to_float<DT>((uint16_t)(w[j >> 1] >> (16 * (j & 1))));
+}
+__device__ __forceinline__ bool finite(float v) { return __builtin_fabsf(v) < __builtin_inff(); }
+
+template <int DT> __device__ __forceinline__ float largest(const uint4 &x, float most)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float v = element<DT>(x, j);
+        most = finite(v) ? fmaxf(most, __builtin_fabsf(v)) : most;
+    }
+    return most;
+}
+
+// The sketches of 16 blocks: a lane's share, and (lanes alike in lane % 16) a block's weight.
+template <int DP> struct Sketches {
+    i32x4_t x[DP / 64];
+    float weight;
+    __device__ __forceinline__ void bring(const KvGeom &g, int b, int h, int first, int end)
+    {
+        const int lane = threadIdx.x & 63, block = first + (lane & 15);
+        const int32_t pool = block < end ? pool_block(g, b, block) : -1;
+        const int64_t unit = unit_of(g, max(pool, 0), h);
+        weight = pool < 0 ? 0.f : g.weights[unit];
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c) {
+            x[c] = i32x4_t{0, 0, 0, 0};
+            if (pool >= 0) x[c] = *reinterpret_cast<const i32x4_t *>(g.sketches + unit * DP + 64 * c + (lane >> 4) * 16);
+        }
+    }
+    // keys of blocks 4 (lane / 16) + i and token lane % 16
+    __device__ __forceinline__ void score(const i32x4_t (&hi)[DP / 64], const i32x4_t (&lo)[DP / 64], uint32_t (&keys)[4]) const
+    {
+        i32x4_t up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c) {
+            up = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[c], hi[c], up, 0, 0, 0);
+            down = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[c], lo[c], down, 0, 0, 0);
+        }
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) keys[i] = key_of((float)(128 * up[i] + down[i]) * __shfl(weight, (lane >> 4) * 4 + i));
+    }
+};
+
+// The first entries, the last ones, and whole lists of tokens with few blocks.  Returns whether blocks have to be chosen.
+__device__ __forceinline__ bool fixed_entries(const SelectArgs &a, int own, int32_t *out, int at, int step)
+{
+    const int width = a.first + a.last + a.top;
+    if (own + 1 <= width) {
+        for (int i = at; i < width; i += step) out[i] = i <= own ? i : -1;
+        return false;
+    }
+    for (int i = at; i < a.first; i += step) out[i] = i;
+    for (int i = at; i < a.last; i += step) out[a.first + a.top + i] = own - a.last + 1 + i;
+    return a.top != 0;
+}
+
+// Entries of candidates from .. to - 1: those above the threshold, and those at it while `ties` of them are not yet used up.
+__device__ __forceinline__ void write_entries(const uint32_t *keys, int from, int to, uint32_t threshold, int ties, int32_t first, int32_t *out)
+{
+    const int lane = threadIdx.x & 63;
+    const uint64_t below = (1ull << lane) - 1;
+    for (int i = from; i < to; i += 64) {
+        const bool inside = i + lane < to;
+        const uint32_t key = inside ? keys[i + lane] : 0;
+        const uint64_t equals = __ballot(inside && key == threshold);
+        const bool take = inside && (key > threshold || (key == threshold && (int)__popcll(equals & below) < ties));
+        const uint64_t takes = __ballot(take);
+        if (take) out[__popcll(takes & below)] = first + i + lane;
+        ties -= (int)__popcll(equals);
+        out += __popcll(takes);
+    }
+}
+
+// The largest threshold with at least `top` keys at or above it, by one wave.  (A trial with exactly that many will do.)
+template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint32_t *keys, int n, int top, int &above)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t held[REGS > 0 ? REGS : 1];
+#pragma unroll
+    for (int r = 0; r < REGS; ++r) held[r] = 64 * r + lane < n ? keys[64 * r + lane] : 0;      // (no key is 0: no score is that low)
+    auto count = [&](uint32_t trial) {
+        int c = 0;
+        if constexpr (REGS > 0) {
+#pragma unroll
+            for (int r = 0; r < REGS; ++r) c += (int)__popcll(__ballot(held[r] >= trial));
+        } else {
+            for (int i = 0; i < n; i += 64) c += (int)__popcll(__ballot(i + lane < n && keys[i + lane] >= trial));
+        }
+        return c;
+    };
+    uint32_t threshold = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t trial = threshold | 1u << bit;
+        const int c = count(trial);
+        if (c >= top) threshold = trial;
+        if (c == top) break;
+    }
+    above = threshold == ~0u ? 0 : count(threshold + 1);
+    return threshold;
+}
+
 template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_select(SelectArgs a)
 {
     constexpr int kChunks = DP / 64, kShare = kThreads / QT;        // threads of a token
     extern __shared__ uint32_t lds_keys[];
     __shared__ __align__(16) int8_t q8[2][QT][DP];                  // hi, lo
     __shared__ uint32_t amax[QT];
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreads) a.clear[i] = 0;
     const KvGeom &g = a.kv;
     uint32_t at = blockIdx.x;
     const int tile = at % a.tiles;
@@ -43,26 +155,19 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
     if (tokens <= 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
     const int last_pos = s.pos0 + token0 + tokens - 1, width = a.first + a.last + a.top;
-    // blocks that a score is wanted for: first .. scored - 1, unless every token takes all its blocks
+    // blocks that a score is wanted for: below `scored`; none where every token takes all its blocks
     const int own_most = last_pos < 0 ? -1 : last_pos / kBlock;
     const int scored = own_most + 1 <= width || a.top == 0 ? 0 : own_most - a.last + 1;
 
-    if (scored > a.first) {
+    if (scored > 0) {
         const int mine = threadIdx.x / kShare, share = threadIdx.x % kShare;
         if (threadIdx.x < QT) amax[threadIdx.x] = 0;
         __syncthreads();
         const uint16_t *const q = a.q + (int64_t)(s.row0 + token0 + mine) * a.q_row + (int64_t)h * a.group * a.q_head;
         if (mine < tokens) {
             float most = 0.f;
-            for (int i = share; i < a.group * (DP / 8); i += kShare) {
-                const uint4 x = load8(q + (int64_t)(i / (DP / 8)) * a.q_head, i % (DP / 8) * 8, g.d, a.wide);
-                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float v = __builtin_fabsf(bits_to_float<DT>((uint16_t)(w[j >> 1] >> (16 * (j & 1)))));
-                    most = v < __builtin_inff() ? fmaxf(most, v) : most;
-                }
-            }
+            for (int i = share; i < a.group * (DP / 8); i += kShare)
+                most = largest<DT>(load8(q + (int64_t)(i / (DP / 8)) * a.q_head, i % (DP / 8) * 8, g.d, a.wide), most);
             atomicMax(&amax[mine], __float_as_uint(most));
         }
         __syncthreads();
@@ -72,11 +177,10 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
             if (mine < tokens)
                 for (int head = 0; head < a.group; ++head) {
                     const uint4 x = load8(q + head * a.q_head, 8 * c, g.d, a.wide);
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float v = bits_to_float<DT>((uint16_t)(w[j >> 1] >> (16 * (j & 1))));
-                        sum[j] += __builtin_fabsf(v) < __builtin_inff() ? (int)__builtin_rintf(v * inverse) : 0;
+                        const float v = element<DT>(x, j);
+                        sum[j] += finite(v) ? (int)__builtin_rintf(v * inverse) : 0;
                     }
                 }
 #pragma unroll
@@ -95,25 +199,19 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
                 lo[c] = *reinterpret_cast<const i32x4_t *>(&q8[1][col % QT][64 * c + 16 * quarter]);
             }
         }
-        for (int first = wave * 16; first < scored; first += 64) {
-            const int block = first + col;
-            const int32_t pool = block < scored ? pool_block(g, b, block) : -1;
-            const int64_t unit = unit_of(g, max(pool, 0), h);
-            const float weight = pool < 0 ? 0.f : g.weights[unit];
-            i32x4_t up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
+        auto put = [&](const Sketches<DP> &x, int first) {
+            uint32_t keys[4];
+            x.score(hi, lo, keys);
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                i32x4_t x = {0, 0, 0, 0};
-                if (pool >= 0) x = *reinterpret_cast<const i32x4_t *>(g.sketches + unit * DP + 64 * c + 16 * quarter);
-                up = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, hi[c], up, 0, 0, 0);
-                down = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, lo[c], down, 0, 0, 0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = __shfl(weight, quarter * 4 + i);
-                const int to = first + quarter * 4 + i;
-                if (col < QT && to < scored) lds_keys[col * a.stride + to] = key_of((float)(128 * up[i] + down[i]) * w);
-            }
+            for (int i = 0; i < 4; ++i)
+                if (col < QT && first + quarter * 4 + i < scored) lds_keys[col * a.stride + first + quarter * 4 + i] = keys[i];
+        };
+        for (int first = wave * 16; first < scored; first += 128) {
+            Sketches<DP> x0, x1;
+            x0.bring(g, b, h, first, scored);
+            x1.bring(g, b, h, first + 64, scored);
+            put(x0, first);
+            put(x1, first + 64);
         }
         __syncthreads();
     }
@@ -121,49 +219,149 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
     for (int mine = wave; mine < tokens; mine += kThreads / 64) {
         const int pos = s.pos0 + token0 + mine, own = pos < 0 ? -1 : pos / kBlock;
         int32_t *const out = a.selected + ((int64_t)(s.row0 + token0 + mine) * g.kv_heads + h) * width;
-        if (own + 1 <= width) {
-            for (int i = lane; i < width; i += 64) out[i] = i <= own ? i : -1;
-            continue;
-        }
-        for (int i = lane; i < a.first; i += 64) out[i] = i;
-        for (int i = lane; i < a.last; i += 64) out[a.first + a.top + i] = own - a.last + 1 + i;
-        if (a.top == 0) continue;
+        if (!fixed_entries(a, own, out, lane, 64)) continue;
         const int candidates = own + 1 - a.first - a.last;      // (more than top)
         const uint32_t *const keys = lds_keys + mine * a.stride + a.first;
-        uint32_t threshold = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t trial = threshold | 1u << bit;
-            int count = 0;
-            for (int i = 0; i < candidates; i += 64) count += __popcll(__ballot(i + lane < candidates && keys[i + lane] >= trial));
-            if (count >= a.top) threshold = trial;
+        int above;
+        const uint32_t threshold = candidates <= 256 ? threshold_of<4>(keys, candidates, a.top, above) :
+                                   candidates <= 512 ? threshold_of<8>(keys, candidates, a.top, above) :
+                                   candidates <= 1024 ? threshold_of<16>(keys, candidates, a.top, above) : threshold_of<0>(keys, candidates, a.top, above);
+        write_entries(keys, 0, candidates, threshold, a.top - above, a.first, out + a.first);
+    }
+}
+
+template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_select_one(SelectArgs a)
+{
+    constexpr int kChunks = DP / 64, kWaves = kThreadsOne / 64, kHeld = 16;
+    extern __shared__ uint32_t lds_keys[];
+    __shared__ __align__(16) int8_t q8[2][DP];
+    __shared__ int sums[DP], counts[2][kWaves], equal[kWaves];
+    __shared__ uint32_t amax;
+    for (int i = blockIdx.x * kThreadsOne + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreadsOne) a.clear[i] = 0;
+    const KvGeom &g = a.kv;
+    uint32_t at = blockIdx.x;
+    const int token = at % a.tiles;
+    at /= a.tiles;
+    const int h = at % g.kv_heads, b = at / g.kv_heads;
+    const Sequence s = sequence_of(g, b);
+    if (token >= s.n) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
+    const int pos = s.pos0 + token, own = pos < 0 ? -1 : pos / kBlock, width = a.first + a.last + a.top;
+    int32_t *const out = a.selected + ((int64_t)(s.row0 + token) * g.kv_heads + h) * width;
+    if (!fixed_entries(a, own, out, threadIdx.x, kThreadsOne)) return;
+    const int scored = own - a.last + 1, candidates = scored - a.first;
+
+    Sketches<DP> x;
+    x.bring(g, b, h, 16 * wave, scored);
+    for (int i = threadIdx.x; i < DP; i += kThreadsOne) sums[i] = 0;
+    if (threadIdx.x == 0) amax = 0;
+    const uint16_t *const q = a.q + (int64_t)(s.row0 + token) * a.q_row + (int64_t)h * a.group * a.q_head;
+    const int pieces = a.group * (DP / 8);
+    uint4 mine = make_uint4(0, 0, 0, 0);
+    if ((int)threadIdx.x < pieces) mine = load8(q + (int64_t)(threadIdx.x / (DP / 8)) * a.q_head, threadIdx.x % (DP / 8) * 8, g.d, a.wide);
+    __syncthreads();
+    auto each_piece = [&](auto f) {     // (of more than 1024 the others are read twice)
+        if ((int)threadIdx.x < pieces) f(mine, threadIdx.x % (DP / 8) * 8);
+        for (int i = threadIdx.x + kThreadsOne; i < pieces; i += kThreadsOne)
+            f(load8(q + (int64_t)(i / (DP / 8)) * a.q_head, i % (DP / 8) * 8, g.d, a.wide), i % (DP / 8) * 8);
+    };
+    {
+        float most = 0.f;
+        each_piece([&](const uint4 &v, int) { most = largest<DT>(v, most); });
+        if ((int)threadIdx.x < pieces) atomicMax(&amax, __float_as_uint(most));
+    }
+    __syncthreads();
+    const float inverse = pow2_of(-unit_exponent(__uint_as_float(amax)));
+    each_piece([&](const uint4 &v, int c) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float e = element<DT>(v, j);
+            if (finite(e)) atomicAdd(&sums[c + j], (int)__builtin_rintf(e * inverse));
         }
-        int above = 0;
-        for (int i = 0; i < candidates; i += 64) above += __popcll(__ballot(i + lane < candidates && keys[i + lane] > threshold));
-        const int ties = a.top - above;                          // of those at the threshold, the lowest numbers
-        int seen = 0, put = a.first;
-        const uint64_t below = (1ull << lane) - 1;
-        for (int i = 0; i < candidates; i += 64) {
-            const uint32_t key = i + lane < candidates ? keys[i + lane] : 0;
-            const bool equal = i + lane < candidates && key == threshold;
-            const uint64_t equals = __ballot(equal);
-            const bool take = (i + lane < candidates && key > threshold) || (equal && seen + __popcll(equals & below) < ties);
-            const uint64_t takes = __ballot(take);
-            if (take) out[put + __popcll(takes & below)] = a.first + i + lane;
-            seen += __popcll(equals);
-            put += __popcll(takes);
+    });
+    __syncthreads();
+    if (threadIdx.x < DP) {
+        q8[0][threadIdx.x] = (int8_t)(sums[threadIdx.x] >> 7);
+        q8[1][threadIdx.x] = (int8_t)(sums[threadIdx.x] & 127);
+    }
+    __syncthreads();
+    i32x4_t hi[kChunks], lo[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {     // (one column of the sixteen)
+        hi[c] = lo[c] = i32x4_t{0, 0, 0, 0};
+        if (col == 0) {
+            hi[c] = *reinterpret_cast<const i32x4_t *>(&q8[0][64 * c + 16 * quarter]);
+            lo[c] = *reinterpret_cast<const i32x4_t *>(&q8[1][64 * c + 16 * quarter]);
         }
     }
+    for (int first = 16 * wave; first < scored; first += 16 * kWaves) {
+        uint32_t keys[4];
+        x.score(hi, lo, keys);
+        if (first + 16 * kWaves < scored) x.bring(g, b, h, first + 16 * kWaves, scored);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col == 0 && first + quarter * 4 + i < scored) lds_keys[first + quarter * 4 + i] = keys[i];
+    }
+    __syncthreads();
+
+    const uint32_t *const keys = lds_keys + a.first;
+    uint32_t held[kHeld];
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) held[r] = 64 * r + lane < candidates ? keys[64 * r + lane] : 0;        // (no key is 0)
+    uint32_t threshold = 0;
+    for (int shift = 28; shift >= 0; shift -= 4) {
+        const uint32_t trial = threshold | (uint32_t)wave << shift;     // (wave 0: the threshold itself, which has enough)
+        int c = 0;
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r) c += (int)__popcll(__ballot(held[r] >= trial));
+        for (int i = 64 * kHeld; i < candidates; i += 64) c += (int)__popcll(__ballot(i + lane < candidates && keys[i + lane] >= trial));
+        int *const row = counts[shift >> 2 & 1];
+        if (lane == 0) row[wave] = c;
+        __syncthreads();
+        const int other = row[lane & (kWaves - 1)];
+        const uint64_t enough = __ballot(other >= a.top || lane == 0) & 0xffffu;
+        threshold |= (uint32_t)(63 - __clzll(enough)) << shift;
+        if (__ballot(other == a.top && lane > 0) & 0xffffu) break;      // (then the highest with enough is one with exactly as many)
+    }
+
+    // a wave writes the entries of its part of the candidates
+    const int part = (candidates + 64 * kWaves - 1) / (64 * kWaves) * 64, from = min(wave * part, candidates), to = min(from + part, candidates);
+    int above = 0, same = 0;
+    for (int i = from; i < to; i += 64) {
+        const uint32_t key = i + lane < to ? keys[i + lane] : 0;
+        above += (int)__popcll(__ballot(key > threshold));
+        same += (int)__popcll(__ballot(i + lane < to && key == threshold));
+    }
+    __syncthreads();        // (the last round's counts have been read)
+    if (lane == 0) {
+        counts[0][wave] = above;
+        equal[wave] = same;
+    }
+    __syncthreads();
+    int above_before = 0, same_before = 0, above_all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        above_all += counts[0][w];
+        above_before += w < wave ? counts[0][w] : 0;
+        same_before += w < wave ? equal[w] : 0;
+    }
+    const int ties = a.top - above_all;         // of those at the threshold, the lowest numbers
+    write_entries(keys, from, to, threshold, ties - same_before, a.first, out + a.first + above_before + min(same_before, ties));
 }
 
 template <int DT, int DP, int QT> hipError_t run_tokens(SelectArgs a, hipStream_t s)
 {
     a.tiles = (a.kv.max_new + QT - 1) / QT;
     const size_t lds = (size_t)QT * a.stride * sizeof(uint32_t);
+    const dim3 grid((uint32_t)((int64_t)a.kv.batch * a.kv.kv_heads * a.tiles));
     if (lds > 32 * 1024) {
-        const hipError_t e = raise_lds<k_select<DT, DP, QT>>((size_t)128 * 1024);
+        hipError_t e;
+        if constexpr (QT == 1) e = raise_lds<k_select_one<DT, DP>>((size_t)128 * 1024);
+        else e = raise_lds<k_select<DT, DP, QT>>((size_t)128 * 1024);
         if (e != hipSuccess) return e;
     }
-    k_select<DT, DP, QT><<<dim3((uint32_t)((int64_t)a.kv.batch * a.kv.kv_heads * a.tiles)), kThreads, lds, s>>>(a);
+    if constexpr (QT == 1) k_select_one<DT, DP><<<grid, kThreadsOne, lds, s>>>(a);
+    else k_select<DT, DP, QT><<<grid, kThreads, lds, s>>>(a);
     return hipGetLastError();
 }
 
@@ -187,10 +385,10 @@ template <int DT> hipError_t run_type(const SelectArgs &a, hipStream_t s)
 } // namespace
 
 hipError_t launch_select(const KvGeom &g, int dtype, const uint16_t *q, int64_t q_row, int64_t q_head, int heads, bool wide, int first, int last,
-                         int top, int32_t *selected, hipStream_t s)
+                         int top, int32_t *selected, int32_t *clear, int32_t n_clear, hipStream_t s)
 {
     const int stride = (int)align_up((size_t)(g.max_len + kBlock - 1) / kBlock, 16);
-    const SelectArgs a = {g, q, q_row, q_head, heads / g.kv_heads, wide, first, last, top, 0, stride, selected};
+    const SelectArgs a = {g, q, q_row, q_head, heads / g.kv_heads, wide, first, last, top, 0, stride, selected, clear, n_clear};
     return dtype == FC_BF16 ? run_type<FC_BF16>(a, s) : run_type<FC_F16>(a, s);
 }
 

@@ -12,17 +12,10 @@ namespace fc {
 namespace {
 
 constexpr int kThreads = 2 * kTileRows;
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-
-// the value of the lane 32 away
-__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
-
 template <int DT> __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, const f32x16_t &c) { return mfma32<DT>(a, b, c); }
 
 // Rows of 16-byte pieces in LDS; a row's pieces are exchanged by its number, so that rows read together lie in different banks.
 __device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t row_bytes, uint32_t piece) { return row * row_bytes + ((piece ^ (row & 7u)) << 4); }
-
-constexpr float kSlack = 8.f;   // a row's weights are at most 2^kSlack before its maximum is brought up to date
 
 template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
 {
@@ -91,14 +84,12 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
     if (begin < end) bring(begin);
     uint32_t buffer = 0;
     for (int block = begin; block < end; ++block, buffer ^= kBuffer) {
-        // Values keep the unit they have in LDS as long as a code is exact there (multiples of 2^-9, at most 448: 16 times more or less)
         const bool here = there;
         const float scale_k = here ? scales.x : 1.f, scale_v = here ? __builtin_fabsf(scales.y) : unit_v;
         const bool strange = here && scales.y < 0.f;
-        const float ratio = scale_v / unit_v;
-        float to_unit = ratio;
-        if (!(ratio <= 16.f && ratio >= 0.0625f)) {
-            const float factor = fminf(unit_v / scale_v, 0x1p127f);
+        float to_unit = scale_v / unit_v;
+        if (!keeps_unit(scale_v, unit_v)) {
+            const float factor = fminf(unit_v / scale_v, 0x1p127f);     // (finite: zero stays zero)
 #pragma unroll
             for (int t = 0; t < kOut; ++t) o[t] *= factor;
             unit_v = scale_v;
@@ -113,14 +104,11 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
             *reinterpret_cast<uint4 *>(keys + piece_at(row, kKeyRow, 2 * c + 1)) = codes_to_16<DT>(kx[i].z, kx[i].w);
             // four words of four tokens 16 s + 4 quarter .. + 3: as the scores' lanes hold them, half `quarter & 1`
             const uint32_t channel = piece >> 2, quarter = piece & 3;
-            const uint32_t words[4] = {vx[i].x, vx[i].y, vx[i].z, vx[i].w};
+            const uint4 first = codes_to_f16(vx[i].x, vx[i].y, to_unit), second = codes_to_f16(vx[i].z, vx[i].w, to_unit);
+            const uint2 words[4] = {make_uint2(first.x, first.y), make_uint2(first.z, first.w), make_uint2(second.x, second.y), make_uint2(second.z, second.w)};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                u32x2_t two;
-                two.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(words[w], to_unit, false));
-                two.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(words[w], to_unit, true));
-                *reinterpret_cast<u32x2_t *>(values + piece_at(channel, kValueRow, 2 * w + (quarter & 1)) + 8 * (quarter >> 1)) = two;
-            }
+            for (int w = 0; w < 4; ++w)
+                *reinterpret_cast<uint2 *>(values + piece_at(channel, kValueRow, 2 * w + (quarter & 1)) + 8 * (quarter >> 1)) = words[w];
         }
         __syncthreads();
         if (block + 1 < end) bring(block + 1);
@@ -148,7 +136,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
         float most = z[0][0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) most = fmaxf(most, z[i >> 4][i & 15]);
-        most = fmaxf(most, other_half(most)) * to_log2;
+        most = max_over_32(most) * to_log2;
         if (to_log2 == 0.f) most = most == most ? most : -__builtin_inff();             // (all masked)
         if (__any(most - m > kSlack)) {
             const float m_new = fmaxf(m, most);
@@ -217,20 +205,31 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
                 o[t] = mfma_32<FC_F16>(*reinterpret_cast<const uint4 *>(values + piece_at(32 * t + col, kValueRow, 2 * step + half)), p[step], o[t]);
     }
 
-    l += other_half(l);
-    if (!valid) return;
-    const int64_t part = ((((int64_t)b * g.kv_heads + h) * a.tiles + tile) * a.splits + split) * kRows + wave * 32 + col;
-    const int64_t row = (int64_t)(s.row0 + token) * a.heads + h * a.group + head;
-    if (active > 1 && half == 0) a.part_ml[part] = make_float2(m, l);
+    l += __shfl_xor(l, 32);
+    const int64_t unit = (int64_t)unit_rows * a.tiles + tile;
+    const Pieces<DP> pieces(a, unit, kRows);
+    auto out_row = [&](int row) {
+        const RowPlace p = row_place(a, tile * kRows + row);
+        return (int64_t)(s.row0 + p.token) * a.heads + h * a.group + p.head;
+    };
+    if (valid) {
+        const int64_t row = out_row(wave * 32 + col);
+        const uint32_t part = (uint32_t)(split * kRows + wave * 32 + col);
+        if (active > 1 && half == 0) pieces.put_ml(part, m, l);
 #pragma unroll
-    for (int t = 0; t < kOut; ++t)
+        for (int t = 0; t < kOut; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int c = 32 * t + 2 * i + 4 * half;
-            const f32x4_t v = {o[t][i] * unit_v, o[t][i + 1] * unit_v, o[t][i + 2] * unit_v, o[t][i + 3] * unit_v};
-            if (active > 1) *reinterpret_cast<f32x4_t *>(a.part_out + part * DP + c) = v;
-            else finish_row<DT>(a, row, c, v, m, l);
-        }
+            for (int i = 0; i < 16; i += 4) {
+                const int c = 32 * t + 2 * i + 4 * half;
+                const f32x4_t v = {o[t][i] * unit_v, o[t][i + 1] * unit_v, o[t][i + 2] * unit_v, o[t][i + 3] * unit_v};
+                if (active > 1) pieces.put(part, c, v);
+                else finish_row<DT>(a, row, c, v, m, l);
+            }
+    }
+    if (active == 1) return;
+    __syncthreads();        // (the flag lies where operands were)
+    if (!last_to_arrive(a, unit, active, reinterpret_cast<int32_t *>(lds))) return;
+    join_pieces<DT, DP, kThreads>(a, pieces, rows, kRows, active, reinterpret_cast<float *>(lds) + 4, out_row);
 }
 
 template <int DT, int DP> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
@@ -240,8 +239,7 @@ template <int DT, int DP> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
     if (raised != hipSuccess) return raised;
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
     k_attend_tile<DT, DP><<<dim3((uint32_t)(units * a.splits)), kThreads, lds, s>>>(a);
-    const hipError_t e = hipGetLastError();
-    return e != hipSuccess || a.splits == 1 ? e : launch_attend_join(a, DT, kTileRows, false, s);
+    return hipGetLastError();
 }
 
 template <int DT> hipError_t run_type(const AttnArgs &a, hipStream_t s)

@@ -61,8 +61,10 @@ struct Plan {
     size_t counters, workspace; // bytes; none where nothing is split
 };
 
-// Pieces of the long axis: enough workgroups to fill the chip, no fewer than four blocks a piece (one a wave).
-constexpr int64_t kWorkgroups = 1024;
+// Pieces of the long axis: two workgroups a CU, as many as are there at once, and no fewer than four blocks a piece (one a wave).  More pieces
+// balance nothing and take longer to join: us at 512 / 768 / 1024 / 2048 workgroups, 64 sequences of 2000 to 8192 tokens, 8 key heads of 128,
+// 134 / 145 / 145 / 146; one of 131000 57 / 63 / 69 / 94; pieces of 517 tokens of three over 5003 103 / 119 / 119 / 118.
+constexpr int64_t kWorkgroups = 512;
 // Lists: from this many on there are enough to fill the chip with a wave each.
 constexpr int64_t kWholeLists = 4096;
 

@@ -284,7 +284,7 @@ __device__ __forceinline__ bool last_to_arrive(const AttnArgs &a, int64_t unit, 
 template <int DT, int DP, int THREADS, typename F>
 __device__ __forceinline__ void join_pieces(const AttnArgs &a, const Pieces<DP> &pieces, int rows, int rows_tile, int active, float *lds, F out_row)
 {
-    constexpr int kPieces = DP / 4, kUnroll = 4;
+        constexpr int kPieces = DP / 4, kUnroll = 8;
     const int items = rows * kPieces, sets = items < THREADS ? THREADS / items : 1;
     for (int first = 0; first < items; first += THREADS) {
         const int item = sets > 1 ? (int)threadIdx.x % items : first + (int)threadIdx.x, set = sets > 1 ? (int)threadIdx.x / items : 0;

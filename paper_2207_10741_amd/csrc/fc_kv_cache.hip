@@ -1,7 +1,8 @@
 // The key/value cache in 8 bits: appending tokens and reading them back.
 //
-// A workgroup takes one block of one head that new tokens of a sequence fall into: it reads their rows, finds the largest magnitude,
-// makes the scale, and writes codes.  Both are bound by memory: 4 bytes read and 2 written a channel of a token.
+// k_kv_append: a workgroup takes one block of one head that new tokens of a sequence fall into: it reads their rows, finds the largest magnitude,
+// makes the scale, and writes codes.  Bound by memory: 4 bytes read and 2 written a channel of a token.
+// k_kv_append_one: a sequence's single new token; a wave takes a head, so that a step of a batch is one round of waves without a barrier.
 #include "fc_attn_internal.hpp"
 
 namespace fc {
@@ -23,6 +24,25 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float ratio)
     int r = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(c, 0) * ratio, __builtin_amdgcn_cvt_f32_fp8(c, 1) * ratio, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(c, 2) * ratio, __builtin_amdgcn_cvt_f32_fp8(c, 3) * ratio, r, true);
 }
+
+__device__ __forceinline__ void rescale16(uint4 *p, float ratio)
+{
+    const uint4 x = *p;
+    *p = make_uint4(rescale4(x.x, ratio), rescale4(x.y, ratio), rescale4(x.z, ratio), rescale4(x.w, ratio));
+}
+
+// Adds eight codes, NaN as zero.
+__device__ __forceinline__ void add_codes(uint2 x, float (&sum)[8])
+{
+    const float f[8] = {__builtin_amdgcn_cvt_f32_fp8(x.x, 0), __builtin_amdgcn_cvt_f32_fp8(x.x, 1), __builtin_amdgcn_cvt_f32_fp8(x.x, 2),
+                        __builtin_amdgcn_cvt_f32_fp8(x.x, 3), __builtin_amdgcn_cvt_f32_fp8(x.y, 0), __builtin_amdgcn_cvt_f32_fp8(x.y, 1),
+                        __builtin_amdgcn_cvt_f32_fp8(x.y, 2), __builtin_amdgcn_cvt_f32_fp8(x.y, 3)};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] += f[j] == f[j] ? f[j] : 0.f;
+}
+
+// A channel's sum of codes in units of 2^-9, as a sketch holds it under 2^e.
+__device__ __forceinline__ int8_t sketch_of(int sum, int e) { return (int8_t)(int)__builtin_rintf((float)sum * (pow2_of(-e) * (1.f / 512.f))); }
 
 // A value in units of its scale; what is not finite becomes NaN.
 __device__ __forceinline__ float code_of(float v, float inverse)
@@ -129,6 +149,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
     if (threadIdx.x == 0) g.scales[unit] = make_float2(ks, strange ? -vs : vs);
 
     const float ki = 1.f / ks, vi = 1.f / vs;
+    uint2 codes[kRounds][4];
 #pragma unroll
     for (int round = 0; round < kRounds; ++round) {
         uint32_t column[8] = {};
@@ -137,20 +158,21 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
             const int t = round * kRows + 4 * r + j;
             const uint32_t kw[4] = {kx[round][j].x, kx[round][j].y, kx[round][j].z, kx[round][j].w};
             const uint32_t vw[4] = {vx[round][j].x, vx[round][j].y, vx[round][j].z, vx[round][j].w};
-            uint32_t codes[2] = {0, 0};
+            uint32_t packed[2] = {0, 0};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float k0 = code_of(bits_to_float<DT>((uint16_t)kw[i]), ki), k1 = code_of(bits_to_float<DT>((uint16_t)(kw[i] >> 16)), ki);
                 const float v0 = code_of(bits_to_float<DT>((uint16_t)vw[i]), vi), v1 = code_of(bits_to_float<DT>((uint16_t)(vw[i] >> 16)), vi);
                 const uint32_t two = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(k0, k1, 0, false) & 0xffffu;
-                codes[i >> 1] |= two << (16 * (i & 1));
+                packed[i >> 1] |= two << (16 * (i & 1));
                 const uint32_t v2 = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v0, v1, 0, false);
                 column[2 * i] |= (v2 & 0xffu) << (8 * j);
                 column[2 * i + 1] |= (v2 >> 8 & 0xffu) << (8 * j);
             }
-            // a block that is begun is written whole, so that what lies behind its tokens is zero
+            codes[round][j] = make_uint2(packed[0], packed[1]);
+            // a block that is begun is written whole, so that no place of it holds a NaN that its scale does not tell of
             if (4 * r < kRows && t < kBlock && t >= old && (old == 0 || t < end))
-                *reinterpret_cast<uint2 *>(kc + t * DP + 8 * c) = make_uint2(codes[0], codes[1]);
+                *reinterpret_cast<uint2 *>(kc + t * DP + 8 * c) = codes[round][j];
         }
         const int t0 = round * kRows + 4 * r;
         if (4 * r < kRows && t0 < kBlock)
@@ -176,32 +198,118 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
 
     if (end < kBlock) return;
     // The block is full: its sketch.  Codes are multiples of 2^-9 below 2^9, so their sums over 64 tokens are whole numbers below 2^24 in those units.
+    // A block that was begun by this call has its codes in registers.
     for (int i = threadIdx.x; i < DP; i += kThreads) sums[i] = 0;
     __syncthreads();
-    {
-        constexpr int kWords = DP / 4, kParts = kThreads / kWords;
-        const int w = threadIdx.x % kWords, part = threadIdx.x / kWords;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        if (part < kParts)
-            for (int t = part; t < kBlock; t += kParts) {
-                const uint32_t x = *reinterpret_cast<const uint32_t *>(kc + t * DP + 4 * w);
-                const float f[4] = {__builtin_amdgcn_cvt_f32_fp8(x, 0), __builtin_amdgcn_cvt_f32_fp8(x, 1), __builtin_amdgcn_cvt_f32_fp8(x, 2),
-                                    __builtin_amdgcn_cvt_f32_fp8(x, 3)};
+    if (old == 0) {
+        if (4 * r < kRows) {
+            float sum[8] = {};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum[j] += f[j] == f[j] ? f[j] : 0.f;
-            }
-        if (part < kParts)
+            for (int round = 0; round < kRounds; ++round)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) atomicAdd(&sums[4 * w + j], (int)(sum[j] * 512.f));
+                for (int j = 0; j < 4; ++j) add_codes(codes[round][j], sum);    // (rows past the block are zero)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) atomicAdd(&sums[8 * c + j], (int)(sum[j] * 512.f));
+        }
+    } else {
+        for (int i = threadIdx.x; i < kBlock * kChunks; i += kThreads) {
+            float sum[8] = {};
+            add_codes(*reinterpret_cast<const uint2 *>(kc + 8 * i), sum);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) atomicAdd(&sums[i % kChunks * 8 + j], (int)(sum[j] * 512.f));
+        }
     }
     __syncthreads();
     float most = 0.f;
     for (int i = threadIdx.x; i < DP; i += kThreads) most = fmaxf(most, __builtin_fabsf((float)sums[i]));
     most = max_over_workgroup(most, scratch);
     const int e = unit_exponent(most * (1.f / 512.f));
-    const float inverse = pow2_of(-e) * (1.f / 512.f);
-    for (int i = threadIdx.x; i < DP; i += kThreads) g.sketches[unit * DP + i] = (int8_t)(int)__builtin_rintf((float)sums[i] * inverse);
+    for (int i = threadIdx.x; i < DP; i += kThreads) g.sketches[unit * DP + i] = sketch_of(sums[i], e);
     if (threadIdx.x == 0) g.weights[unit] = ks * pow2_of(e) * (1.f / kBlock);
+}
+
+// A wave's lane holds channels DP / 64 * lane on.
+template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_append_one(AppendArgs a)
+{
+    constexpr int kEach = DP / 64;
+    const KvGeom &g = a.kv;
+    const int lane = threadIdx.x & 63;
+    const uint32_t at = blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = at % g.kv_heads, b = at / g.kv_heads;
+    if (b >= g.batch) return;
+    const Sequence s = sequence_of(g, b);
+    if (s.n != 1 || s.len <= 0) return;
+    const int token = s.len - 1, old = token % kBlock;
+    const uint16_t *const krow = a.k + s.row0 * a.k_row + h * a.k_head, *const vrow = a.v + s.row0 * a.v_row + h * a.v_head;
+    float kv[kEach], vv[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int c = lane * kEach + i;
+        kv[i] = c < g.d ? bits_to_float<DT>(krow[c]) : 0.f;
+        vv[i] = c < g.d ? bits_to_float<DT>(vrow[c]) : 0.f;
+    }
+    const int32_t pool = pool_block(g, b, token / kBlock);
+    if (pool < 0) return;
+    const int64_t unit = unit_of(g, pool, h);
+    uint8_t *const kc = g.codes + unit * (2 * kBlock * DP), *const vc = kc + kBlock * DP;
+    const float2 was = old ? g.scales[unit] : make_float2(0.f, 0.f);
+    float ka = 0.f, va = 0.f;
+    bool strange = was.y < 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const float x = __builtin_fabsf(kv[i]), y = __builtin_fabsf(vv[i]);
+        ka = x < __builtin_inff() ? fmaxf(ka, x) : ka;
+        va = y < __builtin_inff() ? fmaxf(va, y) : va;
+        strange |= !(y < __builtin_inff());
+    }
+    strange = __any(strange);
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        ka = fmaxf(ka, __shfl_xor(ka, m));
+        va = fmaxf(va, __shfl_xor(va, m));
+    }
+    const float was_v = __builtin_fabsf(was.y);
+    const float ks = fmaxf(pow2_of(scale_exponent(ka)), was.x), vs = fmaxf(pow2_of(scale_exponent(va)), was_v);
+    if (old && ks != was.x)
+        for (int i = lane; i < old * (DP / 16); i += 64) rescale16(reinterpret_cast<uint4 *>(kc) + i, was.x / ks);
+    if (old == 0) {         // (a block that is begun: see k_kv_append)
+        for (int i = lane; i < kBlock * (DP / 16); i += 64) reinterpret_cast<uint4 *>(vc)[i] = make_uint4(0, 0, 0, 0);
+    } else if (vs != was_v) {
+        for (int i = lane; i < kBlock * (DP / 16); i += 64) rescale16(reinterpret_cast<uint4 *>(vc) + i, was_v / vs);
+    }
+    if (old == 0 || vs != was_v) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");     // other lanes' stores to the bytes below
+    const float ki = 1.f / ks, vi = 1.f / vs;
+    const int place = value_place(old);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int c = lane * kEach + i;
+        const int two = __builtin_amdgcn_cvt_pk_fp8_f32(code_of(kv[i], ki), code_of(vv[i], vi), 0, false);
+        kc[old * DP + c] = (uint8_t)two;
+        vc[c * kBlock + place] = (uint8_t)(two >> 8);
+    }
+    if (lane == 0) g.scales[unit] = make_float2(ks, strange ? -vs : vs);
+    if (old < kBlock - 1) return;
+
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // (the token's own codes, and rounded ones)
+    int sum[kEach] = {};
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        float x = 0.f;
+#pragma unroll 8
+        for (int t = 0; t < kBlock; ++t) {
+            const float f = __builtin_amdgcn_cvt_f32_fp8(kc[t * DP + lane * kEach + i], 0);
+            x += f == f ? f : 0.f;
+        }
+        sum[i] = (int)(x * 512.f);
+        most = fmaxf(most, __builtin_fabsf((float)sum[i]));
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+    const int e = unit_exponent(most * (1.f / 512.f));
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) g.sketches[unit * DP + lane * kEach + i] = sketch_of(sum[i], e);
+    if (lane == 0) g.weights[unit] = ks * pow2_of(e) * (1.f / kBlock);
 }
 
 struct ReadArgs {
@@ -236,19 +344,43 @@ template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs
     const uint8_t *const kc = g.codes + unit * (2 * kBlock * DP), *const vc = kc + kBlock * DP;
     const float2 scale = there ? g.scales[unit] : make_float2(0.f, 0.f);
     const float vs = __builtin_fabsf(scale.y);
-    if (a.v && there)
-        for (int i = threadIdx.x; i < DP * 16; i += kThreads) turned[(i >> 4) * 17 + (i & 15)] = reinterpret_cast<const uint32_t *>(vc)[i];
-    __syncthreads();
     const int64_t row0 = s.row0 + (int64_t)(at - s.pos0);
-    for (int i = threadIdx.x; i < kBlock * DP; i += kThreads) {
-        const int t = i / DP, c = i % DP;
-        if (t < begin || t >= end || c >= g.d) continue;
-        const int64_t to = ((row0 + t) * g.kv_heads + h) * g.d + c;
-        if (a.k) a.k[to] = there ? __builtin_amdgcn_cvt_f32_fp8(kc[t * DP + c], 0) * scale.x : 0.f;
-        if (a.v) {
-            const int place = value_place(t);
-            a.v[to] = there ? __builtin_amdgcn_cvt_f32_fp8(turned[c * 17 + place / 4] >> (8 * (place & 3)) & 0xffu, 0) * vs : 0.f;
+    const bool quads = (g.d & 3) == 0;      // (then rows are 16-byte pieces)
+    auto put = [&](float *to, int t, int c, const float (&x)[4]) {
+        float *const row = to + ((row0 + t) * g.kv_heads + h) * g.d + c;
+        if (quads) {
+            if (c < g.d) *reinterpret_cast<float4 *>(row) = make_float4(x[0], x[1], x[2], x[3]);
+            return;
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < g.d) row[i] = x[i];
+    };
+    if (a.k)
+        for (int i = threadIdx.x; i < kBlock * (DP / 4); i += kThreads) {
+            const int t = i / (DP / 4), c = i % (DP / 4) * 4;
+            if (t < begin || t >= end) continue;
+            const uint32_t x = there ? reinterpret_cast<const uint32_t *>(kc)[i] : 0;
+            const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(x, 0) * scale.x, __builtin_amdgcn_cvt_f32_fp8(x, 1) * scale.x,
+                                __builtin_amdgcn_cvt_f32_fp8(x, 2) * scale.x, __builtin_amdgcn_cvt_f32_fp8(x, 3) * scale.x};
+            put(a.k, t, c, v);
+        }
+    if (!a.v) return;
+    for (int i = threadIdx.x; i < DP * 16; i += kThreads) turned[(i >> 4) * 17 + (i & 15)] = there ? reinterpret_cast<const uint32_t *>(vc)[i] : 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * (DP / 4); i += kThreads) {
+        const int c = i % (DP / 4) * 4, t = i / (DP / 4) * 4;       // four tokens of four channels
+        if (t + 3 < begin || t >= end) continue;
+        float v[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = turned[(c + j) * 17 + value_place(t) / 4];
+            v[0][j] = __builtin_amdgcn_cvt_f32_fp8(x, 0) * vs, v[1][j] = __builtin_amdgcn_cvt_f32_fp8(x, 1) * vs;
+            v[2][j] = __builtin_amdgcn_cvt_f32_fp8(x, 2) * vs, v[3][j] = __builtin_amdgcn_cvt_f32_fp8(x, 3) * vs;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (t + j >= begin && t + j < end) put(a.v, t + j, c, v[j]);
     }
 }
 
@@ -257,6 +389,11 @@ int touched_blocks(const KvGeom &g) { return (int)((int64_t)g.max_new + kBlock -
 
 template <int DT, int DP> hipError_t run_append(const AppendArgs &a, hipStream_t s)
 {
+    if (a.kv.max_new == 1) {
+        const int64_t waves = (int64_t)a.kv.batch * a.kv.kv_heads;
+        k_kv_append_one<DT, DP><<<dim3((uint32_t)((waves + kThreads / 64 - 1) / (kThreads / 64))), kThreads, 0, s>>>(a);
+        return hipGetLastError();
+    }
     const int blocks = min(touched_blocks(a.kv), (a.kv.max_len + kBlock - 1) / kBlock);
     k_kv_append<DT, DP><<<dim3(blocks, a.kv.kv_heads, a.kv.batch), kThreads, 0, s>>>(a);
     return hipGetLastError();

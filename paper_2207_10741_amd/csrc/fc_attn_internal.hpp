@@ -354,9 +354,15 @@ __device__ __forceinline__ uint4 codes_to_f16(uint32_t lo, uint32_t hi, float sc
     return r;
 }
 
-// The unit that values are held in while it stays within 16 times the blocks' scales, either way, where every code times their ratio is exact in
-// f16 (multiples of 2^-13 up to 7168); else the block's own scale.  Returns the ratio; factor: what sums in the old unit are multiplied by.
+// The unit that values are held in stays while it is within 16 times the blocks' scales, either way, where every code times their ratio is exact in
+// f16 (multiples of 2^-13 up to 7168); else it becomes the block's own scale.
 __device__ __forceinline__ bool keeps_unit(float scale, float unit) { return scale <= unit * 16.f && scale * 16.f >= unit; }
+// a / b of two powers of two, held to 2^-126 .. 2^127 (finite: a sum of zero stays zero).
+__device__ __forceinline__ float pow2_ratio(float a, float b)
+{
+    const int e = (int)(__float_as_uint(a) >> 23) - (int)(__float_as_uint(b) >> 23);
+    return pow2_of(min(max(e, -126), 127));
+}
 
 hipError_t launch_kv_append(const KvGeom &g, int dtype, const uint16_t *k, const uint16_t *v, int64_t k_row, int64_t k_head, int64_t v_row,
                             int64_t v_head, bool wide_k, bool wide_v, hipStream_t s);

@@ -93,34 +93,37 @@ template <int DT, int DP, int MT> struct Rows {
             if (more) bring_keys();
 
             if (here) {
-                const float to_log2 = a.scale_log2 * scales.x, scale_v = __builtin_fabsf(scales.y);
+                const float scale_v = __builtin_fabsf(scales.y);
+                float to_log2 = a.scale_log2 * scales.x;
                 const int from = block * kBlock;
                 const bool partly = from + kBlock - 1 > last_least;
-                float to_unit = scale_v / unit_v;
                 if (!keeps_unit(scale_v, unit_v)) {
-                    const float factor = fminf(unit_v / scale_v, 0x1p127f);     // (finite: zero stays zero)
+                    const float factor = pow2_ratio(unit_v, scale_v);
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int t = 0; t < kTiles; ++t) o[mt][t] *= factor;
                     unit_v = scale_v;
-                    to_unit = 1.f;
+                }
+                const float to_unit = pow2_ratio(scale_v, unit_v);
+                if (partly) {
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        const int left = last[mt] - from - 4 * quarter;     // scores i of tile t with 16 t + i <= left are seen
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) z[mt][t][i] = 16 * t + i <= left ? z[mt][t][i] * to_log2 : -__builtin_inff();
+                    }
+                    to_log2 = 1.f;      // (a factor of zero would make NaN of what is masked)
                 }
                 uint4 p[MT][2];
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
-                    const int left = last[mt] - from - 4 * quarter;     // scores i of tile t with 16 t + i <= left are seen
-                    if (partly) {
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) z[mt][t][i] = 16 * t + i <= left ? z[mt][t][i] : -__builtin_inff();
-                    }
                     float most = z[mt][0][0];
 #pragma unroll
                     for (int i = 1; i < 16; ++i) most = fmaxf(most, z[mt][i >> 2][i & 3]);
                     most = max_over_16(max_over_32(most)) * to_log2;
-                    if (to_log2 == 0.f) most = most == most ? most : -__builtin_inff();     // (all masked)
                     if (__any(most - m[mt] > kSlack)) {
                         const float m_new = fmaxf(m[mt], most);
                         const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);
@@ -132,16 +135,12 @@ template <int DT, int DP, int MT> struct Rows {
                     const float base = m[mt] == -__builtin_inff() ? 0.f : -m[mt];
                     uint32_t w[8];
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        float e[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mt][t][i], to_log2, base));
-                            if (partly) e[i] = 16 * t + i <= left ? e[i] : 0.f;      // (a factor of zero makes NaN of what is masked)
-                            l[mt] += e[i];
-                        }
-                        w[2 * t] = pack2<FC_F16>(e[0], e[1]);
-                        w[2 * t + 1] = pack2<FC_F16>(e[2], e[3]);
+                    for (int i = 0; i < 16; i += 2) {
+                        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mt][i >> 2][i & 3], to_log2, base));
+                        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mt][i >> 2][(i & 3) + 1], to_log2, base));
+                        l[mt] += e0;
+                        l[mt] += e1;
+                        w[i >> 1] = pack2<FC_F16>(e0, e1);
                     }
                     p[mt][0] = make_uint4(w[0], w[1], w[2], w[3]);
                     p[mt][1] = make_uint4(w[4], w[5], w[6], w[7]);

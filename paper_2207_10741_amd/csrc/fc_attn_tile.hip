@@ -14,14 +14,15 @@ namespace {
 constexpr int kThreads = 2 * kTileRows;
 template <int DT> __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, const f32x16_t &c) { return mfma32<DT>(a, b, c); }
 
-// Rows of 16-byte pieces in LDS; a row's pieces are exchanged by its number, so that rows read together lie in different banks.
-__device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t row_bytes, uint32_t piece) { return row * row_bytes + ((piece ^ (row & 7u)) << 4); }
+template <int DP> constexpr uint32_t kKeyPitch = 2 * DP + 16;
+constexpr uint32_t kValuePitch = 2 * kBlock + 16;
 
 template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
 {
     constexpr int kRows = kTileRows, kSteps = DP / 16, kOut = DP / 32;
     constexpr int kShare = 4 * DP / kThreads;       // 16-byte pieces of the codes of keys (values) a thread brings
-    constexpr uint32_t kKeyRow = 2 * DP, kKeys = kBlock * kKeyRow, kValueRow = 2 * kBlock, kBuffer = kKeys + DP * kValueRow;
+    // rows of keys and values in LDS; the 16 bytes behind each put rows that are read together into different banks
+    constexpr uint32_t kKeyRow = kKeyPitch<DP>, kKeys = kBlock * kKeyRow, kValueRow = kValuePitch, kBuffer = kKeys + DP * kValueRow;
     extern __shared__ __align__(16) unsigned char lds[];
     const KvGeom &g = a.kv;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
@@ -73,42 +74,46 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
         const int32_t pool = pool_block(g, b, block);
         there = pool >= 0;
         const int64_t unit = unit_of(g, max(pool, 0), h);
-        const uint4 *const from = reinterpret_cast<const uint4 *>(g.codes + unit * (2 * kBlock * DP));
+        const uint8_t *const from = g.codes + unit * (2 * kBlock * DP);
         scales = g.scales[unit];
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
-            kx[i] = from[threadIdx.x + i * kThreads];
-            vx[i] = from[4 * DP + threadIdx.x + i * kThreads];
+            kx[i] = *reinterpret_cast<const uint4 *>(from + i * kThreads * 16 + threadIdx.x * 16u);
+            vx[i] = *reinterpret_cast<const uint4 *>(from + (4 * DP + i * kThreads) * 16 + threadIdx.x * 16u);
         }
     };
     if (begin < end) bring(begin);
+    // where the thread's pieces go and where the lane's operands are, from the buffer's start on
+    const uint32_t key_to = threadIdx.x / (DP / 16) * kKeyRow + threadIdx.x % (DP / 16) * 32;
+    // four words of four tokens 16 w + 4 quarter .. + 3: as the scores' lanes hold them, half `quarter & 1`
+    const uint32_t value_to = kKeys + (threadIdx.x >> 2) * kValueRow + (threadIdx.x & 1) * 16 + (threadIdx.x >> 1 & 1) * 8;
+    const uint32_t key_at = col * kKeyRow + half * 16, value_at = kKeys + col * kValueRow + half * 16;
     uint32_t buffer = 0;
-    for (int block = begin; block < end; ++block, buffer ^= kBuffer) {
+    for (int block = begin; block < end; ++block, buffer = kBuffer - buffer) {
         const bool here = there;
         const float scale_k = here ? scales.x : 1.f, scale_v = here ? __builtin_fabsf(scales.y) : unit_v;
         const bool strange = here && scales.y < 0.f;
-        float to_unit = scale_v / unit_v;
         if (!keeps_unit(scale_v, unit_v)) {
-            const float factor = fminf(unit_v / scale_v, 0x1p127f);     // (finite: zero stays zero)
+            const float factor = pow2_ratio(unit_v, scale_v);
 #pragma unroll
             for (int t = 0; t < kOut; ++t) o[t] *= factor;
             unit_v = scale_v;
-            to_unit = 1.f;
         }
-        unsigned char *const keys = lds + buffer, *const values = keys + kKeys;
+        const float to_unit = pow2_ratio(scale_v, unit_v);
+        unsigned char *const keys_to = lds + buffer + key_to, *const values_to = lds + buffer + value_to;
+        const unsigned char *const keys = lds + buffer + key_at, *const values = lds + buffer + value_at;
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
-            const uint32_t piece = threadIdx.x + i * kThreads;
-            const uint32_t row = piece / (DP / 16), c = piece % (DP / 16);
-            *reinterpret_cast<uint4 *>(keys + piece_at(row, kKeyRow, 2 * c)) = codes_to_16<DT>(kx[i].x, kx[i].y);
-            *reinterpret_cast<uint4 *>(keys + piece_at(row, kKeyRow, 2 * c + 1)) = codes_to_16<DT>(kx[i].z, kx[i].w);
-            // four words of four tokens 16 s + 4 quarter .. + 3: as the scores' lanes hold them, half `quarter & 1`
-            const uint32_t channel = piece >> 2, quarter = piece & 3;
+            // (kThreads pieces further: so many rows of keys, so many channels)
+            constexpr uint32_t kKeyStep = kThreads / (DP / 16) * kKeyRow, kValueStep = kThreads / 4 * kValueRow;
+            uint32_t key_step = i * kKeyStep;
+            if constexpr (kThreads % (DP / 16)) key_step = (threadIdx.x + i * kThreads) / (DP / 16) * kKeyRow + (threadIdx.x + i * kThreads) % (DP / 16) * 32 - key_to;
+            *reinterpret_cast<uint4 *>(keys_to + key_step) = codes_to_16<DT>(kx[i].x, kx[i].y);
+            *reinterpret_cast<uint4 *>(keys_to + key_step + 16) = codes_to_16<DT>(kx[i].z, kx[i].w);
             const uint4 first = codes_to_f16(vx[i].x, vx[i].y, to_unit), second = codes_to_f16(vx[i].z, vx[i].w, to_unit);
             const uint2 words[4] = {make_uint2(first.x, first.y), make_uint2(first.z, first.w), make_uint2(second.x, second.y), make_uint2(second.z, second.w)};
 #pragma unroll
-            for (int w = 0; w < 4; ++w)
-                *reinterpret_cast<uint2 *>(values + piece_at(channel, kValueRow, 2 * w + (quarter & 1)) + 8 * (quarter >> 1)) = words[w];
+            for (int w = 0; w < 4; ++w) *reinterpret_cast<uint2 *>(values_to + i * kValueStep + 32 * w) = words[w];
         }
         __syncthreads();
         if (block + 1 < end) bring(block + 1);
@@ -121,23 +126,23 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
             for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
 #pragma unroll
             for (int c = 0; c < kSteps; ++c)
-                z[t] = mfma_32<DT>(*reinterpret_cast<const uint4 *>(keys + piece_at(32 * t + col, kKeyRow, 2 * c + half)), q[c], z[t]);
+                z[t] = mfma_32<DT>(*reinterpret_cast<const uint4 *>(keys + 32 * t * kKeyRow + 32 * c), q[c], z[t]);
         }
 
-        const float to_log2 = a.scale_log2 * scale_k;
+        float to_log2 = a.scale_log2 * scale_k;
         const bool partly = block * kBlock + kBlock - 1 > wave_first;
         const int left = last - block * kBlock - 4 * half;      // scores i of tile t whose token 32 t + 8 (i / 4) + i % 4 is at most this are seen
         if (partly) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[t][i] = 32 * t + 8 * (i >> 2) + (i & 3) <= left ? z[t][i] : -__builtin_inff();
+                for (int i = 0; i < 16; ++i) z[t][i] = 32 * t + 8 * (i >> 2) + (i & 3) <= left ? z[t][i] * to_log2 : -__builtin_inff();
+            to_log2 = 1.f;      // (a factor of zero would make NaN of what is masked)
         }
         float most = z[0][0];
 #pragma unroll
         for (int i = 1; i < 32; ++i) most = fmaxf(most, z[i >> 4][i & 15]);
         most = max_over_32(most) * to_log2;
-        if (to_log2 == 0.f) most = most == most ? most : -__builtin_inff();             // (all masked)
         if (__any(most - m > kSlack)) {
             const float m_new = fmaxf(m, most);
             const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -147,26 +152,21 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
             for (int t = 0; t < kOut; ++t) o[t] *= factor;
         }
         const float base = m == -__builtin_inff() ? 0.f : -m;
-        float sum = 0.f;
         uint4 p[4];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             uint32_t w[8];
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-                float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i], to_log2, base)), e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i + 1], to_log2, base));
-                if (partly) {   // (a factor of zero makes NaN of what is masked)
-                    e0 = 32 * t + 8 * (i >> 2) + (i & 3) <= left ? e0 : 0.f;
-                    e1 = 32 * t + 8 * (i >> 2) + (i & 3) + 1 <= left ? e1 : 0.f;
-                }
-                sum += e0;
-                sum += e1;
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i], to_log2, base));
+                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i + 1], to_log2, base));
+                l += e0;
+                l += e1;
                 w[i >> 1] = pack2<FC_F16>(e0, e1);
             }
             p[2 * t] = make_uint4(w[0], w[1], w[2], w[3]);
             p[2 * t + 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
-        l += sum;
 
         if (partly && strange) {
             // NaN among values that some rows do not see: see k_attend_rows
@@ -189,7 +189,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
 #pragma unroll
                 for (int step = 0; step < 4; ++step) {
                     uint4 clean, marks;
-                    split_nan(*reinterpret_cast<const uint4 *>(values + piece_at(32 * t + col, kValueRow, 2 * step + half)), clean, marks);
+                    split_nan(*reinterpret_cast<const uint4 *>(values + 32 * t * kValueRow + 32 * step), clean, marks);
                     o[t] = mfma_32<FC_F16>(clean, p[step], o[t]);
                     count = mfma_32<FC_F16>(marks, seen[step], count);
                 }
@@ -202,7 +202,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
         for (int t = 0; t < kOut; ++t)
 #pragma unroll
             for (int step = 0; step < 4; ++step)
-                o[t] = mfma_32<FC_F16>(*reinterpret_cast<const uint4 *>(values + piece_at(32 * t + col, kValueRow, 2 * step + half)), p[step], o[t]);
+                o[t] = mfma_32<FC_F16>(*reinterpret_cast<const uint4 *>(values + 32 * t * kValueRow + 32 * step), p[step], o[t]);
     }
 
     l += __shfl_xor(l, 32);
@@ -234,7 +234,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
 
 template <int DT, int DP> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
 {
-    constexpr size_t lds = 2 * (size_t)(kBlock * 2 * DP + DP * 2 * kBlock);
+    constexpr size_t lds = 2 * (size_t)(kBlock * kKeyPitch<DP> + DP * kValuePitch);
     const hipError_t raised = raise_lds<k_attend_tile<DT, DP>>(lds);
     if (raised != hipSuccess) return raised;
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;

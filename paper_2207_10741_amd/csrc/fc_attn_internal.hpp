@@ -1,16 +1,17 @@
 // Declarations shared by the attention operators' translation units: the cache's layout, what a sequence's arrays say, conversions.
 //
 // Layout of the cache.  A unit is one block of one key/value head: unit = pool block * kv_heads + head.
-//   codes    [unit][128 * dp] bytes: keys [64 tokens][dp], then values [dp][64 places]; dp = head_dim rounded up to a multiple of 64, zeros behind
+//   codes    [unit][128 * dp] bytes: keys, then values; dp = head_dim rounded up to a multiple of 64, zeros behind
 //   scales   [unit] of two floats: the keys' scale; the values', negative where a value of the block is NaN
 //   sketches [unit][dp] signed bytes, weights [unit] floats
-// Everything that a wave reads of a unit is then in one piece: the matrix instructions' own order.  A lane of the 16x16 instructions
-// holds eight consecutive places of the reduction, lanes 16 apart the next eight (g = lane / 16):
-//   scores S^T = K q^T: a lane's rows are tokens, and sixteen channels 64 c + 16 g .. + 15 of one token make its share of two
-//     instructions; a load of 16 bytes a lane reads 64-byte pieces of 16 tokens.
-//   out^T = V^T P^T: P^T comes out of the first product with tokens 4 g + i of each 16 (i = 0 .. 3) in the lane that needs them as
-//     operand, so no weight moves between lanes if V's rows are held in that order too: token 32 h + 16 k + 4 g + i is at place
-//     16 g + 8 h + 4 k + i of its row, and 16 bytes a lane, 1 KB a wave in one piece, are its share for a whole block.
+// Keys and values lie in the order in which the matrix instructions want them, so that a load of 16 bytes a lane is 1 KB in one piece.  (The L1 gives
+// 65 bytes a clock then, and 18 where sixteen lanes read from rows of 128 bytes, keys as [token][channel].)  A lane of the 16x16 instructions holds
+// eight consecutive places of the reduction, lanes 16 apart the next eight (quarter = lane / 16):
+//   scores S^T = K q^T: a lane's row is a token, and 16 channels of it are its share of two instructions: pieces
+//     [token / 16][channel / 64][channel / 16 % 4][token % 16] of 16 channels.
+//   out^T = V^T P^T: P^T comes out of the first product with tokens 4 quarter + i of each 16 (i = 0 .. 3) in the lane that needs them as operand, so no
+//     weight moves between lanes if V's rows are in that order too: token 32 h + 16 k + 4 quarter + i is at place 16 quarter + 8 h + 4 k + i:
+//     pieces [channel / 16][place / 16][channel % 16] of 16 places, a lane's share for a whole block.
 #pragma once
 #include <atomic>
 #include "fc_mfma_util.hpp"
@@ -83,6 +84,16 @@ __host__ __device__ __forceinline__ int value_place(int token)
     return (token >> 2 & 3) << 4 | (token >> 5) << 3 | (token >> 4 & 1) << 2 | (token & 3);
 }
 
+// Offsets in a unit's codes of the piece of 16 bytes that holds an element; element & 15 is its place in the piece.
+template <int DP> __host__ __device__ __forceinline__ uint32_t key_piece(uint32_t token, uint32_t channel)
+{
+    return ((((token >> 4) * (DP / 64) + (channel >> 6)) * 4 + (channel >> 4 & 3)) * 16 + (token & 15)) * 16;
+}
+template <int DP> __host__ __device__ __forceinline__ uint32_t value_piece(uint32_t channel, uint32_t place)
+{
+    return kBlock * DP + (((channel >> 4) * 4 + (place >> 4)) * 16 + (channel & 15)) * 16;
+}
+
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4_t;
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4_t;
@@ -151,20 +162,25 @@ __device__ __forceinline__ int least_exponent(float a, uint32_t limit_fraction, 
 __device__ __forceinline__ int scale_exponent(float amax) { return min(max(least_exponent(amax, 0x600000u, 8), -64), 120); }
 __device__ __forceinline__ int unit_exponent(float amax) { return min(max(least_exponent(amax, 0x7e0000u, 6), -126), 120); }
 
-// Eight f16 values: NaN replaced by zero, and ones where they were.
-__device__ __forceinline__ void split_nan(const uint4 &x, uint4 &clean, uint4 &marks)
+// NaN among the values of a block that some rows see in part: a weight of zero does not silence it in a matrix product.  So the product runs on
+// zeros in NaN's place, and a second one, of ones at the NaN and at what a row sees, finds the outputs that are NaN.
+// The bytes of four codes that are NaN, as 0xff.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t codes)
 {
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t c[4], m[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = (w[i] & 0x7fffu) > 0x7c00u ? 0xffffu : 0u, hi = (w[i] & 0x7fff0000u) > 0x7c000000u ? 0xffff0000u : 0u;
-        c[i] = w[i] & ~(lo | hi);
-        m[i] = (lo | hi) & 0x3c003c00u;
-    }
-    clean = make_uint4(c[0], c[1], c[2], c[3]);
-    marks = make_uint4(m[0], m[1], m[2], m[3]);
+    const uint32_t n = (((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+    return (n << 8) - n;
 }
+__device__ __forceinline__ uint4 without_nan(const uint4 &x)
+{
+    return make_uint4(x.x & ~nan_bytes(x.x), x.y & ~nan_bytes(x.y), x.z & ~nan_bytes(x.z), x.w & ~nan_bytes(x.w));
+}
+// Eight codes -> f16 ones where they are NaN.
+__device__ __forceinline__ uint4 nan_marks(uint32_t lo, uint32_t hi)
+{
+    return codes_to_16<FC_F16>(nan_bytes(lo) & 0x38383838u, nan_bytes(hi) & 0x38383838u);
+}
+// Two f16 ones: are tokens `first` and the next at most `left`?
+__device__ __forceinline__ uint32_t seen_pair(int first, int left) { return (first <= left ? 0x3c00u : 0u) | (first + 1 <= left ? 0x3c000000u : 0u); }
 
 __device__ __forceinline__ uint4 flip_signs(uint4 x, uint32_t signs) { return make_uint4(x.x ^ signs, x.y ^ signs, x.z ^ signs, x.w ^ signs); }
 

@@ -42,37 +42,61 @@ template <int DT, int DP, int MT> struct Rows {
     {
         const KvGeom &g = a.kv;
         if (first >= end) return;
-        const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4;
-        const uint32_t k_lane = (uint32_t)(col * DP + 16 * quarter), v_lane = (uint32_t)(kBlock * DP + col * 64 + 16 * quarter);
-        auto block_at = [&](int j) { return LIST ? list[j] : j; };
-        auto codes_of = [&](int32_t pool) { return g.codes + unit_of(g, max(pool, 0), h) * (2 * kBlock * DP); };
-        int block = block_at(first), block_next = first + step < end ? block_at(first + step) : 0;
-        int32_t pool = pool_block(g, b, block), pool_next = first + step < end ? pool_block(g, b, block_next) : -1;
-        const uint8_t *codes = codes_of(pool);
-        float2 scales = g.scales[unit_of(g, max(pool, 0), h)];
+        const int lane = threadIdx.x & 63, quarter = lane >> 4;
+        // Lane i holds what the loop needs to know of its i-th block of 64 (of the list's blocks, where they are in the pool, their scales): the loop
+        // itself waits for keys and values only.
+        int held_block = 0, held_pool = -1;
+        float2 held_scales = make_float2(1.f, 1.f);
+        auto look_up = [&](int from) {
+            const int j = from + lane * step;
+            held_block = 0, held_pool = -1;
+            if (j < end) {
+                held_block = LIST ? list[j] : j;
+                held_pool = pool_block(g, b, held_block);
+                held_scales = g.scales[unit_of(g, max(held_pool, 0), h)];
+            }
+            __asm__ volatile("" : "+v"(held_block), "+v"(held_pool), "+v"(held_scales.x), "+v"(held_scales.y));      // (waited for here, not in the loop)
+        };
+        look_up(first);
+        int block = __builtin_amdgcn_readlane(held_block, 0), pool = __builtin_amdgcn_readlane(held_pool, 0);
+        float2 scales;
+        auto scales_at = [&](int i) {
+            return make_float2(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_scales.x), i)),
+                               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_scales.y), i)));
+        };
+        scales = scales_at(0);
+        // A block's codes: keys at 0, values behind them.  A block that is not there, and the one behind the last, is an empty buffer.
+        auto codes_of = [&](int32_t p) {
+            return __builtin_amdgcn_make_buffer_rsrc(g.codes + unit_of(g, max(p, 0), h) * (2 * kBlock * DP), 0, p < 0 ? 0 : 2 * kBlock * DP, 0x00020000);
+        };
         uint4 kx[4][kChunks], vx[kTiles];
-        auto bring_keys = [&] {
+        auto bring_keys = [&](__amdgpu_buffer_rsrc_t from, int t) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c) kx[t][c] = *reinterpret_cast<const uint4 *>(codes + k_lane + 16 * t * DP + 64 * c);
+            for (int c = 0; c < kChunks; ++c)
+                kx[t][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16, (t * kChunks + c) * 1024, 0));
         };
-        auto bring_values = [&] {
-#pragma unroll
-            for (int t = 0; t < kTiles; ++t) vx[t] = *reinterpret_cast<const uint4 *>(codes + v_lane + 16 * t * 64);
+        auto bring_values = [&](__amdgpu_buffer_rsrc_t from, int t) {
+            vx[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16, kBlock * DP + t * 1024, 0));
         };
-        bring_keys();
-        bring_values();
+        {
+            const auto codes = codes_of(pool);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) bring_keys(codes, t);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) bring_values(codes, t);
+        }
 
-        for (int j = first; j < end; j += step) {
-            // (blocks behind the last are looked up as the last, and not brought)
+        int i_next = 1;
+        for (int j = first; j < end; j += step, ++i_next) {
             const bool more = j + step < end;
-            const int j2 = min(j + 2 * step, end - 1);
-            const int block_after = block_at(j2);
-            const int32_t pool_after = pool_block(g, b, block_after);
-            const uint8_t *const codes_next = codes_of(pool_next);
-            const float2 scales_next = g.scales[unit_of(g, max(pool_next, 0), h)];
+            if (i_next == 64 && more) {
+                look_up(j + step);
+                i_next = 0;
+            }
+            const int block_next = __builtin_amdgcn_readlane(held_block, i_next & 63), pool_next = __builtin_amdgcn_readlane(held_pool, i_next & 63);
+            const float2 scales_next = scales_at(i_next & 63);
             const bool here = pool >= 0;
+            const auto codes_next = codes_of(more ? pool_next : -1);
 
             f32x4_t z[MT][4];
 #pragma unroll
@@ -88,9 +112,8 @@ template <int DT, int DP, int MT> struct Rows {
                         z[mt][t] = mfma16<DT>(k1, q[mt][2 * c + 1], z[mt][t]);
                     }
                 }
+                bring_keys(codes_next, t);
             }
-            codes = codes_next;
-            if (more) bring_keys();
 
             if (here) {
                 const float scale_v = __builtin_fabsf(scales.y);
@@ -147,46 +170,39 @@ template <int DT, int DP, int MT> struct Rows {
                 }
 
                 if (partly && scales.y < 0.f) {
-                    // NaN among the values of a block that some rows see in part: a weight of zero does not silence it in a matrix product.
-                    // The product runs on zeros in NaN's place, and a second one counts the NaN that a row does see.
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
                         const int left = last[mt] - from - 4 * quarter;
-                        uint32_t w[8];
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) w[2 * t + i] = (16 * t + 2 * i <= left ? 0x3c00u : 0u) | (16 * t + 2 * i + 1 <= left ? 0x3c000000u : 0u);
-                        const uint4 seen[2] = {make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7])};
+                        uint4 seen[2];
+                        seen[0] = make_uint4(seen_pair(0, left), seen_pair(2, left), seen_pair(16, left), seen_pair(18, left));
+                        seen[1] = make_uint4(seen_pair(32, left), seen_pair(34, left), seen_pair(48, left), seen_pair(50, left));
 #pragma unroll
                         for (int t = 0; t < kTiles; ++t) {
-                            uint4 clean[2], marks[2];
-                            split_nan(codes_to_f16(vx[t].x, vx[t].y, to_unit), clean[0], marks[0]);
-                            split_nan(codes_to_f16(vx[t].z, vx[t].w, to_unit), clean[1], marks[1]);
-                            o[mt][t] = mfma16<FC_F16>(clean[0], p[mt][0], o[mt][t]);
-                            o[mt][t] = mfma16<FC_F16>(clean[1], p[mt][1], o[mt][t]);
                             f32x4_t count = {0.f, 0.f, 0.f, 0.f};
-                            count = mfma16<FC_F16>(marks[0], seen[0], count);
-                            count = mfma16<FC_F16>(marks[1], seen[1], count);
+                            count = mfma16<FC_F16>(nan_marks(vx[t].x, vx[t].y), seen[0], count);
+                            count = mfma16<FC_F16>(nan_marks(vx[t].z, vx[t].w), seen[1], count);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) o[mt][t][i] = count[i] > 0.f ? __builtin_nanf("") : o[mt][t][i];
                         }
                     }
-                } else {
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) {
-                        const uint4 v0 = codes_to_f16(vx[t].x, vx[t].y, to_unit), v1 = codes_to_f16(vx[t].z, vx[t].w, to_unit);
-#pragma unroll
-                        for (int mt = 0; mt < MT; ++mt) {
-                            o[mt][t] = mfma16<FC_F16>(v0, p[mt][0], o[mt][t]);
-                            o[mt][t] = mfma16<FC_F16>(v1, p[mt][1], o[mt][t]);
-                        }
-                    }
+                    for (int t = 0; t < kTiles; ++t) vx[t] = without_nan(vx[t]);
                 }
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    const uint4 v0 = codes_to_f16(vx[t].x, vx[t].y, to_unit), v1 = codes_to_f16(vx[t].z, vx[t].w, to_unit);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        o[mt][t] = mfma16<FC_F16>(v0, p[mt][0], o[mt][t]);
+                        o[mt][t] = mfma16<FC_F16>(v1, p[mt][1], o[mt][t]);
+                    }
+                    bring_values(codes_next, t);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) bring_values(codes_next, t);
             }
-            if (more) bring_values();
             block = block_next, pool = pool_next, scales = scales_next;
-            block_next = block_after, pool_next = pool_after;
         }
     }
 };
@@ -202,7 +218,7 @@ __device__ __forceinline__ float row_sum(float v)
 __device__ __forceinline__ int listed_blocks(const AttnArgs &a, int pos) { return pos < 0 ? 0 : min(pos / kBlock + 1, a.selected_width); }
 
 // Waves a SIMD that the registers allow without spilling.
-template <int DP, int MT> constexpr int kOccupancy = DP * MT <= 64 ? 3 : DP * MT <= 128 ? 2 : 1;
+template <int DP, int MT> constexpr int kOccupancy = DP * MT <= 64 ? 4 : DP * MT <= 128 ? 2 : 1;
 
 template <int DT, int DP, int MT, bool LIST> __global__ __launch_bounds__(kThreads, (kOccupancy<DP, MT>)) void k_attend_rows(AttnArgs a)
 {

@@ -83,16 +83,20 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
         }
     };
     if (begin < end) bring(begin);
-    // where the thread's pieces go and where the lane's operands are, from the buffer's start on
-    const uint32_t key_to = threadIdx.x / (DP / 16) * kKeyRow + threadIdx.x % (DP / 16) * 32;
+    // where the thread's first pieces go and where the lane's operands are, from the buffer's start on
+    auto key_place = [](uint32_t piece) {       // (see key_piece)
+        const uint32_t channel = (piece >> 6) % (DP / 64) * 64 + (piece >> 4 & 3) * 16, token = (piece >> 6) / (DP / 64) * 16 + (piece & 15);
+        return token * kKeyRow + channel * 2;
+    };
+    const uint32_t key_to = key_place(threadIdx.x);
     // four words of four tokens 16 w + 4 quarter .. + 3: as the scores' lanes hold them, half `quarter & 1`
-    const uint32_t value_to = kKeys + (threadIdx.x >> 2) * kValueRow + (threadIdx.x & 1) * 16 + (threadIdx.x >> 1 & 1) * 8;
+    const uint32_t value_to = kKeys + ((threadIdx.x >> 6) * 16 + (threadIdx.x & 15)) * kValueRow + (threadIdx.x >> 4 & 1) * 16 + (threadIdx.x >> 5 & 1) * 8;
     const uint32_t key_at = col * kKeyRow + half * 16, value_at = kKeys + col * kValueRow + half * 16;
     uint32_t buffer = 0;
     for (int block = begin; block < end; ++block, buffer = kBuffer - buffer) {
         const bool here = there;
         const float scale_k = here ? scales.x : 1.f, scale_v = here ? __builtin_fabsf(scales.y) : unit_v;
-        const bool strange = here && scales.y < 0.f;
+        const bool strange = here && scales.y < 0.f;        // (NaN among the values: zeros in LDS, found again below)
         if (!keeps_unit(scale_v, unit_v)) {
             const float factor = pow2_ratio(unit_v, scale_v);
 #pragma unroll
@@ -104,12 +108,12 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
         const unsigned char *const keys = lds + buffer + key_at, *const values = lds + buffer + value_at;
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
-            // (kThreads pieces further: so many rows of keys, so many channels)
-            constexpr uint32_t kKeyStep = kThreads / (DP / 16) * kKeyRow, kValueStep = kThreads / 4 * kValueRow;
-            uint32_t key_step = i * kKeyStep;
-            if constexpr (kThreads % (DP / 16)) key_step = (threadIdx.x + i * kThreads) / (DP / 16) * kKeyRow + (threadIdx.x + i * kThreads) % (DP / 16) * 32 - key_to;
+            // (kThreads pieces further; a constant unless they split a token's channels)
+            constexpr uint32_t kValueStep = kThreads / 4 * kValueRow;
+            const uint32_t key_step = DP % 192 ? key_place(i * kThreads) : key_place(threadIdx.x + i * kThreads) - key_to;
             *reinterpret_cast<uint4 *>(keys_to + key_step) = codes_to_16<DT>(kx[i].x, kx[i].y);
             *reinterpret_cast<uint4 *>(keys_to + key_step + 16) = codes_to_16<DT>(kx[i].z, kx[i].w);
+            if (strange) vx[i] = without_nan(vx[i]);
             const uint4 first = codes_to_f16(vx[i].x, vx[i].y, to_unit), second = codes_to_f16(vx[i].z, vx[i].w, to_unit);
             const uint2 words[4] = {make_uint2(first.x, first.y), make_uint2(first.z, first.w), make_uint2(second.x, second.y), make_uint2(second.z, second.w)};
 #pragma unroll
@@ -168,19 +172,13 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
             p[2 * t + 1] = make_uint4(w[4], w[5], w[6], w[7]);
         }
 
-        if (partly && strange) {
-            // NaN among values that some rows do not see: see k_attend_rows
-            uint4 seen[4];
 #pragma unroll
-            for (int step = 0; step < 4; ++step) {
-                uint32_t w[4];
+        for (int t = 0; t < kOut; ++t)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int first = 16 * step + 8 * (j >> 1) + 2 * (j & 1);
-                    w[j] = (first <= left ? 0x3c00u : 0u) | (first + 1 <= left ? 0x3c000000u : 0u);
-                }
-                seen[step] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
+            for (int step = 0; step < 4; ++step)
+                o[t] = mfma_32<FC_F16>(*reinterpret_cast<const uint4 *>(values + 32 * t * kValueRow + 32 * step), p[step], o[t]);
+        if (strange) {
+            const uint8_t *const codes = g.codes + unit_of(g, max(pool_block(g, b, block), 0), h) * (2 * kBlock * DP);
 #pragma unroll
             for (int t = 0; t < kOut; ++t) {
                 f32x16_t count;
@@ -188,21 +186,17 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
                 for (int i = 0; i < 16; ++i) count[i] = 0.f;
 #pragma unroll
                 for (int step = 0; step < 4; ++step) {
-                    uint4 clean, marks;
-                    split_nan(*reinterpret_cast<const uint4 *>(values + 32 * t * kValueRow + 32 * step), clean, marks);
-                    o[t] = mfma_32<FC_F16>(clean, p[step], o[t]);
-                    count = mfma_32<FC_F16>(marks, seen[step], count);
+                    // tokens 16 step + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
+                    const uint32_t lo = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * half) + 4 * step);
+                    const uint32_t hi = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * (half + 2)) + 4 * step);
+                    const uint4 seen = make_uint4(seen_pair(16 * step, left), seen_pair(16 * step + 2, left), seen_pair(16 * step + 8, left),
+                                                  seen_pair(16 * step + 10, left));
+                    count = mfma_32<FC_F16>(nan_marks(lo, hi), seen, count);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[t][i] = count[i] > 0.f ? __builtin_nanf("") : o[t][i];
             }
-            continue;
         }
-#pragma unroll
-        for (int t = 0; t < kOut; ++t)
-#pragma unroll
-            for (int step = 0; step < 4; ++step)
-                o[t] = mfma_32<FC_F16>(*reinterpret_cast<const uint4 *>(values + 32 * t * kValueRow + 32 * step), p[step], o[t]);
     }
 
     l += __shfl_xor(l, 32);

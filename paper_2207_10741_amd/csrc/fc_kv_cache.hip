@@ -78,9 +78,8 @@ template <int DT> __device__ __forceinline__ float finite_amax(const uint4 &x, f
 template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a)
 {
     constexpr int kChunks = DP / 8, kRows = kThreads / kChunks * 4, kRounds = (kBlock + kRows - 1) / kRows;
-    constexpr int kPitch = 17;      // words of a row of values in LDS
     __shared__ float scratch[4];
-    __shared__ uint32_t turned[DP * kPitch];
+    __shared__ __align__(16) uint8_t image[2 * kBlock * DP];        // the unit's codes: new tokens' (of a block that is begun, all)
     __shared__ int sums[DP];
     const KvGeom &g = a.kv;
     const int b = blockIdx.z, h = blockIdx.y;
@@ -93,7 +92,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
     if (pool < 0) return;
     const int old = min(max(from - at, 0), kBlock), end = min(s.len - at, kBlock);    // new tokens of the block: old .. end - 1
     const int64_t unit = unit_of(g, pool, h);
-    uint8_t *const kc = g.codes + unit * (2 * kBlock * DP), *const vc = kc + kBlock * DP;
+    uint8_t *const unit_codes = g.codes + unit * (2 * kBlock * DP);
     const int c = threadIdx.x % kChunks, r = threadIdx.x / kChunks;
 
     uint4 kx[kRounds][4], vx[kRounds][4];
@@ -134,17 +133,12 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
         strange |= was.y < 0.f;
         ks = fmaxf(ks, was.x);
         vs = fmaxf(vs, was_v);
+        // (of tokens that are not there nothing is read)
         if (ks != was.x)
-            for (int i = threadIdx.x; i < old * (DP / 4); i += kThreads) {
-                uint32_t *p = reinterpret_cast<uint32_t *>(kc) + i;
-                *p = rescale4(*p, was.x / ks);
-            }
-        if (vs != was_v)        // (places behind the old tokens hold nothing yet)
-            for (int i = threadIdx.x; i < kBlock * (DP / 4); i += kThreads) {
-                uint32_t *p = reinterpret_cast<uint32_t *>(vc) + i;
-                *p = rescale4(*p, was_v / vs);
-            }
-        __syncthreads();        // (the scales have been read, and values' words are rewritten by other threads below)
+            for (int i = threadIdx.x; i < kBlock * (DP / 16); i += kThreads) rescale16(reinterpret_cast<uint4 *>(unit_codes) + i, was.x / ks);
+        if (vs != was_v)
+            for (int i = threadIdx.x; i < kBlock * (DP / 16); i += kThreads) rescale16(reinterpret_cast<uint4 *>(unit_codes + kBlock * DP) + i, was_v / vs);
+        __syncthreads();        // (the scales have been read, and pieces are rewritten by other threads below)
     }
     if (threadIdx.x == 0) g.scales[unit] = make_float2(ks, strange ? -vs : vs);
 
@@ -170,29 +164,37 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
                 column[2 * i + 1] |= (v2 >> 8 & 0xffu) << (8 * j);
             }
             codes[round][j] = make_uint2(packed[0], packed[1]);
-            // a block that is begun is written whole, so that no place of it holds a NaN that its scale does not tell of
-            if (4 * r < kRows && t < kBlock && t >= old && (old == 0 || t < end))
-                *reinterpret_cast<uint2 *>(kc + t * DP + 8 * c) = codes[round][j];
+            if (4 * r < kRows && t < kBlock) *reinterpret_cast<uint2 *>(image + key_piece<DP>(t, 8 * c) + 8 * (c & 1)) = codes[round][j];
         }
         const int t0 = round * kRows + 4 * r;
         if (4 * r < kRows && t0 < kBlock)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) turned[(8 * c + i) * kPitch + value_place(t0) / 4] = column[i];
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t *>(image + value_piece<DP>(8 * c + i, value_place(t0)) + (value_place(t0) & 15)) = column[i];
     }
     __syncthreads();
-    // words of four tokens; a word with old or absent tokens keeps their bytes
-    for (int i = threadIdx.x; i < DP * 16; i += kThreads) {
-        const int channel = i >> 4, word = i & 15;
-        const int t0 = (word >> 1 & 1) << 5 | (word & 1) << 4 | word >> 2 << 2;
-        uint32_t *p = reinterpret_cast<uint32_t *>(vc) + i;
-        const uint32_t fresh = turned[channel * kPitch + word];
+    // A block that is begun is written whole, so that no place of it holds a NaN that its scale does not tell of; else the old tokens keep their bytes.
+    for (int i = threadIdx.x; i < 2 * kBlock * (DP / 16); i += kThreads) {
+        uint4 *const p = reinterpret_cast<uint4 *>(unit_codes) + i;
+        const uint4 fresh = reinterpret_cast<const uint4 *>(image)[i];
         if (old == 0) {
             *p = fresh;
-        } else if (t0 + 3 >= old && t0 < end) {
-            uint32_t take = 0;
+        } else if (i < kBlock * (DP / 16)) {
+            const int t = i / DP * 16 + (i & 15);            // (a piece of keys is one token's)
+            if (t >= old && t < end) *p = fresh;
+        } else {
+            uint32_t take[4];                               // four words of four tokens
 #pragma unroll
-            for (int j = 0; j < 4; ++j) take |= t0 + j >= old && t0 + j < end ? 0xffu << (8 * j) : 0u;
-            *p = (*p & ~take) | (fresh & take);
+            for (int w = 0; w < 4; ++w) {
+                const int t0 = 16 * w + 4 * (i >> 4 & 3);
+                take[w] = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) take[w] |= t0 + j >= old && t0 + j < end ? 0xffu << (8 * j) : 0u;
+            }
+            if (take[0] | take[1] | take[2] | take[3]) {
+                const uint4 had = *p;
+                *p = make_uint4((had.x & ~take[0]) | (fresh.x & take[0]), (had.y & ~take[1]) | (fresh.y & take[1]),
+                                (had.z & ~take[2]) | (fresh.z & take[2]), (had.w & ~take[3]) | (fresh.w & take[3]));
+            }
         }
     }
 
@@ -213,10 +215,11 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
         }
     } else {
         for (int i = threadIdx.x; i < kBlock * kChunks; i += kThreads) {
+            const int channel = i % kChunks * 8;
             float sum[8] = {};
-            add_codes(*reinterpret_cast<const uint2 *>(kc + 8 * i), sum);
+            add_codes(*reinterpret_cast<const uint2 *>(unit_codes + key_piece<DP>(i / kChunks, channel) + (channel & 8)), sum);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) atomicAdd(&sums[i % kChunks * 8 + j], (int)(sum[j] * 512.f));
+            for (int j = 0; j < 8; ++j) atomicAdd(&sums[channel + j], (int)(sum[j] * 512.f));
         }
     }
     __syncthreads();
@@ -251,7 +254,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
     const int32_t pool = pool_block(g, b, token / kBlock);
     if (pool < 0) return;
     const int64_t unit = unit_of(g, pool, h);
-    uint8_t *const kc = g.codes + unit * (2 * kBlock * DP), *const vc = kc + kBlock * DP;
+    uint8_t *const unit_codes = g.codes + unit * (2 * kBlock * DP);
     const float2 was = old ? g.scales[unit] : make_float2(0.f, 0.f);
     float ka = 0.f, va = 0.f;
     bool strange = was.y < 0.f;
@@ -270,22 +273,24 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
     }
     const float was_v = __builtin_fabsf(was.y);
     const float ks = fmaxf(pow2_of(scale_exponent(ka)), was.x), vs = fmaxf(pow2_of(scale_exponent(va)), was_v);
-    if (old && ks != was.x)
-        for (int i = lane; i < old * (DP / 16); i += 64) rescale16(reinterpret_cast<uint4 *>(kc) + i, was.x / ks);
-    if (old == 0) {         // (a block that is begun: see k_kv_append)
-        for (int i = lane; i < kBlock * (DP / 16); i += 64) reinterpret_cast<uint4 *>(vc)[i] = make_uint4(0, 0, 0, 0);
-    } else if (vs != was_v) {
-        for (int i = lane; i < kBlock * (DP / 16); i += 64) rescale16(reinterpret_cast<uint4 *>(vc) + i, was_v / vs);
+    uint4 *const keys = reinterpret_cast<uint4 *>(unit_codes), *const values = reinterpret_cast<uint4 *>(unit_codes + kBlock * DP);
+    if (old == 0) {         // (a block that is begun: see k_kv_append; of keys that are not there nothing is read)
+        for (int i = lane; i < kBlock * (DP / 16); i += 64) values[i] = make_uint4(0, 0, 0, 0);
+    } else {
+        if (ks != was.x)
+            for (int i = lane; i < kBlock * (DP / 16); i += 64) rescale16(keys + i, was.x / ks);
+        if (vs != was_v)
+            for (int i = lane; i < kBlock * (DP / 16); i += 64) rescale16(values + i, was_v / vs);
     }
-    if (old == 0 || vs != was_v) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");     // other lanes' stores to the bytes below
+    if (old == 0 || ks != was.x || vs != was_v) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // other lanes' stores to the bytes below
     const float ki = 1.f / ks, vi = 1.f / vs;
     const int place = value_place(old);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int c = lane * kEach + i;
         const int two = __builtin_amdgcn_cvt_pk_fp8_f32(code_of(kv[i], ki), code_of(vv[i], vi), 0, false);
-        kc[old * DP + c] = (uint8_t)two;
-        vc[c * kBlock + place] = (uint8_t)(two >> 8);
+        unit_codes[key_piece<DP>(old, c) + (c & 15)] = (uint8_t)two;
+        unit_codes[value_piece<DP>(c, place) + (place & 15)] = (uint8_t)(two >> 8);
     }
     if (lane == 0) g.scales[unit] = make_float2(ks, strange ? -vs : vs);
     if (old < kBlock - 1) return;
@@ -298,7 +303,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
         float x = 0.f;
 #pragma unroll 8
         for (int t = 0; t < kBlock; ++t) {
-            const float f = __builtin_amdgcn_cvt_f32_fp8(kc[t * DP + lane * kEach + i], 0);
+            const float f = __builtin_amdgcn_cvt_f32_fp8(unit_codes[key_piece<DP>(t, lane * kEach + i) + (lane * kEach + i & 15)], 0);
             x += f == f ? f : 0.f;
         }
         sum[i] = (int)(x * 512.f);
@@ -319,7 +324,7 @@ struct ReadArgs {
 
 template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs a)
 {
-    __shared__ uint32_t turned[DP * 17];
+    __shared__ __align__(16) uint8_t image[2 * kBlock * DP];
     const KvGeom &g = a.kv;
     const int b = blockIdx.z, h = blockIdx.y;
     const Sequence s = sequence_of(g, b);
@@ -341,7 +346,9 @@ template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs
     const int32_t pool = pool_block(g, b, block);
     const bool there = pool >= 0;
     const int64_t unit = unit_of(g, max(pool, 0), h);
-    const uint8_t *const kc = g.codes + unit * (2 * kBlock * DP), *const vc = kc + kBlock * DP;
+    const uint4 *const codes = reinterpret_cast<const uint4 *>(g.codes + unit * (2 * kBlock * DP));
+    for (int i = threadIdx.x; i < 2 * kBlock * (DP / 16); i += kThreads) reinterpret_cast<uint4 *>(image)[i] = there ? codes[i] : make_uint4(0, 0, 0, 0);
+    __syncthreads();
     const float2 scale = there ? g.scales[unit] : make_float2(0.f, 0.f);
     const float vs = __builtin_fabsf(scale.y);
     const int64_t row0 = s.row0 + (int64_t)(at - s.pos0);
@@ -360,21 +367,19 @@ template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs
         for (int i = threadIdx.x; i < kBlock * (DP / 4); i += kThreads) {
             const int t = i / (DP / 4), c = i % (DP / 4) * 4;
             if (t < begin || t >= end) continue;
-            const uint32_t x = there ? reinterpret_cast<const uint32_t *>(kc)[i] : 0;
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(image + key_piece<DP>(t, c) + (c & 15));
             const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(x, 0) * scale.x, __builtin_amdgcn_cvt_f32_fp8(x, 1) * scale.x,
                                 __builtin_amdgcn_cvt_f32_fp8(x, 2) * scale.x, __builtin_amdgcn_cvt_f32_fp8(x, 3) * scale.x};
             put(a.k, t, c, v);
         }
     if (!a.v) return;
-    for (int i = threadIdx.x; i < DP * 16; i += kThreads) turned[(i >> 4) * 17 + (i & 15)] = there ? reinterpret_cast<const uint32_t *>(vc)[i] : 0;
-    __syncthreads();
     for (int i = threadIdx.x; i < 16 * (DP / 4); i += kThreads) {
         const int c = i % (DP / 4) * 4, t = i / (DP / 4) * 4;       // four tokens of four channels
         if (t + 3 < begin || t >= end) continue;
         float v[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t x = turned[(c + j) * 17 + value_place(t) / 4];
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(image + value_piece<DP>(c + j, value_place(t)) + (value_place(t) & 15));
             v[0][j] = __builtin_amdgcn_cvt_f32_fp8(x, 0) * vs, v[1][j] = __builtin_amdgcn_cvt_f32_fp8(x, 1) * vs;
             v[2][j] = __builtin_amdgcn_cvt_f32_fp8(x, 2) * vs, v[3][j] = __builtin_amdgcn_cvt_f32_fp8(x, 3) * vs;
         }

@@ -55,18 +55,43 @@ bool known_type(int32_t dtype) { return dtype == FC_BF16 || dtype == FC_F16; }
 
 // How a call's rows and blocks are cut.
 struct Plan {
-    int32_t rows_tile, tiles, splits, per_split;
+    int32_t rows_tile, tiles, splits, per_split, waves;
     int64_t units;              // of rows: sequences x key heads x tiles
     bool whole;                 // a wave takes a token's whole list
     size_t counters, workspace; // bytes; none where nothing is split
 };
 
-// Pieces of the long axis: two workgroups a CU, as many as are there at once, and no fewer than four blocks a piece (one a wave).  More pieces
-// balance nothing and take longer to join: us at 512 / 768 / 1024 / 2048 workgroups, 64 sequences of 2000 to 8192 tokens, 8 key heads of 128,
-// 134 / 145 / 145 / 146; one of 131000 57 / 63 / 69 / 94; pieces of 517 tokens of three over 5003 103 / 119 / 119 / 118.
-constexpr int64_t kWorkgroups = 512;
-// Lists: from this many on there are enough to fill the chip with a wave each.
-constexpr int64_t kWholeLists = 4096;
+// Pieces of the long axis where memory is the bound: eight waves a CU, as many as are there at once, and no piece of less than a block a wave.  More pieces
+// balance nothing and take longer to join.
+void cut_to_fill(int64_t units, int32_t blocks, int waves, int32_t *splits, int32_t *per_split)
+{
+    const int64_t workgroups = 2048 / waves, most = (blocks + waves - 1) / waves;
+    int64_t n = (workgroups + units - 1) / units;
+    n = n < 1 ? 1 : n > most ? most : n;
+    *per_split = (int32_t)((blocks + n - 1) / n + waves - 1) / waves * waves;
+    *splits = (blocks + *per_split - 1) / *per_split;
+}
+
+// ... and where the matrix cores are: workgroups run in rounds of two a CU, one of them alone 1.4 times as fast, so the number of pieces that gives the
+// shortest rounds, with four blocks' time to begin and end a piece and half a block's to join one.  `units` is what the call's rows come to, not the
+// bound: pieces of up to 517 tokens of three sequences, us at 1 / 2 / 3 / 4 / 5 / 6 pieces 130 / 102 / 88 / 77 / 96 / 92.
+void cut_for_rounds(int64_t units, int32_t blocks, int32_t *splits, int32_t *per_split)
+{
+    int64_t best = 0;
+    *splits = 1, *per_split = blocks;
+    for (int64_t n = 1; n <= 64 && n <= blocks; ++n) {
+        const int64_t per = (blocks + n - 1) / n, pieces = (blocks + per - 1) / per, workgroups = units * pieces;
+        const int64_t round = workgroups <= 256 ? 10 : (workgroups + 511) / 512 * 14;
+        const int64_t cost = round * (per + 4) + (pieces > 1 ? 5 * (pieces + 4) : 0);
+        if (n == 1 || cost < best) {
+            best = cost;
+            *splits = (int32_t)pieces;
+            *per_split = (int32_t)per;
+        }
+    }
+}
+
+constexpr int64_t kWholeLists = 1024;
 
 int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *p)
 {
@@ -91,13 +116,23 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
     }
     const int64_t units = p->units = (int64_t)d->batch * d->kv_heads * p->tiles;
     p->whole = list && units >= kWholeLists;
-    int64_t splits = p->whole ? 1 : (kWorkgroups + units - 1) / units;
-    const int64_t most = (blocks + 3) / 4;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
-    const int64_t per = ((blocks + splits - 1) / splits + 3) / 4 * 4;
-    p->per_split = (int32_t)per;
-    p->splits = p->whole ? 1 : (int32_t)((blocks + per - 1) / per);
+    if (p->whole) {
+        p->per_split = blocks;
+        p->splits = 1;
+    } else if (p->rows_tile == kTileRows) {
+        const int64_t filled = ((int64_t)d->tokens * group / kTileRows + (d->batch + 1) / 2) * d->kv_heads;
+        cut_for_rounds(filled < units ? filled : units, blocks, &p->splits, &p->per_split);
+    } else {
+        p->waves = 4;
+        cut_to_fill(units, blocks, p->waves, &p->splits, &p->per_split);
+        // Few sequences over long axes: half as many pieces of eight waves (us at 4 -> 8 waves, tokens of sequences with 8 key heads of 128: one of 2000 /
+        // 4000 / 8000 / 16000 / 32000 8.9 / 9.8 / 12.6 / 19.8 / 25.4 -> 10.0 / 10.6 / 11.4 / 13.4 / 19.5, two of 16000 22.7 -> 19.2, four of 8000
+        // 18.9 -> 18.9, 64 of 2000 44.2 -> 47.2)
+        if (!list && p->rows_tile == 16 && g.dp <= 128 && p->splits > 16) {
+            p->waves = 8;
+            cut_to_fill(units, blocks, p->waves, &p->splits, &p->per_split);
+        }
+    }
     if (units * p->splits >= INT32_MAX || (int64_t)p->splits * p->rows_tile * g.dp * 4 >= INT32_MAX) return FC_ERR_RANGE;
     p->counters = p->splits == 1 ? 0 : align_up((size_t)units * sizeof(int32_t), 256);
     p->workspace = p->counters + (p->splits == 1 ? 0 : (size_t)units * p->splits * p->rows_tile * (g.dp * sizeof(float) + sizeof(float2)));
@@ -160,7 +195,7 @@ int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, con
         if (e == hipSuccess) e = launch_attend_lists(a, d->dtype, p.whole, s);
     } else {
         e = counters ? launch_zero_i32(a.arrived, counters, s) : hipSuccess;
-        if (e == hipSuccess) e = p.rows_tile <= 32 ? launch_attend_rows(a, d->dtype, p.rows_tile, s) : launch_attend_tile(a, d->dtype, s);
+        if (e == hipSuccess) e = p.rows_tile <= 32 ? launch_attend_rows(a, d->dtype, p.rows_tile, p.waves, s) : launch_attend_tile(a, d->dtype, s);
     }
     return e == hipSuccess ? FC_OK : FC_ERR_HIP;
 }

@@ -384,8 +384,8 @@ hipError_t launch_kv_append(const KvGeom &g, int dtype, const uint16_t *k, const
                             int64_t v_head, bool wide_k, bool wide_v, hipStream_t s);
 hipError_t launch_kv_read(const KvGeom &g, float *k, float *v, hipStream_t s);
 
-// Few rows (see fc_attn_rows.hip); rows_tile: rows a workgroup holds, 16 or 32.
-hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s);
+// Few rows (see fc_attn_rows.hip); rows_tile: rows a workgroup holds, 16 or 32; waves: its waves, 4 or (16 rows of up to 128 channels) 8.
+hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, int waves, hipStream_t s);
 // 16 rows of one token, over its list of blocks; a wave's, or (a.splits counts the pieces) a workgroup's.
 hipError_t launch_attend_lists(const AttnArgs &a, int dtype, bool whole, hipStream_t s);
 

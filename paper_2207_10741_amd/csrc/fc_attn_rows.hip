@@ -4,16 +4,13 @@
 // from memory to registers in the order the matrix instructions want it (fc_attn_internal.hpp): no LDS, and no lane exchange but for the
 // rows' maximum.  The next block's keys are on their way as soon as this one's are used, and its values likewise, so that a wave always has
 // half a block in flight.
-//   k_attend_rows: the four waves of a workgroup take every fourth block of a piece of the sequence (or of a token's list) and are joined through
-//     LDS; the last workgroup joins the pieces.
+//   k_attend_rows: the waves of a workgroup take a piece's blocks of the sequence (or of a token's list) in turn and are joined through LDS; the last workgroup joins the pieces.
 //   k_attend_lists: a wave takes a token's whole list.
 #include "fc_attn_internal.hpp"
 
 namespace fc {
 
 namespace {
-
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 // A wave's rows and its running softmax.
 template <int DT, int DP, int MT> struct Rows {
@@ -219,9 +216,11 @@ __device__ __forceinline__ int listed_blocks(const AttnArgs &a, int pos) { retur
 
 // Waves a SIMD that the registers allow without spilling.
 template <int DP, int MT> constexpr int kOccupancy = DP * MT <= 64 ? 4 : DP * MT <= 128 ? 2 : 1;
+constexpr int kListWaves = 4;
 
-template <int DT, int DP, int MT, bool LIST> __global__ __launch_bounds__(kThreads, (kOccupancy<DP, MT>)) void k_attend_rows(AttnArgs a)
+template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_bounds__(64 * WAVES, (kOccupancy<DP, MT>)) void k_attend_rows(AttnArgs a)
 {
+    constexpr int kWaves = WAVES, kThreads = 64 * kWaves;
     constexpr int kChunks = DP / 64, kTiles = DP / 16, kRows = 16 * MT, kPitch = DP + 4;
     extern __shared__ __align__(16) float lds[];
     float *const lds_o = lds, *const lds_m = lds + kWaves * kRows * kPitch, *const lds_l = lds_m + kWaves * kRows;
@@ -324,13 +323,13 @@ template <int DT, int DP, int MT, bool LIST> __global__ __launch_bounds__(kThrea
 
 // A wave takes up to 16 heads of one token and the token's whole list.  An XCD takes an eighth of the units in one piece: neighbouring tokens of a head
 // share blocks.
-template <int DT, int DP> __global__ __launch_bounds__(kThreads, (kOccupancy<DP, 1>)) void k_attend_lists(AttnArgs a)
+template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupancy<DP, 1>)) void k_attend_lists(AttnArgs a)
 {
     constexpr int kChunks = DP / 64, kTiles = DP / 16;
     const KvGeom &g = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
     const uint32_t eighth = gridDim.x / 8;      // (the grid is a multiple of eight)
-    uint32_t at = (blockIdx.x % 8 * eighth + blockIdx.x / 8) * kWaves + wave;
+    uint32_t at = (blockIdx.x % 8 * eighth + blockIdx.x / 8) * kListWaves + wave;
     const int tile = at % a.tiles;
     at /= a.tiles;
     const int h = at % g.kv_heads, b = at / g.kv_heads;
@@ -359,43 +358,45 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, (kOccupancy<DP,
     for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit_v, w.m[0], sum);
 }
 
-template <int DT, int DP, int MT, bool LIST> hipError_t run_rows(const AttnArgs &a, hipStream_t s)
+template <int DT, int DP, int MT, int WAVES, bool LIST> hipError_t run_rows(const AttnArgs &a, hipStream_t s)
 {
-    constexpr size_t lds = ((size_t)kWaves * 16 * MT * (DP + 4 + 2) + 4) * sizeof(float);
+    constexpr size_t lds = ((size_t)WAVES * 16 * MT * (DP + 4 + 2) + 4) * sizeof(float);
     if (lds > 64 * 1024) {
-        const hipError_t e = raise_lds<k_attend_rows<DT, DP, MT, LIST>>(lds);
+        const hipError_t e = raise_lds<k_attend_rows<DT, DP, MT, WAVES, LIST>>(lds);
         if (e != hipSuccess) return e;
     }
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
-    k_attend_rows<DT, DP, MT, LIST><<<dim3((uint32_t)(units * a.splits)), kThreads, lds, s>>>(a);
+    k_attend_rows<DT, DP, MT, WAVES, LIST><<<dim3((uint32_t)(units * a.splits)), 64 * WAVES, lds, s>>>(a);
     return hipGetLastError();
 }
 
 template <int DT, int DP> hipError_t run_lists(const AttnArgs &a, bool whole, hipStream_t s)
 {
-    if (!whole) return run_rows<DT, DP, 1, true>(a, s);
+    if (!whole) return run_rows<DT, DP, 1, 4, true>(a, s);
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
-    k_attend_lists<DT, DP><<<dim3((uint32_t)((units + 8 * kWaves - 1) / (8 * kWaves) * 8)), kThreads, 0, s>>>(a);
+    k_attend_lists<DT, DP><<<dim3((uint32_t)((units + 8 * kListWaves - 1) / (8 * kListWaves) * 8)), 64 * kListWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <int DT, int DP> hipError_t run_dim(const AttnArgs &a, int rows_tile, hipStream_t s)
+template <int DT, int DP> hipError_t run_dim(const AttnArgs &a, int rows_tile, int waves, hipStream_t s)
 {
-    if constexpr (DP <= 128)
-        if (rows_tile == 32) return run_rows<DT, DP, 2, false>(a, s);
-    return run_rows<DT, DP, 1, false>(a, s);
+    if constexpr (DP <= 128) {
+        if (rows_tile == 32) return run_rows<DT, DP, 2, 4, false>(a, s);
+        if (waves == 8) return run_rows<DT, DP, 1, 8, false>(a, s);
+    }
+    return run_rows<DT, DP, 1, 4, false>(a, s);
 }
 
 } // namespace
 
-hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s)
+hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, int waves, hipStream_t s)
 {
     const bool b = dtype == FC_BF16;
     switch (a.kv.dp) {
-    case 64: return b ? run_dim<FC_BF16, 64>(a, rows_tile, s) : run_dim<FC_F16, 64>(a, rows_tile, s);
-    case 128: return b ? run_dim<FC_BF16, 128>(a, rows_tile, s) : run_dim<FC_F16, 128>(a, rows_tile, s);
-    case 192: return b ? run_dim<FC_BF16, 192>(a, rows_tile, s) : run_dim<FC_F16, 192>(a, rows_tile, s);
-    default: return b ? run_dim<FC_BF16, 256>(a, rows_tile, s) : run_dim<FC_F16, 256>(a, rows_tile, s);
+    case 64: return b ? run_dim<FC_BF16, 64>(a, rows_tile, waves, s) : run_dim<FC_F16, 64>(a, rows_tile, waves, s);
+    case 128: return b ? run_dim<FC_BF16, 128>(a, rows_tile, waves, s) : run_dim<FC_F16, 128>(a, rows_tile, waves, s);
+    case 192: return b ? run_dim<FC_BF16, 192>(a, rows_tile, waves, s) : run_dim<FC_F16, 192>(a, rows_tile, waves, s);
+    default: return b ? run_dim<FC_BF16, 256>(a, rows_tile, waves, s) : run_dim<FC_F16, 256>(a, rows_tile, waves, s);
     }
 }
 

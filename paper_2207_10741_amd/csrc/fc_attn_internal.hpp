@@ -136,10 +136,14 @@ template <int DT> __device__ __forceinline__ uint32_t pack2(float a, float b)
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2_t));
 }
 
-// Eight elements c .. c + 7 of a row of d, zeros behind its end.  wide: 16 bytes lie together (d a multiple of 8, the row 16-byte aligned).
-__device__ __forceinline__ uint4 load8(const uint16_t *__restrict__ row, int c, int d, bool wide)
+// Eight elements c .. c + 7 of a row of d, zeros behind its end.  wide: 16 bytes lie together (d a multiple of 8, the row 16-byte aligned); without a
+// branch, so that loads written one after another are under way together.
+template <bool WIDE> __device__ __forceinline__ uint4 load8(const uint16_t *__restrict__ row, int c, int d)
 {
-    if (wide) return c < d ? *reinterpret_cast<const uint4 *>(row + c) : make_uint4(0, 0, 0, 0);
+    if constexpr (WIDE) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(row + (c < d ? c : 0));
+        return c < d ? x : make_uint4(0, 0, 0, 0);
+    }
     uint32_t v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -148,6 +152,8 @@ __device__ __forceinline__ uint4 load8(const uint16_t *__restrict__ row, int c, 
     }
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
+// The same for code that makes one load at a time.
+__device__ __forceinline__ uint4 load8(const uint16_t *__restrict__ row, int c, int d, bool wide) { return wide ? load8<true>(row, c, d) : load8<false>(row, c, d); }
 
 __device__ __forceinline__ float pow2_of(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }     // -126 <= e <= 127
 

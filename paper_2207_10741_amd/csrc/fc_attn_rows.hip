@@ -33,6 +33,19 @@ template <int DT, int DP, int MT> struct Rows {
         }
     }
 
+    // The lane's row of tile mt.
+    __device__ __forceinline__ void bring_queries(const AttnArgs &a, int mt, const uint16_t *row)
+    {
+        const int quarter = (threadIdx.x & 63) >> 4, d = a.kv.d;
+        if (a.wide) {
+#pragma unroll
+            for (int c = 0; c < 2 * kChunks; ++c) q[mt][c] = flip_signs(load8<true>(row, (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, d), a.signs);
+        } else {
+#pragma unroll
+            for (int c = 0; c < 2 * kChunks; ++c) q[mt][c] = flip_signs(load8<false>(row, (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, d), a.signs);
+        }
+    }
+
     // Blocks first, first + step, ... below end of the sequence or of its list (both in order).
     template <bool LIST>
     __device__ __forceinline__ void run(const AttnArgs &a, int b, int h, const int32_t *__restrict__ list, int first, int step, int end)
@@ -52,16 +65,14 @@ template <int DT, int DP, int MT> struct Rows {
                 held_pool = pool_block(g, b, held_block);
                 held_scales = g.scales[unit_of(g, max(held_pool, 0), h)];
             }
-            __asm__ volatile("" : "+v"(held_block), "+v"(held_pool), "+v"(held_scales.x), "+v"(held_scales.y));      // (waited for here, not in the loop)
         };
+        auto looked_up = [&] { __asm__ volatile("" : "+v"(held_block), "+v"(held_pool), "+v"(held_scales.x), "+v"(held_scales.y)); };    // (waited for there)
         look_up(first);
         int block = __builtin_amdgcn_readlane(held_block, 0), pool = __builtin_amdgcn_readlane(held_pool, 0);
-        float2 scales;
         auto scales_at = [&](int i) {
             return make_float2(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_scales.x), i)),
                                __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_scales.y), i)));
         };
-        scales = scales_at(0);
         // A block's codes: keys at 0, values behind them.  A block that is not there, and the one behind the last, is an empty buffer.
         auto codes_of = [&](int32_t p) {
             return __builtin_amdgcn_make_buffer_rsrc(g.codes + unit_of(g, max(p, 0), h) * (2 * kBlock * DP), 0, p < 0 ? 0 : 2 * kBlock * DP, 0x00020000);
@@ -82,12 +93,15 @@ template <int DT, int DP, int MT> struct Rows {
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) bring_values(codes, t);
         }
+        looked_up();
+        float2 scales = scales_at(0);
 
         int i_next = 1;
         for (int j = first; j < end; j += step, ++i_next) {
             const bool more = j + step < end;
             if (i_next == 64 && more) {
                 look_up(j + step);
+                looked_up();
                 i_next = 0;
             }
             const int block_next = __builtin_amdgcn_readlane(held_block, i_next & 63), pool_next = __builtin_amdgcn_readlane(held_pool, i_next & 63);
@@ -221,7 +235,7 @@ constexpr int kListWaves = 4;
 template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_bounds__(64 * WAVES, (kOccupancy<DP, MT>)) void k_attend_rows(AttnArgs a)
 {
     constexpr int kWaves = WAVES, kThreads = 64 * kWaves;
-    constexpr int kChunks = DP / 64, kTiles = DP / 16, kRows = 16 * MT, kPitch = DP + 4;
+    constexpr int kTiles = DP / 16, kRows = 16 * MT, kPitch = DP + 4;
     extern __shared__ __align__(16) float lds[];
     float *const lds_o = lds, *const lds_m = lds + kWaves * kRows * kPitch, *const lds_l = lds_m + kWaves * kRows;
     int32_t *const lds_flag = reinterpret_cast<int32_t *>(lds_l + kWaves * kRows);
@@ -262,16 +276,11 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
     w.last_least = a.causal ? s.pos0 + token0 : s.len - 1;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-        const int r = 16 * mt + col;
+        // (rows behind the last repeat it and are left out below)
+        const int r = min(16 * mt + col, rows - 1);
         const RowPlace p = LIST ? RowPlace{0, head0 + r} : row_place(a, head0 + r);
-        w.last[mt] = r < rows ? (a.causal ? s.pos0 + token0 + p.token : s.len - 1) : -1;
-#pragma unroll
-        for (int c = 0; c < 2 * kChunks; ++c) {
-            w.q[mt][c] = make_uint4(0, 0, 0, 0);
-            if (r < rows)
-                w.q[mt][c] = flip_signs(load8(a.q + (s.row0 + token0 + p.token) * a.q_row + (int64_t)(h * a.group + p.head) * a.q_head,
-                                              (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, g.d, a.wide), a.signs);
-        }
+        w.last[mt] = a.causal ? s.pos0 + token0 + p.token : s.len - 1;
+        w.bring_queries(a, mt, a.q + (s.row0 + token0 + p.token) * a.q_row + (int64_t)(h * a.group + p.head) * a.q_head);
     }
     const int32_t *const list = LIST ? a.selected + ((int64_t)(s.row0 + token0) * g.kv_heads + h) * a.selected_width : nullptr;
     w.template run<LIST>(a, b, h, list, split * a.per_split + wave, kWaves, end);
@@ -325,7 +334,7 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
 // share blocks.
 template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupancy<DP, 1>)) void k_attend_lists(AttnArgs a)
 {
-    constexpr int kChunks = DP / 64, kTiles = DP / 16;
+    constexpr int kTiles = DP / 16;
     const KvGeom &g = a.kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
     const uint32_t eighth = gridDim.x / 8;      // (the grid is a multiple of eight)
@@ -335,21 +344,14 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     const int h = at % g.kv_heads, b = at / g.kv_heads;
     if (b >= g.batch) return;
     const Sequence s = sequence_of(g, b);
-    const int per_token = (a.group + 15) / 16, token = tile / per_token, head = tile % per_token * 16 + col;
+    const int per_token = (a.group + 15) / 16, token = tile / per_token, head0 = tile % per_token * 16;
     if (token >= s.n) return;
-    const bool valid = head < a.group;
-    const int pos = s.pos0 + token;
+    const bool valid = head0 + col < a.group;
+    const int pos = s.pos0 + token, head = min(head0 + col, a.group - 1);
     Rows<DT, DP, 1> w;
     w.clear();
-    w.last_least = pos;
-    w.last[0] = valid ? pos : -1;
-#pragma unroll
-    for (int c = 0; c < 2 * kChunks; ++c) {
-        w.q[0][c] = make_uint4(0, 0, 0, 0);
-        if (valid)
-            w.q[0][c] = flip_signs(load8(a.q + (s.row0 + token) * a.q_row + (int64_t)(h * a.group + head) * a.q_head,
-                                         (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, g.d, a.wide), a.signs);
-    }
+    w.last_least = w.last[0] = pos;
+    w.bring_queries(a, 0, a.q + (s.row0 + token) * a.q_row + (int64_t)(h * a.group + head) * a.q_head);
     w.template run<true>(a, b, h, a.selected + ((int64_t)(s.row0 + token) * g.kv_heads + h) * a.selected_width, 0, 1, listed_blocks(a, pos));
     const float sum = row_sum(w.l[0]);
     if (!valid) return;

@@ -5,8 +5,8 @@
 // those at or above a threshold, which is found from its highest bit on by counting (ballots), and the list comes out in order by ballots, as the
 // kept lists of masks are made.
 //   k_select: 16 (4) tokens a workgroup; a wave finds one token's threshold.  Prompts.
-//   k_select_one: one token a workgroup of 16 waves, which each count for one of 15 thresholds: four bits a round.  Single tokens, where the
-//     chain of dependent steps is all that counts, and sequences so long that more tokens' scores do not fit LDS.
+//   k_select_one: one token a workgroup of 16 waves, the threshold eight bits a round by counting their values in LDS.  Single tokens, where
+//     the chain of dependent steps is all that counts, and sequences so long that more tokens' scores do not fit LDS.
 #include "fc_attn_internal.hpp"
 
 namespace fc {
@@ -56,14 +56,13 @@ template <int DP> struct Sketches {
     __device__ __forceinline__ void bring(const KvGeom &g, int b, int h, int first, int end)
     {
         const int lane = threadIdx.x & 63, block = first + (lane & 15);
-        const int32_t pool = block < end ? pool_block(g, b, block) : -1;
+        const int32_t pool = pool_block(g, b, min(block, end - 1));
         const int64_t unit = unit_of(g, max(pool, 0), h);
-        weight = pool < 0 ? 0.f : g.weights[unit];
+        // (of a block that is not there another one's sketch, without weight)
+        weight = g.weights[unit];
 #pragma unroll
-        for (int c = 0; c < DP / 64; ++c) {
-            x[c] = i32x4_t{0, 0, 0, 0};
-            if (pool >= 0) x[c] = *reinterpret_cast<const i32x4_t *>(g.sketches + unit * DP + 64 * c + (lane >> 4) * 16);
-        }
+        for (int c = 0; c < DP / 64; ++c) x[c] = *reinterpret_cast<const i32x4_t *>(g.sketches + unit * DP + 64 * c + (lane >> 4) * 16);
+        if (pool < 0) weight = 0.f;
     }
     // keys of blocks 4 (lane / 16) + i and token lane % 16
     __device__ __forceinline__ void score(const i32x4_t (&hi)[DP / 64], const i32x4_t (&lo)[DP / 64], uint32_t (&keys)[4]) const
@@ -230,13 +229,29 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
     }
 }
 
+// Inclusive sum over the wave's lanes, and the sum over each 16 of them in their last lane.
+__device__ __forceinline__ int sum_over_row(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);     // row_shr by 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    return v;
+}
+__device__ __forceinline__ int sum_up_to(int v)
+{
+    v = sum_over_row(v);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);     // the last lane of a row to the next row
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);     // ... of the first half to the second
+    return v;
+}
+
 template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_select_one(SelectArgs a)
 {
-    constexpr int kChunks = DP / 64, kWaves = kThreadsOne / 64, kHeld = 16;
+    constexpr int kChunks = DP / 64, kWaves = kThreadsOne / 64;
     extern __shared__ uint32_t lds_keys[];
-    __shared__ __align__(16) int8_t q8[2][DP];
-    __shared__ int sums[DP], counts[2][kWaves], equal[kWaves];
-    __shared__ uint32_t amax;
+    __shared__ __align__(16) int bins[4][256];
+    __shared__ int aboves[kWaves], equals[kWaves];
     for (int i = blockIdx.x * kThreadsOne + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreadsOne) a.clear[i] = 0;
     const KvGeom &g = a.kv;
     uint32_t at = blockIdx.x;
@@ -250,100 +265,120 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
     int32_t *const out = a.selected + ((int64_t)(s.row0 + token) * g.kv_heads + h) * width;
     if (!fixed_entries(a, own, out, threadIdx.x, kThreadsOne)) return;
     const int scored = own - a.last + 1, candidates = scored - a.first;
+    bins[threadIdx.x >> 8][threadIdx.x & 255] = 0;
 
+    // Every wave rounds the queries for itself: column `col` of the product is head 16 i + col, its scores are summed behind it.
     Sketches<DP> x;
     x.bring(g, b, h, 16 * wave, scored);
-    for (int i = threadIdx.x; i < DP; i += kThreadsOne) sums[i] = 0;
-    if (threadIdx.x == 0) amax = 0;
     const uint16_t *const q = a.q + (int64_t)(s.row0 + token) * a.q_row + (int64_t)h * a.group * a.q_head;
-    const int pieces = a.group * (DP / 8);
-    uint4 mine = make_uint4(0, 0, 0, 0);
-    if ((int)threadIdx.x < pieces) mine = load8(q + (int64_t)(threadIdx.x / (DP / 8)) * a.q_head, threadIdx.x % (DP / 8) * 8, g.d, a.wide);
-    __syncthreads();
-    auto each_piece = [&](auto f) {     // (of more than 1024 the others are read twice)
-        if ((int)threadIdx.x < pieces) f(mine, threadIdx.x % (DP / 8) * 8);
-        for (int i = threadIdx.x + kThreadsOne; i < pieces; i += kThreadsOne)
-            f(load8(q + (int64_t)(i / (DP / 8)) * a.q_head, i % (DP / 8) * 8, g.d, a.wide), i % (DP / 8) * 8);
+    auto piece = [&](int head, int c, int half) {
+        return head < a.group ? load8(q + head * a.q_head, 64 * c + 16 * quarter + 8 * half, g.d, a.wide) : make_uint4(0, 0, 0, 0);
     };
+    uint4 mine[kChunks][2];
     {
-        float most = 0.f;
-        each_piece([&](const uint4 &v, int) { most = largest<DT>(v, most); });
-        if ((int)threadIdx.x < pieces) atomicMax(&amax, __float_as_uint(most));
-    }
-    __syncthreads();
-    const float inverse = pow2_of(-unit_exponent(__uint_as_float(amax)));
-    each_piece([&](const uint4 &v, int c) {
+        const uint16_t *const row = q + min(col, a.group - 1) * a.q_head;
+        if (a.wide) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float e = element<DT>(v, j);
-            if (finite(e)) atomicAdd(&sums[c + j], (int)__builtin_rintf(e * inverse));
-        }
-    });
-    __syncthreads();
-    if (threadIdx.x < DP) {
-        q8[0][threadIdx.x] = (int8_t)(sums[threadIdx.x] >> 7);
-        q8[1][threadIdx.x] = (int8_t)(sums[threadIdx.x] & 127);
-    }
-    __syncthreads();
-    i32x4_t hi[kChunks], lo[kChunks];
+            for (int c = 0; c < 2 * kChunks; ++c) mine[c >> 1][c & 1] = load8<true>(row, (c >> 1) * 64 + 16 * quarter + (c & 1) * 8, g.d);
+        } else {
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c) {     // (one column of the sixteen)
-        hi[c] = lo[c] = i32x4_t{0, 0, 0, 0};
-        if (col == 0) {
-            hi[c] = *reinterpret_cast<const i32x4_t *>(&q8[0][64 * c + 16 * quarter]);
-            lo[c] = *reinterpret_cast<const i32x4_t *>(&q8[1][64 * c + 16 * quarter]);
+            for (int c = 0; c < 2 * kChunks; ++c) mine[c >> 1][c & 1] = load8<false>(row, (c >> 1) * 64 + 16 * quarter + (c & 1) * 8, g.d);
         }
     }
+    float most = 0.f;
+#pragma unroll
+    for (int c = 0; c < 2 * kChunks; ++c) {
+        if (col >= a.group) mine[c >> 1][c & 1] = make_uint4(0, 0, 0, 0);
+        most = largest<DT>(mine[c >> 1][c & 1], most);
+    }
+    for (int head = 16 + col; head < a.group; head += 16)
+        for (int c = 0; c < kChunks; ++c) most = largest<DT>(piece(head, c, 1), largest<DT>(piece(head, c, 0), most));
+#pragma unroll
+    for (int m = 1; m < 16; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+    most = max_over_16(max_over_32(most));
+    const float inverse = pow2_of(-unit_exponent(most));
+    auto rounded = [&](const uint4 &lo, const uint4 &hi) {
+        i32x4_t r = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float v = element<DT>(j < 8 ? lo : hi, j & 7);
+            const int n = finite(v) ? (int)__builtin_rintf(v * inverse) : 0;
+            r[j >> 2] |= (n & 0xff) << (8 * (j & 3));
+        }
+        return r;
+    };
+    i32x4_t q8[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) q8[c] = rounded(mine[c][0], mine[c][1]);
     for (int first = 16 * wave; first < scored; first += 16 * kWaves) {
-        uint32_t keys[4];
-        x.score(hi, lo, keys);
+        i32x4_t sum = {0, 0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x.x[c], q8[c], sum, 0, 0, 0);
+        for (int head = 16; head < a.group; head += 16)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c)
+                sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x.x[c], rounded(piece(head + col, c, 0), piece(head + col, c, 1)), sum, 0, 0, 0);
+        const float weight = x.weight;
         if (first + 16 * kWaves < scored) x.bring(g, b, h, first + 16 * kWaves, scored);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (col == 0 && first + quarter * 4 + i < scored) lds_keys[first + quarter * 4 + i] = keys[i];
+        for (int i = 0; i < 4; ++i) {
+            const int total = sum_over_row(sum[i]), to = first + quarter * 4 + i;
+            const float w = __shfl(weight, quarter * 4 + i);
+            if (col == 15 && to < scored) lds_keys[to] = key_of((float)total * w);
+        }
     }
     __syncthreads();
 
+    // The threshold, eight bits a round: how many keys have each value of them, and the value at which the `top` best are together.  Every wave finds it.
+    // A wave looks after its part of the candidates.
     const uint32_t *const keys = lds_keys + a.first;
-    uint32_t held[kHeld];
-#pragma unroll
-    for (int r = 0; r < kHeld; ++r) held[r] = 64 * r + lane < candidates ? keys[64 * r + lane] : 0;        // (no key is 0)
+    const int part = (candidates + 64 * kWaves - 1) / (64 * kWaves) * 64, from = min(wave * part, candidates), to = min(from + part, candidates);
     uint32_t threshold = 0;
-    for (int shift = 28; shift >= 0; shift -= 4) {
-        const uint32_t trial = threshold | (uint32_t)wave << shift;     // (wave 0: the threshold itself, which has enough)
-        int c = 0;
+    int wanted = a.top;             // of the keys that agree with the threshold so far
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r) c += (int)__popcll(__ballot(held[r] >= trial));
-        for (int i = 64 * kHeld; i < candidates; i += 64) c += (int)__popcll(__ballot(i + lane < candidates && keys[i + lane] >= trial));
-        int *const row = counts[shift >> 2 & 1];
-        if (lane == 0) row[wave] = c;
+    for (int round = 0; round < 4; ++round) {
+        const int shift = 24 - 8 * round;
+        for (int i = from + lane; i < to; i += 64) {
+            const uint32_t key = keys[i];
+            if (round == 0 || (key ^ threshold) >> (shift + 8) == 0) atomicAdd(&bins[round][key >> shift & 255], 1);
+        }
         __syncthreads();
-        const int other = row[lane & (kWaves - 1)];
-        const uint64_t enough = __ballot(other >= a.top || lane == 0) & 0xffffu;
-        threshold |= (uint32_t)(63 - __clzll(enough)) << shift;
-        if (__ballot(other == a.top && lane > 0) & 0xffffu) break;      // (then the highest with enough is one with exactly as many)
+        const int4 four = *reinterpret_cast<const int4 *>(&bins[round][252 - 4 * lane]);      // lane 0 has the largest values
+        const int mine_sum = four.x + four.y + four.z + four.w, up_to = sum_up_to(mine_sum);
+        const int at_lane = __ffsll((unsigned long long)__ballot(up_to >= wanted)) - 1;
+        int before = __builtin_amdgcn_readlane(up_to - mine_sum, at_lane);
+        const int n[4] = {__builtin_amdgcn_readlane(four.w, at_lane), __builtin_amdgcn_readlane(four.z, at_lane), __builtin_amdgcn_readlane(four.y, at_lane),
+                          __builtin_amdgcn_readlane(four.x, at_lane)};
+        int value = 255 - 4 * at_lane, here = n[0];
+#pragma unroll
+        for (int j = 1; j < 4; ++j)
+            if (before + here < wanted) {
+                before += here;
+                here = n[j];
+                --value;
+            }
+        threshold |= (uint32_t)value << shift;
+        wanted -= before;
+        if (here == wanted) break;  // all of these
     }
 
-    // a wave writes the entries of its part of the candidates
-    const int part = (candidates + 64 * kWaves - 1) / (64 * kWaves) * 64, from = min(wave * part, candidates), to = min(from + part, candidates);
     int above = 0, same = 0;
     for (int i = from; i < to; i += 64) {
         const uint32_t key = i + lane < to ? keys[i + lane] : 0;
         above += (int)__popcll(__ballot(key > threshold));
         same += (int)__popcll(__ballot(i + lane < to && key == threshold));
     }
-    __syncthreads();        // (the last round's counts have been read)
     if (lane == 0) {
-        counts[0][wave] = above;
-        equal[wave] = same;
+        aboves[wave] = above;
+        equals[wave] = same;
     }
     __syncthreads();
     int above_before = 0, same_before = 0, above_all = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        above_all += counts[0][w];
-        above_before += w < wave ? counts[0][w] : 0;
-        same_before += w < wave ? equal[w] : 0;
+        above_all += aboves[w];
+        above_before += w < wave ? aboves[w] : 0;
+        same_before += w < wave ? equals[w] : 0;
     }
     const int ties = a.top - above_all;         // of those at the threshold, the lowest numbers
     write_entries(keys, from, to, threshold, ties - same_before, a.first, out + a.first + above_before + min(same_before, ties));

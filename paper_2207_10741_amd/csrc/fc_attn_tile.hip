@@ -39,7 +39,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
     if (rows == 0) return;
     const int r = tile * kRows + wave * 32 + col;
     const bool valid = wave * 32 + col < rows;
-    const int token = (int)fast_div((uint32_t)r, a.div_group), head = r - token * a.group;
+    const int token = row_place(a, r).token;
     const int last = valid ? (a.causal ? s.pos0 + token : s.len - 1) : -1;
     const int token_last = (int)fast_div((uint32_t)(tile * kRows + rows - 1), a.div_group);
     const int last_most = a.causal ? s.pos0 + token_last : s.len - 1;
@@ -53,11 +53,17 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
     const int begin = split * a.per_split, end = min(blocks, begin + a.per_split);
 
     uint4 q[kSteps];
+    {
+        // (rows behind the last repeat it and are left out below)
+        const RowPlace p = row_place(a, min(r, tile * kRows + rows - 1));
+        const uint16_t *const row = a.q + (s.row0 + p.token) * a.q_row + (int64_t)(h * a.group + p.head) * a.q_head;
+        if (a.wide) {
 #pragma unroll
-    for (int c = 0; c < kSteps; ++c) {
-        q[c] = make_uint4(0, 0, 0, 0);
-        if (valid)
-            q[c] = flip_signs(load8(a.q + (s.row0 + token) * a.q_row + (int64_t)(h * a.group + head) * a.q_head, 16 * c + 8 * half, g.d, a.wide), a.signs);
+            for (int c = 0; c < kSteps; ++c) q[c] = flip_signs(load8<true>(row, 16 * c + 8 * half, g.d), a.signs);
+        } else {
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c) q[c] = flip_signs(load8<false>(row, 16 * c + 8 * half, g.d), a.signs);
+        }
     }
 
     f32x16_t o[kOut];

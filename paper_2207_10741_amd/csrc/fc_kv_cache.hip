@@ -18,6 +18,10 @@ struct AppendArgs {
     int32_t wide_k, wide_v;
 };
 
+template <bool V> struct Const {
+    static constexpr bool value = V;
+};
+
 // Four codes under another scale; ratio = old scale / new scale, a power of two.
 __device__ __forceinline__ uint32_t rescale4(uint32_t c, float ratio)
 {
@@ -98,22 +102,31 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
     uint4 kx[kRounds][4], vx[kRounds][4];
     float ka = 0.f, va = 0.f;
     bool strange = false;
+    // (all loads under way together: rows that are not new ones repeat one that is, and count as zeros below)
+    auto bring = [&](auto wide, const uint16_t *x, int64_t x_row, uint4 (&to)[kRounds][4]) {
+        constexpr bool kWide = decltype(wide)::value;
+#pragma unroll
+        for (int round = 0; round < kRounds; ++round)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = min(max(round * kRows + 4 * r + j, old), end - 1);
+                to[round][j] = load8<kWide>(x + (int64_t)(s.row0 + (at + t - s.pos0)) * x_row, 8 * c, g.d);
+            }
+    };
+    const uint16_t *const krows = a.k + h * a.k_head, *const vrows = a.v + h * a.v_head;
+    if (a.wide_k & a.wide_v) {
+        bring(Const<true>(), krows, a.k_row, kx);
+        bring(Const<true>(), vrows, a.v_row, vx);
+    } else {
+        bring(Const<false>(), krows, a.k_row, kx);
+        bring(Const<false>(), vrows, a.v_row, vx);
+    }
 #pragma unroll
     for (int round = 0; round < kRounds; ++round)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int t = round * kRows + 4 * r + j;
-            kx[round][j] = vx[round][j] = make_uint4(0, 0, 0, 0);
-            if (4 * r < kRows && t >= old && t < end) {
-                const int64_t row = s.row0 + (at + t - s.pos0);
-                kx[round][j] = load8(a.k + row * a.k_row + h * a.k_head, 8 * c, g.d, a.wide_k);
-                vx[round][j] = load8(a.v + row * a.v_row + h * a.v_head, 8 * c, g.d, a.wide_v);
-            }
-        }
-#pragma unroll
-    for (int round = 0; round < kRounds; ++round)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+            if (4 * r >= kRows || t < old || t >= end) kx[round][j] = vx[round][j] = make_uint4(0, 0, 0, 0);
             ka = finite_amax<DT>(kx[round][j], ka);
             va = finite_amax<DT>(vx[round][j], va);
             const uint32_t w[4] = {vx[round][j].x, vx[round][j].y, vx[round][j].z, vx[round][j].w};

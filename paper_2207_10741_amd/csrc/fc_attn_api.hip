@@ -73,17 +73,19 @@ void cut_to_fill(int64_t units, int32_t blocks, int waves, int32_t *splits, int3
     *splits = (blocks + *per_split - 1) / *per_split;
 }
 
-// ... and where the matrix cores are: workgroups run in rounds of two a CU, one of them alone 1.4 times as fast, so the number of pieces that gives the
-// shortest rounds, with four blocks' time to begin and end a piece and half a block's to join one.  `units` is what the call's rows come to, not the
-// bound: pieces of up to 517 tokens of three sequences, us at 1 / 2 / 3 / 4 / 5 / 6 pieces 130 / 102 / 88 / 77 / 96 / 92.
-void cut_for_rounds(int64_t units, int32_t blocks, int32_t *splits, int32_t *per_split)
+// ... and where the matrix cores are: one piece where the rows are a workgroup for every CU (us, in one piece -> in two: 4096 tokens of 32 heads of 128 over 8
+// 144 -> 216, 3000 87 -> 131, 1024 28 -> 29), else as many as take the least time.  In tenths of a block's time of a workgroup that has its CU for itself: two on
+// a CU take 1.4 times as long each, and the launch no less than its longest piece or its share of all of them; four blocks' time goes to beginning and ending
+// a piece, three to joining one.  `units` is what the call's rows come to and `mean` the blocks that a row sees on average.  (512 tokens after 16000 329 -> 154
+// in four pieces, 128 after 4000, a key head a head, 87 -> 39.)
+void cut_for_rounds(int64_t units, int32_t blocks, int32_t mean, int32_t *splits, int32_t *per_split)
 {
     int64_t best = 0;
     *splits = 1, *per_split = blocks;
-    for (int64_t n = 1; n <= 64 && n <= blocks; ++n) {
-        const int64_t per = (blocks + n - 1) / n, pieces = (blocks + per - 1) / per, workgroups = units * pieces;
-        const int64_t round = workgroups <= 256 ? 10 : (workgroups + 511) / 512 * 14;
-        const int64_t cost = round * (per + 4) + (pieces > 1 ? 5 * (pieces + 4) : 0);
+    for (int64_t n = 1; n <= (units < 256 ? 64 : 1) && n <= blocks; ++n) {
+        const int64_t per = (blocks + n - 1) / n, pieces = (blocks + per - 1) / per, workgroups = units * ((mean + per - 1) / per);
+        const int64_t share = (units * mean + 4 * workgroups) / 512;
+        const int64_t cost = (workgroups <= 256 ? 10 : 14) * (share > per + 4 ? share : per + 4) + (pieces > 1 ? 32 * pieces : 0);
         if (n == 1 || cost < best) {
             best = cost;
             *splits = (int32_t)pieces;
@@ -92,6 +94,8 @@ void cut_for_rounds(int64_t units, int32_t blocks, int32_t *splits, int32_t *per
     }
 }
 
+// Lists: from this many on there are enough to fill the chip with a wave each (us, split -> whole, 16 and 32 blocks of 8 key heads of 128: 512 units 36 -> 39,
+// 57 -> 69; 1024 68 -> 67, 121 -> 119; 1600 120 -> 118; 2800 of 9 blocks 53 -> 44).
 constexpr int64_t kWholeLists = 1024;
 
 int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *p)
@@ -112,7 +116,10 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
         p->rows_tile = 16;
         p->tiles = d->max_new * ((group + 15) / 16);
     } else {
-        p->rows_tile = rows <= 16 ? 16 : rows <= 32 && g.dp <= 128 ? 32 : kTileRows;
+        // 256 rows share a block's conversion where there are enough of them for two rounds of a workgroup a CU (us, 128 -> 256 rows, 32 heads of 128 over 8:
+        // 8192 tokens 565 -> 544, 4096 158 -> 148, two times 2048 after 16000 996 -> 932; 2048 56 -> 83)
+        const int64_t large = (rows + 255) / 256 * d->batch * d->kv_heads;
+        p->rows_tile = rows <= 16 ? 16 : rows <= 32 && g.dp <= 128 ? 32 : large >= 512 && g.dp == 128 ? 256 : 128;
         p->tiles = (int32_t)((rows + p->rows_tile - 1) / p->rows_tile);
     }
     const int64_t units = p->units = (int64_t)d->batch * d->kv_heads * p->tiles;
@@ -120,9 +127,10 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
     if (p->whole) {
         p->per_split = blocks;
         p->splits = 1;
-    } else if (p->rows_tile == kTileRows) {
-        const int64_t filled = ((int64_t)d->tokens * group / kTileRows + (d->batch + 1) / 2) * d->kv_heads;
-        cut_for_rounds(filled < units ? filled : units, blocks, &p->splits, &p->per_split);
+    } else if (p->rows_tile >= 128) {
+        const int64_t filled = ((int64_t)d->tokens * group / p->rows_tile + (d->batch + 1) / 2) * d->kv_heads;
+        const int32_t mean = d->flags & FC_CAUSAL ? blocks - d->max_new / (2 * kBlock) : blocks;
+        cut_for_rounds(filled < units ? filled : units, blocks, mean < 1 ? 1 : mean, &p->splits, &p->per_split);
     } else {
         p->waves = 4;
         cut_to_fill(units, blocks, p->waves, &p->splits, &p->per_split);
@@ -196,7 +204,7 @@ int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, con
         if (e == hipSuccess) e = launch_attend_lists(a, d->dtype, p.whole, s);
     } else {
         e = counters ? launch_zero_i32(a.arrived, counters, s) : hipSuccess;
-        if (e == hipSuccess) e = p.rows_tile <= 32 ? launch_attend_rows(a, d->dtype, p.rows_tile, p.waves, s) : launch_attend_tile(a, d->dtype, s);
+        if (e == hipSuccess) e = p.rows_tile <= 32 ? launch_attend_rows(a, d->dtype, p.rows_tile, p.waves, s) : launch_attend_tile(a, d->dtype, p.rows_tile, s);
     }
     return e == hipSuccess ? FC_OK : FC_ERR_HIP;
 }

@@ -190,6 +190,10 @@ __device__ __forceinline__ uint32_t seen_pair(int first, int left) { return (fir
 
 __device__ __forceinline__ uint4 flip_signs(uint4 x, uint32_t signs) { return make_uint4(x.x ^ signs, x.y ^ signs, x.z ^ signs, x.w ^ signs); }
 
+template <int V> struct Const {
+    static constexpr int value = V;
+};
+
 struct AttnArgs {
     KvGeom kv;
     const uint16_t *q;
@@ -266,19 +270,19 @@ template <int DP> struct Pieces {
         out = __builtin_amdgcn_make_buffer_rsrc(a.part_out + unit * rows * DP, 0, rows * DP * (uint32_t)sizeof(float), 0x00020000);
         ml = __builtin_amdgcn_make_buffer_rsrc(a.part_ml + unit * rows, 0, rows * (uint32_t)sizeof(float2), 0x00020000);
     }
-    // row: split * rows_tile + row of the tile
-    __device__ __forceinline__ void put(uint32_t row, int c, f32x4_t v) const
+    // item: split * rows_tile * DP / 4 + the place of four channels of a row, in whichever order the kernel has them together; row: split * rows_tile + row
+    __device__ __forceinline__ void put(uint32_t item, f32x4_t v) const
     {
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), out, (row * DP + (uint32_t)c) * 4u, 0, kPastCaches);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), out, item * 16u, 0, kPastCaches);
     }
     __device__ __forceinline__ void put_ml(uint32_t row, float m, float l) const
     {
         const u32x2_t v = {__float_as_uint(m), __float_as_uint(l)};
         __builtin_amdgcn_raw_buffer_store_b64(v, ml, row * 8u, 0, kPastCaches);
     }
-    __device__ __forceinline__ f32x4_t get(uint32_t row, int c) const
+    __device__ __forceinline__ f32x4_t get(uint32_t item) const
     {
-        return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(out, (row * DP + (uint32_t)c) * 4u, 0, kPastCaches));
+        return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(out, item * 16u, 0, kPastCaches));
     }
     __device__ __forceinline__ float2 get_ml(uint32_t row) const
     {
@@ -301,56 +305,102 @@ __device__ __forceinline__ bool last_to_arrive(const AttnArgs &a, int64_t unit, 
     return *lds_flag;
 }
 
-// The last workgroup's part: rows `first` .. of the tile, out_row(r) is row r's place in the output.  A thread takes four channels of a row and,
-// where there are threads to spare, every so-manyth piece.
-template <int DT, int DP, int THREADS, typename F>
-__device__ __forceinline__ void join_pieces(const AttnArgs &a, const Pieces<DP> &pieces, int rows, int rows_tile, int active, float *lds, F out_row)
-{
-        constexpr int kPieces = DP / 4, kUnroll = 8;
-    const int items = rows * kPieces, sets = items < THREADS ? THREADS / items : 1;
-    for (int first = 0; first < items; first += THREADS) {
-        const int item = sets > 1 ? (int)threadIdx.x % items : first + (int)threadIdx.x, set = sets > 1 ? (int)threadIdx.x / items : 0;
-        const bool mine = item < items && set < sets;
-        const int r = item / kPieces, c = item % kPieces * 4;
-        float m = -__builtin_inff(), l = 0.f;
-        f32x4_t o = {0.f, 0.f, 0.f, 0.f};
-        auto add = [&](float2 ml, f32x4_t v) {
-            const float most = fmaxf(m, ml.x), base = most == -__builtin_inff() ? 0.f : most;
-            const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(ml.x - base);
-            l = l * f0 + ml.y * f1;
-            o = o * f0 + v * f1;
-            m = most;
-        };
-        if (mine)
-            for (int i = set; i < active; i += sets * kUnroll) {
-                float2 ml[kUnroll];
-                f32x4_t v[kUnroll];
-#pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    const uint32_t row = (uint32_t)(min(i + u * sets, active - 1) * rows_tile + r);
-                    ml[u] = pieces.get_ml(row);
-                    v[u] = pieces.get(row, c);
-                }
-#pragma unroll
-                for (int u = 0; u < kUnroll; ++u)
-                    if (i + u * sets < active) add(ml[u], v[u]);
-            }
-        if (sets > 1) {
-            __syncthreads();
-            float *const at = lds + threadIdx.x * 8;
-            if (mine && set) {
-                at[0] = m, at[1] = l;
-                *reinterpret_cast<f32x4_t *>(at + 4) = o;
-            }
-            __syncthreads();
-            if (mine && !set)
-                for (int i = 1; i < sets; ++i) {
-                    const float *const other = lds + (i * items + item) * 8;
-                    add(make_float2(other[0], other[1]), *reinterpret_cast<const f32x4_t *>(other + 4));
-                }
-        }
-        if (mine && !set) finish_row<DT>(a, out_row(r), c, o, m, l);
+// A row's running join: pieces with their references and sums added one by one.
+struct Joined {
+    f32x4_t o;
+    float m, l;
+    __device__ __forceinline__ void clear()
+    {
+        o = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        m = -__builtin_inff();
+        l = 0.f;
     }
+    __device__ __forceinline__ void add(float2 ml, f32x4_t v)
+    {
+        const float most = fmaxf(m, ml.x), base = most == -__builtin_inff() ? 0.f : most;
+        const float f0 = __builtin_amdgcn_exp2f(m - base), f1 = __builtin_amdgcn_exp2f(ml.x - base);
+        l = l * f0 + ml.y * f1;
+        o = o * f0 + v * f1;
+        m = most;
+    }
+};
+
+// The last workgroup's part: `items` places of four channels of a row; place(item) is the tile's row (kNoRow: none) and the first channel, out_row(row) the
+// row's place in the output.  With fewer items than threads a thread takes every so-manyth piece of one, with more several items at once, so that eight
+// loads are under way either way.
+constexpr int kNoRow = -1;
+struct ItemPlace {
+    int row, c;
+};
+template <int DT, int DP, int THREADS, typename P, typename F>
+__device__ __forceinline__ void join_pieces(const AttnArgs &a, const Pieces<DP> &pieces, int items, int rows_tile, int active, float *lds, P place, F out_row)
+{
+    const uint32_t next = (uint32_t)(rows_tile * (DP / 4));     // items from a piece to the next
+    if (items > THREADS / 2) {
+        constexpr int kItems = 4, kUnroll = 2;
+        for (int first = threadIdx.x; first < items; first += kItems * THREADS) {
+            Joined x[kItems];
+            ItemPlace at[kItems];
+            int item[kItems];
+#pragma unroll
+            for (int n = 0; n < kItems; ++n) {
+                x[n].clear();
+                item[n] = min(first + n * THREADS, items - 1);
+                at[n] = place(item[n]);
+            }
+            for (int i = 0; i < active; i += kUnroll) {
+                float2 ml[kItems][kUnroll];
+                f32x4_t v[kItems][kUnroll];
+#pragma unroll
+                for (int n = 0; n < kItems; ++n)
+#pragma unroll
+                    for (int u = 0; u < kUnroll; ++u) {
+                        const int piece = min(i + u, active - 1);
+                        ml[n][u] = pieces.get_ml((uint32_t)(piece * rows_tile + max(at[n].row, 0)));
+                        v[n][u] = pieces.get(piece * next + item[n]);
+                    }
+#pragma unroll
+                for (int n = 0; n < kItems; ++n)
+#pragma unroll
+                    for (int u = 0; u < kUnroll; ++u)
+                        if (i + u < active) x[n].add(ml[n][u], v[n][u]);
+            }
+#pragma unroll
+            for (int n = 0; n < kItems; ++n)
+                if (first + n * THREADS < items && at[n].row != kNoRow) finish_row<DT>(a, out_row(at[n].row), at[n].c, x[n].o, x[n].m, x[n].l);
+        }
+        return;
+    }
+    constexpr int kUnroll = 8;
+    const int sets = THREADS / items, item = (int)threadIdx.x % items, set = (int)threadIdx.x / items;
+    const ItemPlace at = place(item);
+    Joined x;
+    x.clear();
+    if (set < sets)
+        for (int i = set; i < active; i += sets * kUnroll) {
+            float2 ml[kUnroll];
+            f32x4_t v[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int piece = min(i + u * sets, active - 1);
+                ml[u] = pieces.get_ml((uint32_t)(piece * rows_tile + max(at.row, 0)));
+                v[u] = pieces.get(piece * next + item);
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u)
+                if (i + u * sets < active) x.add(ml[u], v[u]);
+        }
+    __syncthreads();
+    float *const mine = lds + threadIdx.x * 8;
+    mine[0] = x.m, mine[1] = x.l;
+    *reinterpret_cast<f32x4_t *>(mine + 4) = x.o;
+    __syncthreads();
+    if (set) return;
+    for (int i = 1; i < sets; ++i) {
+        const float *const other = lds + (i * items + item) * 8;
+        x.add(make_float2(other[0], other[1]), *reinterpret_cast<const f32x4_t *>(other + 4));
+    }
+    if (at.row != kNoRow) finish_row<DT>(a, out_row(at.row), at.c, x.o, x.m, x.l);
 }
 
 // max over the lanes 16 and 32 apart
@@ -395,9 +445,8 @@ hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, int w
 // 16 rows of one token, over its list of blocks; a wave's, or (a.splits counts the pieces) a workgroup's.
 hipError_t launch_attend_lists(const AttnArgs &a, int dtype, bool whole, hipStream_t s);
 
-// Many rows (see fc_attn_tile.hip): kTileRows a workgroup.
-constexpr int kTileRows = 128;
-hipError_t launch_attend_tile(const AttnArgs &a, int dtype, hipStream_t s);
+// Many rows (see fc_attn_tile.hip); rows_tile: rows a workgroup holds, 128 or (up to 128 channels) 256.
+hipError_t launch_attend_tile(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s);
 
 // The selection (see fc_attn_select.hip).
 constexpr int kSelectMaxBlocks = 32768;     // blocks of a sequence whose scores fit LDS

@@ -322,12 +322,13 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
         if (active == 1) {
             finish_row<DT>(a, out_row(r), c, sum, most, total);
         } else {
-            pieces.put((uint32_t)(split * kRows + r), c, sum);
+            pieces.put((uint32_t)(split * kRows * kPieces + i), sum);
             if (c == 0) pieces.put_ml((uint32_t)(split * kRows + r), most, total);
         }
     }
     if (active == 1 || !last_to_arrive(a, unit, active, lds_flag)) return;
-    join_pieces<DT, DP, kThreads>(a, pieces, rows, kRows, active, lds, out_row);
+    auto place = [](int item) { return ItemPlace{item / kPieces, item % kPieces * 4}; };
+    join_pieces<DT, DP, kThreads>(a, pieces, rows * kPieces, kRows, active, lds, place, out_row);
 }
 
 // A wave takes up to 16 heads of one token and the token's whole list.  An XCD takes an eighth of the units in one piece: neighbouring tokens of a head

@@ -11,18 +11,18 @@ namespace fc {
 
 namespace {
 
-constexpr int kThreads = 2 * kTileRows;
 template <int DT> __device__ __forceinline__ f32x16_t mfma_32(const uint4 &a, const uint4 &b, const f32x16_t &c) { return mfma32<DT>(a, b, c); }
 
+constexpr int kAhead = 4;
 template <int DP> constexpr uint32_t kKeyPitch = 2 * DP + 16;
 constexpr uint32_t kValuePitch = 2 * kBlock + 16;
 
-template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
+template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * WAVES, DP * MT <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
 {
-    constexpr int kRows = kTileRows, kSteps = DP / 16, kOut = DP / 32;
+    constexpr int kWaves = WAVES, kThreads = 64 * kWaves, kWaveRows = 32 * MT, kRows = kWaveRows * kWaves, kSteps = DP / 16, kOut = DP / 32;
     constexpr int kShare = 4 * DP / kThreads;       // 16-byte pieces of the codes of keys (values) a thread brings
     // rows of keys and values in LDS; the 16 bytes behind each put rows that are read together into different banks
-    constexpr uint32_t kKeyRow = kKeyPitch<DP>, kKeys = kBlock * kKeyRow, kValueRow = kValuePitch, kBuffer = kKeys + DP * kValueRow;
+    constexpr uint32_t kKeyRow = kKeyPitch<DP>, kValues = kBlock * kKeyRow, kValueRow = kValuePitch, kBuffer = kValues + DP * kValueRow;
     extern __shared__ __align__(16) unsigned char lds[];
     const KvGeom &g = a.kv;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
@@ -37,226 +37,345 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads, DP <= 128 ? 2 :
     const Sequence s = sequence_of(g, b);
     const int rows = min(max(s.n * a.group - tile * kRows, 0), kRows);
     if (rows == 0) return;
-    const int r = tile * kRows + wave * 32 + col;
-    const bool valid = wave * 32 + col < rows;
-    const int token = row_place(a, r).token;
-    const int last = valid ? (a.causal ? s.pos0 + token : s.len - 1) : -1;
+    int last[MT];       // the last position that the lane's row attends to
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const int r = wave * kWaveRows + 32 * mt + col;
+        last[mt] = r < rows ? (a.causal ? s.pos0 + row_place(a, tile * kRows + r).token : s.len - 1) : -1;
+    }
     const int token_last = (int)fast_div((uint32_t)(tile * kRows + rows - 1), a.div_group);
     const int last_most = a.causal ? s.pos0 + token_last : s.len - 1;
-    // the wave's own bounds
-    const int wave_rows = min(max(rows - wave * 32, 0), 32);
-    const int wave_first = a.causal ? s.pos0 + (int)fast_div((uint32_t)(tile * kRows + wave * 32), a.div_group) : s.len - 1;
-    const int wave_last = wave_rows == 0 ? -1 : a.causal ? s.pos0 + (int)fast_div((uint32_t)(tile * kRows + wave * 32 + wave_rows - 1), a.div_group) : s.len - 1;
+    const int wave_first = a.causal ? s.pos0 + row_place(a, tile * kRows + wave * kWaveRows).token : s.len - 1;     // the least `last` of the wave's rows
     const int blocks = last_most < 0 ? 0 : last_most / kBlock + 1;
     const int active = max((blocks + a.per_split - 1) / a.per_split, 1);
     if (split >= active) return;
     const int begin = split * a.per_split, end = min(blocks, begin + a.per_split);
 
-    uint4 q[kSteps];
-    {
+    uint4 q[MT][kSteps];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
         // (rows behind the last repeat it and are left out below)
-        const RowPlace p = row_place(a, min(r, tile * kRows + rows - 1));
+        const RowPlace p = row_place(a, tile * kRows + min(wave * kWaveRows + 32 * mt + col, rows - 1));
         const uint16_t *const row = a.q + (s.row0 + p.token) * a.q_row + (int64_t)(h * a.group + p.head) * a.q_head;
         if (a.wide) {
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) q[c] = flip_signs(load8<true>(row, 16 * c + 8 * half, g.d), a.signs);
+            for (int c = 0; c < kSteps; ++c) q[mt][c] = flip_signs(load8<true>(row, 16 * c + 8 * half, g.d), a.signs);
         } else {
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) q[c] = flip_signs(load8<false>(row, 16 * c + 8 * half, g.d), a.signs);
+            for (int c = 0; c < kSteps; ++c) q[mt][c] = flip_signs(load8<false>(row, 16 * c + 8 * half, g.d), a.signs);
         }
     }
 
-    f32x16_t o[kOut];
+    // what a row holds: o in units of unit_v, weights 2^(z - m), m a whole number, l this lane's part of their sum
+    f32x16_t o[MT][kOut], z[MT];
+    float m[MT], l[MT], unit_v = 1.f;
+    uint4 p[MT][2];     // weights of the last half-block whose product with the values is still to come
 #pragma unroll
-    for (int t = 0; t < kOut; ++t)
+    for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    float m = -__builtin_inff(), l = 0.f, unit_v = 1.f;     // m: the row's weights are 2^(z - m)
+        for (int t = 0; t < kOut; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[mt][t][i] = 0.f;
+        m[mt] = -__builtin_inff();
+        l[mt] = 0.f;
+        p[mt][0] = p[mt][1] = make_uint4(0, 0, 0, 0);
+    }
 
-    uint4 kx[kShare], vx[kShare];
-    float2 scales;
-    bool there;
-    auto bring = [&](int block) {
-        const int32_t pool = pool_block(g, b, block);
-        there = pool >= 0;
-        const int64_t unit = unit_of(g, max(pool, 0), h);
-        const uint8_t *const from = g.codes + unit * (2 * kBlock * DP);
-        scales = g.scales[unit];
-#pragma unroll
-        for (int i = 0; i < kShare; ++i) {
-            kx[i] = *reinterpret_cast<const uint4 *>(from + i * kThreads * 16 + threadIdx.x * 16u);
-            vx[i] = *reinterpret_cast<const uint4 *>(from + (4 * DP + i * kThreads) * 16 + threadIdx.x * 16u);
-        }
-    };
-    if (begin < end) bring(begin);
-    // where the thread's first pieces go and where the lane's operands are, from the buffer's start on
+    // where the thread's first pieces go and where the lane's operands are, from a buffer's start on
     auto key_place = [](uint32_t piece) {       // (see key_piece)
         const uint32_t channel = (piece >> 6) % (DP / 64) * 64 + (piece >> 4 & 3) * 16, token = (piece >> 6) / (DP / 64) * 16 + (piece & 15);
         return token * kKeyRow + channel * 2;
     };
     const uint32_t key_to = key_place(threadIdx.x);
     // four words of four tokens 16 w + 4 quarter .. + 3: as the scores' lanes hold them, half `quarter & 1`
-    const uint32_t value_to = kKeys + ((threadIdx.x >> 6) * 16 + (threadIdx.x & 15)) * kValueRow + (threadIdx.x >> 4 & 1) * 16 + (threadIdx.x >> 5 & 1) * 8;
-    const uint32_t key_at = col * kKeyRow + half * 16, value_at = kKeys + col * kValueRow + half * 16;
-    uint32_t buffer = 0;
-    for (int block = begin; block < end; ++block, buffer = kBuffer - buffer) {
-        const bool here = there;
-        const float scale_k = here ? scales.x : 1.f, scale_v = here ? __builtin_fabsf(scales.y) : unit_v;
-        const bool strange = here && scales.y < 0.f;        // (NaN among the values: zeros in LDS, found again below)
-        if (!keeps_unit(scale_v, unit_v)) {
-            const float factor = pow2_ratio(unit_v, scale_v);
-#pragma unroll
-            for (int t = 0; t < kOut; ++t) o[t] *= factor;
-            unit_v = scale_v;
-        }
-        const float to_unit = pow2_ratio(scale_v, unit_v);
-        unsigned char *const keys_to = lds + buffer + key_to, *const values_to = lds + buffer + value_to;
-        const unsigned char *const keys = lds + buffer + key_at, *const values = lds + buffer + value_at;
-#pragma unroll
-        for (int i = 0; i < kShare; ++i) {
-            // (kThreads pieces further; a constant unless they split a token's channels)
-            constexpr uint32_t kValueStep = kThreads / 4 * kValueRow;
-            const uint32_t key_step = DP % 192 ? key_place(i * kThreads) : key_place(threadIdx.x + i * kThreads) - key_to;
-            *reinterpret_cast<uint4 *>(keys_to + key_step) = codes_to_16<DT>(kx[i].x, kx[i].y);
-            *reinterpret_cast<uint4 *>(keys_to + key_step + 16) = codes_to_16<DT>(kx[i].z, kx[i].w);
-            if (strange) vx[i] = without_nan(vx[i]);
-            const uint4 first = codes_to_f16(vx[i].x, vx[i].y, to_unit), second = codes_to_f16(vx[i].z, vx[i].w, to_unit);
-            const uint2 words[4] = {make_uint2(first.x, first.y), make_uint2(first.z, first.w), make_uint2(second.x, second.y), make_uint2(second.z, second.w)};
-#pragma unroll
-            for (int w = 0; w < 4; ++w) *reinterpret_cast<uint2 *>(values_to + i * kValueStep + 32 * w) = words[w];
-        }
-        __syncthreads();
-        if (block + 1 < end) bring(block + 1);
-        if (!here || block * kBlock > wave_last) continue;
+    const uint32_t value_to = kValues + ((threadIdx.x >> 6) * 16 + (threadIdx.x & 15)) * kValueRow + (threadIdx.x >> 4 & 1) * 16 + (threadIdx.x >> 5 & 1) * 8;
+    const uint32_t key_at = col * kKeyRow + half * 16, value_at = kValues + col * kValueRow + half * 16;
 
-        f32x16_t z[2];
+    // A block's codes on their way: global memory -> registers -> LDS, as 16-bit floats.
+    uint4 kx[kShare], vx[kShare];
+    auto codes_of = [&](int32_t pool) { return g.codes + unit_of(g, max(pool, 0), h) * (2 * kBlock * DP); };
+    auto bring = [&](const uint8_t *from, uint4 (&x)[kShare]) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z[t][i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < kSteps; ++c)
-                z[t] = mfma_32<DT>(*reinterpret_cast<const uint4 *>(keys + 32 * t * kKeyRow + 32 * c), q[c], z[t]);
-        }
+        for (int i = 0; i < kShare; ++i) x[i] = *reinterpret_cast<const uint4 *>(from + i * kThreads * 16 + threadIdx.x * 16u);
+    };
+    // (kThreads pieces further: a constant unless they split a token's channels)
+    auto key_step = [&](int i) { return DP % 192 ? key_place(i * kThreads) : key_place(threadIdx.x + i * kThreads) - key_to; };
+    // half a piece of keys (16 bytes in LDS) and of values (two words of four tokens)
+    auto put_keys = [&](uint32_t buffer, int i, int n) {
+        *reinterpret_cast<uint4 *>(lds + buffer + key_to + key_step(i) + 16 * n) = n ? codes_to_16<DT>(kx[i].z, kx[i].w) : codes_to_16<DT>(kx[i].x, kx[i].y);
+    };
+    auto put_values = [&](uint32_t buffer, float to_unit, int i, int n) {
+        const uint4 x = n ? codes_to_f16(vx[i].z, vx[i].w, to_unit) : codes_to_f16(vx[i].x, vx[i].y, to_unit);
+        unsigned char *const to = lds + buffer + value_to + i * (kThreads / 4 * kValueRow) + 64 * n;
+        *reinterpret_cast<uint2 *>(to) = make_uint2(x.x, x.y);
+        *reinterpret_cast<uint2 *>(to + 32) = make_uint2(x.z, x.w);
+    };
+    auto key_operand = [&](uint32_t buffer, int t, int c) { return *reinterpret_cast<const uint4 *>(lds + buffer + key_at + 32 * t * kKeyRow + 32 * c); };
+    auto value_operand = [&](uint32_t buffer, int t, int step) {
+        return *reinterpret_cast<const uint4 *>(lds + buffer + value_at + 32 * t * kValueRow + 32 * step);
+    };
 
-        float to_log2 = a.scale_log2 * scale_k;
-        const bool partly = block * kBlock + kBlock - 1 > wave_first;
-        const int left = last - block * kBlock - 4 * half;      // scores i of tile t whose token 32 t + 8 (i / 4) + i % 4 is at most this are seen
-        if (partly) {
+    // Half t (32 tokens) of a block: its scores z become weights, while the matrix cores make the next half's scores (from keys_next, half t ^ 1)
+    // and add the last half's part to o (from values_last, weights p).  The two share no operand, so their instructions alternate.
+    auto half_block = [&](auto t_const, int block, bool here, float to_log2, uint32_t keys_next, uint32_t values_last, auto beside) {
+        constexpr int t = decltype(t_const)::value;
+        const int from = block * kBlock + 32 * t;
+        if (!here || from + 31 > wave_first) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int mt = 0; mt < MT; ++mt) {
+                const int left = here ? last[mt] - from - 4 * half : -1;        // scores i whose token 8 (i / 4) + i % 4 is at most this are seen
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[t][i] = 32 * t + 8 * (i >> 2) + (i & 3) <= left ? z[t][i] * to_log2 : -__builtin_inff();
+                for (int i = 0; i < 16; ++i) z[mt][i] = 8 * (i >> 2) + (i & 3) <= left ? z[mt][i] * to_log2 : -__builtin_inff();
+            }
             to_log2 = 1.f;      // (a factor of zero would make NaN of what is masked)
         }
-        float most = z[0][0];
+        float most[MT], base[MT];
+        bool rises = false;
 #pragma unroll
-        for (int i = 1; i < 32; ++i) most = fmaxf(most, z[i >> 4][i & 15]);
-        most = max_over_32(most) * to_log2;
-        if (__any(most - m > kSlack)) {
-            const float m_new = fmaxf(m, most);
-            const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
-            m = m_new;
-            l *= factor;
+        for (int mt = 0; mt < MT; ++mt) {
+            most[mt] = z[mt][0];
 #pragma unroll
-            for (int t = 0; t < kOut; ++t) o[t] *= factor;
+            for (int i = 1; i < 16; ++i) most[mt] = fmaxf(most[mt], z[mt][i]);
+            most[mt] = max_over_32(most[mt]) * to_log2;
+            rises |= most[mt] - m[mt] > kSlack;
         }
-        const float base = m == -__builtin_inff() ? 0.f : -m;
-        uint4 p[4];
+        if (__any(rises)) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            uint32_t w[8];
+            for (int mt = 0; mt < MT; ++mt) {
+                const float m_new = fmaxf(m[mt], __builtin_ceilf(most[mt]));
+                const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);     // (a power of two: nothing is rounded)
+                m[mt] = m_new;
+                l[mt] *= factor;
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i], to_log2, base));
-                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[t][i + 1], to_log2, base));
-                l += e0;
-                l += e1;
-                w[i >> 1] = pack2<FC_F16>(e0, e1);
+                for (int i = 0; i < kOut; ++i) o[mt][i] *= factor;
+                const f16x2_t two = __builtin_bit_cast(f16x2_t, pack2<FC_F16>(factor, factor));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t w[4] = {p[mt][i].x, p[mt][i].y, p[mt][i].z, p[mt][i].w};
+                    uint32_t r[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) r[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, w[j]) * two);
+                    p[mt][i] = make_uint4(r[0], r[1], r[2], r[3]);
+                }
             }
-            p[2 * t] = make_uint4(w[0], w[1], w[2], w[3]);
-            p[2 * t + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) base[mt] = m[mt] == -__builtin_inff() ? 0.f : -m[mt];
+        f32x16_t z_next[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z_next[mt][i] = 0.f;
+        // Step by step, in this order: matrix instructions on one operand from LDS, the operand of one kAhead steps on, and the vector unit's work of that time.
+        constexpr int kProducts = 2 * kSteps;
+        auto operand = [&](int i) {
+            return i % 2 == 0 ? key_operand(keys_next, t ^ 1, i / 2) : value_operand(values_last, i / 2 % kOut, 2 * (t ^ 1) + i / 2 / kOut);
+        };
+        uint4 x[kProducts];
+        uint32_t w[MT][8];
+        float e[MT][16];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) x[i] = operand(i);
+#pragma unroll
+        for (int i = 0; i < kProducts; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + kAhead < kProducts) x[i + kAhead] = operand(i + kAhead);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                if (i % 2 == 0) z_next[mt] = mfma_32<DT>(x[i], q[mt][i / 2], z_next[mt]);
+                else o[mt][i / 2 % kOut] = mfma_32<FC_F16>(x[i], p[mt][i / 2 / kOut], o[mt][i / 2 % kOut]);
+#pragma unroll
+                for (int j = 16 * i / kProducts; j < 16 * (i + 1) / kProducts; ++j) {
+                    e[mt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mt][j], to_log2, base[mt]));
+                    l[mt] += e[mt][j];
+                    if (j & 1) {
+                        w[mt][j >> 1] = pack2<FC_F16>(e[mt][j - 1], e[mt][j]);
+                        __asm__ volatile("" : "+v"(w[mt][j >> 1]), "+v"(l[mt]));     // (here, not where it is used)
+                    }
+                }
+                if (MT > 1) __builtin_amdgcn_sched_barrier(0);
+            }
+            // (late: what it works on has then been on its way for longer than a half)
+            if (i >= kProducts / 2 && (i - kProducts / 2) % (kProducts / 2 / (4 * kShare)) == 0) beside((i - kProducts / 2) / (kProducts / 2 / (4 * kShare)));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            p[mt][0] = make_uint4(w[mt][0], w[mt][1], w[mt][2], w[mt][3]);
+            p[mt][1] = make_uint4(w[mt][4], w[mt][5], w[mt][6], w[mt][7]);
+            z[mt] = z_next[mt];
+        }
+    };
+
+    if (begin < end) {
+        // Block j's first half runs with keys of j and values of j - 1 in LDS, its second with keys of j + 1 and values of j.  These are put there beside the
+        // first half, so that a barrier between the halves is the only one; both are brought to registers beside the second half before.
+        // Lane i holds where the i-th of 64 blocks is in the pool and its scales (two blocks ahead of the loop): no scalar load in the loop, behind which the
+        // waits for LDS would be waits for all of it.
+        int32_t held_pool = -1;
+        float2 held_scales = make_float2(1.f, 1.f);
+        auto look_up = [&](int first) {
+            held_pool = -1;
+            if (first + lane < end) {
+                held_pool = pool_block(g, b, first + lane);
+                held_scales = g.scales[unit_of(g, max(held_pool, 0), h)];
+            }
+            __asm__ volatile("" : "+v"(held_pool), "+v"(held_scales.x), "+v"(held_scales.y));      // (waited for here)
+        };
+        auto pool_at = [&](int i) { return __builtin_amdgcn_readlane(held_pool, i & 63); };
+        auto scales_at = [&](int i) {
+            return make_float2(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_scales.x), i & 63)),
+                               __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_scales.y), i & 63)));
+        };
+        look_up(begin);
+        int32_t pool = pool_at(0), pool_next = pool_at(1);
+        float2 scales = scales_at(0), scales_next = scales_at(1);
+        bring(codes_of(pool), kx);
+#pragma unroll
+        for (int i = 0; i < 2 * kShare; ++i) put_keys(0, i / 2, i % 2);
+        bring(codes_of(pool_next), kx);
+        bring(codes_of(pool) + kBlock * DP, vx);
+        for (uint32_t i = threadIdx.x * 16; i < DP * kValueRow; i += kThreads * 16)      // (values before the first: finite, for weights of zero)
+            *reinterpret_cast<uint4 *>(lds + kBuffer + kValues + i) = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[mt][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c) z[mt] = mfma_32<DT>(key_operand(0, 0, c), q[mt][c], z[mt]);
         }
 
+        uint32_t buffer = 0;        // of block j's keys and values; the other one is its neighbours'
+        for (int block = begin; block < end; ++block, buffer = kBuffer - buffer) {
+            const bool here = pool >= 0;
+            const float scale_v = here ? __builtin_fabsf(scales.y) : unit_v;
+            const float to_log2 = here ? a.scale_log2 * scales.x : 1.f;
+            const bool strange = here && scales.y < 0.f;    // NaN among the values: zeros in LDS, found again here
+            if (strange) {
+                const uint8_t *const codes = codes_of(pool);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    const int left = last[mt] - block * kBlock - 4 * half;
+#pragma unroll
+                    for (int t = 0; t < kOut; ++t) {
+                        f32x16_t count;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) count[i] = 0.f;
+#pragma unroll
+                        for (int step = 0; step < 4; ++step) {
+                            // tokens 16 step + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
+                            const uint32_t lo = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * half) + 4 * step);
+                            const uint32_t hi = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * (half + 2)) + 4 * step);
+                            const uint4 seen = make_uint4(seen_pair(16 * step, left), seen_pair(16 * step + 2, left), seen_pair(16 * step + 8, left),
+                                                          seen_pair(16 * step + 10, left));
+                            count = mfma_32<FC_F16>(nan_marks(lo, hi), seen, count);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[mt][t][i] = count[i] > 0.f ? __builtin_nanf("") : o[mt][t][i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kShare; ++i) vx[i] = without_nan(vx[i]);
+            }
+            if (!here)
+#pragma unroll
+                for (int i = 0; i < kShare; ++i) vx[i] = make_uint4(0, 0, 0, 0);     // (finite, for weights of zero)
+            const bool new_unit = !keeps_unit(scale_v, unit_v);
+            const float to_unit = new_unit ? 1.f : pow2_ratio(scale_v, unit_v);
+            half_block(Const<0>(), block, here, to_log2, buffer, kBuffer - buffer, [&](int i) {
+                if (i < 2 * kShare) put_keys(kBuffer - buffer, i / 2, i % 2);
+                else put_values(buffer, to_unit, i / 2 - kShare, i % 2);
+            });
+            __syncthreads();
+
+            if (new_unit) {         // (o has all of the values that are in the old one)
+                const float factor = pow2_ratio(unit_v, scale_v);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int t = 0; t < kOut; ++t) o[mt][t] *= factor;
+                unit_v = scale_v;
+            }
+            pool = pool_next;
+            scales = scales_next;
+            if (block + 1 < end) bring(codes_of(pool) + kBlock * DP, vx);
+            const int after = block + 2 - begin;        // (what is behind the end is not there)
+            if (after % 64 == 0) look_up(block + 2);
+            pool_next = pool_at(after);
+            scales_next = scales_at(after);
+            if (block + 2 < end) bring(codes_of(pool_next), kx);
+            half_block(Const<1>(), block, here, to_log2, kBuffer - buffer, buffer, [](int) {});
+        }
+        // the last half's values
+        buffer = kBuffer - buffer;
 #pragma unroll
         for (int t = 0; t < kOut; ++t)
 #pragma unroll
-            for (int step = 0; step < 4; ++step)
-                o[t] = mfma_32<FC_F16>(*reinterpret_cast<const uint4 *>(values + 32 * t * kValueRow + 32 * step), p[step], o[t]);
-        if (strange) {
-            const uint8_t *const codes = g.codes + unit_of(g, max(pool_block(g, b, block), 0), h) * (2 * kBlock * DP);
+            for (int step = 0; step < 2; ++step)
 #pragma unroll
-            for (int t = 0; t < kOut; ++t) {
-                f32x16_t count;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) count[i] = 0.f;
-#pragma unroll
-                for (int step = 0; step < 4; ++step) {
-                    // tokens 16 step + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
-                    const uint32_t lo = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * half) + 4 * step);
-                    const uint32_t hi = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * (half + 2)) + 4 * step);
-                    const uint4 seen = make_uint4(seen_pair(16 * step, left), seen_pair(16 * step + 2, left), seen_pair(16 * step + 8, left),
-                                                  seen_pair(16 * step + 10, left));
-                    count = mfma_32<FC_F16>(nan_marks(lo, hi), seen, count);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[t][i] = count[i] > 0.f ? __builtin_nanf("") : o[t][i];
-            }
-        }
+                for (int mt = 0; mt < MT; ++mt) o[mt][t] = mfma_32<FC_F16>(value_operand(buffer, t, 2 + step), p[mt][step], o[mt][t]);
     }
 
-    l += __shfl_xor(l, 32);
     const int64_t unit = (int64_t)unit_rows * a.tiles + tile;
     const Pieces<DP> pieces(a, unit, kRows);
     auto out_row = [&](int row) {
         const RowPlace p = row_place(a, tile * kRows + row);
         return (int64_t)(s.row0 + p.token) * a.heads + h * a.group + p.head;
     };
-    if (valid) {
-        const int64_t row = out_row(wave * 32 + col);
-        const uint32_t part = (uint32_t)(split * kRows + wave * 32 + col);
-        if (active > 1 && half == 0) pieces.put_ml(part, m, l);
+    // Pieces are written as the registers hold them, 1 KB a store: [wave][row tile][output tile][four channels][lane].
+    constexpr int kLanes = kOut * 4 * 64;
+    auto place = [&](int item) {
+        const int tile_at = item / kLanes, in = item % kLanes, row = tile_at * 32 + (in & 31);
+        return ItemPlace{row < rows ? row : kNoRow, (in >> 8) * 32 + (in >> 6 & 3) * 8 + (in >> 5 & 1) * 4};
+    };
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const float sum = l[mt] + __shfl_xor(l[mt], 32);
+        const int r = wave * kWaveRows + 32 * mt + col;
+        const int64_t row = out_row(min(r, rows - 1));
+        if (active > 1 && half == 0) pieces.put_ml((uint32_t)(split * kRows + r), m[mt], sum);
+        const uint32_t item = (uint32_t)(split * kRows * (DP / 4) + (wave * MT + mt) * kLanes + lane);
 #pragma unroll
         for (int t = 0; t < kOut; ++t)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const int c = 32 * t + 2 * i + 4 * half;
-                const f32x4_t v = {o[t][i] * unit_v, o[t][i + 1] * unit_v, o[t][i + 2] * unit_v, o[t][i + 3] * unit_v};
-                if (active > 1) pieces.put(part, c, v);
-                else finish_row<DT>(a, row, c, v, m, l);
+                const f32x4_t v = {o[mt][t][i] * unit_v, o[mt][t][i + 1] * unit_v, o[mt][t][i + 2] * unit_v, o[mt][t][i + 3] * unit_v};
+                if (active > 1) pieces.put(item + (t * 4 + i / 4) * 64, v);
+                else if (r < rows) finish_row<DT>(a, row, 32 * t + 2 * i + 4 * half, v, m[mt], sum);
             }
     }
     if (active == 1) return;
     __syncthreads();        // (the flag lies where operands were)
     if (!last_to_arrive(a, unit, active, reinterpret_cast<int32_t *>(lds))) return;
-    join_pieces<DT, DP, kThreads>(a, pieces, rows, kRows, active, reinterpret_cast<float *>(lds) + 4, out_row);
+    join_pieces<DT, DP, kThreads>(a, pieces, (rows + 31) / 32 * kLanes, kRows, active, reinterpret_cast<float *>(lds) + 4, place, out_row);
 }
 
-template <int DT, int DP> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
+template <int DT, int DP, int MT, int WAVES> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
 {
     constexpr size_t lds = 2 * (size_t)(kBlock * kKeyPitch<DP> + DP * kValuePitch);
-    const hipError_t raised = raise_lds<k_attend_tile<DT, DP>>(lds);
+    const hipError_t raised = raise_lds<k_attend_tile<DT, DP, MT, WAVES>>(lds);
     if (raised != hipSuccess) return raised;
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
-    k_attend_tile<DT, DP><<<dim3((uint32_t)(units * a.splits)), kThreads, lds, s>>>(a);
+    k_attend_tile<DT, DP, MT, WAVES><<<dim3((uint32_t)(units * a.splits)), 64 * WAVES, lds, s>>>(a);
     return hipGetLastError();
 }
 
-template <int DT> hipError_t run_type(const AttnArgs &a, hipStream_t s)
+template <int DT> hipError_t run_type(const AttnArgs &a, int rows_tile, hipStream_t s)
 {
     switch (a.kv.dp) {
-    case 64: return run_tile<DT, 64>(a, s);
-    case 128: return run_tile<DT, 128>(a, s);
-    case 192: return run_tile<DT, 192>(a, s);
-    default: return run_tile<DT, 256>(a, s);
+    case 64: return rows_tile == 256 ? run_tile<DT, 64, 1, 4>(a, s) : run_tile<DT, 64, 1, 4>(a, s);
+    case 128: return rows_tile == 256 ? run_tile<DT, 128, 1, 8>(a, s) : run_tile<DT, 128, 1, 4>(a, s);
+    case 192: return run_tile<DT, 192, 1, 4>(a, s);
+    default: return run_tile<DT, 256, 1, 4>(a, s);
     }
 }
 
 } // namespace
 
-hipError_t launch_attend_tile(const AttnArgs &a, int dtype, hipStream_t s)
+hipError_t launch_attend_tile(const AttnArgs &a, int dtype, int rows_tile, hipStream_t s)
 {
-    return dtype == FC_BF16 ? run_type<FC_BF16>(a, s) : run_type<FC_F16>(a, s);
+    return dtype == FC_BF16 ? run_type<FC_BF16>(a, rows_tile, s) : run_type<FC_F16>(a, rows_tile, s);
 }
 
 } // namespace fc

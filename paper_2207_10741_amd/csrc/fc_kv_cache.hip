@@ -18,10 +18,6 @@ struct AppendArgs {
     int32_t wide_k, wide_v;
 };
 
-template <bool V> struct Const {
-    static constexpr bool value = V;
-};
-
 // Four codes under another scale; ratio = old scale / new scale, a power of two.
 __device__ __forceinline__ uint32_t rescale4(uint32_t c, float ratio)
 {

@@ -44,6 +44,9 @@ __device__ __forceinline__ void add_codes(uint2 x, float (&sum)[8])
 // A channel's sum of codes in units of 2^-9, as a sketch holds it under 2^e.
 __device__ __forceinline__ int8_t sketch_of(int sum, int e) { return (int8_t)(int)__builtin_rintf((float)sum * (pow2_of(-e) * (1.f / 512.f))); }
 
+// A unit's codes in LDS: the pieces of every 256 bytes are exchanged by the number of the 256, or the accesses that step by 256 would meet in one bank.
+__device__ __forceinline__ uint32_t in_image(uint32_t offset) { return offset ^ (offset >> 4 & 0xf0u); }
+
 // A value in units of its scale; what is not finite becomes NaN.
 __device__ __forceinline__ float code_of(float v, float inverse)
 {
@@ -173,18 +176,18 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
                 column[2 * i + 1] |= (v2 >> 8 & 0xffu) << (8 * j);
             }
             codes[round][j] = make_uint2(packed[0], packed[1]);
-            if (4 * r < kRows && t < kBlock) *reinterpret_cast<uint2 *>(image + key_piece<DP>(t, 8 * c) + 8 * (c & 1)) = codes[round][j];
+            if (4 * r < kRows && t < kBlock) *reinterpret_cast<uint2 *>(image + in_image(key_piece<DP>(t, 8 * c)) + 8 * (c & 1)) = codes[round][j];
         }
         const int t0 = round * kRows + 4 * r;
         if (4 * r < kRows && t0 < kBlock)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t *>(image + value_piece<DP>(8 * c + i, value_place(t0)) + (value_place(t0) & 15)) = column[i];
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t *>(image + in_image(value_piece<DP>(8 * c + i, value_place(t0))) + (value_place(t0) & 15)) = column[i];
     }
     __syncthreads();
     // A block that is begun is written whole, so that no place of it holds a NaN that its scale does not tell of; else the old tokens keep their bytes.
     for (int i = threadIdx.x; i < 2 * kBlock * (DP / 16); i += kThreads) {
         uint4 *const p = reinterpret_cast<uint4 *>(unit_codes) + i;
-        const uint4 fresh = reinterpret_cast<const uint4 *>(image)[i];
+        const uint4 fresh = *reinterpret_cast<const uint4 *>(image + in_image(16 * i));
         if (old == 0) {
             *p = fresh;
         } else if (i < kBlock * (DP / 16)) {
@@ -356,7 +359,7 @@ template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs
     const bool there = pool >= 0;
     const int64_t unit = unit_of(g, max(pool, 0), h);
     const uint4 *const codes = reinterpret_cast<const uint4 *>(g.codes + unit * (2 * kBlock * DP));
-    for (int i = threadIdx.x; i < 2 * kBlock * (DP / 16); i += kThreads) reinterpret_cast<uint4 *>(image)[i] = there ? codes[i] : make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < 2 * kBlock * (DP / 16); i += kThreads) *reinterpret_cast<uint4 *>(image + in_image(16 * i)) = there ? codes[i] : make_uint4(0, 0, 0, 0);
     __syncthreads();
     const float2 scale = there ? g.scales[unit] : make_float2(0.f, 0.f);
     const float vs = __builtin_fabsf(scale.y);
@@ -376,7 +379,7 @@ template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs
         for (int i = threadIdx.x; i < kBlock * (DP / 4); i += kThreads) {
             const int t = i / (DP / 4), c = i % (DP / 4) * 4;
             if (t < begin || t >= end) continue;
-            const uint32_t x = *reinterpret_cast<const uint32_t *>(image + key_piece<DP>(t, c) + (c & 15));
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(image + in_image(key_piece<DP>(t, c)) + (c & 15));
             const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(x, 0) * scale.x, __builtin_amdgcn_cvt_f32_fp8(x, 1) * scale.x,
                                 __builtin_amdgcn_cvt_f32_fp8(x, 2) * scale.x, __builtin_amdgcn_cvt_f32_fp8(x, 3) * scale.x};
             put(a.k, t, c, v);
@@ -388,7 +391,7 @@ template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs
         float v[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t x = *reinterpret_cast<const uint32_t *>(image + value_piece<DP>(c + j, value_place(t)) + (value_place(t) & 15));
+            const uint32_t x = *reinterpret_cast<const uint32_t *>(image + in_image(value_piece<DP>(c + j, value_place(t))) + (value_place(t) & 15));
             v[0][j] = __builtin_amdgcn_cvt_f32_fp8(x, 0) * vs, v[1][j] = __builtin_amdgcn_cvt_f32_fp8(x, 1) * vs;
             v[2][j] = __builtin_amdgcn_cvt_f32_fp8(x, 2) * vs, v[3][j] = __builtin_amdgcn_cvt_f32_fp8(x, 3) * vs;
         }

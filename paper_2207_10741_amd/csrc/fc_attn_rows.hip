@@ -131,7 +131,7 @@ template <int DT, int DP, int MT> struct Rows {
                 float to_log2 = a.scale_log2 * scales.x;
                 const int from = block * kBlock;
                 const bool partly = from + kBlock - 1 > last_least;
-                if (!keeps_unit(scale_v, unit_v)) {
+                if (__builtin_expect(!keeps_unit(scale_v, unit_v), 0)) {
                     const float factor = pow2_ratio(unit_v, scale_v);
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
@@ -158,7 +158,7 @@ template <int DT, int DP, int MT> struct Rows {
 #pragma unroll
                     for (int i = 1; i < 16; ++i) most = fmaxf(most, z[mt][i >> 2][i & 3]);
                     most = max_over_16(max_over_32(most)) * to_log2;
-                    if (__any(most - m[mt] > kSlack)) {
+                    if (__builtin_expect(__any(most - m[mt] > kSlack), 0)) {
                         const float m_new = fmaxf(m[mt], most);
                         const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);
                         m[mt] = m_new;
@@ -180,7 +180,7 @@ template <int DT, int DP, int MT> struct Rows {
                     p[mt][1] = make_uint4(w[4], w[5], w[6], w[7]);
                 }
 
-                if (partly && scales.y < 0.f) {
+                if (__builtin_expect(partly && scales.y < 0.f, 0)) {
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
                         const int left = last[mt] - from - 4 * quarter;

@@ -109,24 +109,66 @@ __device__ __forceinline__ void write_entries(const uint32_t *keys, int from, in
     }
 }
 
-// The largest threshold with at least `top` keys at or above it, by one wave.  (A trial with exactly that many will do.)
-template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint32_t *keys, int n, int top, int &above)
+// A threshold that `top` of the lanes' keys or more are at or above (exactly as many, or the largest), bit by bit.
+__device__ __forceinline__ uint32_t threshold_of_lanes(uint32_t key, int top)
+{
+    uint32_t threshold = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t trial = threshold | 1u << bit;
+        const int c = (int)__popcll(__ballot(key >= trial));
+        if (c >= top) threshold = trial;
+        if (c == top) break;
+    }
+    return threshold;
+}
+
+// The same for n keys in LDS, by one wave; above: keys above it.  `few`: 64 words of the wave's own.
+// Up to 64: the lanes' largest keys give a threshold that is no higher than the one looked for, and few keys are at or above that one, which then are one a
+// lane: two searches of one key a lane in place of one of all.
+template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint32_t *keys, int n, int top, uint32_t *few, int &above)
 {
     const int lane = threadIdx.x & 63;
     uint32_t held[REGS > 0 ? REGS : 1];
 #pragma unroll
     for (int r = 0; r < REGS; ++r) held[r] = 64 * r + lane < n ? keys[64 * r + lane] : 0;      // (no key is 0: no score is that low)
-    auto count = [&](uint32_t trial) {
-        int c = 0;
+    auto each = [&](auto f) {
         if constexpr (REGS > 0) {
 #pragma unroll
-            for (int r = 0; r < REGS; ++r) c += (int)__popcll(__ballot(held[r] >= trial));
+            for (int r = 0; r < REGS; ++r) f(held[r]);
         } else {
-            for (int i = 0; i < n; i += 64) c += (int)__popcll(__ballot(i + lane < n && keys[i + lane] >= trial));
+            for (int i = 0; i < n; i += 64) f(i + lane < n ? keys[i + lane] : 0);
         }
+    };
+    auto count = [&](uint32_t trial) {
+        int c = 0;
+        each([&](uint32_t key) { c += (int)__popcll(__ballot(key >= trial)); });
         return c;
     };
     uint32_t threshold = 0;
+    if (top <= 64) {
+        uint32_t largest_key = 0;
+        each([&](uint32_t key) { largest_key = max(largest_key, key); });
+        const uint32_t least = max(threshold_of_lanes(largest_key, top), 1u);
+        const int some = count(least);
+        if (some == top) {
+            above = count(least + 1);
+            return least;
+        }
+        if (some <= 64) {
+            const uint64_t below = (1ull << lane) - 1;
+            int at = 0;
+            each([&](uint32_t key) {
+                const uint64_t takes = __ballot(key >= least);
+                if (key >= least) few[at + __popcll(takes & below)] = key;
+                at += (int)__popcll(takes);
+            });
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const uint32_t key = lane < some ? few[lane] : 0;
+            threshold = threshold_of_lanes(key, top);
+            above = (int)__popcll(__ballot(key > threshold));
+            return threshold;
+        }
+    }
     for (int bit = 31; bit >= 0; --bit) {
         const uint32_t trial = threshold | 1u << bit;
         const int c = count(trial);
@@ -142,7 +184,7 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
     constexpr int kChunks = DP / 64, kShare = kThreads / QT;        // threads of a token
     extern __shared__ uint32_t lds_keys[];
     __shared__ __align__(16) int8_t q8[2][QT][DP];                  // hi, lo
-    __shared__ uint32_t amax[QT];
+    __shared__ uint32_t amax[QT], few[kThreads / 64][64];
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreads) a.clear[i] = 0;
     const KvGeom &g = a.kv;
     uint32_t at = blockIdx.x;
@@ -222,9 +264,9 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
         const int candidates = own + 1 - a.first - a.last;      // (more than top)
         const uint32_t *const keys = lds_keys + mine * a.stride + a.first;
         int above;
-        const uint32_t threshold = candidates <= 256 ? threshold_of<4>(keys, candidates, a.top, above) :
-                                   candidates <= 512 ? threshold_of<8>(keys, candidates, a.top, above) :
-                                   candidates <= 1024 ? threshold_of<16>(keys, candidates, a.top, above) : threshold_of<0>(keys, candidates, a.top, above);
+        const uint32_t threshold = candidates <= 256 ? threshold_of<4>(keys, candidates, a.top, few[wave], above) :
+                                   candidates <= 512 ? threshold_of<8>(keys, candidates, a.top, few[wave], above) :
+                                   candidates <= 1024 ? threshold_of<16>(keys, candidates, a.top, few[wave], above) : threshold_of<0>(keys, candidates, a.top, few[wave], above);
         write_entries(keys, 0, candidates, threshold, a.top - above, a.first, out + a.first);
     }
 }

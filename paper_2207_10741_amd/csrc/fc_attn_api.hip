@@ -58,6 +58,7 @@ struct Plan {
     int32_t rows_tile, tiles, splits, per_split, waves;
     int64_t units;              // of rows: sequences x key heads x tiles
     bool whole;                 // a wave takes a token's whole list
+    int32_t shared, mask_words, entries;        // ... or those of several tokens
     size_t counters, workspace; // bytes; none where nothing is split
 };
 
@@ -97,6 +98,10 @@ void cut_for_rounds(int64_t units, int32_t blocks, int32_t mean, int32_t *splits
 // Lists: from this many on there are enough to fill the chip with a wave each (us, split -> whole, 16 and 32 blocks of 8 key heads of 128: 512 units 36 -> 39,
 // 57 -> 69; 1024 68 -> 67, 121 -> 119; 1600 120 -> 118; 2800 of 9 blocks 53 -> 44).
 constexpr int64_t kWholeLists = 1024;
+// Neighbouring tokens' lists together: from this many waves on (us, apart -> together, lists of 16 blocks of 8 key heads of 128, keys that select independently:
+// 4 heads a key head, 512 / 1024 / 2048 / 4096 tokens (1024 waves on) 79 / 132 / 245 / 475 -> 81 / 114 / 203 / 389; one head a key head, 4096 tokens 469 -> 333;
+// tokens that select alike gain as much more as they share).
+constexpr int64_t kSharedLists = 2048;
 
 int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *p)
 {
@@ -107,14 +112,24 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
     if ((int64_t)d->tokens * d->heads >= INT32_MAX || (int64_t)d->max_new * group >= INT32_MAX / 2) return FC_ERR_RANGE;
     const int64_t rows = (int64_t)d->max_new * group;
     int32_t blocks = (g.max_len + kBlock - 1) / kBlock;
+    p->shared = 1, p->mask_words = p->entries = 0;
     if (list) {
         if (d->first < 0 || d->last < 1 || d->top < 0 || d->first > FC_MAX_SELECTED || d->last > FC_MAX_SELECTED || d->top > FC_MAX_SELECTED ||
             d->first + d->last + d->top > FC_MAX_SELECTED)
             return FC_ERR_SHAPE;
         if (blocks > kSelectMaxBlocks) return FC_ERR_RANGE;
-        blocks = blocks < d->first + d->last + d->top ? blocks : d->first + d->last + d->top;
+        const int32_t width = d->first + d->last + d->top, all = blocks;
+        blocks = blocks < width ? blocks : width;
         p->rows_tile = 16;
         p->tiles = d->max_new * ((group + 15) / 16);
+        const int32_t together = group <= 8 ? 16 / group : 1;
+        const int32_t tiles = (d->max_new + together - 1) / together;
+        if (together > 1 && all <= kSharedMaxBlocks && (int64_t)d->batch * d->kv_heads * tiles >= kSharedLists) {
+            p->shared = together;
+            p->tiles = tiles;
+            p->mask_words = (all + 1) / 2;
+            p->entries = (int64_t)together * width < all ? together * width : all;
+        }
     } else {
         // 256 rows share a block's conversion where there are enough of them for two rounds of a workgroup a CU (us, 128 -> 256 rows, 32 heads of 128 over 8:
         // 8192 tokens 565 -> 544, 4096 158 -> 148, two times 2048 after 16000 996 -> 932; 2048 56 -> 83)
@@ -123,7 +138,7 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
         p->tiles = (int32_t)((rows + p->rows_tile - 1) / p->rows_tile);
     }
     const int64_t units = p->units = (int64_t)d->batch * d->kv_heads * p->tiles;
-    p->whole = list && units >= kWholeLists;
+    p->whole = list && (p->shared > 1 || units >= kWholeLists);
     if (p->whole) {
         p->per_split = blocks;
         p->splits = 1;
@@ -193,6 +208,7 @@ int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, con
     a.div_group = make_fastdiv((uint32_t)a.group);
     a.selected = list ? selected : nullptr;
     a.selected_width = d->first + d->last + d->top;
+    a.shared = p.shared; a.mask_words = p.mask_words; a.entries = p.entries;
     a.tiles = p.tiles; a.splits = p.splits; a.per_split = p.per_split;
     a.arrived = static_cast<int32_t *>(workspace);
     a.part_out = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.counters);

@@ -202,6 +202,7 @@ struct AttnArgs {
     float *lse;
     const int32_t *selected;    // (list form)
     int32_t selected_width;
+    int32_t shared, mask_words, entries;    // tokens a wave takes together; words of its LDS for masks and entries
     int32_t heads, group, causal;
     int32_t wide;               // q's rows are 16-byte pieces
     float scale_log2;           // |scale| * log2(e); a negative scale changes the queries' signs
@@ -442,7 +443,9 @@ hipError_t launch_kv_read(const KvGeom &g, float *k, float *v, hipStream_t s);
 
 // Few rows (see fc_attn_rows.hip); rows_tile: rows a workgroup holds, 16 or 32; waves: its waves, 4 or (16 rows of up to 128 channels) 8.
 hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, int waves, hipStream_t s);
-// 16 rows of one token, over its list of blocks; a wave's, or (a.splits counts the pieces) a workgroup's.
+// Rows of one token, over its list of blocks; a wave's (of a.shared tokens, over all of theirs), or (a.splits counts the pieces) a workgroup's.
+constexpr int kSharedMaxBlocks = 2048;                                  // of a sequence: masks and entries fit a wave's share of LDS
+constexpr int kSharedMaxWords = kSharedMaxBlocks / 2 + kSharedMaxBlocks;
 hipError_t launch_attend_lists(const AttnArgs &a, int dtype, bool whole, hipStream_t s);
 
 // Many rows (see fc_attn_tile.hip); rows_tile: rows a workgroup holds, 128 or (up to 128 channels) 256.

@@ -6,11 +6,16 @@
 // half a block in flight.
 //   k_attend_rows: the waves of a workgroup take a piece's blocks of the sequence (or of a token's list) in turn and are joined through LDS; the last workgroup joins the pieces.
 //   k_attend_lists: a wave takes a token's whole list.
+//   k_attend_shared: a wave takes as many neighbouring tokens as fill its 16 rows, and every block that one of them has in its list once.
 #include "fc_attn_internal.hpp"
 
 namespace fc {
 
 namespace {
+
+// The blocks a wave goes over: the sequence's own, those of a list, or entries of several tokens' lists together (the block, and from bit 16 on a bit for every
+// token that has it).
+enum { kAllBlocks, kListed, kShared };
 
 // A wave's rows and its running softmax.
 template <int DT, int DP, int MT> struct Rows {
@@ -20,6 +25,7 @@ template <int DT, int DP, int MT> struct Rows {
     float m[MT], l[MT], unit_v;     // weights are 2^(z - m); l: this lane's part of their sum
     int last[MT];                   // the last position that the lane's row attends to
     int last_least;                 // ... of all rows
+    uint32_t token, tokens;         // (kShared: the lane's token of the entries', and the bits of all)
 
     __device__ __forceinline__ void clear()
     {
@@ -47,7 +53,7 @@ template <int DT, int DP, int MT> struct Rows {
     }
 
     // Blocks first, first + step, ... below end of the sequence or of its list (both in order).
-    template <bool LIST>
+    template <int BLOCKS>
     __device__ __forceinline__ void run(const AttnArgs &a, int b, int h, const int32_t *__restrict__ list, int first, int step, int end)
     {
         const KvGeom &g = a.kv;
@@ -61,8 +67,8 @@ template <int DT, int DP, int MT> struct Rows {
             const int j = from + lane * step;
             held_block = 0, held_pool = -1;
             if (j < end) {
-                held_block = LIST ? list[j] : j;
-                held_pool = pool_block(g, b, held_block);
+                held_block = BLOCKS == kAllBlocks ? j : list[j];
+                held_pool = pool_block(g, b, BLOCKS == kShared ? held_block & 0xffff : held_block);
                 held_scales = g.scales[unit_of(g, max(held_pool, 0), h)];
             }
         };
@@ -129,8 +135,10 @@ template <int DT, int DP, int MT> struct Rows {
             if (here) {
                 const float scale_v = __builtin_fabsf(scales.y);
                 float to_log2 = a.scale_log2 * scales.x;
-                const int from = block * kBlock;
+                const int from = (BLOCKS == kShared ? block & 0xffff : block) * kBlock;
                 const bool partly = from + kBlock - 1 > last_least;
+                const uint32_t have = (uint32_t)block >> 16;            // (kShared) the tokens that have the block
+                const bool mine = BLOCKS != kShared || (have >> token & 1u), all = BLOCKS != kShared || have == tokens;
                 if (__builtin_expect(!keeps_unit(scale_v, unit_v), 0)) {
                     const float factor = pow2_ratio(unit_v, scale_v);
 #pragma unroll
@@ -158,6 +166,7 @@ template <int DT, int DP, int MT> struct Rows {
 #pragma unroll
                     for (int i = 1; i < 16; ++i) most = fmaxf(most, z[mt][i >> 2][i & 3]);
                     most = max_over_16(max_over_32(most)) * to_log2;
+                    if (BLOCKS == kShared) most = mine ? most : -__builtin_inff();
                     if (__builtin_expect(__any(most - m[mt] > kSlack), 0)) {
                         const float m_new = fmaxf(m[mt], most);
                         const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);
@@ -168,22 +177,29 @@ template <int DT, int DP, int MT> struct Rows {
                     }
                     const float base = m[mt] == -__builtin_inff() ? 0.f : -m[mt];
                     uint32_t w[8];
+                    float sum = 0.f;
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
                         const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mt][i >> 2][i & 3], to_log2, base));
                         const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mt][i >> 2][(i & 3) + 1], to_log2, base));
-                        l[mt] += e0;
-                        l[mt] += e1;
+                        sum += e0;
+                        sum += e1;
                         w[i >> 1] = pack2<FC_F16>(e0, e1);
                     }
+                    if (BLOCKS == kShared && !all) {
+                        sum = mine ? sum : 0.f;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = mine ? w[i] : 0;
+                    }
+                    l[mt] += sum;
                     p[mt][0] = make_uint4(w[0], w[1], w[2], w[3]);
                     p[mt][1] = make_uint4(w[4], w[5], w[6], w[7]);
                 }
 
-                if (__builtin_expect(partly && scales.y < 0.f, 0)) {
+                if (__builtin_expect((partly || !all) && scales.y < 0.f, 0)) {
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
-                        const int left = last[mt] - from - 4 * quarter;
+                        const int left = mine ? last[mt] - from - 4 * quarter : -1;
                         uint4 seen[2];
                         seen[0] = make_uint4(seen_pair(0, left), seen_pair(2, left), seen_pair(16, left), seen_pair(18, left));
                         seen[1] = make_uint4(seen_pair(32, left), seen_pair(34, left), seen_pair(48, left), seen_pair(50, left));
@@ -283,7 +299,7 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
         w.bring_queries(a, mt, a.q + (s.row0 + token0 + p.token) * a.q_row + (int64_t)(h * a.group + p.head) * a.q_head);
     }
     const int32_t *const list = LIST ? a.selected + ((int64_t)(s.row0 + token0) * g.kv_heads + h) * a.selected_width : nullptr;
-    w.template run<LIST>(a, b, h, list, split * a.per_split + wave, kWaves, end);
+    w.template run<LIST ? kListed : kAllBlocks>(a, b, h, list, split * a.per_split + wave, kWaves, end);
 
     // the waves' parts through LDS
 #pragma unroll
@@ -353,10 +369,70 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     w.clear();
     w.last_least = w.last[0] = pos;
     w.bring_queries(a, 0, a.q + (s.row0 + token) * a.q_row + (int64_t)(h * a.group + head) * a.q_head);
-    w.template run<true>(a, b, h, a.selected + ((int64_t)(s.row0 + token) * g.kv_heads + h) * a.selected_width, 0, 1, listed_blocks(a, pos));
+    w.template run<kListed>(a, b, h, a.selected + ((int64_t)(s.row0 + token) * g.kv_heads + h) * a.selected_width, 0, 1, listed_blocks(a, pos));
     const float sum = row_sum(w.l[0]);
     if (!valid) return;
     const int64_t row = (int64_t)(s.row0 + token) * a.heads + h * a.group + head;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit_v, w.m[0], sum);
+}
+
+// A wave takes a.shared neighbouring tokens of a sequence (a.shared * group <= 16 rows).  Their lists are put together in LDS: a mask of tokens for every block
+// of the sequence, and the blocks with one, in order.  Blocks that neighbours share, the first and the last ones among them, are read and multiplied once,
+// and the rows of the matrix instructions, of which one token fills `group`, are used.
+template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupancy<DP, 1>)) void k_attend_shared(AttnArgs a)
+{
+    constexpr int kTiles = DP / 16;
+    extern __shared__ __align__(16) uint32_t lds_words[];
+    const KvGeom &g = a.kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
+    const uint32_t eighth = gridDim.x / 8;      // (the grid is a multiple of eight)
+    uint32_t at = (blockIdx.x % 8 * eighth + blockIdx.x / 8) * kListWaves + wave;
+    const int tile = at % a.tiles;
+    at /= a.tiles;
+    const int h = at % g.kv_heads, b = at / g.kv_heads;
+    if (b >= g.batch) return;
+    const Sequence s = sequence_of(g, b);
+    const int token0 = tile * a.shared, tokens = min(a.shared, s.n - token0);
+    if (tokens <= 0) return;
+    uint32_t *const words = lds_words + wave * (a.mask_words + a.entries);      // two blocks' masks a word
+    int32_t *const entries = reinterpret_cast<int32_t *>(words + a.mask_words);
+
+    const int pos = s.pos0 + token0, pos_last = pos + tokens - 1, blocks = pos_last < 0 ? 0 : pos_last / kBlock + 1;
+    for (int i = lane; i < (blocks + 1) / 2; i += 64) words[i] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int32_t *const lists = a.selected + ((int64_t)(s.row0 + token0) * g.kv_heads + h) * a.selected_width;
+    for (int i = lane; i < tokens * a.selected_width; i += 64) {
+        const int t = i / a.selected_width;
+        const int32_t block = lists[(int64_t)t * g.kv_heads * a.selected_width + i % a.selected_width];
+        if ((uint32_t)block < (uint32_t)blocks) atomicOr(&words[block >> 1], 1u << (t + 16 * (block & 1)));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    int count = 0;
+    const uint64_t below = (1ull << lane) - 1;
+    for (int i = 0; i < blocks; i += 64) {
+        const int block = i + lane;
+        const uint32_t have = block < blocks ? words[block >> 1] >> (16 * (block & 1)) & 0xffffu : 0;
+        const uint64_t takes = __ballot(have != 0);
+        if (have) entries[count + (int)__popcll(takes & below)] = block | (int32_t)(have << 16);
+        count += (int)__popcll(takes);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+
+    const int rows = tokens * a.group;
+    const bool valid = col < rows;
+    const RowPlace p = row_place(a, min(col, rows - 1));        // (rows behind the last repeat it and are left out below)
+    Rows<DT, DP, 1> w;
+    w.clear();
+    w.last_least = pos;
+    w.last[0] = pos + p.token;
+    w.token = (uint32_t)p.token;
+    w.tokens = (1u << tokens) - 1u;
+    w.bring_queries(a, 0, a.q + (s.row0 + token0 + p.token) * a.q_row + (int64_t)(h * a.group + p.head) * a.q_head);
+    w.template run<kShared>(a, b, h, entries, 0, 1, count);
+    const float sum = row_sum(w.l[0]);
+    if (!valid) return;
+    const int64_t row = (int64_t)(s.row0 + token0 + p.token) * a.heads + h * a.group + p.head;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit_v, w.m[0], sum);
 }
@@ -376,6 +452,14 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> hipError_t run_rows(cons
 template <int DT, int DP> hipError_t run_lists(const AttnArgs &a, bool whole, hipStream_t s)
 {
     if (!whole) return run_rows<DT, DP, 1, 4, true>(a, s);
+    if (a.shared > 1) {
+        const size_t lds = (size_t)kListWaves * (a.mask_words + a.entries) * sizeof(uint32_t);
+        const hipError_t e = raise_lds<k_attend_shared<DT, DP>>((size_t)kListWaves * kSharedMaxWords * sizeof(uint32_t));
+        if (e != hipSuccess) return e;
+        const int64_t waves = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
+        k_attend_shared<DT, DP><<<dim3((uint32_t)((waves + 8 * kListWaves - 1) / (8 * kListWaves) * 8)), 64 * kListWaves, lds, s>>>(a);
+        return hipGetLastError();
+    }
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
     k_attend_lists<DT, DP><<<dim3((uint32_t)((units + 8 * kListWaves - 1) / (8 * kListWaves) * 8)), 64 * kListWaves, 0, s>>>(a);
     return hipGetLastError();

@@ -137,3 +137,41 @@ def test_nan_in_pieces(new):
     assert np.isnan(out[sees][:, :, 3]).all() and np.isfinite(out[~sees][:, :, 3]).all()
     others = [c for c in range(128) if c not in (3, 5)]
     assert np.isfinite(out[:, :, others]).all()
+
+
+@pytest.mark.parametrize("group,dim,dtype,top", [(1, 64, B.BF16, 2), (2, 128, B.F16, 9), (3, 64, B.BF16, 5), (5, 96, B.F16, 20), (8, 192, B.BF16, 3)])
+def test_neighbouring_tokens_together(group, dim, dtype, top):
+    """Tokens whose lists a wave takes together: rows that share some blocks and not others, sequences' last tokens that do not fill a wave."""
+    length, batch, new = 64 * 40 + 13, 1100, 19
+    setup, table, lengths = _shared(length, batch, dim, dtype)
+    q, qn = setup.queries(batch * new, group)
+    out, selected = A.focused_attention(setup.cache, q, table, lengths, first=1, last=1, top=top)
+    picks = [(b * new + i, length - new + i) for b, i in ((0, 0), (0, 18), (311, 4), (311, 5), (1099, 15), (1099, 16), (1099, 18))]
+    lists = {r: O.select(setup.oracle[0], qn[r], position, 1, 1, top) for r, position in picks}
+    for r, _ in picks:
+        assert np.array_equal(selected[r].cpu().numpy(), lists[r])
+    _check(setup, out, qn, [(0, r, position) for r, position in picks], None, lists=lists)
+
+
+def test_blocks_of_other_tokens_have_no_influence():
+    """Keys and values that are NaN or infinite in a block that neighbours select and a token does not."""
+    length, batch, new = 64 * 40, 2100, 8
+
+    def poisoned(b, k, v):
+        k[64 * 7 + 3, :, 2] = np.nan
+        v[64 * 9 + 5, :, 4] = np.inf
+        return k, v
+    setup = Setup([length], 1, 64, B.BF16, tokens=poisoned)
+    table, lengths = setup.table.expand(batch, -1).contiguous(), _int32([length] * batch)
+    q, qn = setup.queries(batch * new, 2)
+    out, selected = A.focused_attention(setup.cache, q, table, lengths, first=0, last=1, top=4)
+    out, selected = G.to_f64(out), selected.cpu().numpy()[:, 0]
+    key, value = (selected == 7).any(axis=1), (selected == 9).any(axis=1)
+    assert 0 < key.sum() < len(key) and 0 < value.sum() < len(value)
+    assert np.isnan(out[key]).all()
+    assert np.isfinite(out[~key & ~value]).all()
+    assert np.isnan(out[~key & value][:, :, 4]).all() and np.isfinite(np.delete(out[~key & value], 4, axis=2)).all()
+    # the same rows one by one
+    for r in np.flatnonzero(~key)[:3]:
+        want, _, error = O.attend(setup.oracle[0], qn[r], length - new + r % new, 0.125, True, selected[r][None])
+        assert (np.abs(out[r] - want)[~np.isnan(want)] <= (error + LAST_PLACE[B.BF16] * (np.abs(want) + error))[~np.isnan(want)]).all()

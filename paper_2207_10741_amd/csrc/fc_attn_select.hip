@@ -271,18 +271,13 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
     }
 }
 
-// Inclusive sum over the wave's lanes, and the sum over each 16 of them in their last lane.
-__device__ __forceinline__ int sum_over_row(int v)
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int sum_up_to(int v)
 {
     v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);     // row_shr by 1, 2, 4, 8
     v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
     v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
     v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-    return v;
-}
-__device__ __forceinline__ int sum_up_to(int v)
-{
-    v = sum_over_row(v);
     v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);     // the last lane of a row to the next row
     v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);     // ... of the first half to the second
     return v;
@@ -293,7 +288,9 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
     constexpr int kChunks = DP / 64, kWaves = kThreadsOne / 64;
     extern __shared__ uint32_t lds_keys[];
     __shared__ __align__(16) int bins[4][256];
-    __shared__ int aboves[kWaves], equals[kWaves];
+    __shared__ __align__(16) int8_t q8[2][DP];      // hi, lo
+    __shared__ int sums[DP], aboves[kWaves], equals[kWaves];
+    __shared__ uint32_t amax;
     for (int i = blockIdx.x * kThreadsOne + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreadsOne) a.clear[i] = 0;
     const KvGeom &g = a.kv;
     uint32_t at = blockIdx.x;
@@ -309,64 +306,55 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
     const int scored = own - a.last + 1, candidates = scored - a.first;
     bins[threadIdx.x >> 8][threadIdx.x & 255] = 0;
 
-    // Every wave rounds the queries for itself: column `col` of the product is head 16 i + col, its scores are summed behind it.
+    for (int i = threadIdx.x; i < DP; i += kThreadsOne) sums[i] = 0;
+    if (threadIdx.x == 0) amax = 0;
+
     Sketches<DP> x;
     x.bring(g, b, h, 16 * wave, scored);
+    // The queries, an element a thread (of more than 1024 the others are read twice)
     const uint16_t *const q = a.q + (int64_t)(s.row0 + token) * a.q_row + (int64_t)h * a.group * a.q_head;
-    auto piece = [&](int head, int c, int half) {
-        return head < a.group ? load8(q + head * a.q_head, 64 * c + 16 * quarter + 8 * half, g.d, a.wide) : make_uint4(0, 0, 0, 0);
+    const int elements = a.group * DP;
+    auto query = [&](int i) {
+        const int head = i / DP, c = i % DP;
+        const float v = i < elements && c < g.d ? bits_to_float<DT>(q[head * a.q_head + c]) : 0.f;
+        return finite(v) ? v : 0.f;
     };
-    uint4 mine[kChunks][2];
-    {
-        const uint16_t *const row = q + min(col, a.group - 1) * a.q_head;
-        if (a.wide) {
-#pragma unroll
-            for (int c = 0; c < 2 * kChunks; ++c) mine[c >> 1][c & 1] = load8<true>(row, (c >> 1) * 64 + 16 * quarter + (c & 1) * 8, g.d);
-        } else {
-#pragma unroll
-            for (int c = 0; c < 2 * kChunks; ++c) mine[c >> 1][c & 1] = load8<false>(row, (c >> 1) * 64 + 16 * quarter + (c & 1) * 8, g.d);
-        }
-    }
-    float most = 0.f;
-#pragma unroll
-    for (int c = 0; c < 2 * kChunks; ++c) {
-        if (col >= a.group) mine[c >> 1][c & 1] = make_uint4(0, 0, 0, 0);
-        most = largest<DT>(mine[c >> 1][c & 1], most);
-    }
-    for (int head = 16 + col; head < a.group; head += 16)
-        for (int c = 0; c < kChunks; ++c) most = largest<DT>(piece(head, c, 1), largest<DT>(piece(head, c, 0), most));
+    const float mine = query(threadIdx.x);
+    float most = __builtin_fabsf(mine);
+    for (int i = threadIdx.x + kThreadsOne; i < elements; i += kThreadsOne) most = fmaxf(most, __builtin_fabsf(query(i)));
 #pragma unroll
     for (int m = 1; m < 16; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
     most = max_over_16(max_over_32(most));
-    const float inverse = pow2_of(-unit_exponent(most));
-    auto rounded = [&](const uint4 &lo, const uint4 &hi) {
-        i32x4_t r = {0, 0, 0, 0};
+    __syncthreads();
+    if (lane == 0 && most > 0.f) atomicMax(&amax, __float_as_uint(most));
+    __syncthreads();
+    const float inverse = pow2_of(-unit_exponent(__uint_as_float(amax)));
+    for (int i = threadIdx.x; i < elements; i += kThreadsOne)
+        atomicAdd(&sums[i % DP], (int)__builtin_rintf((i < kThreadsOne ? mine : query(i)) * inverse));
+    __syncthreads();
+    if (threadIdx.x < DP) {
+        q8[0][threadIdx.x] = (int8_t)(sums[threadIdx.x] >> 7);
+        q8[1][threadIdx.x] = (int8_t)(sums[threadIdx.x] & 127);
+    }
+    __syncthreads();
+    i32x4_t parts[kChunks];         // column 0 of the product's operand is hi, column 1 lo
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float v = element<DT>(j < 8 ? lo : hi, j & 7);
-            const int n = finite(v) ? (int)__builtin_rintf(v * inverse) : 0;
-            r[j >> 2] |= (n & 0xff) << (8 * (j & 3));
-        }
-        return r;
-    };
-    i32x4_t q8[kChunks];
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) q8[c] = rounded(mine[c][0], mine[c][1]);
+    for (int c = 0; c < kChunks; ++c) {
+        parts[c] = i32x4_t{0, 0, 0, 0};
+        if (col < 2) parts[c] = *reinterpret_cast<const i32x4_t *>(&q8[col][64 * c + 16 * quarter]);
+    }
     for (int first = 16 * wave; first < scored; first += 16 * kWaves) {
         i32x4_t sum = {0, 0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x.x[c], q8[c], sum, 0, 0, 0);
-        for (int head = 16; head < a.group; head += 16)
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-                sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x.x[c], rounded(piece(head + col, c, 0), piece(head + col, c, 1)), sum, 0, 0, 0);
+        for (int c = 0; c < kChunks; ++c) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(x.x[c], parts[c], sum, 0, 0, 0);
         const float weight = x.weight;
         if (first + 16 * kWaves < scored) x.bring(g, b, h, first + 16 * kWaves, scored);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int total = sum_over_row(sum[i]), to = first + quarter * 4 + i;
+            const int lo = __builtin_amdgcn_update_dpp(0, sum[i], 0x101, 0xf, 0xf, false);      // row_shl by 1: column 1's
+            const int to = first + quarter * 4 + i;
             const float w = __shfl(weight, quarter * 4 + i);
-            if (col == 15 && to < scored) lds_keys[to] = key_of((float)total * w);
+            if (col == 0 && to < scored) lds_keys[to] = key_of((float)(128 * sum[i] + lo) * w);
         }
     }
     __syncthreads();

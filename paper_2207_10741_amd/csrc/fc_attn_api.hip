@@ -41,6 +41,9 @@ int32_t make_kv_geom(const fc_attention_desc *d, const void *cache, const int32_
     return FC_OK;
 }
 
+// A workgroup of 256 threads a touched block and head: one dimension of a grid, which is counted in threads.
+bool blocks_fit(const KvGeom &g) { return ((int64_t)touched_blocks(g) + 1) * g.kv_heads < 1 << 24; }
+
 int32_t check_pointers(const void *cache, const int32_t *table, const int32_t *lengths, const int32_t *starts)
 {
     if (!cache || !table || !lengths) return FC_ERR_NULL;
@@ -245,6 +248,7 @@ int32_t fc_kv_append(const fc_attention_desc *d, void *cache, const void *k, con
     int32_t rc = make_kv_geom(d, cache, table, lengths, starts, &g);
     if (rc != FC_OK) return rc;
     if (!known_type(d->dtype)) return FC_ERR_DTYPE;
+    if (!blocks_fit(g)) return FC_ERR_RANGE;
     if (d->k_row < 0 || d->k_head < 0 || d->v_row < 0 || d->v_head < 0) return FC_ERR_SHAPE;
     if (d->tokens == 0) return FC_OK;
     rc = check_pointers(cache, table, lengths, starts);
@@ -262,6 +266,7 @@ int32_t fc_kv_read(const fc_attention_desc *d, const void *cache, const int32_t 
     KvGeom g;
     int32_t rc = make_kv_geom(d, cache, table, lengths, starts, &g);
     if (rc != FC_OK) return rc;
+    if (!blocks_fit(g)) return FC_ERR_RANGE;
     if (d->tokens == 0) return FC_OK;
     rc = check_pointers(cache, table, lengths, starts);
     if (rc != FC_OK) return rc;

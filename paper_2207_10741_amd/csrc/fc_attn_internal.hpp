@@ -48,6 +48,14 @@ static inline KvLayout kv_layout(int32_t blocks, int32_t kv_heads, int32_t head_
     return l;
 }
 
+// Blocks that a sequence's new tokens can touch, at most.
+static inline int32_t touched_blocks(const KvGeom &g)
+{
+    const int32_t n = g.max_new < g.tokens ? g.max_new : g.tokens;
+    const int32_t touched = (int32_t)(((int64_t)n + kBlock - 2) / kBlock) + 1, held = (int32_t)(((int64_t)g.max_len + kBlock - 1) / kBlock);
+    return touched < held ? touched : held;
+}
+
 // A sequence as its arrays describe it, cut to the call's bounds: rows row0 .. row0 + n - 1 are its new tokens, row0 has position pos0
 // (negative: rows without a position come first).
 struct Sequence {

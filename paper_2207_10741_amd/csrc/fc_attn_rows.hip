@@ -248,6 +248,8 @@ __device__ __forceinline__ int listed_blocks(const AttnArgs &a, int pos) { retur
 template <int DP, int MT> constexpr int kOccupancy = DP * MT <= 64 ? 4 : DP * MT <= 128 ? 2 : 1;
 constexpr int kListWaves = 4;
 
+// Bound by memory where there are blocks enough: 64 tokens over caches of up to 8192, 8 heads of 128 with 4 queries each, 685 MB: 134 us, 5.1 TB/s, the rate of
+// a large copy; one token over 131 000, 268 MB: 55 us, 4.9 TB/s.  Below, by round trips (lengths, table, scales and codes, pieces, join): one token over 1000: 8.5 us.
 template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_bounds__(64 * WAVES, (kOccupancy<DP, MT>)) void k_attend_rows(AttnArgs a)
 {
     constexpr int kWaves = WAVES, kThreads = 64 * kWaves;
@@ -347,6 +349,8 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
     join_pieces<DT, DP, kThreads>(a, pieces, rows * kPieces, kRows, active, lds, place, out_row);
 }
 
+// Bound by the vector unit, which converts a block's codes for the few rows of one token, and by latency where there are few lists: 2800 lists of nine blocks,
+// two heads of 96 with five queries each: 27 us, one round of waves.
 // A wave takes up to 16 heads of one token and the token's whole list.  An XCD takes an eighth of the units in one piece: neighbouring tokens of a head
 // share blocks.
 template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupancy<DP, 1>)) void k_attend_lists(AttnArgs a)
@@ -377,6 +381,8 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit_v, w.m[0], sum);
 }
 
+// Bound by the vector unit as the lists alone are: 235 instructions a block, most of them conversions of codes.  4096 tokens over 512 blocks, lists of 16,
+// 8 heads of 128 with 4 queries each: 355 us in the profile (lists one a wave: 500).
 // A wave takes a.shared neighbouring tokens of a sequence (a.shared * group <= 16 rows).  Their lists are put together in LDS: a mask of tokens for every block
 // of the sequence, and the blocks with one, in order.  Blocks that neighbours share, the first and the last ones among them, are read and multiplied once,
 // and the rows of the matrix instructions, of which one token fills `group`, are used.

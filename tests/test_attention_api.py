@@ -89,6 +89,13 @@ def test_append_and_read_refuse():
     assert _read(_desc(), k=None, v=None) == NULL and _read(_desc(), v=ctypes.c_void_p(20)) == ALIGN
 
 
+@pytest.mark.parametrize("call", [_append, _read])
+def test_more_blocks_than_a_grid_holds_are_refused(call):
+    many = dict(batch=1, kv_heads=16, heads=16, max_new=2 ** 26, max_len=2 ** 30, table_width=2 ** 24)
+    assert call(_desc(tokens=2 ** 26, **many), starts=_p(9)) == RANGE
+    assert call(_desc(tokens=0, **many), starts=_p(9)) == 0         # (the rows bound the blocks that new tokens touch)
+
+
 @pytest.mark.parametrize("call", [_attend, _focused])
 def test_attention_refuses(call):
     assert call(_desc(heads=7)) == SHAPE and call(_desc(heads=0)) == SHAPE and call(_desc(heads=-2)) == SHAPE

@@ -1,14 +1,16 @@
 // Declarations shared by the attention operators' translation units: the cache's layout, what a sequence's arrays say, conversions.
 //
 // Layout of the cache.  A unit is one block of one key/value head: unit = pool block * kv_heads + head.
-//   codes    [unit][128 * dp] bytes: keys, then values; dp = head_dim rounded up to a multiple of 64, zeros behind
+//   codes    [unit][128 * dp] bytes: keys, then values; dp = head_dim rounded up to 64, 96, 128, 192 or 256, zeros behind
 //   scales   [unit] of two floats: the keys' scale; the values', negative where a value of the block is NaN
-//   sketches [unit][dp] signed bytes, weights [unit] floats
+//   sketches [unit][dp rounded up to a multiple of 64] signed bytes (behind dp anything: queries are zeros there), weights [unit] floats
 // Keys and values lie in the order in which the matrix instructions want them, so that a load of 16 bytes a lane is 1 KB in one piece.  (The L1 gives
 // 65 bytes a clock then, and 18 where sixteen lanes read from rows of 128 bytes, keys as [token][channel].)  A lane of the 16x16 instructions holds
 // eight consecutive places of the reduction, lanes 16 apart the next eight (quarter = lane / 16):
 //   scores S^T = K q^T: a lane's row is a token, and 16 channels of it are its share of two instructions: pieces
-//     [token / 16][channel / 64][channel / 16 % 4][token % 16] of 16 channels.
+//     [token / 16][channel / 64][channel / 16 % 4][token % 16] of 16 channels.  Of 96 channels the last 32 are one instruction's: the pieces
+//     [token / 32][1][channel / 8 % 4][token % 16] hold 8 channels of a token and the same of the token 16 further, between those tokens' first 64 channels
+//     [token / 32][0 or 2][channel / 16][token % 16].
 //   out^T = V^T P^T: P^T comes out of the first product with tokens 4 quarter + i of each 16 (i = 0 .. 3) in the lane that needs them as operand, so no
 //     weight moves between lanes if V's rows are in that order too: token 32 h + 16 k + 4 quarter + i is at place 16 quarter + 8 h + 4 k + i:
 //     pieces [channel / 16][place / 16][channel % 16] of 16 places, a lane's share for a whole block.
@@ -31,7 +33,10 @@ struct KvGeom {
     const int32_t *table, *lengths, *starts;
 };
 
-static inline int32_t padded_dim(int32_t d) { return (d + 63) / 64 * 64; }
+// (96 for the head sizes 65 to 96, which a multiple of 64 would make 128 of: a quarter less to keep, read, convert and multiply; us at 128 -> at 96, pieces of up to 517
+// tokens over 5003 with heads of 80 63.1 -> 57.5, lists of 9 blocks with heads of 96 39.5 -> 35.3)
+static inline int32_t padded_dim(int32_t d) { return d > 64 && d <= 96 ? 96 : (d + 63) / 64 * 64; }
+template <int DP> constexpr int kSketch = (DP + 63) / 64 * 64;
 
 // Byte offsets of the cache's sections and its size.
 struct KvLayout {
@@ -43,7 +48,7 @@ static inline KvLayout kv_layout(int32_t blocks, int32_t kv_heads, int32_t head_
     KvLayout l;
     l.scales = units * 2 * kBlock * dp;
     l.sketches = l.scales + align_up(units * sizeof(float2), 256);
-    l.weights = l.sketches + align_up(units * dp, 256);
+    l.weights = l.sketches + align_up(units * ((dp + 63) / 64 * 64), 256);
     l.bytes = l.weights + align_up(units * sizeof(float), 256);
     return l;
 }
@@ -92,10 +97,29 @@ __host__ __device__ __forceinline__ int value_place(int token)
     return (token >> 2 & 3) << 4 | (token >> 5) << 3 | (token >> 4 & 1) << 2 | (token & 3);
 }
 
-// Offsets in a unit's codes of the piece of 16 bytes that holds an element; element & 15 is its place in the piece.
-template <int DP> __host__ __device__ __forceinline__ uint32_t key_piece(uint32_t token, uint32_t channel)
+// Offsets in a unit's codes: of a key's channel, and of the piece of 16 bytes that holds a value (place & 15 is its place in the piece).
+// Channels c .. c + 7, c a multiple of 8, are next to each other.
+template <int DP> __host__ __device__ __forceinline__ uint32_t key_at(uint32_t token, uint32_t channel)
 {
-    return ((((token >> 4) * (DP / 64) + (channel >> 6)) * 4 + (channel >> 4 & 3)) * 16 + (token & 15)) * 16;
+    if (DP == 96) {
+        const uint32_t pair = (token >> 5) * 3, which = token >> 4 & 1;
+        if (channel >= 64) return (((pair + 1) * 4 + (channel >> 3 & 3)) * 16 + (token & 15)) * 16 + which * 8 + (channel & 7);
+        return (((pair + which * 2) * 4 + (channel >> 4)) * 16 + (token & 15)) * 16 + (channel & 15);
+    }
+    return ((((token >> 4) * (DP / 64) + (channel >> 6)) * 4 + (channel >> 4 & 3)) * 16 + (token & 15)) * 16 + (channel & 15);
+}
+// What half `half` (of 8 channels) of piece `piece` of the keys holds.
+struct KeyHalf {
+    uint32_t token, channel;
+};
+template <int DP> __host__ __device__ __forceinline__ KeyHalf key_half(uint32_t piece, uint32_t half)
+{
+    const uint32_t load = piece >> 6, group = piece >> 4 & 3, token = piece & 15;
+    if (DP == 96) {
+        const uint32_t nth = load % 3;
+        return nth == 1 ? KeyHalf{load / 3 * 32 + half * 16 + token, 64 + group * 8} : KeyHalf{load / 3 * 32 + nth * 8 + token, group * 16 + half * 8};
+    }
+    return {load / (DP / 64) * 16 + token, load % (DP / 64) * 64 + group * 16 + half * 8};
 }
 template <int DP> __host__ __device__ __forceinline__ uint32_t value_piece(uint32_t channel, uint32_t place)
 {

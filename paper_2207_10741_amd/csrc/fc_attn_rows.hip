@@ -19,8 +19,8 @@ enum { kAllBlocks, kListed, kShared };
 
 // A wave's rows and its running softmax.
 template <int DT, int DP, int MT> struct Rows {
-    static constexpr int kChunks = DP / 64, kTiles = DP / 16;
-    uint4 q[MT][2 * kChunks];
+    static constexpr int kLoads = DP / 16, kTiles = DP / 16, kOperands = DP / 32;      // loads of a block's keys, of its values; instructions of 16 tokens' scores
+    uint4 q[MT][kOperands];
     f32x4_t o[MT][kTiles];          // in units of unit_v
     float m[MT], l[MT], unit_v;     // weights are 2^(z - m); l: this lane's part of their sum
     int last[MT];                   // the last position that the lane's row attends to
@@ -45,12 +45,15 @@ template <int DT, int DP, int MT> struct Rows {
         const int quarter = (threadIdx.x & 63) >> 4, d = a.kv.d;
         if (a.wide) {
 #pragma unroll
-            for (int c = 0; c < 2 * kChunks; ++c) q[mt][c] = flip_signs(load8<true>(row, (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, d), a.signs);
+            for (int c = 0; c < kOperands; ++c) q[mt][c] = flip_signs(load8<true>(row, channel_of(c, quarter), d), a.signs);
         } else {
 #pragma unroll
-            for (int c = 0; c < 2 * kChunks; ++c) q[mt][c] = flip_signs(load8<false>(row, (c >> 1) * 64 + quarter * 16 + (c & 1) * 8, d), a.signs);
+            for (int c = 0; c < kOperands; ++c) q[mt][c] = flip_signs(load8<false>(row, channel_of(c, quarter), d), a.signs);
         }
     }
+
+    // The first of the eight channels that the lane holds of operand c (key_at's order).
+    __device__ static __forceinline__ int channel_of(int c, int quarter) { return DP == 96 && c == 2 ? 64 + quarter * 8 : (c >> 1) * 64 + quarter * 16 + (c & 1) * 8; }
 
     // Blocks first, first + step, ... below end of the sequence or of its list (both in order).
     template <int BLOCKS>
@@ -83,11 +86,9 @@ template <int DT, int DP, int MT> struct Rows {
         auto codes_of = [&](int32_t p) {
             return __builtin_amdgcn_make_buffer_rsrc(g.codes + unit_of(g, max(p, 0), h) * (2 * kBlock * DP), 0, p < 0 ? 0 : 2 * kBlock * DP, 0x00020000);
         };
-        uint4 kx[4][kChunks], vx[kTiles];
-        auto bring_keys = [&](__amdgpu_buffer_rsrc_t from, int t) {
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-                kx[t][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16, (t * kChunks + c) * 1024, 0));
+        uint4 kx[kLoads], vx[kTiles];
+        auto bring_keys = [&](__amdgpu_buffer_rsrc_t from, int n) {
+            kx[n] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16, n * 1024, 0));
         };
         auto bring_values = [&](__amdgpu_buffer_rsrc_t from, int t) {
             vx[t] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(from, lane * 16, kBlock * DP + t * 1024, 0));
@@ -95,7 +96,7 @@ template <int DT, int DP, int MT> struct Rows {
         {
             const auto codes = codes_of(pool);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) bring_keys(codes, t);
+            for (int n = 0; n < kLoads; ++n) bring_keys(codes, n);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) bring_values(codes, t);
         }
@@ -117,19 +118,39 @@ template <int DT, int DP, int MT> struct Rows {
 
             f32x4_t z[MT][4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) z[mt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            auto scores = [&](int t, const uint4 &k, int c) {
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
-                    const uint4 k0 = codes_to_16<DT>(kx[t][c].x, kx[t][c].y), k1 = codes_to_16<DT>(kx[t][c].z, kx[t][c].w);
+                for (int mt = 0; mt < MT; ++mt) z[mt][t] = mfma16<DT>(k, q[mt][c], z[mt][t]);
+            };
+            if constexpr (DP == 96) {
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        z[mt][t] = mfma16<DT>(k0, q[mt][2 * c], z[mt][t]);
-                        z[mt][t] = mfma16<DT>(k1, q[mt][2 * c + 1], z[mt][t]);
-                    }
+                for (int pair = 0; pair < 2; ++pair) {
+                    scores(2 * pair, codes_to_16<DT>(kx[3 * pair].x, kx[3 * pair].y), 0);
+                    scores(2 * pair, codes_to_16<DT>(kx[3 * pair].z, kx[3 * pair].w), 1);
+                    bring_keys(codes_next, 3 * pair);
+                    scores(2 * pair, codes_to_16<DT>(kx[3 * pair + 1].x, kx[3 * pair + 1].y), 2);
+                    scores(2 * pair + 1, codes_to_16<DT>(kx[3 * pair + 1].z, kx[3 * pair + 1].w), 2);
+                    bring_keys(codes_next, 3 * pair + 1);
+                    scores(2 * pair + 1, codes_to_16<DT>(kx[3 * pair + 2].x, kx[3 * pair + 2].y), 0);
+                    scores(2 * pair + 1, codes_to_16<DT>(kx[3 * pair + 2].z, kx[3 * pair + 2].w), 1);
+                    bring_keys(codes_next, 3 * pair + 2);
                 }
-                bring_keys(codes_next, t);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+#pragma unroll
+                    for (int c = 0; c < DP / 64; ++c) {
+                        const int n = t * (DP / 64) + c;
+                        const uint4 k0 = codes_to_16<DT>(kx[n].x, kx[n].y), k1 = codes_to_16<DT>(kx[n].z, kx[n].w);
+                        scores(t, k0, 2 * c);
+                        scores(t, k1, 2 * c + 1);
+                    }
+#pragma unroll
+                    for (int c = 0; c < DP / 64; ++c) bring_keys(codes_next, t * (DP / 64) + c);
+                }
             }
 
             if (here) {
@@ -350,7 +371,7 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
 }
 
 // Bound by the vector unit, which converts a block's codes for the few rows of one token, and by latency where there are few lists: 2800 lists of nine blocks,
-// two heads of 96 with five queries each: 27 us, one round of waves.
+// two heads of 96 with five queries each: 25 us, one round of waves.
 // A wave takes up to 16 heads of one token and the token's whole list.  An XCD takes an eighth of the units in one piece: neighbouring tokens of a head
 // share blocks.
 template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupancy<DP, 1>)) void k_attend_lists(AttnArgs a)
@@ -382,7 +403,7 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
 }
 
 // Bound by the vector unit as the lists alone are: 235 instructions a block, most of them conversions of codes.  4096 tokens over 512 blocks, lists of 16,
-// 8 heads of 128 with 4 queries each: 355 us in the profile (lists one a wave: 500).
+// 8 heads of 128 with 4 queries each: 355 - 363 us (lists one a wave: 500).
 // A wave takes a.shared neighbouring tokens of a sequence (a.shared * group <= 16 rows).  Their lists are put together in LDS: a mask of tokens for every block
 // of the sequence, and the blocks with one, in order.  Blocks that neighbours share, the first and the last ones among them, are read and multiplied once,
 // and the rows of the matrix instructions, of which one token fills `group`, are used.
@@ -487,6 +508,7 @@ hipError_t launch_attend_rows(const AttnArgs &a, int dtype, int rows_tile, int w
     const bool b = dtype == FC_BF16;
     switch (a.kv.dp) {
     case 64: return b ? run_dim<FC_BF16, 64>(a, rows_tile, waves, s) : run_dim<FC_F16, 64>(a, rows_tile, waves, s);
+    case 96: return b ? run_dim<FC_BF16, 96>(a, rows_tile, waves, s) : run_dim<FC_F16, 96>(a, rows_tile, waves, s);
     case 128: return b ? run_dim<FC_BF16, 128>(a, rows_tile, waves, s) : run_dim<FC_F16, 128>(a, rows_tile, waves, s);
     case 192: return b ? run_dim<FC_BF16, 192>(a, rows_tile, waves, s) : run_dim<FC_F16, 192>(a, rows_tile, waves, s);
     default: return b ? run_dim<FC_BF16, 256>(a, rows_tile, waves, s) : run_dim<FC_F16, 256>(a, rows_tile, waves, s);
@@ -498,6 +520,7 @@ hipError_t launch_attend_lists(const AttnArgs &a, int dtype, bool whole, hipStre
     const bool b = dtype == FC_BF16;
     switch (a.kv.dp) {
     case 64: return b ? run_lists<FC_BF16, 64>(a, whole, s) : run_lists<FC_F16, 64>(a, whole, s);
+    case 96: return b ? run_lists<FC_BF16, 96>(a, whole, s) : run_lists<FC_F16, 96>(a, whole, s);
     case 128: return b ? run_lists<FC_BF16, 128>(a, whole, s) : run_lists<FC_F16, 128>(a, whole, s);
     case 192: return b ? run_lists<FC_BF16, 192>(a, whole, s) : run_lists<FC_F16, 192>(a, whole, s);
     default: return b ? run_lists<FC_BF16, 256>(a, whole, s) : run_lists<FC_F16, 256>(a, whole, s);

@@ -51,7 +51,8 @@ template <int DT> __device__ __forceinline__ float largest(const uint4 &x, float
 
 // The sketches of 16 blocks: a lane's share, and (lanes alike in lane % 16) a block's weight.
 template <int DP> struct Sketches {
-    i32x4_t x[DP / 64];
+    static constexpr int kChunks = kSketch<DP> / 64;
+    i32x4_t x[kChunks];
     float weight;
     __device__ __forceinline__ void bring(const KvGeom &g, int b, int h, int first, int end)
     {
@@ -61,15 +62,15 @@ template <int DP> struct Sketches {
         // (of a block that is not there another one's sketch, without weight)
         weight = g.weights[unit];
 #pragma unroll
-        for (int c = 0; c < DP / 64; ++c) x[c] = *reinterpret_cast<const i32x4_t *>(g.sketches + unit * DP + 64 * c + (lane >> 4) * 16);
+        for (int c = 0; c < kChunks; ++c) x[c] = *reinterpret_cast<const i32x4_t *>(g.sketches + unit * kSketch<DP> + 64 * c + (lane >> 4) * 16);
         if (pool < 0) weight = 0.f;
     }
     // keys of blocks 4 (lane / 16) + i and token lane % 16
-    __device__ __forceinline__ void score(const i32x4_t (&hi)[DP / 64], const i32x4_t (&lo)[DP / 64], uint32_t (&keys)[4]) const
+    __device__ __forceinline__ void score(const i32x4_t (&hi)[kChunks], const i32x4_t (&lo)[kChunks], uint32_t (&keys)[4]) const
     {
         i32x4_t up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < DP / 64; ++c) {
+        for (int c = 0; c < kChunks; ++c) {
             up = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[c], hi[c], up, 0, 0, 0);
             down = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[c], lo[c], down, 0, 0, 0);
         }
@@ -183,9 +184,9 @@ template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint3
 // each, up to 512 blocks: 60 us.
 template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_select(SelectArgs a)
 {
-    constexpr int kChunks = DP / 64, kShare = kThreads / QT;        // threads of a token
+    constexpr int SP = kSketch<DP>, kChunks = SP / 64, kShare = kThreads / QT;        // threads of a token
     extern __shared__ uint32_t lds_keys[];
-    __shared__ __align__(16) int8_t q8[2][QT][DP];                  // hi, lo
+    __shared__ __align__(16) int8_t q8[2][QT][SP];                  // hi, lo
     __shared__ uint32_t amax[QT], few[kThreads / 64][64];
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreads) a.clear[i] = 0;
     const KvGeom &g = a.kv;
@@ -215,7 +216,7 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
         }
         __syncthreads();
         const float inverse = pow2_of(-unit_exponent(__uint_as_float(amax[mine])));
-        for (int c = share; c < DP / 8; c += kShare) {
+        for (int c = share; c < SP / 8; c += kShare) {       // (behind head_dim: zeros)
             int sum[8] = {};
             if (mine < tokens)
                 for (int head = 0; head < a.group; ++head) {
@@ -288,11 +289,11 @@ __device__ __forceinline__ int sum_up_to(int v)
 // One token over 512 blocks, 8 heads of 128: 7.8 us; 16 tokens over up to 1016 blocks: 11.9 us (queries, sketches, two to four rounds of counting, the list: dependent steps).
 template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_select_one(SelectArgs a)
 {
-    constexpr int kChunks = DP / 64, kWaves = kThreadsOne / 64;
+    constexpr int SP = kSketch<DP>, kChunks = SP / 64, kWaves = kThreadsOne / 64;
     extern __shared__ uint32_t lds_keys[];
     __shared__ __align__(16) int bins[4][256];
-    __shared__ __align__(16) int8_t q8[2][DP];      // hi, lo
-    __shared__ int sums[DP], aboves[kWaves], equals[kWaves];
+    __shared__ __align__(16) int8_t q8[2][SP];      // hi, lo
+    __shared__ int sums[SP], aboves[kWaves], equals[kWaves];
     __shared__ uint32_t amax;
     for (int i = blockIdx.x * kThreadsOne + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreadsOne) a.clear[i] = 0;
     const KvGeom &g = a.kv;
@@ -309,7 +310,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
     const int scored = own - a.last + 1, candidates = scored - a.first;
     bins[threadIdx.x >> 8][threadIdx.x & 255] = 0;
 
-    for (int i = threadIdx.x; i < DP; i += kThreadsOne) sums[i] = 0;
+    for (int i = threadIdx.x; i < SP; i += kThreadsOne) sums[i] = 0;
     if (threadIdx.x == 0) amax = 0;
 
     Sketches<DP> x;
@@ -335,7 +336,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
     for (int i = threadIdx.x; i < elements; i += kThreadsOne)
         atomicAdd(&sums[i % DP], (int)__builtin_rintf((i < kThreadsOne ? mine : query(i)) * inverse));
     __syncthreads();
-    if (threadIdx.x < DP) {
+    if (threadIdx.x < SP) {
         q8[0][threadIdx.x] = (int8_t)(sums[threadIdx.x] >> 7);
         q8[1][threadIdx.x] = (int8_t)(sums[threadIdx.x] & 127);
     }
@@ -444,6 +445,7 @@ template <int DT> hipError_t run_type(const SelectArgs &a, hipStream_t s)
 {
     switch (a.kv.dp) {
     case 64: return run_dim<DT, 64>(a, s);
+    case 96: return run_dim<DT, 96>(a, s);
     case 128: return run_dim<DT, 128>(a, s);
     case 192: return run_dim<DT, 192>(a, s);
     default: return run_dim<DT, 256>(a, s);

@@ -24,7 +24,8 @@ constexpr uint32_t kValuePitch = 2 * kBlock + 16;
 template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * WAVES, DP * MT <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
 {
     constexpr int kWaves = WAVES, kThreads = 64 * kWaves, kWaveRows = 32 * MT, kRows = kWaveRows * kWaves, kSteps = DP / 16, kOut = DP / 32;
-    constexpr int kShare = 4 * DP / kThreads;       // 16-byte pieces of the codes of keys (values) a thread brings
+    constexpr int kShare = (4 * DP + kThreads - 1) / kThreads;      // 16-byte pieces of the codes of keys (values) a thread brings
+    constexpr bool kEven = 4 * DP % kThreads == 0;                  // (every thread; else the last ones are some waves')
     // rows of keys and values in LDS; the 16 bytes behind each put rows that are read together into different banks
     constexpr uint32_t kKeyRow = kKeyPitch<DP>, kValues = kBlock * kKeyRow, kValueRow = kValuePitch, kBuffer = kValues + DP * kValueRow;
     extern __shared__ __align__(16) unsigned char lds[];
@@ -86,11 +87,11 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
     }
 
     // where the thread's first pieces go and where the lane's operands are, from a buffer's start on
-    auto key_place = [](uint32_t piece) {       // (see key_piece)
-        const uint32_t channel = (piece >> 6) % (DP / 64) * 64 + (piece >> 4 & 3) * 16, token = (piece >> 6) / (DP / 64) * 16 + (piece & 15);
-        return token * kKeyRow + channel * 2;
+    auto key_place = [](uint32_t piece, uint32_t n) {
+        const KeyHalf k = key_half<DP>(piece, n);
+        return k.token * kKeyRow + k.channel * 2;
     };
-    const uint32_t key_to = key_place(threadIdx.x);
+    const uint32_t key_to = key_place(threadIdx.x, 0);
     // four words of four tokens 16 w + 4 quarter .. + 3: as the scores' lanes hold them, half `quarter & 1`
     const uint32_t value_to = kValues + ((threadIdx.x >> 6) * 16 + (threadIdx.x & 15)) * kValueRow + (threadIdx.x >> 4 & 1) * 16 + (threadIdx.x >> 5 & 1) * 8;
     const uint32_t key_at = col * kKeyRow + half * 16, value_at = kValues + col * kValueRow + half * 16;
@@ -100,15 +101,18 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
     auto codes_of = [&](int32_t pool) { return g.codes + unit_of(g, max(pool, 0), h) * (2 * kBlock * DP); };
     auto bring = [&](const uint8_t *from, uint4 (&x)[kShare]) {
 #pragma unroll
-        for (int i = 0; i < kShare; ++i) x[i] = *reinterpret_cast<const uint4 *>(from + i * kThreads * 16 + threadIdx.x * 16u);
+        for (int i = 0; i < kShare; ++i)
+            if (kEven || i * kThreads + (int)threadIdx.x < 4 * DP) x[i] = *reinterpret_cast<const uint4 *>(from + i * kThreads * 16 + threadIdx.x * 16u);
     };
     // (kThreads pieces further: a constant unless they split a token's channels)
-    auto key_step = [&](int i) { return DP % 192 ? key_place(i * kThreads) : key_place(threadIdx.x + i * kThreads) - key_to; };
+    auto key_step = [&](int i, int n) { return DP % 96 ? key_place(i * kThreads, n) : key_place(threadIdx.x + i * kThreads, n) - key_to; };
     // half a piece of keys (16 bytes in LDS) and of values (two words of four tokens)
     auto put_keys = [&](uint32_t buffer, int i, int n) {
-        *reinterpret_cast<uint4 *>(lds + buffer + key_to + key_step(i) + 16 * n) = n ? codes_to_16<DT>(kx[i].z, kx[i].w) : codes_to_16<DT>(kx[i].x, kx[i].y);
+        if (!kEven && i * kThreads + (int)threadIdx.x >= 4 * DP) return;
+        *reinterpret_cast<uint4 *>(lds + buffer + key_to + key_step(i, n)) = n ? codes_to_16<DT>(kx[i].z, kx[i].w) : codes_to_16<DT>(kx[i].x, kx[i].y);
     };
     auto put_values = [&](uint32_t buffer, float to_unit, int i, int n) {
+        if (!kEven && i * kThreads + (int)threadIdx.x >= 4 * DP) return;
         const uint4 x = n ? codes_to_f16(vx[i].z, vx[i].w, to_unit) : codes_to_f16(vx[i].x, vx[i].y, to_unit);
         unsigned char *const to = lds + buffer + value_to + i * (kThreads / 4 * kValueRow) + 64 * n;
         *reinterpret_cast<uint2 *>(to) = make_uint2(x.x, x.y);
@@ -200,7 +204,9 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
                 if (MT > 1) __builtin_amdgcn_sched_barrier(0);
             }
             // (late: what it works on has then been on its way for longer than a half)
-            if (i >= kProducts / 2 && (i - kProducts / 2) % (kProducts / 2 / (4 * kShare)) == 0) beside((i - kProducts / 2) / (kProducts / 2 / (4 * kShare)));
+            constexpr int kLate = kProducts / 2, kBeside = 4 * kShare;
+#pragma unroll
+            for (int n = ((i - kLate) * kBeside + kLate - 1) / kLate; i >= kLate && n < ((i + 1 - kLate) * kBeside + kLate - 1) / kLate; ++n) beside(n);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -369,6 +375,7 @@ template <int DT> hipError_t run_type(const AttnArgs &a, int rows_tile, hipStrea
 {
     switch (a.kv.dp) {
     case 64: return rows_tile == 256 ? run_tile<DT, 64, 1, 4>(a, s) : run_tile<DT, 64, 1, 4>(a, s);
+    case 96: return run_tile<DT, 96, 1, 4>(a, s);
     case 128: return rows_tile == 256 ? run_tile<DT, 128, 1, 8>(a, s) : run_tile<DT, 128, 1, 4>(a, s);
     case 192: return run_tile<DT, 192, 1, 4>(a, s);
     default: return run_tile<DT, 256, 1, 4>(a, s);

@@ -127,7 +127,7 @@ def test_selection_refuses():
 
 def test_sizes():
     assert A.cache_bytes(10, 2, 128) >= 10 * 2 * 128 * 128
-    assert A.cache_bytes(10, 2, 65) == A.cache_bytes(10, 2, 128)
+    assert A.cache_bytes(10, 2, 65) == A.cache_bytes(10, 2, 96) < A.cache_bytes(10, 2, 97) == A.cache_bytes(10, 2, 128)
     assert A.cache_bytes(2 ** 20, 16, 128) > 2 ** 37
     with pytest.raises(B.FcError) as e:
         A.cache_bytes(0, 2, 128)

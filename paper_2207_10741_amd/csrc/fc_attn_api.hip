@@ -135,9 +135,10 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
         }
     } else {
         // 256 rows share a block's conversion where there are enough of them for two rounds of a workgroup a CU (us, 128 -> 256 rows, 32 heads of 128 over 8:
-        // 8192 tokens 565 -> 544, 4096 158 -> 148, two times 2048 after 16000 996 -> 932; 2048 56 -> 83)
+        // 8192 tokens 565 -> 544, 4096 158 -> 148, two times 2048 after 16000 996 -> 932; 2048 56 -> 83; of 96: 8192 481 -> 459, 4096 137 -> 125, of 80, two times 3000 over
+        // 9000, 634 -> 601; of 64, where a block is as soon converted: 8192 357 -> 365, 4096 107 -> 101, not taken)
         const int64_t large = (rows + 255) / 256 * d->batch * d->kv_heads;
-        p->rows_tile = rows <= 16 ? 16 : rows <= 32 && g.dp <= 128 ? 32 : large >= 512 && g.dp == 128 ? 256 : 128;
+        p->rows_tile = rows <= 16 ? 16 : rows <= 32 && g.dp <= 128 ? 32 : large >= 512 && (g.dp == 96 || g.dp == 128) ? 256 : 128;
         p->tiles = (int32_t)((rows + p->rows_tile - 1) / p->rows_tile);
     }
     const int64_t units = p->units = (int64_t)d->batch * d->kv_heads * p->tiles;

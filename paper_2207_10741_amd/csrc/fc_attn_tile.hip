@@ -374,8 +374,8 @@ template <int DT, int DP, int MT, int WAVES> hipError_t run_tile(const AttnArgs 
 template <int DT> hipError_t run_type(const AttnArgs &a, int rows_tile, hipStream_t s)
 {
     switch (a.kv.dp) {
-    case 64: return rows_tile == 256 ? run_tile<DT, 64, 1, 4>(a, s) : run_tile<DT, 64, 1, 4>(a, s);
-    case 96: return run_tile<DT, 96, 1, 4>(a, s);
+    case 64: return run_tile<DT, 64, 1, 4>(a, s);
+    case 96: return rows_tile == 256 ? run_tile<DT, 96, 1, 8>(a, s) : run_tile<DT, 96, 1, 4>(a, s);
     case 128: return rows_tile == 256 ? run_tile<DT, 128, 1, 8>(a, s) : run_tile<DT, 128, 1, 4>(a, s);
     case 192: return run_tile<DT, 192, 1, 4>(a, s);
     default: return run_tile<DT, 256, 1, 4>(a, s);

@@ -59,3 +59,12 @@ def test_neighbouring_tokens_of_head_sizes_about_96(group, dim, dtype, top):
 @pytest.mark.parametrize("heads,group,dim,dtype", [(2, 4, 96, B.BF16), (1, 18, 72, B.F16)])
 def test_lists_of_head_sizes_about_96(heads, group, dim, dtype):
     long.test_lists_of_a_piece_of_a_prompt(heads, group, dim, dtype)
+
+
+@pytest.mark.parametrize("length,new,heads,group,dim,dtype,causal", [
+    (2100, 2100, 16, 4, 64, B.BF16, True),
+    (2100, 2050, 16, 4, 40, B.F16, False),
+    (2100, 2050, 16, 4, 72, B.F16, False),
+])
+def test_many_rows_of_small_heads(length, new, heads, group, dim, dtype, causal):
+    long.test_rows_of_long_calls(length, new, heads, group, dim, dtype, causal)

@@ -42,7 +42,7 @@
  *     the `top` with the largest score, ties to the lowest number.
  *   - score = float(sum over the group's heads and the channels of q8 * sketch) * weight, q8 = round(q / 2^g) to nearest even, 2^g the least power of
  *     two (g of [-126, 120]) with |q| <= 127 * 2^g over the group's heads (not-finite values count as zero).  The sum is of whole numbers, so a
- *     selection does not depend on the order of summation.
+ *     selection does not depend on the order of summation.  A group has at most 32767 heads, a sequence's bound is at most 32768 blocks (FC_ERR_RANGE).
  *   - selected: [tokens][kv_heads][first + last + top], block numbers of the sequence, ascending, -1 behind the last.
  *
  * Conventions are those of focused_conv.h: device pointers, a stream, nothing allocated and no waiting, argument errors found before

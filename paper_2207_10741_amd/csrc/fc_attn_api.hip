@@ -120,7 +120,7 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
         if (d->first < 0 || d->last < 1 || d->top < 0 || d->first > FC_MAX_SELECTED || d->last > FC_MAX_SELECTED || d->top > FC_MAX_SELECTED ||
             d->first + d->last + d->top > FC_MAX_SELECTED)
             return FC_ERR_SHAPE;
-        if (blocks > kSelectMaxBlocks) return FC_ERR_RANGE;
+        if (blocks > kSelectMaxBlocks || group > kMostGroup) return FC_ERR_RANGE;
         const int32_t width = d->first + d->last + d->top, all = blocks;
         blocks = blocks < width ? blocks : width;
         p->rows_tile = 16;

@@ -485,6 +485,7 @@ hipError_t launch_attend_tile(const AttnArgs &a, int dtype, int rows_tile, hipSt
 
 // The selection (see fc_attn_select.hip).
 constexpr int kSelectMaxBlocks = 32768;     // blocks of a sequence whose scores fit LDS
+constexpr int kMostGroup = 32767;           // heads of a group whose rounded queries' sum fits three signed 8-bit digits: 255 * 32767 <= 127 * (65536 + 256 + 1)
 // clear, n_clear: counters that the attention behind it wants zero.
 hipError_t launch_select(const KvGeom &g, int dtype, const uint16_t *q, int64_t q_row, int64_t q_head, int heads, bool wide, int first, int last,
                          int top, int32_t *selected, int32_t *clear, int32_t n_clear, hipStream_t s);

@@ -1,7 +1,7 @@
 // Which blocks a token attends to: every block's sketch against the token's queries, then the best ones in order.
 //
 // The scores are products of 8-bit whole numbers on the matrix cores (v_mfma_i32_16x16x64_i8: 16 blocks x 16 tokens; the group's queries are
-// summed first and taken apart again into 128 hi + lo), so they do not depend on an order of summation; they stay in LDS.  The `top` best are
+// summed first and taken apart again into signed digits, lo + 256 hi + 65536 top), so they do not depend on an order of summation; they stay in LDS.  The `top` best are
 // those at or above a threshold, which is found from its highest bit on by counting (ballots), and the list comes out in order by ballots, as the
 // kept lists of masks are made.
 //   k_select: 16 (4) tokens a workgroup; a wave finds one token's threshold.  Prompts.
@@ -37,6 +37,15 @@ template <int DT> __device__ __forceinline__ float element(const uint4 &x, int j
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
     return bits_to_float<DT>((uint16_t)(w[j >> 1] >> (16 * (j & 1))));
 }
+// The digits of a sum of rounded queries.  A rounded query is at most 255 (127 below the units' bound), so two digits hold the sums of groups of up to kTwoDigits
+// heads (255 * 127 = 32385 of 32639) and three those of up to kMostGroup; two digits' products with sketches of 256 channels add up in 32 bits, three in 64.
+constexpr int kTwoDigits = 127;
+__device__ __forceinline__ int digit_of(int sum, int nth)
+{
+    const int lo = (int8_t)sum, hi = (int8_t)((sum - lo) >> 8);
+    return nth == 0 ? lo : nth == 1 ? hi : (sum - lo - 256 * hi) >> 16;
+}
+
 __device__ __forceinline__ bool finite(float v) { return __builtin_fabsf(v) < __builtin_inff(); }
 
 template <int DT> __device__ __forceinline__ float largest(const uint4 &x, float most)
@@ -66,17 +75,23 @@ template <int DP> struct Sketches {
         if (pool < 0) weight = 0.f;
     }
     // keys of blocks 4 (lane / 16) + i and token lane % 16
-    __device__ __forceinline__ void score(const i32x4_t (&hi)[kChunks], const i32x4_t (&lo)[kChunks], uint32_t (&keys)[4]) const
+    template <int DIGITS> __device__ __forceinline__ void score(const i32x4_t (&q)[DIGITS][kChunks], uint32_t (&keys)[4]) const
     {
-        i32x4_t up = {0, 0, 0, 0}, down = {0, 0, 0, 0};
+        i32x4_t sum[DIGITS];
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            up = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[c], hi[c], up, 0, 0, 0);
-            down = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[c], lo[c], down, 0, 0, 0);
+        for (int n = 0; n < DIGITS; ++n) {
+            sum[n] = i32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) sum[n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[c], q[n][c], sum[n], 0, 0, 0);
         }
         const int lane = threadIdx.x & 63;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) keys[i] = key_of((float)(128 * up[i] + down[i]) * __shfl(weight, (lane >> 4) * 4 + i));
+        for (int i = 0; i < 4; ++i) {
+            float total;
+            if constexpr (DIGITS == 2) total = (float)(256 * sum[1][i] + sum[0][i]);
+            else total = (float)(65536 * (int64_t)sum[2][i] + 256 * (int64_t)sum[1][i] + sum[0][i]);
+            keys[i] = key_of(total * __shfl(weight, (lane >> 4) * 4 + i));
+        }
     }
 };
 
@@ -182,11 +197,11 @@ template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint3
 
 // Bound by the counting of the thresholds (a compare and a ballot for 64 scores a bit, at most 32 bits, scalar additions beside them).  4096 tokens, 8 heads of 128 with 4 queries
 // each, up to 512 blocks: 60 us.
-template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_select(SelectArgs a)
+template <int DT, int DP, int QT, int DIGITS> __global__ __launch_bounds__(kThreads) void k_select(SelectArgs a)
 {
     constexpr int SP = kSketch<DP>, kChunks = SP / 64, kShare = kThreads / QT;        // threads of a token
     extern __shared__ uint32_t lds_keys[];
-    __shared__ __align__(16) int8_t q8[2][QT][SP];                  // hi, lo
+    __shared__ __align__(16) int8_t q8[DIGITS][QT][SP];             // lo, hi and top
     __shared__ uint32_t amax[QT], few[kThreads / 64][64];
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreads) a.clear[i] = 0;
     const KvGeom &g = a.kv;
@@ -228,24 +243,22 @@ template <int DT, int DP, int QT> __global__ __launch_bounds__(kThreads) void k_
                     }
                 }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                q8[0][mine][8 * c + j] = (int8_t)(sum[j] >> 7);
-                q8[1][mine][8 * c + j] = (int8_t)(sum[j] & 127);
-            }
+            for (int n = 0; n < DIGITS; ++n)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) q8[n][mine][8 * c + j] = (int8_t)digit_of(sum[j], n);
         }
         __syncthreads();
-        i32x4_t hi[kChunks], lo[kChunks];
+        i32x4_t digits[DIGITS][kChunks];
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            hi[c] = lo[c] = i32x4_t{0, 0, 0, 0};
-            if (col < QT) {
-                hi[c] = *reinterpret_cast<const i32x4_t *>(&q8[0][col % QT][64 * c + 16 * quarter]);
-                lo[c] = *reinterpret_cast<const i32x4_t *>(&q8[1][col % QT][64 * c + 16 * quarter]);
+        for (int n = 0; n < DIGITS; ++n)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                digits[n][c] = i32x4_t{0, 0, 0, 0};
+                if (col < QT) digits[n][c] = *reinterpret_cast<const i32x4_t *>(&q8[n][col % QT][64 * c + 16 * quarter]);
             }
-        }
         auto put = [&](const Sketches<DP> &x, int first) {
             uint32_t keys[4];
-            x.score(hi, lo, keys);
+            x.score(digits, keys);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (col < QT && first + quarter * 4 + i < scored) lds_keys[col * a.stride + first + quarter * 4 + i] = keys[i];
@@ -292,7 +305,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
     constexpr int SP = kSketch<DP>, kChunks = SP / 64, kWaves = kThreadsOne / 64;
     extern __shared__ uint32_t lds_keys[];
     __shared__ __align__(16) int bins[4][256];
-    __shared__ __align__(16) int8_t q8[2][SP];      // hi, lo
+    __shared__ __align__(16) int8_t q8[3][SP];      // lo, hi, top
     __shared__ int sums[SP], aboves[kWaves], equals[kWaves];
     __shared__ uint32_t amax;
     for (int i = blockIdx.x * kThreadsOne + threadIdx.x; i < a.n_clear; i += gridDim.x * kThreadsOne) a.clear[i] = 0;
@@ -337,15 +350,17 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
         atomicAdd(&sums[i % DP], (int)__builtin_rintf((i < kThreadsOne ? mine : query(i)) * inverse));
     __syncthreads();
     if (threadIdx.x < SP) {
-        q8[0][threadIdx.x] = (int8_t)(sums[threadIdx.x] >> 7);
-        q8[1][threadIdx.x] = (int8_t)(sums[threadIdx.x] & 127);
+        const int sum = sums[threadIdx.x];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) q8[n][threadIdx.x] = (int8_t)digit_of(sum, n);
     }
     __syncthreads();
-    i32x4_t parts[kChunks];         // column 0 of the product's operand is hi, column 1 lo
+    i32x4_t parts[kChunks];         // columns 0 to 2 of the product's operand are lo, hi and top
+    const bool three = a.group > kTwoDigits;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
         parts[c] = i32x4_t{0, 0, 0, 0};
-        if (col < 2) parts[c] = *reinterpret_cast<const i32x4_t *>(&q8[col][64 * c + 16 * quarter]);
+        if (col < 3) parts[c] = *reinterpret_cast<const i32x4_t *>(&q8[col][64 * c + 16 * quarter]);
     }
     for (int first = 16 * wave; first < scored; first += 16 * kWaves) {
         i32x4_t sum = {0, 0, 0, 0};
@@ -355,10 +370,12 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
         if (first + 16 * kWaves < scored) x.bring(g, b, h, first + 16 * kWaves, scored);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int lo = __builtin_amdgcn_update_dpp(0, sum[i], 0x101, 0xf, 0xf, false);      // row_shl by 1: column 1's
+            const int hi = __builtin_amdgcn_update_dpp(0, sum[i], 0x101, 0xf, 0xf, false);      // row_shl by 1: column 1's
+            const int top = __builtin_amdgcn_update_dpp(0, sum[i], 0x102, 0xf, 0xf, false);     // by 2
             const int to = first + quarter * 4 + i;
             const float w = __shfl(weight, quarter * 4 + i);
-            if (col == 0 && to < scored) lds_keys[to] = key_of((float)(128 * sum[i] + lo) * w);
+            const float total = three ? (float)(65536 * (int64_t)top + 256 * (int64_t)hi + sum[i]) : (float)(256 * hi + sum[i]);
+            if (col == 0 && to < scored) lds_keys[to] = key_of(total * w);
         }
     }
     __syncthreads();
@@ -418,7 +435,7 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_selec
     write_entries(keys, from, to, threshold, ties - same_before, a.first, out + a.first + above_before + min(same_before, ties));
 }
 
-template <int DT, int DP, int QT> hipError_t run_tokens(SelectArgs a, hipStream_t s)
+template <int DT, int DP, int QT, int DIGITS> hipError_t run_tokens(SelectArgs a, hipStream_t s)
 {
     a.tiles = (a.kv.max_new + QT - 1) / QT;
     const size_t lds = (size_t)QT * a.stride * sizeof(uint32_t);
@@ -426,19 +443,21 @@ template <int DT, int DP, int QT> hipError_t run_tokens(SelectArgs a, hipStream_
     if (lds > 32 * 1024) {
         hipError_t e;
         if constexpr (QT == 1) e = raise_lds<k_select_one<DT, DP>>((size_t)128 * 1024);
-        else e = raise_lds<k_select<DT, DP, QT>>((size_t)128 * 1024);
+        else e = raise_lds<k_select<DT, DP, QT, DIGITS>>((size_t)128 * 1024);
         if (e != hipSuccess) return e;
     }
     if constexpr (QT == 1) k_select_one<DT, DP><<<grid, kThreadsOne, lds, s>>>(a);
-    else k_select<DT, DP, QT><<<grid, kThreads, lds, s>>>(a);
+    else k_select<DT, DP, QT, DIGITS><<<grid, kThreads, lds, s>>>(a);
     return hipGetLastError();
 }
 
 template <int DT, int DP> hipError_t run_dim(const SelectArgs &a, hipStream_t s)
 {
     // as many tokens a workgroup as their scores have room in LDS; single tokens alone
-    if (a.kv.max_new == 1 || a.stride > 8192) return run_tokens<DT, DP, 1>(a, s);
-    return a.stride > 2048 ? run_tokens<DT, DP, 4>(a, s) : run_tokens<DT, DP, 16>(a, s);
+    if (a.kv.max_new == 1 || a.stride > 8192) return run_tokens<DT, DP, 1, 3>(a, s);
+    // (apart because the third digit's registers cost two of eight waves a SIMD)
+    if (a.group > kTwoDigits) return a.stride > 2048 ? run_tokens<DT, DP, 4, 3>(a, s) : run_tokens<DT, DP, 16, 3>(a, s);
+    return a.stride > 2048 ? run_tokens<DT, DP, 4, 2>(a, s) : run_tokens<DT, DP, 16, 2>(a, s);
 }
 
 template <int DT> hipError_t run_type(const SelectArgs &a, hipStream_t s)

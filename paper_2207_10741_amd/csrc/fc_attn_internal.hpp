@@ -242,7 +242,7 @@ struct AttnArgs {
     FastDiv div_group;
     int32_t tiles;              // row tiles of a sequence and key head
     int32_t splits, per_split;  // pieces of the long axis and a piece's blocks
-    float *part_out;            // [unit of rows][split][rows][dp], not yet divided by the sum of the weights
+    float *part_out;            // [unit of rows][split][rows][dp], not yet divided by the sum of the weights, in units of kFromSums
     float2 *part_ml;            // [unit of rows][split][rows]: the weights' reference (base 2) and their sum
     int32_t *arrived;           // [unit of rows]: pieces that are done; zero before and after every call
 };
@@ -257,13 +257,18 @@ __device__ __forceinline__ RowPlace row_place(const AttnArgs &a, int row)
     return {token, row - token * a.group};
 }
 
+// Sums of weighted values that are not yet divided by the sum of the weights leave a wave in units of 2^56.  They may be 2^47 times the largest value (2^8 a token, 2^31
+// tokens, and codes up to 2^8 of scales up to 2^120 come to 2^167), which 32 bits do not hold; in this unit they do, and the least code's part (2^-73) is still far
+// above the least normal number.  A power of two: nothing is rounded.
+constexpr float kToSums = 0x1p-56f, kFromSums = 0x1p56f;
+
 // Four channels c .. c + 3 of a finished row (head `row` of the output's tokens x heads), not yet divided by the sum of the weights.
 template <int DT> __device__ __forceinline__ void finish_row(const AttnArgs &a, int64_t row, int c, f32x4_t sum, float most, float total)
 {
     if (a.lse && c == 0) a.lse[row] = total == 0.f ? -__builtin_inff() : (most + __builtin_amdgcn_logf(total)) * 0.693147180559945f;
     const int d = a.kv.d;
     if (c >= d) return;
-    const float inverse = total == 0.f ? 0.f : 1.f / total;     // (nothing to attend to: the sum is zero)
+    const float inverse = total == 0.f ? 0.f : kFromSums / total;     // (nothing to attend to: the sum is zero)
     const uint32_t lo = pack2<DT>(sum[0] * inverse, sum[1] * inverse), hi = pack2<DT>(sum[2] * inverse, sum[3] * inverse);
     uint16_t *const to = a.out + row * d + c;
     if ((d & 3) == 0) {

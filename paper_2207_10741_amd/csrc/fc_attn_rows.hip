@@ -335,7 +335,7 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
         }
         if (16 * mt + col < rows)
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) *reinterpret_cast<f32x4_t *>(lds_o + r * kPitch + 16 * t + 4 * quarter) = w.o[mt][t] * w.unit_v;
+            for (int t = 0; t < kTiles; ++t) *reinterpret_cast<f32x4_t *>(lds_o + r * kPitch + 16 * t + 4 * quarter) = w.o[mt][t] * (w.unit_v * kToSums);
     }
     __syncthreads();
     constexpr int kPieces = DP / 4;
@@ -399,7 +399,7 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     if (!valid) return;
     const int64_t row = (int64_t)(s.row0 + token) * a.heads + h * a.group + head;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit_v, w.m[0], sum);
+    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * (w.unit_v * kToSums), w.m[0], sum);
 }
 
 // Bound by the vector unit as the lists alone are: 235 instructions a block, most of them conversions of codes.  4096 tokens over 512 blocks, lists of 16,
@@ -461,7 +461,7 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     if (!valid) return;
     const int64_t row = (int64_t)(s.row0 + token0 + p.token) * a.heads + h * a.group + p.head;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit_v, w.m[0], sum);
+    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * (w.unit_v * kToSums), w.m[0], sum);
 }
 
 template <int DT, int DP, int MT, int WAVES, bool LIST> hipError_t run_rows(const AttnArgs &a, hipStream_t s)

@@ -327,6 +327,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
                 for (int mt = 0; mt < MT; ++mt) o[mt][t] = mfma_32<FC_F16>(value_operand(buffer, t, 2 + step), p[mt][step], o[mt][t]);
     }
 
+    const float to_sums = unit_v * kToSums;
     const int64_t unit = (int64_t)unit_rows * a.tiles + tile;
     const Pieces<DP> pieces(a, unit, kRows);
     auto out_row = [&](int row) {
@@ -350,7 +351,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         for (int t = 0; t < kOut; ++t)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                const f32x4_t v = {o[mt][t][i] * unit_v, o[mt][t][i + 1] * unit_v, o[mt][t][i + 2] * unit_v, o[mt][t][i + 3] * unit_v};
+                const f32x4_t v = {o[mt][t][i] * to_sums, o[mt][t][i + 1] * to_sums, o[mt][t][i + 2] * to_sums, o[mt][t][i + 3] * to_sums};
                 if (active > 1) pieces.put(item + (t * 4 + i / 4) * 64, v);
                 else if (r < rows) finish_row<DT>(a, row, 32 * t + 2 * i + 4 * half, v, m[mt], sum);
             }

@@ -260,7 +260,8 @@ __device__ __forceinline__ RowPlace row_place(const AttnArgs &a, int row)
 // Sums of weighted values that are not yet divided by the sum of the weights leave a wave in units of 2^56.  They may be 2^47 times the largest value (2^8 a token, 2^31
 // tokens, and codes up to 2^8 of scales up to 2^120 come to 2^167), which 32 bits do not hold; in this unit they do, and the least code's part (2^-73) is still far
 // above the least normal number.  A power of two: nothing is rounded.
-constexpr float kToSums = 0x1p-56f, kFromSums = 0x1p56f;
+constexpr int kSumsExponent = 56;
+constexpr float kFromSums = 0x1p56f;
 
 // Four channels c .. c + 3 of a finished row (head `row` of the output's tokens x heads), not yet divided by the sum of the weights.
 template <int DT> __device__ __forceinline__ void finish_row(const AttnArgs &a, int64_t row, int c, f32x4_t sum, float most, float total)
@@ -464,15 +465,34 @@ __device__ __forceinline__ uint4 codes_to_f16(uint32_t lo, uint32_t hi, float sc
     return r;
 }
 
-// The unit that values are held in stays while it is within 16 times the blocks' scales, either way, where every code times their ratio is exact in
-// f16 (multiples of 2^-13 up to 7168); else it becomes the block's own scale.
-__device__ __forceinline__ bool keeps_unit(float scale, float unit) { return scale <= unit * 16.f && scale * 16.f >= unit; }
-// a / b of two powers of two, held to 2^-126 .. 2^127 (finite: a sum of zero stays zero).
-__device__ __forceinline__ float pow2_ratio(float a, float b)
-{
-    const int e = (int)(__float_as_uint(a) >> 23) - (int)(__float_as_uint(b) >> 23);
-    return pow2_of(min(max(e, -126), 127));
-}
+// The exponent of the unit that a running sum of values is held in.  It stays while it is within 16 times the blocks' scales, either way, where every code times
+// their ratio is exact in f16 (multiples of 2^-13 up to 7168); else it becomes the block's own scale's and the sum is brought to it.  That is sound while the scales
+// so far are not further apart than 2^kUnitSpan: the sum is then below 2^(48 + 64 + 4) of any unit, and the least code at a weight of one above 2^-(9 + 64 + 4).  From
+// there on (a block of zeros has the least scale there is, 2^-64) the unit is that of finished sums, and what blocks far from it add is multiplied by their ratio
+// in 32 bits.
+constexpr int kUnitSpan = 64, kNoUnit = -1024;
+__device__ __forceinline__ int exponent_of(float scale) { return (int)(__float_as_uint(scale) >> 23 & 0xffu) - 127; }      // (whatever its sign)
+__device__ __forceinline__ float pow2_held(int e) { return pow2_of(min(max(e, -126), 127)); }       // (finite: a sum of zero stays zero)
+struct RunningUnit {
+    int e, least, most;     // of the blocks' scales, where they changed the unit
+    __device__ __forceinline__ void clear()
+    {
+        e = kNoUnit;
+        least = 1024;
+        most = -1024;
+    }
+    static __device__ __forceinline__ bool far(int scale, int unit) { return scale - unit > 4 || unit - scale > 4; }
+    // The unit with a block of this scale's exponent among what is summed.
+    __device__ __forceinline__ int with(int scale)
+    {
+        if (__builtin_expect(!far(scale, e), 1)) return e;
+        least = min(least, scale);
+        most = max(most, scale);
+        return most - least <= kUnitSpan ? scale : kSumsExponent;
+    }
+    // a sum's factor from this unit to that of finished sums
+    __device__ __forceinline__ float to_sums() const { return pow2_held(e - kSumsExponent); }
+};
 
 hipError_t launch_kv_append(const KvGeom &g, int dtype, const uint16_t *k, const uint16_t *v, int64_t k_row, int64_t k_head, int64_t v_row,
                             int64_t v_head, bool wide_k, bool wide_v, hipStream_t s);

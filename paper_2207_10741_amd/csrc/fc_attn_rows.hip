@@ -21,15 +21,16 @@ enum { kAllBlocks, kListed, kShared };
 template <int DT, int DP, int MT> struct Rows {
     static constexpr int kLoads = DP / 16, kTiles = DP / 16, kOperands = DP / 32;      // loads of a block's keys, of its values; instructions of 16 tokens' scores
     uint4 q[MT][kOperands];
-    f32x4_t o[MT][kTiles];          // in units of unit_v
-    float m[MT], l[MT], unit_v;     // weights are 2^(z - m); l: this lane's part of their sum
+    f32x4_t o[MT][kTiles];          // in its unit
+    RunningUnit unit;
+    float m[MT], l[MT];             // weights are 2^(z - m); l: this lane's part of their sum
     int last[MT];                   // the last position that the lane's row attends to
     int last_least;                 // ... of all rows
     uint32_t token, tokens;         // (kShared: the lane's token of the entries', and the bits of all)
 
     __device__ __forceinline__ void clear()
     {
-        unit_v = 1.f;
+        unit.clear();
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             m[mt] = -__builtin_inff();
@@ -154,21 +155,22 @@ template <int DT, int DP, int MT> struct Rows {
             }
 
             if (here) {
-                const float scale_v = __builtin_fabsf(scales.y);
                 float to_log2 = a.scale_log2 * scales.x;
                 const int from = (BLOCKS == kShared ? block & 0xffff : block) * kBlock;
                 const bool partly = from + kBlock - 1 > last_least;
                 const uint32_t have = (uint32_t)block >> 16;            // (kShared) the tokens that have the block
                 const bool mine = BLOCKS != kShared || (have >> token & 1u), all = BLOCKS != kShared || have == tokens;
-                if (__builtin_expect(!keeps_unit(scale_v, unit_v), 0)) {
-                    const float factor = pow2_ratio(unit_v, scale_v);
+                const int scale_v = exponent_of(scales.y), unit_new = unit.with(scale_v);
+                if (__builtin_expect(unit_new != unit.e, 0)) {
+                    const float factor = pow2_held(unit.e - unit_new);
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int t = 0; t < kTiles; ++t) o[mt][t] *= factor;
-                    unit_v = scale_v;
+                    unit.e = unit_new;
                 }
-                const float to_unit = pow2_ratio(scale_v, unit_v);
+                const bool far = RunningUnit::far(scale_v, unit.e);
+                const float to_unit = far ? 1.f : pow2_held(scale_v - unit.e);
                 if (partly) {
 #pragma unroll
                     for (int mt = 0; mt < MT; ++mt) {
@@ -235,6 +237,23 @@ template <int DT, int DP, int MT> struct Rows {
                     }
 #pragma unroll
                     for (int t = 0; t < kTiles; ++t) vx[t] = without_nan(vx[t]);
+                }
+                if (__builtin_expect(far, 0)) {     // exact products in units of the block's scale, added to o in 32 bits; the weights below are zeros then
+                    const float ratio = pow2_held(scale_v - unit.e);
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) {
+                        __builtin_amdgcn_sched_barrier(0);      // (one after another, in few registers)
+                        const uint4 v0 = codes_to_16<FC_F16>(vx[t].x, vx[t].y), v1 = codes_to_16<FC_F16>(vx[t].z, vx[t].w);
+#pragma unroll
+                        for (int mt = 0; mt < MT; ++mt) {
+                            f32x4_t adds = {0.f, 0.f, 0.f, 0.f};
+                            adds = mfma16<FC_F16>(v0, p[mt][0], adds);
+                            adds = mfma16<FC_F16>(v1, p[mt][1], adds);
+                            o[mt][t] += adds * ratio;
+                        }
+                    }
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) p[mt][0] = p[mt][1] = make_uint4(0, 0, 0, 0);
                 }
 #pragma unroll
                 for (int t = 0; t < kTiles; ++t) {
@@ -335,7 +354,7 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
         }
         if (16 * mt + col < rows)
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) *reinterpret_cast<f32x4_t *>(lds_o + r * kPitch + 16 * t + 4 * quarter) = w.o[mt][t] * (w.unit_v * kToSums);
+            for (int t = 0; t < kTiles; ++t) *reinterpret_cast<f32x4_t *>(lds_o + r * kPitch + 16 * t + 4 * quarter) = w.o[mt][t] * w.unit.to_sums();
     }
     __syncthreads();
     constexpr int kPieces = DP / 4;
@@ -399,7 +418,7 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     if (!valid) return;
     const int64_t row = (int64_t)(s.row0 + token) * a.heads + h * a.group + head;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * (w.unit_v * kToSums), w.m[0], sum);
+    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit.to_sums(), w.m[0], sum);
 }
 
 // Bound by the vector unit as the lists alone are: 235 instructions a block, most of them conversions of codes.  4096 tokens over 512 blocks, lists of 16,
@@ -461,7 +480,7 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     if (!valid) return;
     const int64_t row = (int64_t)(s.row0 + token0 + p.token) * a.heads + h * a.group + p.head;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * (w.unit_v * kToSums), w.m[0], sum);
+    for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit.to_sums(), w.m[0], sum);
 }
 
 template <int DT, int DP, int MT, int WAVES, bool LIST> hipError_t run_rows(const AttnArgs &a, hipStream_t s)

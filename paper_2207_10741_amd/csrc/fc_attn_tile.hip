@@ -71,9 +71,11 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         }
     }
 
-    // what a row holds: o in units of unit_v, weights 2^(z - m), m a whole number, l this lane's part of their sum
+    // what a row holds: o in its unit, weights 2^(z - m), m a whole number, l this lane's part of their sum
     f32x16_t o[MT][kOut], z[MT];
-    float m[MT], l[MT], unit_v = 1.f;
+    float m[MT], l[MT];
+    RunningUnit o_unit;
+    o_unit.clear();
     uint4 p[MT][2];     // weights of the last half-block whose product with the values is still to come
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -217,6 +219,32 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         }
     };
 
+    // What half t of a block adds to o (weights p), its values taken from memory: exact products in units of its scale, added to o in 32 bits.
+    auto far_values = [&](int32_t pool, int t, int to_unit) {
+        uint32_t at = value_piece<DP>(col, 16 * half) + 8 * t;
+        __asm__ volatile("" : "+v"(at));        // (made here, not kept in a register all along)
+        const uint8_t *const from = codes_of(pool) + at;
+        const float ratio = pow2_held(to_unit);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int n = 0; n < kOut; ++n) {
+                f32x16_t adds;
+                __builtin_amdgcn_sched_barrier(0);      // (one after another, in few registers)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) adds[i] = 0.f;
+#pragma unroll
+                for (int step = 0; step < 2; ++step) {
+                    // tokens 16 (2 t + step) + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
+                    uint32_t lo = *reinterpret_cast<const uint32_t *>(from + value_piece<DP>(32 * n, 0) - value_piece<DP>(0, 0) + 4 * step);
+                    uint32_t hi = *reinterpret_cast<const uint32_t *>(from + value_piece<DP>(32 * n, 32) - value_piece<DP>(0, 0) + 4 * step);
+                    adds = mfma_32<FC_F16>(codes_to_16<FC_F16>(lo & ~nan_bytes(lo), hi & ~nan_bytes(hi)), p[mt][step], adds);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[mt][n][i] = __builtin_fmaf(adds[i], ratio, o[mt][n][i]);
+            }
+    };
+
     if (begin < end) {
         // Block j's first half runs with keys of j and values of j - 1 in LDS, its second with keys of j + 1 and values of j.  These are put there beside the
         // first half, so that a barrier between the halves is the only one; both are brought to registers beside the second half before.
@@ -259,7 +287,6 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         uint32_t buffer = 0;        // of block j's keys and values; the other one is its neighbours'
         for (int block = begin; block < end; ++block, buffer = kBuffer - buffer) {
             const bool here = pool >= 0;
-            const float scale_v = here ? __builtin_fabsf(scales.y) : unit_v;
             const float to_log2 = here ? a.scale_log2 * scales.x : 1.f;
             const bool strange = here && scales.y < 0.f;    // NaN among the values: zeros in LDS, found again here
             if (strange) {
@@ -288,25 +315,28 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
 #pragma unroll
                 for (int i = 0; i < kShare; ++i) vx[i] = without_nan(vx[i]);
             }
-            if (!here)
+            const int scale_v = here ? exponent_of(scales.y) : o_unit.e, unit_new = here ? o_unit.with(scale_v) : o_unit.e;
+            const bool far = RunningUnit::far(scale_v, unit_new);       // values that f16 does not hold in the unit: zeros in LDS, and far_values
+            const int32_t pool_far = pool;
+            if (!here || far)
 #pragma unroll
                 for (int i = 0; i < kShare; ++i) vx[i] = make_uint4(0, 0, 0, 0);     // (finite, for weights of zero)
-            const bool new_unit = !keeps_unit(scale_v, unit_v);
-            const float to_unit = new_unit ? 1.f : pow2_ratio(scale_v, unit_v);
+            const float to_unit = far ? 1.f : pow2_held(scale_v - unit_new);
             half_block(Const<0>(), block, here, to_log2, buffer, kBuffer - buffer, [&](int i) {
                 if (i < 2 * kShare) put_keys(kBuffer - buffer, i / 2, i % 2);
                 else put_values(buffer, to_unit, i / 2 - kShare, i % 2);
             });
             __syncthreads();
 
-            if (new_unit) {         // (o has all of the values that are in the old one)
-                const float factor = pow2_ratio(unit_v, scale_v);
+            if (unit_new != o_unit.e) {         // (o has all of the values that are in the old one)
+                const float factor = pow2_held(o_unit.e - unit_new);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                     for (int t = 0; t < kOut; ++t) o[mt][t] *= factor;
-                unit_v = scale_v;
+                o_unit.e = unit_new;
             }
+            if (__builtin_expect(far, 0)) far_values(pool_far, 0, scale_v - unit_new);
             pool = pool_next;
             scales = scales_next;
             if (block + 1 < end) bring(codes_of(pool) + kBlock * DP, vx);
@@ -316,6 +346,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
             scales_next = scales_at(after);
             if (block + 2 < end) bring(codes_of(pool_next), kx);
             half_block(Const<1>(), block, here, to_log2, kBuffer - buffer, buffer, [](int) {});
+            if (__builtin_expect(far, 0)) far_values(pool_far, 1, scale_v - unit_new);
         }
         // the last half's values
         buffer = kBuffer - buffer;
@@ -327,7 +358,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
                 for (int mt = 0; mt < MT; ++mt) o[mt][t] = mfma_32<FC_F16>(value_operand(buffer, t, 2 + step), p[mt][step], o[mt][t]);
     }
 
-    const float to_sums = unit_v * kToSums;
+    const float to_sums = o_unit.to_sums();
     const int64_t unit = (int64_t)unit_rows * a.tiles + tile;
     const Pieces<DP> pieces(a, unit, kRows);
     auto out_row = [&](int row) {

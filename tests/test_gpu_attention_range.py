@@ -81,3 +81,62 @@ def test_means_of_small_values(length, new, heads, group, dim, causal):
     """Below the least scale's 448: the codes get smaller, and so do the sums."""
     setup = Setup([length], heads, dim, B.BF16, scale_of=lambda n: np.full(n, 2.0 ** -64))
     _attend(setup, new, group, causal)
+
+
+def _blocks_of(exponents, poison=()):
+    """Values of about 2^e in the blocks, one exponent after another (None: zeros), every other channel of a block: those of the next one's are zero there, so
+    that nothing hides what a block of small values adds.  poison: (token, channel) of values that are infinite."""
+    def tokens(b, k, v):
+        n = v.shape[0]
+        nth = np.arange(n) // 64 % len(exponents)
+        v = v * np.array([0.0 if e is None else 2.0 ** e for e in exponents])[nth][:, None, None]
+        v *= ((np.arange(n)[:, None] // 64 + np.arange(v.shape[2])[None, :]) % 2)[:, None, :]
+        for t, c in poison:
+            v[t, :, c] = np.inf
+        return k, v
+    return tokens
+
+
+PATTERNS = [
+    (66, None),                     # what a block of zeros has for a scale is far below
+    (None, 66),
+    (None, None, 124),
+    (-64, 124),
+    (124, -64, 0, 60, -20),
+    (-64, -20, 20, 60, 100, 124),
+    (10, -50),                      # (the sums follow the blocks)
+]
+
+
+@pytest.mark.parametrize("exponents", PATTERNS)
+@pytest.mark.parametrize("length,new,heads,group,dim,causal", DENSE)
+def test_blocks_of_very_different_values(length, new, heads, group, dim, causal, exponents):
+    setup = Setup([length], heads, dim, B.BF16, tokens=_blocks_of(exponents))
+    _attend(setup, new, group, causal, magnitude=0.3)
+
+
+@pytest.mark.parametrize("exponents", [(66, None), (124, -64, 0, 60, -20), (10, -50)])
+@pytest.mark.parametrize("length,batch,new,group,dim,first,last,top", FOCUSED)
+def test_selected_blocks_of_very_different_values(length, batch, new, group, dim, first, last, top, exponents):
+    setup = Setup([length], 1, dim, B.BF16, tokens=_blocks_of(exponents))
+    _focus(setup, batch, new, group, first, last, top, magnitude=0.3)
+
+
+@pytest.mark.parametrize("new", [1, 5, 140])
+@pytest.mark.parametrize("exponents", [(124, -64), (-64, 124)])
+def test_nan_in_blocks_of_very_different_values(exponents, new):
+    """A value that later rows see and earlier ones do not, in the last block or the one before it."""
+    for at in (190, 255):
+        length = 64 * 4
+        setup = Setup([length], 1, 64, B.BF16, tokens=_blocks_of(exponents, [(at, 3)]))
+        q, qn = setup.queries(new, 2, 0.3)
+        out = A.cache_attention(setup.cache, q, setup.table, setup.lengths_dev)
+        sees = np.arange(length - new, length) >= at
+        got = G.to_f64(out)
+        assert np.isnan(got[sees][:, :, 3]).all() and np.isfinite(got[~sees]).all()
+        got = np.delete(got, 3, axis=2)
+        assert np.isfinite(got).all()
+        for row in _rows(new):
+            want, _, error = O.attend(setup.oracle[0], qn[row], length - new + row, 0.125)
+            off = np.abs(got[row] - np.delete(want, 3, axis=1))
+            assert (off <= np.delete(error + LAST_PLACE[B.BF16] * (np.abs(want) + error) + LEAST[B.BF16], 3, axis=1)).all()

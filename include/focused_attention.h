@@ -33,7 +33,8 @@
  *   - Query head h reads key/value head h / (heads / kv_heads).  Row i of the n new tokens of a sequence has position
  *     p = length - n + i and attends to positions 0 .. p with FC_CAUSAL, to all of the length without.
  *   - out = sum_t softmax_t(scale * q.k_t) v_t with keys and values as the cache holds them.  Products of stored values accumulated
- *     in 32 bits; softmax in 32 bits; weights rounded to 11 bits (f16) for their product with the values; one rounding to the output type.
+ *     in 32 bits; softmax in 32 bits; weights rounded to 11 bits (f16) for their product with the values, steps of 2^-30 of the largest at
+ *     least; one rounding to the output type.
  *   - What a row does not attend to has no influence on it, NaN included.  A row that attends to nothing is +0.0 with lse = -infinity.
  *   - lse, where it is wanted: log(sum_t exp(scale * q.k_t)) in 32 bits, [tokens][heads].
  *

@@ -257,8 +257,8 @@ __device__ __forceinline__ RowPlace row_place(const AttnArgs &a, int row)
     return {token, row - token * a.group};
 }
 
-// Sums of weighted values that are not yet divided by the sum of the weights leave a wave in units of 2^56.  They may be 2^47 times the largest value (2^8 a token, 2^31
-// tokens, and codes up to 2^8 of scales up to 2^120 come to 2^167), which 32 bits do not hold; in this unit they do, and the least code's part (2^-73) is still far
+// Sums of weighted values that are not yet divided by the sum of the weights leave a wave in units of 2^56.  They may be 2^46 times the largest value (2^15 a token, 2^31
+// tokens, and codes up to 2^9 of scales up to 2^120 come to 2^175), which 32 bits do not hold; in this unit they do, and the least code's part (2^-73) is still far
 // above the least normal number.  A power of two: nothing is rounded.
 constexpr int kSumsExponent = 56;
 constexpr float kFromSums = 0x1p56f;
@@ -296,7 +296,12 @@ template <auto KERNEL> hipError_t raise_lds(size_t bytes)
     return e;
 }
 
-constexpr float kSlack = 8.f;   // a row's weights are at most 2^kSlack before its reference is brought up to date
+// Weights are 2^(z - reference), rounded to f16 (11 bits, least step 2^-24) as operands of the matrix instructions; their sum, which the result is divided by, has them in 32 bits.
+// Rounding is to nearest, so a row's error is a token's 2^-12 of its weight, and far less of many: below an output's own rounding to bf16, about that to f16.  The
+// reference lies kLead below the largest score when it is brought up to date, and that is done when a score is more than kSlack above it: weights are then at
+// most 2^15, which f16 holds, and the least that counts is 2^-31 of the largest (with the largest as reference, 2^-24: of 131 000 tokens that one dominates up to
+// 2^-8 of the weight were lost, always towards zero).
+constexpr float kLead = 7.f, kSlack = 15.f;
 
 // Joining the pieces of a unit of rows.  A workgroup that has written its piece counts itself; the one that comes last reads all pieces (in
 // their order, whoever is last) and finishes the rows.  What workgroups of other XCDs wrote is read past the caches (kDeviceScope both ways).
@@ -467,7 +472,7 @@ __device__ __forceinline__ uint4 codes_to_f16(uint32_t lo, uint32_t hi, float sc
 
 // The exponent of the unit that a running sum of values is held in.  It stays while it is within 16 times the blocks' scales, either way, where every code times
 // their ratio is exact in f16 (multiples of 2^-13 up to 7168); else it becomes the block's own scale's and the sum is brought to it.  That is sound while the scales
-// so far are not further apart than 2^kUnitSpan: the sum is then below 2^(48 + 64 + 4) of any unit, and the least code at a weight of one above 2^-(9 + 64 + 4).  From
+// so far are not further apart than 2^kUnitSpan: the sum is then below 2^(55 + 64 + 4) of any unit, and the least code at a weight of one above 2^-(9 + 64 + 4).  From
 // there on (a block of zeros has the least scale there is, 2^-64) the unit is that of finished sums, and what blocks far from it add is multiplied by their ratio
 // in 32 bits.
 constexpr int kUnitSpan = 64, kNoUnit = -1024;

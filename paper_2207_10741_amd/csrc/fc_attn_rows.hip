@@ -191,7 +191,7 @@ template <int DT, int DP, int MT> struct Rows {
                     most = max_over_16(max_over_32(most)) * to_log2;
                     if (BLOCKS == kShared) most = mine ? most : -__builtin_inff();
                     if (__builtin_expect(__any(most - m[mt] > kSlack), 0)) {
-                        const float m_new = fmaxf(m[mt], most);
+                        const float m_new = fmaxf(m[mt], most - kLead);
                         const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);
                         m[mt] = m_new;
                         l[mt] *= factor;

@@ -152,7 +152,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         if (__any(rises)) {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const float m_new = fmaxf(m[mt], __builtin_ceilf(most[mt]));
+                const float m_new = fmaxf(m[mt], __builtin_ceilf(most[mt]) - kLead);
                 const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);     // (a power of two: nothing is rounded)
                 m[mt] = m_new;
                 l[mt] *= factor;

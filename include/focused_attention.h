@@ -28,6 +28,7 @@
  *   - Rows with no position (more new tokens than the length) are dropped by fc_kv_append, read as zeros, and attend to nothing.
  *   - Bounds known to the host: max_new >= every sequence's new tokens, max_len >= every length.  What the device's arrays say beyond
  *     these bounds, beyond `tokens` or beyond the table is cut off, so wrong contents give wrong results and never an access out of range.
+ *     Work is laid out by the bounds: batch, max_new and heads that come to more workgroups than a launch holds (2^32 threads) give FC_ERR_RANGE.
  *
  * Attention
  *   - Query head h reads key/value head h / (heads / kv_heads).  Row i of the n new tokens of a sequence has position

@@ -41,8 +41,11 @@ int32_t make_kv_geom(const fc_attention_desc *d, const void *cache, const int32_
     return FC_OK;
 }
 
-// A workgroup of 256 threads a touched block and head: one dimension of a grid, which is counted in threads.
-bool blocks_fit(const KvGeom &g) { return ((int64_t)touched_blocks(g) + 1) * g.kv_heads < 1 << 24; }
+// One dimension of a grid is counted in threads.
+bool grid_fits(int64_t workgroups, int threads) { return workgroups < (1ll << 32) / threads; }
+
+// A workgroup of 256 threads a touched block and head.
+bool blocks_fit(const KvGeom &g) { return grid_fits(((int64_t)touched_blocks(g) + 1) * g.kv_heads, 256); }
 
 int32_t check_pointers(const void *cache, const int32_t *table, const int32_t *lengths, const int32_t *starts)
 {
@@ -162,6 +165,13 @@ int32_t make_plan(const fc_attention_desc *d, const KvGeom &g, bool list, Plan *
         }
     }
     if (units * p->splits >= INT32_MAX || (int64_t)p->splits * p->rows_tile * g.dp * 4 >= INT32_MAX) return FC_ERR_RANGE;
+    if (list) {
+        const int32_t tokens = select_tokens(g);
+        if (!grid_fits((int64_t)d->batch * d->kv_heads * ((d->max_new + tokens - 1) / tokens), tokens == 1 ? 1024 : 256)) return FC_ERR_RANGE;
+        if (!grid_fits(p->whole ? (units + 31) / 32 * 8 : units * p->splits, 256)) return FC_ERR_RANGE;
+    } else if (!grid_fits(units * p->splits, p->rows_tile <= 32 ? 64 * p->waves : 2 * p->rows_tile)) {
+        return FC_ERR_RANGE;
+    }
     p->counters = p->splits == 1 ? 0 : align_up((size_t)units * sizeof(int32_t), 256);
     p->workspace = p->counters + (p->splits == 1 ? 0 : (size_t)units * p->splits * p->rows_tile * (g.dp * sizeof(float) + sizeof(float2)));
     return FC_OK;
@@ -249,7 +259,7 @@ int32_t fc_kv_append(const fc_attention_desc *d, void *cache, const void *k, con
     int32_t rc = make_kv_geom(d, cache, table, lengths, starts, &g);
     if (rc != FC_OK) return rc;
     if (!known_type(d->dtype)) return FC_ERR_DTYPE;
-    if (!blocks_fit(g)) return FC_ERR_RANGE;
+    if (!blocks_fit(g) || (g.max_new == 1 && !grid_fits(((int64_t)g.batch * g.kv_heads + 3) / 4, 256))) return FC_ERR_RANGE;
     if (d->k_row < 0 || d->k_head < 0 || d->v_row < 0 || d->v_head < 0) return FC_ERR_SHAPE;
     if (d->tokens == 0) return FC_OK;
     rc = check_pointers(cache, table, lengths, starts);

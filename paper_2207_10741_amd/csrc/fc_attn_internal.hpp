@@ -516,6 +516,13 @@ hipError_t launch_attend_tile(const AttnArgs &a, int dtype, int rows_tile, hipSt
 // The selection (see fc_attn_select.hip).
 constexpr int kSelectMaxBlocks = 32768;     // blocks of a sequence whose scores fit LDS
 constexpr int kMostGroup = 32767;           // heads of a group whose rounded queries' sum fits three signed 8-bit digits: 255 * 32767 <= 127 * (65536 + 256 + 1)
+// Scores of a token in LDS, and tokens a workgroup: as many as their scores have room in LDS; single tokens alone (1024 threads, else 256).
+static inline int32_t select_stride(const KvGeom &g) { return (int32_t)align_up((size_t)(g.max_len + kBlock - 1) / kBlock, 16); }
+static inline int32_t select_tokens(const KvGeom &g)
+{
+    const int32_t stride = select_stride(g);
+    return g.max_new == 1 || stride > 8192 ? 1 : stride > 2048 ? 4 : 16;
+}
 // clear, n_clear: counters that the attention behind it wants zero.
 hipError_t launch_select(const KvGeom &g, int dtype, const uint16_t *q, int64_t q_row, int64_t q_head, int heads, bool wide, int first, int last,
                          int top, int32_t *selected, int32_t *clear, int32_t n_clear, hipStream_t s);

@@ -453,11 +453,11 @@ template <int DT, int DP, int QT, int DIGITS> hipError_t run_tokens(SelectArgs a
 
 template <int DT, int DP> hipError_t run_dim(const SelectArgs &a, hipStream_t s)
 {
-    // as many tokens a workgroup as their scores have room in LDS; single tokens alone
-    if (a.kv.max_new == 1 || a.stride > 8192) return run_tokens<DT, DP, 1, 3>(a, s);
+    const int tokens = select_tokens(a.kv);
+    if (tokens == 1) return run_tokens<DT, DP, 1, 3>(a, s);
     // (apart because the third digit's registers cost two of eight waves a SIMD)
-    if (a.group > kTwoDigits) return a.stride > 2048 ? run_tokens<DT, DP, 4, 3>(a, s) : run_tokens<DT, DP, 16, 3>(a, s);
-    return a.stride > 2048 ? run_tokens<DT, DP, 4, 2>(a, s) : run_tokens<DT, DP, 16, 2>(a, s);
+    if (a.group > kTwoDigits) return tokens == 4 ? run_tokens<DT, DP, 4, 3>(a, s) : run_tokens<DT, DP, 16, 3>(a, s);
+    return tokens == 4 ? run_tokens<DT, DP, 4, 2>(a, s) : run_tokens<DT, DP, 16, 2>(a, s);
 }
 
 template <int DT> hipError_t run_type(const SelectArgs &a, hipStream_t s)
@@ -476,7 +476,7 @@ template <int DT> hipError_t run_type(const SelectArgs &a, hipStream_t s)
 hipError_t launch_select(const KvGeom &g, int dtype, const uint16_t *q, int64_t q_row, int64_t q_head, int heads, bool wide, int first, int last,
                          int top, int32_t *selected, int32_t *clear, int32_t n_clear, hipStream_t s)
 {
-    const int stride = (int)align_up((size_t)(g.max_len + kBlock - 1) / kBlock, 16);
+    const int stride = select_stride(g);
     const SelectArgs a = {g, q, q_row, q_head, heads / g.kv_heads, wide, first, last, top, 0, stride, selected, clear, n_clear};
     return dtype == FC_BF16 ? run_type<FC_BF16>(a, s) : run_type<FC_F16>(a, s);
 }

@@ -25,6 +25,7 @@
  * Sequences
  *   - lengths[b] (device) counts the tokens of sequence b with the new ones, which are its last; rows starts[b] .. starts[b + 1] of the call's
  *     tensors (device, [batch + 1]) are its new tokens.  starts NULL: max_new rows for every sequence, tokens = batch * max_new.
+ *     Without rows (tokens 0) there is nothing to do, whatever max_new is.
  *   - Rows with no position (more new tokens than the length) are dropped by fc_kv_append, read as zeros, and attend to nothing.
  *   - Bounds known to the host: max_new >= every sequence's new tokens, max_len >= every length.  What the device's arrays say beyond
  *     these bounds, beyond `tokens` or beyond the table is cut off, so wrong contents give wrong results and never an access out of range.

@@ -92,12 +92,14 @@ def _desc(cache: KVCache, table, lengths, starts, tokens, max_new, max_len) -> A
     batch, width = table.shape
     if max_new is None:
         max_new = tokens if starts is not None else tokens // batch if batch else 0
-    if starts is None and max_new * batch != tokens:
+    if starts is None and tokens and max_new * batch != tokens:
         raise ValueError("without starts every sequence has the same number of new tokens")
     if max_len is None:
         max_len = min(width * BLOCK, 2 ** 31 - 1)
+    if tokens == 0:     # (nothing to do: the library takes no sizes of zero)
+        batch, width, max_new, max_len = max(batch, 1), max(width, 1), max(max_new, 1), max(max_len, 1)
     return AttentionDesc(blocks=cache.blocks, kv_heads=cache.kv_heads, head_dim=cache.head_dim, batch=batch, tokens=tokens,
-                         max_new=max(int(max_new), 1) if tokens == 0 else int(max_new), max_len=int(max_len), table_width=width)
+                         max_new=int(max_new), max_len=int(max_len), table_width=width)
 
 
 def _rows(x, cache: KVCache, heads, what: str):

@@ -26,7 +26,7 @@ int32_t make_kv_geom(const fc_attention_desc *d, const void *cache, const int32_
     if (d->flags & ~(uint32_t)(FC_CAUSAL | FC_WORKSPACE_READY) || d->reserved) return FC_ERR_DTYPE;
     // (one dimension of a grid)
     if (d->batch > 65535 || d->kv_heads > 65535) return FC_ERR_RANGE;
-    if (!starts && (int64_t)d->batch * d->max_new != d->tokens) return FC_ERR_SHAPE;
+    if (!starts && d->tokens && (int64_t)d->batch * d->max_new != d->tokens) return FC_ERR_SHAPE;
     const KvLayout l = kv_layout(d->blocks, d->kv_heads, d->head_dim);
     uint8_t *const base = static_cast<uint8_t *>(const_cast<void *>(cache));
     g->blocks = d->blocks; g->kv_heads = d->kv_heads; g->d = d->head_dim; g->dp = padded_dim(d->head_dim);

@@ -1,8 +1,10 @@
 """Refusals of sizes that the attention operators cannot take: found on the host before anything is launched (no GPU needed)."""
 import ctypes
 
+import pytest
+
 from paper_2207_10741_amd import attention as A
-from tests.test_attention_api import RANGE, _append, _attend, _desc, _focused, _p
+from tests.test_attention_api import CALLS, RANGE, SHAPE, _append, _attend, _desc, _focused, _p
 
 
 def _workspace(d, name="fc_focused_attention"):
@@ -53,3 +55,11 @@ def test_more_threads_than_a_launch_of_attention_holds():
 def test_more_threads_than_a_launch_of_appending_holds():
     many = dict(batch=65535, max_new=1, tokens=65535, max_len=64, table_width=1, heads=1100)
     _refused(_append, None, kv_heads=1100, **many)
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_no_rows_without_starts(call):
+    """Whatever the bound of new tokens is: nothing to do."""
+    for max_new in (1, 7):
+        assert call(_desc(tokens=0, max_new=max_new), cache=None, table=None, lengths=None) == 0
+    assert call(_desc(tokens=1)) == SHAPE

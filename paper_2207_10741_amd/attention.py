@@ -163,6 +163,8 @@ class PreparedRead(_Prepared):
         if tokens is None:
             if starts is not None:
                 raise ValueError("tokens: the rows that starts counts")
+            if max_new is None:
+                raise ValueError("max_new: the tokens of every sequence to be read, or tokens: those of all of them")
             tokens = table.shape[0] * max_new
         desc = _desc(cache, table, lengths, starts, tokens, max_new, max_len)
         torch = B._torch()
@@ -259,7 +261,8 @@ def kv_append(cache, k, v, table, lengths, starts=None, max_new=None, max_len=No
 
 
 def kv_read(cache, table, lengths, starts=None, tokens=None, max_new=None, max_len=None, k=None, v=None, stream=None):
-    """fc_kv_read: (keys, values) of the sequences' last tokens, float32 [tokens, kv_heads, head_dim]."""
+    """fc_kv_read: (keys, values) of the sequences' last tokens, float32 [tokens, kv_heads, head_dim]: max_new of every sequence, or with
+    starts as many as it counts (tokens in all)."""
     return PreparedRead(cache, table, lengths, starts, tokens, max_new, max_len, k, v, stream)(stream)
 
 

@@ -36,3 +36,12 @@ def test_no_sequences(width):
     setup = Setup([100], 2, 64, B.BF16)
     table = torch.empty((0, width), dtype=torch.int32, device=G.dev())
     _calls(setup.cache, table, table.new_empty((0,)))
+
+
+def test_reading_needs_the_number_of_rows():
+    setup = Setup([100], 2, 64, B.BF16)
+    with pytest.raises(ValueError, match="max_new"):
+        A.kv_read(setup.cache, setup.table, setup.lengths_dev)
+    with pytest.raises(ValueError, match="tokens"):
+        A.kv_read(setup.cache, setup.table, setup.lengths_dev, starts=_int32([0, 5]))
+    assert A.kv_read(setup.cache, setup.table, setup.lengths_dev, max_new=5)[0].shape == (5, 2, 64)

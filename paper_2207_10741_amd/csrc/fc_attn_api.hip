@@ -1,5 +1,6 @@
 // C ABI of the attention operators: argument checks on the host, then launches.
 #include "fc_attn_internal.hpp"
+#include <float.h>
 #include <math.h>
 
 using namespace fc;
@@ -217,7 +218,7 @@ int32_t attend(const fc_attention_desc *d, const void *cache, const void *q, con
     a.heads = d->heads; a.group = d->heads / d->kv_heads;
     a.causal = list || (d->flags & FC_CAUSAL);
     a.wide = wide_rows(q, d->q_row, d->q_head, d->head_dim);
-    a.scale_log2 = fabsf(d->scale) * 1.44269504088896f;
+    a.scale_log2 = fminf(fabsf(d->scale) * 1.44269504088896f, FLT_MAX);
     a.signs = d->scale < 0.f ? 0x80008000u : 0u;
     a.div_group = make_fastdiv((uint32_t)a.group);
     a.selected = list ? selected : nullptr;

@@ -237,7 +237,7 @@ struct AttnArgs {
     int32_t shared, mask_words, entries;    // tokens a wave takes together; words of its LDS for masks and entries
     int32_t heads, group, causal;
     int32_t wide;               // q's rows are 16-byte pieces
-    float scale_log2;           // |scale| * log2(e); a negative scale changes the queries' signs
+    float scale_log2;           // |scale| * log2(e), finite; a negative scale changes the queries' signs
     uint32_t signs;             // of two 16-bit queries
     FastDiv div_group;
     int32_t tiles;              // row tiles of a sequence and key head
@@ -246,6 +246,9 @@ struct AttnArgs {
     float2 *part_ml;            // [unit of rows][split][rows]: the weights' reference (base 2) and their sum
     int32_t *arrived;           // [unit of rows]: pieces that are done; zero before and after every call
 };
+
+// What a block's products of codes with queries are multiplied by.  (Held to the largest finite number: a score of zero stays zero.)
+__device__ __forceinline__ float score_factor(const AttnArgs &a, float keys_scale) { return fminf(a.scale_log2 * keys_scale, 0x1.fffffep127f); }
 
 // Where row r of a tile is: its token among the sequence's new ones, its head among the group's.
 struct RowPlace {

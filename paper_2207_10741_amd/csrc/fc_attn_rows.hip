@@ -155,7 +155,7 @@ template <int DT, int DP, int MT> struct Rows {
             }
 
             if (here) {
-                float to_log2 = a.scale_log2 * scales.x;
+                float to_log2 = score_factor(a, scales.x);
                 const int from = (BLOCKS == kShared ? block & 0xffff : block) * kBlock;
                 const bool partly = from + kBlock - 1 > last_least;
                 const uint32_t have = (uint32_t)block >> 16;            // (kShared) the tokens that have the block

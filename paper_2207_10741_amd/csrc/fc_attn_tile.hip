@@ -287,7 +287,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         uint32_t buffer = 0;        // of block j's keys and values; the other one is its neighbours'
         for (int block = begin; block < end; ++block, buffer = kBuffer - buffer) {
             const bool here = pool >= 0;
-            const float to_log2 = here ? a.scale_log2 * scales.x : 1.f;
+            const float to_log2 = here ? score_factor(a, scales.x) : 1.f;
             const bool strange = here && scales.y < 0.f;    // NaN among the values: zeros in LDS, found again here
             if (strange) {
                 const uint8_t *const codes = codes_of(pool);

@@ -140,3 +140,19 @@ def test_nan_in_blocks_of_very_different_values(exponents, new):
             want, _, error = O.attend(setup.oracle[0], qn[row], length - new + row, 0.125)
             off = np.abs(got[row] - np.delete(want, 3, axis=1))
             assert (off <= np.delete(error + LAST_PLACE[B.BF16] * (np.abs(want) + error) + LEAST[B.BF16], 3, axis=1)).all()
+
+
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("key_size,scale", [(1.0, 3.4e38), (2.0 ** 122, 2.0 ** 20), (2.0 ** 122, -3.4e38)])
+def test_factors_of_scores_beyond_32_bits(key_size, scale, new):
+    """A factor of the scores, with the keys' scale in it, that 32 bits do not hold: scores of zero are still zero."""
+    setup = Setup([700], 1, 64, B.BF16, tokens=lambda b, k, v: (k * key_size, v))
+    q, qn = setup.queries(new, 2, 0.0)
+    out = A.cache_attention(setup.cache, q, setup.table, setup.lengths_dev, scale=scale)
+    listed, selected = A.focused_attention(setup.cache, q, setup.table, setup.lengths_dev, 1, 1, 3, scale=scale)
+    for row in _rows(new):
+        position = 700 - new + row
+        for got, blocks in ((out, None), (listed, selected[row].cpu().numpy())):
+            want, _, error = O.attend(setup.oracle[0], qn[row], position, scale, True, blocks)
+            allowed = error + LAST_PLACE[B.BF16] * (np.abs(want) + error) + LEAST[B.BF16]
+            assert (np.abs(G.to_f64(got[row]) - want) <= allowed).all()

@@ -21,9 +21,9 @@ constexpr uint32_t kValuePitch = 2 * kBlock + 16;
 // block's values with the last step's weights beside this step's scores, so that the matrix cores always have the one while the vector unit works on the other.
 // 8192 tokens, 32 heads of 128 over 8, causal: 539 us, 1020 TFLOP/s, 89 % of what the library's 8192^3 product reaches here.  Bound by the matrix cores, and then by power
 // (the clock falls as their share of idle cycles does).
-template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * WAVES, DP * MT <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
+template <int DT, int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
 {
-    constexpr int kWaves = WAVES, kThreads = 64 * kWaves, kWaveRows = 32 * MT, kRows = kWaveRows * kWaves, kSteps = DP / 16, kOut = DP / 32;
+    constexpr int kWaves = WAVES, kThreads = 64 * kWaves, kRows = 32 * kWaves, kSteps = DP / 16, kOut = DP / 32;
     constexpr int kShare = (4 * DP + kThreads - 1) / kThreads;      // 16-byte pieces of the codes of keys (values) a thread brings
     constexpr bool kEven = 4 * DP % kThreads == 0;                  // (every thread; else the last ones are some waves')
     // rows of keys and values in LDS; the 16 bytes behind each put rows that are read together into different banks
@@ -42,51 +42,41 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
     const Sequence s = sequence_of(g, b);
     const int rows = min(max(s.n * a.group - tile * kRows, 0), kRows);
     if (rows == 0) return;
-    int last[MT];       // the last position that the lane's row attends to
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const int r = wave * kWaveRows + 32 * mt + col;
-        last[mt] = r < rows ? (a.causal ? s.pos0 + row_place(a, tile * kRows + r).token : s.len - 1) : -1;
-    }
+    const int r = wave * 32 + col;      // the lane's row, and the last position that it attends to
+    const int last = r < rows ? (a.causal ? s.pos0 + row_place(a, tile * kRows + r).token : s.len - 1) : -1;
     const int token_last = (int)fast_div((uint32_t)(tile * kRows + rows - 1), a.div_group);
     const int last_most = a.causal ? s.pos0 + token_last : s.len - 1;
-    const int wave_first = a.causal ? s.pos0 + row_place(a, tile * kRows + wave * kWaveRows).token : s.len - 1;     // the least `last` of the wave's rows
+    const int wave_first = a.causal ? s.pos0 + row_place(a, tile * kRows + wave * 32).token : s.len - 1;     // the least `last` of the wave's rows
     const int blocks = last_most < 0 ? 0 : last_most / kBlock + 1;
     const int active = max((blocks + a.per_split - 1) / a.per_split, 1);
     if (split >= active) return;
     const int begin = split * a.per_split, end = min(blocks, begin + a.per_split);
 
-    uint4 q[MT][kSteps];
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    uint4 q[kSteps];
+    {
         // (rows behind the last repeat it and are left out below)
-        const RowPlace p = row_place(a, tile * kRows + min(wave * kWaveRows + 32 * mt + col, rows - 1));
-        const uint16_t *const row = a.q + (s.row0 + p.token) * a.q_row + (int64_t)(h * a.group + p.head) * a.q_head;
+        const RowPlace at_row = row_place(a, tile * kRows + min(r, rows - 1));
+        const uint16_t *const row = a.q + (s.row0 + at_row.token) * a.q_row + (int64_t)(h * a.group + at_row.head) * a.q_head;
         if (a.wide) {
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) q[mt][c] = flip_signs(load8<true>(row, 16 * c + 8 * half, g.d), a.signs);
+            for (int c = 0; c < kSteps; ++c) q[c] = flip_signs(load8<true>(row, 16 * c + 8 * half, g.d), a.signs);
         } else {
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) q[mt][c] = flip_signs(load8<false>(row, 16 * c + 8 * half, g.d), a.signs);
+            for (int c = 0; c < kSteps; ++c) q[c] = flip_signs(load8<false>(row, 16 * c + 8 * half, g.d), a.signs);
         }
     }
 
     // what a row holds: o in its unit, weights 2^(z - m), m a whole number, l this lane's part of their sum
-    f32x16_t o[MT][kOut], z[MT];
-    float m[MT], l[MT];
+    f32x16_t o[kOut], z;
+    float m = -__builtin_inff(), l = 0.f;
     RunningUnit o_unit;
     o_unit.clear();
-    uint4 p[MT][2];     // weights of the last half-block whose product with the values is still to come
+    uint4 p[2];     // weights of the last half-block whose product with the values is still to come
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
+    for (int t = 0; t < kOut; ++t)
 #pragma unroll
-        for (int t = 0; t < kOut; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[mt][t][i] = 0.f;
-        m[mt] = -__builtin_inff();
-        l[mt] = 0.f;
-        p[mt][0] = p[mt][1] = make_uint4(0, 0, 0, 0);
-    }
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    p[0] = p[1] = make_uint4(0, 0, 0, 0);
 
     // where the thread's first pieces go and where the lane's operands are, from a buffer's start on
     auto key_place = [](uint32_t piece, uint32_t n) {
@@ -130,80 +120,61 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
     auto half_block = [&](auto t_const, int block, bool here, float to_log2, uint32_t keys_next, uint32_t values_last, auto beside) {
         constexpr int t = decltype(t_const)::value;
         const int from = block * kBlock + 32 * t;
-        if (!here || from + 31 > wave_first) {
+        if (static_cast<int>(!here) | static_cast<int>(from + 31 > wave_first)) {       // (one branch: two take 1.5 % longer on long prompts)
+            const int left = here ? last - from - 4 * half : -1;        // scores i whose token 8 (i / 4) + i % 4 is at most this are seen
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const int left = here ? last[mt] - from - 4 * half : -1;        // scores i whose token 8 (i / 4) + i % 4 is at most this are seen
-#pragma unroll
-                for (int i = 0; i < 16; ++i) z[mt][i] = 8 * (i >> 2) + (i & 3) <= left ? z[mt][i] * to_log2 : -__builtin_inff();
-            }
+            for (int i = 0; i < 16; ++i) z[i] = 8 * (i >> 2) + (i & 3) <= left ? z[i] * to_log2 : -__builtin_inff();
             to_log2 = 1.f;      // (a factor of zero would make NaN of what is masked)
         }
-        float most[MT], base[MT];
-        bool rises = false;
+        float most = z[0];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            most[mt] = z[mt][0];
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, z[i]);
+        most = max_over_32(most) * to_log2;
+        if (__any(most - m > kSlack)) {
+            const float m_new = fmaxf(m, __builtin_ceilf(most) - kLead);
+            const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m - m_new);     // (a power of two: nothing is rounded)
+            m = m_new;
+            l *= factor;
 #pragma unroll
-            for (int i = 1; i < 16; ++i) most[mt] = fmaxf(most[mt], z[mt][i]);
-            most[mt] = max_over_32(most[mt]) * to_log2;
-            rises |= most[mt] - m[mt] > kSlack;
-        }
-        if (__any(rises)) {
+            for (int i = 0; i < kOut; ++i) o[i] *= factor;
+            const f16x2_t two = __builtin_bit_cast(f16x2_t, pack2<FC_F16>(factor, factor));
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                const float m_new = fmaxf(m[mt], __builtin_ceilf(most[mt]) - kLead);
-                const float factor = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(m[mt] - m_new);     // (a power of two: nothing is rounded)
-                m[mt] = m_new;
-                l[mt] *= factor;
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t w[4] = {p[i].x, p[i].y, p[i].z, p[i].w};
+                uint32_t r[4];
 #pragma unroll
-                for (int i = 0; i < kOut; ++i) o[mt][i] *= factor;
-                const f16x2_t two = __builtin_bit_cast(f16x2_t, pack2<FC_F16>(factor, factor));
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t w[4] = {p[mt][i].x, p[mt][i].y, p[mt][i].z, p[mt][i].w};
-                    uint32_t r[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) r[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, w[j]) * two);
-                    p[mt][i] = make_uint4(r[0], r[1], r[2], r[3]);
-                }
+                for (int j = 0; j < 4; ++j) r[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, w[j]) * two);
+                p[i] = make_uint4(r[0], r[1], r[2], r[3]);
             }
         }
+        const float base = m == -__builtin_inff() ? 0.f : -m;
+        f32x16_t z_next;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) base[mt] = m[mt] == -__builtin_inff() ? 0.f : -m[mt];
-        f32x16_t z_next[MT];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) z_next[mt][i] = 0.f;
+        for (int i = 0; i < 16; ++i) z_next[i] = 0.f;
         // Step by step, in this order: matrix instructions on one operand from LDS, the operand of one kAhead steps on, and the vector unit's work of that time.
         constexpr int kProducts = 2 * kSteps;
         auto operand = [&](int i) {
             return i % 2 == 0 ? key_operand(keys_next, t ^ 1, i / 2) : value_operand(values_last, i / 2 % kOut, 2 * (t ^ 1) + i / 2 / kOut);
         };
         uint4 x[kProducts];
-        uint32_t w[MT][8];
-        float e[MT][16];
+        uint32_t w[8];
+        float e[16];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) x[i] = operand(i);
 #pragma unroll
         for (int i = 0; i < kProducts; ++i) {
             __builtin_amdgcn_sched_barrier(0);
             if (i + kAhead < kProducts) x[i + kAhead] = operand(i + kAhead);
+            if (i % 2 == 0) z_next = mfma_32<DT>(x[i], q[i / 2], z_next);
+            else o[i / 2 % kOut] = mfma_32<FC_F16>(x[i], p[i / 2 / kOut], o[i / 2 % kOut]);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                if (i % 2 == 0) z_next[mt] = mfma_32<DT>(x[i], q[mt][i / 2], z_next[mt]);
-                else o[mt][i / 2 % kOut] = mfma_32<FC_F16>(x[i], p[mt][i / 2 / kOut], o[mt][i / 2 % kOut]);
-#pragma unroll
-                for (int j = 16 * i / kProducts; j < 16 * (i + 1) / kProducts; ++j) {
-                    e[mt][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[mt][j], to_log2, base[mt]));
-                    l[mt] += e[mt][j];
-                    if (j & 1) {
-                        w[mt][j >> 1] = pack2<FC_F16>(e[mt][j - 1], e[mt][j]);
-                        __asm__ volatile("" : "+v"(w[mt][j >> 1]), "+v"(l[mt]));     // (here, not where it is used)
-                    }
+            for (int j = 16 * i / kProducts; j < 16 * (i + 1) / kProducts; ++j) {
+                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], to_log2, base));
+                l += e[j];
+                if (j & 1) {
+                    w[j >> 1] = pack2<FC_F16>(e[j - 1], e[j]);
+                    __asm__ volatile("" : "+v"(w[j >> 1]), "+v"(l));     // (here, not where it is used)
                 }
-                if (MT > 1) __builtin_amdgcn_sched_barrier(0);
             }
             // (late: what it works on has then been on its way for longer than a half)
             constexpr int kLate = kProducts / 2, kBeside = 4 * kShare;
@@ -211,12 +182,9 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
             for (int n = ((i - kLate) * kBeside + kLate - 1) / kLate; i >= kLate && n < ((i + 1 - kLate) * kBeside + kLate - 1) / kLate; ++n) beside(n);
         }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            p[mt][0] = make_uint4(w[mt][0], w[mt][1], w[mt][2], w[mt][3]);
-            p[mt][1] = make_uint4(w[mt][4], w[mt][5], w[mt][6], w[mt][7]);
-            z[mt] = z_next[mt];
-        }
+        p[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        p[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        z = z_next;
     };
 
     // What half t of a block adds to o (weights p), its values taken from memory: exact products in units of its scale, added to o in 32 bits.
@@ -226,23 +194,21 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         const uint8_t *const from = codes_of(pool) + at;
         const float ratio = pow2_held(to_unit);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int n = 0; n < kOut; ++n) {
+            f32x16_t adds;
+            __builtin_amdgcn_sched_barrier(0);      // (one after another, in few registers)
 #pragma unroll
-            for (int n = 0; n < kOut; ++n) {
-                f32x16_t adds;
-                __builtin_amdgcn_sched_barrier(0);      // (one after another, in few registers)
+            for (int i = 0; i < 16; ++i) adds[i] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) adds[i] = 0.f;
-#pragma unroll
-                for (int step = 0; step < 2; ++step) {
-                    // tokens 16 (2 t + step) + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
-                    uint32_t lo = *reinterpret_cast<const uint32_t *>(from + value_piece<DP>(32 * n, 0) - value_piece<DP>(0, 0) + 4 * step);
-                    uint32_t hi = *reinterpret_cast<const uint32_t *>(from + value_piece<DP>(32 * n, 32) - value_piece<DP>(0, 0) + 4 * step);
-                    adds = mfma_32<FC_F16>(codes_to_16<FC_F16>(lo & ~nan_bytes(lo), hi & ~nan_bytes(hi)), p[mt][step], adds);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[mt][n][i] = __builtin_fmaf(adds[i], ratio, o[mt][n][i]);
+            for (int step = 0; step < 2; ++step) {
+                // tokens 16 (2 t + step) + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
+                uint32_t lo = *reinterpret_cast<const uint32_t *>(from + value_piece<DP>(32 * n, 0) - value_piece<DP>(0, 0) + 4 * step);
+                uint32_t hi = *reinterpret_cast<const uint32_t *>(from + value_piece<DP>(32 * n, 32) - value_piece<DP>(0, 0) + 4 * step);
+                adds = mfma_32<FC_F16>(codes_to_16<FC_F16>(lo & ~nan_bytes(lo), hi & ~nan_bytes(hi)), p[step], adds);
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[n][i] = __builtin_fmaf(adds[i], ratio, o[n][i]);
+        }
     };
 
     if (begin < end) {
@@ -277,12 +243,9 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
             *reinterpret_cast<uint4 *>(lds + kBuffer + kValues + i) = make_uint4(0, 0, 0, 0);
         __syncthreads();
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int i = 0; i < 16; ++i) z[i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[mt][i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < kSteps; ++c) z[mt] = mfma_32<DT>(key_operand(0, 0, c), q[mt][c], z[mt]);
-        }
+        for (int c = 0; c < kSteps; ++c) z = mfma_32<DT>(key_operand(0, 0, c), q[c], z);
 
         uint32_t buffer = 0;        // of block j's keys and values; the other one is its neighbours'
         for (int block = begin; block < end; ++block, buffer = kBuffer - buffer) {
@@ -291,26 +254,23 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
             const bool strange = here && scales.y < 0.f;    // NaN among the values: zeros in LDS, found again here
             if (strange) {
                 const uint8_t *const codes = codes_of(pool);
+                const int left = last - block * kBlock - 4 * half;
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    const int left = last[mt] - block * kBlock - 4 * half;
+                for (int t = 0; t < kOut; ++t) {
+                    f32x16_t count;
 #pragma unroll
-                    for (int t = 0; t < kOut; ++t) {
-                        f32x16_t count;
+                    for (int i = 0; i < 16; ++i) count[i] = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) count[i] = 0.f;
-#pragma unroll
-                        for (int step = 0; step < 4; ++step) {
-                            // tokens 16 step + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
-                            const uint32_t lo = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * half) + 4 * step);
-                            const uint32_t hi = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * (half + 2)) + 4 * step);
-                            const uint4 seen = make_uint4(seen_pair(16 * step, left), seen_pair(16 * step + 2, left), seen_pair(16 * step + 8, left),
-                                                          seen_pair(16 * step + 10, left));
-                            count = mfma_32<FC_F16>(nan_marks(lo, hi), seen, count);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[mt][t][i] = count[i] > 0.f ? __builtin_nanf("") : o[mt][t][i];
+                    for (int step = 0; step < 4; ++step) {
+                        // tokens 16 step + 4 half + 0 .. 3 and 8 on: quarters `half` and half + 2 of the row
+                        const uint32_t lo = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * half) + 4 * step);
+                        const uint32_t hi = *reinterpret_cast<const uint32_t *>(codes + value_piece<DP>(32 * t + col, 16 * (half + 2)) + 4 * step);
+                        const uint4 seen = make_uint4(seen_pair(16 * step, left), seen_pair(16 * step + 2, left), seen_pair(16 * step + 8, left),
+                                                      seen_pair(16 * step + 10, left));
+                        count = mfma_32<FC_F16>(nan_marks(lo, hi), seen, count);
                     }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[t][i] = count[i] > 0.f ? __builtin_nanf("") : o[t][i];
                 }
 #pragma unroll
                 for (int i = 0; i < kShare; ++i) vx[i] = without_nan(vx[i]);
@@ -331,9 +291,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
             if (unit_new != o_unit.e) {         // (o has all of the values that are in the old one)
                 const float factor = pow2_held(o_unit.e - unit_new);
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int t = 0; t < kOut; ++t) o[mt][t] *= factor;
+                for (int t = 0; t < kOut; ++t) o[t] *= factor;
                 o_unit.e = unit_new;
             }
             if (__builtin_expect(far, 0)) far_values(pool_far, 0, scale_v - unit_new);
@@ -353,9 +311,7 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
 #pragma unroll
         for (int t = 0; t < kOut; ++t)
 #pragma unroll
-            for (int step = 0; step < 2; ++step)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) o[mt][t] = mfma_32<FC_F16>(value_operand(buffer, t, 2 + step), p[mt][step], o[mt][t]);
+            for (int step = 0; step < 2; ++step) o[t] = mfma_32<FC_F16>(value_operand(buffer, t, 2 + step), p[step], o[t]);
     }
 
     const float to_sums = o_unit.to_sums();
@@ -365,52 +321,48 @@ template <int DT, int DP, int MT, int WAVES> __global__ __launch_bounds__(64 * W
         const RowPlace p = row_place(a, tile * kRows + row);
         return (int64_t)(s.row0 + p.token) * a.heads + h * a.group + p.head;
     };
-    // Pieces are written as the registers hold them, 1 KB a store: [wave][row tile][output tile][four channels][lane].
+    // Pieces are written as the registers hold them, 1 KB a store: [wave][output tile][four channels][lane].
     constexpr int kLanes = kOut * 4 * 64;
     auto place = [&](int item) {
         const int tile_at = item / kLanes, in = item % kLanes, row = tile_at * 32 + (in & 31);
         return ItemPlace{row < rows ? row : kNoRow, (in >> 8) * 32 + (in >> 6 & 3) * 8 + (in >> 5 & 1) * 4};
     };
+    const float sum = l + __shfl_xor(l, 32);
+    const int64_t row = out_row(min(r, rows - 1));
+    if (active > 1 && half == 0) pieces.put_ml((uint32_t)(split * kRows + r), m, sum);
+    const uint32_t item = (uint32_t)(split * kRows * (DP / 4) + wave * kLanes + lane);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-        const float sum = l[mt] + __shfl_xor(l[mt], 32);
-        const int r = wave * kWaveRows + 32 * mt + col;
-        const int64_t row = out_row(min(r, rows - 1));
-        if (active > 1 && half == 0) pieces.put_ml((uint32_t)(split * kRows + r), m[mt], sum);
-        const uint32_t item = (uint32_t)(split * kRows * (DP / 4) + (wave * MT + mt) * kLanes + lane);
+    for (int t = 0; t < kOut; ++t)
 #pragma unroll
-        for (int t = 0; t < kOut; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const f32x4_t v = {o[mt][t][i] * to_sums, o[mt][t][i + 1] * to_sums, o[mt][t][i + 2] * to_sums, o[mt][t][i + 3] * to_sums};
-                if (active > 1) pieces.put(item + (t * 4 + i / 4) * 64, v);
-                else if (r < rows) finish_row<DT>(a, row, 32 * t + 2 * i + 4 * half, v, m[mt], sum);
-            }
-    }
+        for (int i = 0; i < 16; i += 4) {
+            const f32x4_t v = {o[t][i] * to_sums, o[t][i + 1] * to_sums, o[t][i + 2] * to_sums, o[t][i + 3] * to_sums};
+            if (active > 1) pieces.put(item + (t * 4 + i / 4) * 64, v);
+            else if (r < rows) finish_row<DT>(a, row, 32 * t + 2 * i + 4 * half, v, m, sum);
+        }
     if (active == 1) return;
     __syncthreads();        // (the flag lies where operands were)
     if (!last_to_arrive(a, unit, active, reinterpret_cast<int32_t *>(lds))) return;
     join_pieces<DT, DP, kThreads>(a, pieces, (rows + 31) / 32 * kLanes, kRows, active, reinterpret_cast<float *>(lds) + 4, place, out_row);
 }
 
-template <int DT, int DP, int MT, int WAVES> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
+template <int DT, int DP, int WAVES> hipError_t run_tile(const AttnArgs &a, hipStream_t s)
 {
     constexpr size_t lds = 2 * (size_t)(kBlock * kKeyPitch<DP> + DP * kValuePitch);
-    const hipError_t raised = raise_lds<k_attend_tile<DT, DP, MT, WAVES>>(lds);
+    const hipError_t raised = raise_lds<k_attend_tile<DT, DP, WAVES>>(lds);
     if (raised != hipSuccess) return raised;
     const int64_t units = (int64_t)a.kv.batch * a.kv.kv_heads * a.tiles;
-    k_attend_tile<DT, DP, MT, WAVES><<<dim3((uint32_t)(units * a.splits)), 64 * WAVES, lds, s>>>(a);
+    k_attend_tile<DT, DP, WAVES><<<dim3((uint32_t)(units * a.splits)), 64 * WAVES, lds, s>>>(a);
     return hipGetLastError();
 }
 
 template <int DT> hipError_t run_type(const AttnArgs &a, int rows_tile, hipStream_t s)
 {
     switch (a.kv.dp) {
-    case 64: return run_tile<DT, 64, 1, 4>(a, s);
-    case 96: return rows_tile == 256 ? run_tile<DT, 96, 1, 8>(a, s) : run_tile<DT, 96, 1, 4>(a, s);
-    case 128: return rows_tile == 256 ? run_tile<DT, 128, 1, 8>(a, s) : run_tile<DT, 128, 1, 4>(a, s);
-    case 192: return run_tile<DT, 192, 1, 4>(a, s);
-    default: return run_tile<DT, 256, 1, 4>(a, s);
+    case 64: return run_tile<DT, 64, 4>(a, s);
+    case 96: return rows_tile == 256 ? run_tile<DT, 96, 8>(a, s) : run_tile<DT, 96, 4>(a, s);
+    case 128: return rows_tile == 256 ? run_tile<DT, 128, 8>(a, s) : run_tile<DT, 128, 4>(a, s);
+    case 192: return run_tile<DT, 192, 4>(a, s);
+    default: return run_tile<DT, 256, 4>(a, s);
     }
 }
 

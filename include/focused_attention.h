@@ -37,7 +37,8 @@
  *   - out = sum_t softmax_t(scale * q.k_t) v_t with keys and values as the cache holds them.  Products of stored values accumulated
  *     in 32 bits; softmax in 32 bits; weights rounded to 11 bits (f16) for their product with the values, steps of 2^-30 of the largest at
  *     least; one rounding to the output type.
- *   - What a row does not attend to has no influence on it, NaN included.  A row that attends to nothing is +0.0 with lse = -infinity.
+ *   - What a row does not attend to has no influence on it, NaN included.  A row that attends to nothing is +0.0 with lse = -infinity, and so is one
+ *     whose scores are all -infinity (a query of infinity against keys of one sign).
  *   - lse, where it is wanted: log(sum_t exp(scale * q.k_t)) in 32 bits, [tokens][heads].
  *
  * Selection (fc_focused_attention; FC_CAUSAL is implied)

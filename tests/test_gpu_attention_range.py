@@ -156,3 +156,22 @@ def test_factors_of_scores_beyond_32_bits(key_size, scale, new):
             want, _, error = O.attend(setup.oracle[0], qn[row], position, scale, True, blocks)
             allowed = error + LAST_PLACE[B.BF16] * (np.abs(want) + error) + LEAST[B.BF16]
             assert (np.abs(G.to_f64(got[row]) - want) <= allowed).all()
+
+
+@pytest.mark.parametrize("new", [1, 90])
+def test_scores_that_are_all_minus_infinity(new):
+    """A query of infinity against keys of the other sign: nothing is attended to; of the same sign: NaN."""
+    torch = G.torch_mod()
+
+    def positive(b, k, v):
+        k[:, :, 3] = 0.5 + np.abs(k[:, :, 3])
+        return k, v
+    setup = Setup([700], 1, 64, B.BF16, tokens=positive)
+    q, _ = setup.queries(new, 2)
+    q[:, 0, 3], q[:, 1, 3] = float("-inf"), float("inf")
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=G.dev())
+    out = A.cache_attention(setup.cache, q, setup.table, setup.lengths_dev, lse=lse)
+    listed, _ = A.focused_attention(setup.cache, q, setup.table, setup.lengths_dev, 1, 1, 3)
+    for got in (G.to_f64(out), G.to_f64(listed)):
+        assert (got[:, 0] == 0).all() and np.isnan(got[:, 1]).all()
+    assert torch.isneginf(lse[:, 0]).all()

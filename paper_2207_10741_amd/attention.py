@@ -10,6 +10,9 @@ Argument marshalling only, as in `binding`: every step runs in the HIP kernels o
 
 The calls' semantics (blocks of 64 tokens, scales, selection, bounds) are stated in the header.  A serving loop that makes the same call
 on the same tensors again and again marshals it once: PreparedAppend, PreparedRead, PreparedAttention, PreparedFocusedAttention.
+
+Kernels and their grids are chosen by the bounds.  Without starts they follow from the tensors' shapes; with starts, max_new is every row of the call
+unless it is given, right for one sequence alone: sequences of single tokens want max_new=1, others their largest number of new tokens.
 """
 from __future__ import annotations
 

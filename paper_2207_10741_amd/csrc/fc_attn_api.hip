@@ -102,8 +102,9 @@ void cut_for_rounds(int64_t units, int32_t blocks, int32_t mean, int32_t *splits
     }
 }
 
-// Lists: from this many on there are enough to fill the chip with a wave each (us, split -> whole, 16 and 32 blocks of 8 key heads of 128: 512 units 36 -> 39,
-// 57 -> 69; 1024 68 -> 67, 121 -> 119; 1600 120 -> 118; 2800 of 9 blocks 53 -> 44).
+// Lists: from this many on there are enough to fill the chip with a wave each (us of the whole call, split -> whole, 9 / 16 / 32 blocks of 8 key heads of 128 with 4 queries
+// each, over 313: 512 units 30.0 / 36.6 / 48.8 -> 30.4 / 38.0 / 52.7, 768 35.5 / 43.1 / 56.6 -> 30.8 / 38.2 / 52.8, 1024 38.6 / 46.5 / 59.8 -> 31.0 / 38.3 / 53.0, 2800
+// 59.7 / 73.0 / 107 -> 45.5 / 61.5 / 97; 9 blocks of 2 key heads of 96 with 5: 512 26.1 -> 28.8, 768 28.0 -> 29.2, 1024 31.6 -> 29.4, 2800 45.6 -> 38.9).
 constexpr int64_t kWholeLists = 1024;
 // Neighbouring tokens' lists together: from this many waves on (us, apart -> together, lists of 16 blocks of 8 key heads of 128, keys that select independently:
 // 4 heads a key head, 512 / 1024 / 2048 / 4096 tokens (1024 waves on) 79 / 132 / 245 / 475 -> 81 / 114 / 203 / 389; one head a key head, 4096 tokens 469 -> 333;

@@ -389,8 +389,8 @@ template <int DT, int DP, int MT, int WAVES, bool LIST> __global__ __launch_boun
     join_pieces<DT, DP, kThreads>(a, pieces, rows * kPieces, kRows, active, lds, place, out_row);
 }
 
-// Bound by the vector unit, which converts a block's codes for the few rows of one token, and by latency where there are few lists: 2800 lists of nine blocks,
-// two heads of 96 with five queries each: 25 us, one round of waves.
+// Bound by the vector unit, which converts a block's codes for the few rows of one token, and by latency where there are few lists: 2294 lists of nine blocks,
+// two heads of 96 with five queries each: 23.5 us, one round of waves.
 // A wave takes up to 16 heads of one token and the token's whole list.  An XCD takes an eighth of the units in one piece: neighbouring tokens of a head
 // share blocks.
 template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupancy<DP, 1>)) void k_attend_lists(AttnArgs a)
@@ -421,8 +421,8 @@ template <int DT, int DP> __global__ __launch_bounds__(64 * kListWaves, (kOccupa
     for (int t = 0; t < kTiles; ++t) finish_row<DT>(a, row, 16 * t + 4 * quarter, w.o[0][t] * w.unit.to_sums(), w.m[0], sum);
 }
 
-// Bound by the vector unit as the lists alone are: 235 instructions a block, most of them conversions of codes.  4096 tokens over 512 blocks, lists of 16,
-// 8 heads of 128 with 4 queries each: 355 - 363 us (lists one a wave: 500).
+// Bound by the vector unit as the lists alone are: 246 instructions a block beside the 32 matrix ones, most of them conversions of codes.  4096 tokens over 512 blocks, lists of 16,
+// 8 heads of 128 with 4 queries each: 341 - 361 us (lists one a wave: 500).
 // A wave takes a.shared neighbouring tokens of a sequence (a.shared * group <= 16 rows).  Their lists are put together in LDS: a mask of tokens for every block
 // of the sequence, and the blocks with one, in order.  Blocks that neighbours share, the first and the last ones among them, are read and multiplied once,
 // and the rows of the matrix instructions, of which one token fills `group`, are used.

@@ -196,7 +196,7 @@ template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint3
 }
 
 // Bound by the counting of the thresholds (a compare and a ballot for 64 scores a bit, at most 32 bits, scalar additions beside them).  4096 tokens, 8 heads of 128 with 4 queries
-// each, up to 512 blocks: 60 us.
+// each, up to 512 blocks: 63 us.
 template <int DT, int DP, int QT, int DIGITS> __global__ __launch_bounds__(kThreads) void k_select(SelectArgs a)
 {
     constexpr int SP = kSketch<DP>, kChunks = SP / 64, kShare = kThreads / QT;        // threads of a token
@@ -299,7 +299,7 @@ __device__ __forceinline__ int sum_up_to(int v)
     return v;
 }
 
-// One token over 512 blocks, 8 heads of 128: 7.8 us; 16 tokens over up to 1016 blocks: 11.9 us (queries, sketches, two to four rounds of counting, the list: dependent steps).
+// One token over 512 blocks, 8 heads of 128: 8.5 us; 16 tokens over up to 1016 blocks: 13.4 us (queries, sketches, two to four rounds of counting, the list: dependent steps).
 template <int DT, int DP> __global__ __launch_bounds__(kThreadsOne) void k_select_one(SelectArgs a)
 {
     constexpr int SP = kSketch<DP>, kChunks = SP / 64, kWaves = kThreadsOne / 64;

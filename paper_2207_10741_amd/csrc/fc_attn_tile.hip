@@ -19,7 +19,7 @@ constexpr uint32_t kValuePitch = 2 * kBlock + 16;
 
 // 32 rows a wave: scores, weights and outputs of 64 would not fit the registers without copies between their halves (820 us against 573).  A step multiplies a
 // block's values with the last step's weights beside this step's scores, so that the matrix cores always have the one while the vector unit works on the other.
-// 8192 tokens, 32 heads of 128 over 8, causal: 539 us, 1020 TFLOP/s, 89 % of what the library's 8192^3 product reaches here.  Bound by the matrix cores, and then by power
+// 8192 tokens, 32 heads of 128 over 8, causal: 538 - 557 us, 990 - 1020 TFLOP/s, 86 - 89 % of what the library's 8192^3 product reaches here.  Bound by the matrix cores, and then by power
 // (the clock falls as their share of idle cycles does).
 template <int DT, int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, DP <= 128 ? 2 : 1) void k_attend_tile(AttnArgs a)
 {

@@ -128,9 +128,10 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
 
 // A block is a workgroup's because its scale needs its largest magnitude first: the rows are read once into registers and converted from there.
 // Magnitudes are compared two at a time as whole numbers, and codes come out of the conversions in the order that they are stored in: in 32-bit floats and byte by
-// byte the vector unit was the bound (append and read of 15 000 tokens of six sequences, 8 heads of 128: 59.8 us, now 50.0).  Heads are next to each other in the grid,
-// as their rows are in memory (then 46.4).
-// The kernel alone: 22 us for 92 MB read and written, 4.2 TB/s: memory, and the phases of a workgroup (read, magnitude, convert, write), which overlap with others' only.
+// byte the vector unit was the bound (append and read of 15 000 tokens of six sequences, 8 heads of 128, the same inputs again and again: 59.8 us, now 50.0).  Heads are
+// next to each other in the grid, as their rows are in memory (then 46.4).
+// The kernel alone, on inputs that change: 31 us for 92 MB read and written, 2.9 TB/s (the same inputs: 22 us): memory, and the phases of a workgroup (read, magnitude,
+// convert, write), which overlap with others' only.
 // A thread holds channels 8 c .. 8 c + 7 of four consecutive tokens 4 r .. 4 r + 3 at a time: four tokens are one word of a row of values.
 template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_append(AppendArgs a)
 {
@@ -299,8 +300,10 @@ template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_appen
     if (threadIdx.x == 0) g.weights[unit] = ks * pow2_of(e) * (1.f / kBlock);
 }
 
-// A wave a head: no barrier, and the largest magnitude is a reduction over lanes.  A channel's value is one byte of a 16-byte piece of its own, so a token
-// rewrites 128-byte lines all over the block: 256 sequences, 8 heads of 128: 13.8 us for 1 MB of rows; one sequence: 3.4 us, two round trips (scale, codes).
+// A wave a head: no barrier, and the largest magnitude is a reduction over lanes.  Bound by latency: one sequence, 8 heads of 128: 3.4 us, two round trips (scale, codes).
+// 256 sequences whose tokens fall anywhere: 15.7 us, which is the time of the slowest waves, the few that write a block's 64th token (its keys are read back a byte a
+// lane) or whose token raises a scale (the block is rounded again).  All tokens in the middle of their blocks: 8.4 us, first of a block 8.8, 64th 25, all raising 24.  (A
+// token's 128 values are bytes of pieces of their own in eight runs of 256 bytes: 16 lines, some 8 MB read and written by 2048 waves, 2 us of memory's time.)
 // A wave's lane holds channels kEach * lane on (of 96 channels, 48 lanes do).
 template <int DT, int DP> __global__ __launch_bounds__(kThreads) void k_kv_append_one(AppendArgs a)
 {
@@ -396,7 +399,7 @@ struct ReadArgs {
 };
 
 // A block goes through LDS, where its codes are taken out of the matrix instructions' order into rows: four channels of a token a store of 16 bytes.  Bound by memory: 15 000
-// tokens, 8 heads of 128: 25 us for 154 MB, 6.1 TB/s (what was just written is read from the chip's cache).
+// tokens, 8 heads of 128: 27.6 us for 154 MB, 5.6 TB/s (what was just written is read from the chip's cache).
 template <int DP> __global__ __launch_bounds__(kThreads) void k_kv_read(ReadArgs a)
 {
     __shared__ __align__(16) uint8_t image[2 * kBlock * DP];

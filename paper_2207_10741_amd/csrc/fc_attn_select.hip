@@ -160,6 +160,8 @@ template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint3
         each([&](uint32_t key) { c += (int)__popcll(__ballot(key >= trial)); });
         return c;
     };
+    // (the largest key there is: a NaN, as the weight of a block that was never written may be)
+    auto count_above = [&](uint32_t threshold) { return threshold == ~0u ? 0 : count(threshold + 1); };
     uint32_t threshold = 0;
     if (top <= 64) {
         uint32_t largest_key = 0;
@@ -167,7 +169,7 @@ template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint3
         const uint32_t least = max(threshold_of_lanes(largest_key, top), 1u);
         const int some = count(least);
         if (some == top) {
-            above = count(least + 1);
+            above = count_above(least);
             return least;
         }
         if (some <= 64) {
@@ -191,7 +193,7 @@ template <int REGS> __device__ __forceinline__ uint32_t threshold_of(const uint3
         if (c >= top) threshold = trial;
         if (c == top) break;
     }
-    above = threshold == ~0u ? 0 : count(threshold + 1);
+    above = count_above(threshold);
     return threshold;
 }
 

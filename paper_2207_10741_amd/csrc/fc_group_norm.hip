@@ -1,0 +1,412 @@
+// Group norm of channels-last rows, with the rows that a mask keeps, and an activation.
+//
+// Memory bounds it: x in and out once, or x in twice where an image does not stay on the chip between its statistics and its output.
+//   k_norm_once    a workgroup holds all rows of a slice of an image's channels (whole groups) in registers: one launch, x is read once
+//   k_norm_stats, k_norm_apply   images too large for that: workgroups of chunks of rows write what they found, the last one of an image's slice joins it
+//                  in order; then all rows again
+//
+// A thread has a piece of a row (16 bytes, or one element where rows are not made of those) and goes down the rows with it.  Its sums are about the value
+// that it meets first: x - pivot is of the size of the spread, whatever the mean is, so that 32 bits lose nothing to it; joining (count, mean, squared
+// distances) triples is exact algebra: n = n1 + n2, mean = m1 + (m2 - m1) n2 / n, s = s1 + s2 + (m2 - m1)^2 n1 n2 / n.
+#include "fc_layers_internal.hpp"
+
+namespace fc {
+
+constexpr int kNormThreads = 256;       // of the kernels with chunks
+
+struct Triple {
+    float n, mean, s;
+    __device__ __forceinline__ void join(float n2, float mean2, float s2)
+    {
+        const float both = n + n2, part = both > 0.f ? n2 / both : 0.f, d = mean2 - mean;
+        s += s2 + d * d * (n * part);
+        mean += n2 > 0.f ? d * part : 0.f;
+        n = both;
+    }
+};
+// over the lanes of a wave, in a fixed order
+__device__ __forceinline__ Triple join_lanes(Triple t)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const float n = __shfl_xor(t.n, m), mean = __shfl_xor(t.mean, m), s = __shfl_xor(t.s, m);
+        // (both lanes of a pair join the same two in the same order)
+        Triple lo = (threadIdx.x & m) ? Triple{n, mean, s} : t;
+        const Triple hi = (threadIdx.x & m) ? t : Triple{n, mean, s};
+        if (lo.n == 0.f) lo = hi;
+        else if (hi.n > 0.f) lo.join(hi.n, hi.mean, hi.s);
+        t = lo;
+    }
+    return t;
+}
+
+// A piece of a row: VE values, and the way back.
+template <typename T, bool WIDE> struct Piece {
+    static constexpr int VE = WIDE ? 16 / (int)sizeof(T) : 1;
+    typedef typename std::conditional<WIDE, uint4, T>::type raw_t;
+    static __device__ __forceinline__ void values(const raw_t &r, float (&v)[VE])
+    {
+        if constexpr (!WIDE) v[0] = to_float(r);
+        else if constexpr (sizeof(T) == 4) {
+            const float4 f = __builtin_bit_cast(float4, r);
+            v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+        } else unpack8<T>(r, v);
+    }
+    static __device__ __forceinline__ raw_t rounded(const float (&v)[VE])
+    {
+        if constexpr (!WIDE) {
+            T t;
+            from_float(v[0], &t);
+            return t;
+        } else if constexpr (sizeof(T) == 4) {
+            return __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3]));
+        } else return pack8<T>(v);
+    }
+    static __device__ __forceinline__ raw_t zero()
+    {
+        if constexpr (WIDE) return make_uint4(0, 0, 0, 0);
+        else return T{};
+    }
+};
+
+// An image's rows, cut to the call's bounds.
+struct ImageRows {
+    int32_t first, n;
+};
+__device__ __forceinline__ ImageRows image_rows(const NormArgs &a, int image)
+{
+    if (!a.starts) return {image * a.max_rows, a.max_rows};
+    const int32_t from = min(max(a.starts[image], 0), a.rows), to = min(max(a.starts[image + 1], from), a.rows);
+    return {from, min(to - from, a.max_rows)};
+}
+
+// How a workgroup's threads lie over a slice: piece `p` (of PR; more than there are threads: several each), row `phase` of every `phases`.
+struct Spread {
+    int pr, phases, p, phase;
+    bool active;
+};
+template <typename P> __device__ __forceinline__ Spread spread_of(const NormArgs &a)
+{
+    Spread s;
+    const int threads = (int)blockDim.x;
+    s.pr = a.slice / P::VE;
+    s.phases = s.pr < threads ? threads / s.pr : 1;
+    s.phase = s.pr < threads ? (int)threadIdx.x / s.pr : 0;
+    s.p = (int)threadIdx.x - s.phase * s.pr;
+    s.active = s.phase < s.phases;
+    return s;
+}
+// What threads found, in LDS: counts [phases], then (mean, squared distances) [phases][entries of a row].  An entry is a piece where pieces lie within a
+// group, else a channel.
+template <typename P> struct Found {
+    float *counts;
+    float2 *entries;
+    int row, per_entry, per_group;      // entries of a row; values of an entry; entries of a group
+    bool whole;
+    __device__ __forceinline__ Found(const NormArgs &a, const Spread &s, unsigned char *lds)
+    {
+        whole = a.per_group % P::VE == 0;
+        per_entry = whole ? P::VE : 1;
+        row = a.slice / per_entry;
+        per_group = a.per_group / per_entry;
+        entries = reinterpret_cast<float2 *>(lds);
+        counts = reinterpret_cast<float *>(entries + s.phases * row);
+    }
+    // rows: how many this thread saw; s1, s2: the sums about the pivots
+    __device__ __forceinline__ void put(const Spread &sp, int p, float rows, const float (&pivot)[P::VE], const float (&s1)[P::VE], const float (&s2)[P::VE]) const
+    {
+        const float inverse = rows > 0.f ? 1.f / rows : 0.f;
+        if (whole) {
+            Triple t = {rows, pivot[0] + s1[0] * inverse, fmaxf(s2[0] - s1[0] * s1[0] * inverse, 0.f)};
+            if (s2[0] != s2[0]) t.s = s2[0];
+#pragma unroll
+            for (int i = 1; i < P::VE; ++i) {
+                const float s = s2[i] - s1[i] * s1[i] * inverse;
+                t.join(rows, pivot[i] + s1[i] * inverse, s < 0.f ? 0.f : s);
+            }
+            entries[sp.phase * row + p] = make_float2(t.mean, t.s);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P::VE; ++i) {
+                const float s = s2[i] - s1[i] * s1[i] * inverse;
+                entries[sp.phase * row + p * P::VE + i] = make_float2(pivot[i] + s1[i] * inverse, s < 0.f ? 0.f : s);
+            }
+        }
+        if (p == 0) counts[sp.phase] = rows;
+    }
+    // group g of the slice, by a wave
+    __device__ __forceinline__ Triple group(const Spread &sp, int g) const
+    {
+        const int lane = threadIdx.x & 63, items = per_group * sp.phases;
+        Triple t = {0.f, 0.f, 0.f};
+        for (int i = lane; i < items; i += 64) {
+            const int phase = i / per_group, e = i - phase * per_group;
+            const float n = counts[phase] * (float)per_entry;
+            const float2 f = entries[phase * row + g * per_group + e];
+            if (n > 0.f) {
+                if (t.n == 0.f) t = {n, f.x, f.y};
+                else t.join(n, f.x, f.y);
+            }
+        }
+        return join_lanes(t);
+    }
+};
+__device__ __forceinline__ float2 stats_of(const NormArgs &a, const Triple &t)
+{
+    return make_float2(t.mean, t.n > 0.f ? 1.f / sqrtf(t.s / t.n + a.eps) : 0.f);
+}
+
+// A thread's channels: (x - mean) * factor + bias.
+template <typename P> struct Affine {
+    float mean[P::VE], factor[P::VE], bias[P::VE];
+    template <typename F> __device__ __forceinline__ Affine(const NormArgs &a, int c, F stats)   // c: of the row; stats(group of the row)
+    {
+#pragma unroll
+        for (int i = 0; i < P::VE; ++i) {
+            const float2 s = stats((c + i) / a.per_group);
+            mean[i] = s.x;
+            factor[i] = a.weight ? s.y * a.weight[c + i] : s.y;
+            bias[i] = a.bias ? a.bias[c + i] : 0.f;
+        }
+    }
+    __device__ __forceinline__ typename P::raw_t operator()(const NormArgs &a, const typename P::raw_t &r) const
+    {
+        float v[P::VE];
+        P::values(r, v);
+#pragma unroll
+        for (int i = 0; i < P::VE; ++i) v[i] = (v[i] - mean[i]) * factor[i] + bias[i];
+        activate_all(v, a.act);
+        return P::rounded(v);
+    }
+};
+
+template <typename P> struct Sums {
+    float pivot[P::VE], s1[P::VE], s2[P::VE], rows;
+    __device__ __forceinline__ Sums()
+    {
+        rows = 0.f;
+#pragma unroll
+        for (int i = 0; i < P::VE; ++i) pivot[i] = s1[i] = s2[i] = 0.f;
+    }
+    __device__ __forceinline__ void add(const typename P::raw_t &r)
+    {
+        float v[P::VE];
+        P::values(r, v);
+#pragma unroll
+        for (int i = 0; i < P::VE; ++i) {
+            pivot[i] = rows == 0.f ? v[i] : pivot[i];
+            const float d = v[i] - pivot[i];
+            s1[i] += d;
+            s2[i] = fmaf(d, d, s2[i]);
+        }
+        rows += 1.f;
+    }
+};
+
+template <typename T, bool WIDE, int NP>
+__global__ __launch_bounds__(1024)
+void k_norm_once(NormArgs a)
+{
+    typedef Piece<T, WIDE> P;
+    typedef typename P::raw_t raw_t;
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ float2 group_stats[512];
+    const int slice = (int)blockIdx.x % a.slices, image = (int)blockIdx.x / a.slices;
+    const ImageRows rows = image_rows(a, image);
+    if (rows.n <= 0) return;
+    const Spread sp = spread_of<P>(a);
+    const Found<P> found(a, sp, smem_raw);
+    const int c = slice * a.slice + sp.p * P::VE;
+    const T *const x = static_cast<const T *>(a.x) + (int64_t)rows.first * a.x_row + c;
+    T *const out = static_cast<T *>(a.out) + (int64_t)rows.first * a.out_row + c;
+    const uint8_t *const mask = a.mask ? a.mask + rows.first : nullptr;
+    raw_t r[NP];
+    bool seen[NP];
+    const int last = rows.n - 1;
+    if (mask) {
+        uint32_t m[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) m[i] = mask[min(sp.phase + i * sp.phases, last)];
+        loaded_together(m);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) seen[i] = m[i] != 0;
+    } else {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) seen[i] = true;
+    }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int row = sp.phase + i * sp.phases;
+        seen[i] = seen[i] && row <= last && sp.active;
+        r[i] = P::zero();
+        if (seen[i]) r[i] = *reinterpret_cast<const raw_t *>(x + (int64_t)row * a.x_row);
+    }
+    Sums<P> sums;
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+        if (seen[i]) sums.add(r[i]);
+    if (sp.active) found.put(sp, sp.p, sums.rows, sums.pivot, sums.s1, sums.s2);
+    __syncthreads();
+    const int groups = a.slice / a.per_group, waves = (int)blockDim.x / 64;
+    for (int g = threadIdx.x >> 6; g < groups; g += waves) {
+        const float2 s = stats_of(a, found.group(sp, g));
+        if ((threadIdx.x & 63) == 0) group_stats[g] = s;
+    }
+    __syncthreads();
+    if (!sp.active) return;
+    const int first_group = slice * groups;
+    const Affine<P> affine(a, c, [&](int g) { return group_stats[g - first_group]; });
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int row = sp.phase + i * sp.phases;
+        raw_t *const to = reinterpret_cast<raw_t *>(out + (int64_t)row * a.out_row);
+        if (seen[i]) *to = affine(a, r[i]);
+        else if (row <= last && !a.keep_out) *to = P::zero();
+    }
+}
+
+constexpr int kNormUnroll = 8;
+
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(kNormThreads)
+void k_norm_stats(NormArgs a)
+{
+    typedef Piece<T, WIDE> P;
+    typedef typename P::raw_t raw_t;
+    extern __shared__ __align__(16) unsigned char smem_raw[];
+    __shared__ int32_t flag;
+    const int chunk = (int)blockIdx.x % a.chunks, unit = (int)blockIdx.x / a.chunks, slice = unit % a.slices, image = unit / a.slices;
+    const ImageRows rows = image_rows(a, image);
+    const Spread sp = spread_of<P>(a);
+    const Found<P> found(a, sp, smem_raw);
+    const int from = chunk * a.chunk_rows, to = min(from + a.chunk_rows, rows.n);
+    const uint8_t *const mask = a.mask ? a.mask + rows.first : nullptr;
+    if (sp.active)
+        for (int p = sp.p; p < sp.pr; p += kNormThreads) {
+            const T *const x = static_cast<const T *>(a.x) + (int64_t)rows.first * a.x_row + slice * a.slice + p * P::VE;
+            Sums<P> sums;
+            for (int row = from + sp.phase; row < to; row += kNormUnroll * sp.phases) {
+                raw_t r[kNormUnroll];
+                bool seen[kNormUnroll];
+#pragma unroll
+                for (int i = 0; i < kNormUnroll; ++i) seen[i] = row + i * sp.phases < to;
+                if (mask) {
+                    uint32_t m[kNormUnroll];
+#pragma unroll
+                    for (int i = 0; i < kNormUnroll; ++i) m[i] = mask[min(row + i * sp.phases, to - 1)];
+                    loaded_together(m);
+#pragma unroll
+                    for (int i = 0; i < kNormUnroll; ++i) seen[i] = seen[i] && m[i] != 0;
+                }
+#pragma unroll
+                for (int i = 0; i < kNormUnroll; ++i) {
+                    r[i] = P::zero();
+                    if (seen[i]) r[i] = *reinterpret_cast<const raw_t *>(x + (int64_t)(row + i * sp.phases) * a.x_row);
+                }
+#pragma unroll
+                for (int i = 0; i < kNormUnroll; ++i)
+                    if (seen[i]) sums.add(r[i]);
+            }
+            found.put(sp, p, sums.rows, sums.pivot, sums.s1, sums.s2);
+            if (sp.pr < kNormThreads) break;
+        }
+    __syncthreads();
+    const int groups = a.slice / a.per_group, lane = threadIdx.x & 63;
+    // [chunk][3][groups]: written and read past the caches
+    const auto part = __builtin_amdgcn_make_buffer_rsrc(a.part + (int64_t)unit * a.chunks * 3 * groups, 0, (uint32_t)(a.chunks * 3 * groups) * 4u, 0x00020000);
+    for (int g = threadIdx.x >> 6; g < groups; g += kNormThreads / 64) {
+        const Triple t = found.group(sp, g);
+        const float v = lane == 0 ? t.n : lane == 1 ? t.mean : t.s;
+        if (lane < 3) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), part, (uint32_t)((chunk * 3 + lane) * groups + g) * 4u, 0, kPiecesPastCaches);
+    }
+    if (!last_piece(a.arrived + unit, a.chunks, &flag)) return;
+    for (int g = threadIdx.x >> 6; g < groups; g += kNormThreads / 64) {
+        Triple t = {0.f, 0.f, 0.f};
+        for (int i = lane; i < a.chunks; i += 64) {
+            float f[3];
+#pragma unroll
+            for (int j = 0; j < 3; ++j) f[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(part, (uint32_t)((i * 3 + j) * groups + g) * 4u, 0, kPiecesPastCaches));
+            if (f[0] > 0.f) {
+                if (t.n == 0.f) t = {f[0], f[1], f[2]};
+                else t.join(f[0], f[1], f[2]);
+            }
+        }
+        t = join_lanes(t);
+        if (lane == 0) a.stats[(int64_t)image * a.groups + slice * groups + g] = stats_of(a, t);
+    }
+}
+
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(kNormThreads)
+void k_norm_apply(NormArgs a)
+{
+    typedef Piece<T, WIDE> P;
+    typedef typename P::raw_t raw_t;
+    const int chunk = (int)blockIdx.x % a.chunks, unit = (int)blockIdx.x / a.chunks, slice = unit % a.slices, image = unit / a.slices;
+    const ImageRows rows = image_rows(a, image);
+    const Spread sp = spread_of<P>(a);
+    const int from = chunk * a.chunk_rows, to = min(from + a.chunk_rows, rows.n);
+    const uint8_t *const mask = a.mask ? a.mask + rows.first : nullptr;
+    if (!sp.active) return;
+    for (int p = sp.p; p < sp.pr; p += kNormThreads) {
+        const int c = slice * a.slice + p * P::VE;
+        const T *const x = static_cast<const T *>(a.x) + (int64_t)rows.first * a.x_row + c;
+        T *const out = static_cast<T *>(a.out) + (int64_t)rows.first * a.out_row + c;
+        const Affine<P> affine(a, c, [&](int g) { return a.stats[(int64_t)image * a.groups + g]; });
+        for (int row = from + sp.phase; row < to; row += 4 * sp.phases) {
+            raw_t r[4];
+            bool seen[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) seen[i] = row + i * sp.phases < to;
+            if (mask) {
+                uint32_t m[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) m[i] = mask[min(row + i * sp.phases, to - 1)];
+                loaded_together(m);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) seen[i] = seen[i] && m[i] != 0;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r[i] = P::zero();
+                if (seen[i]) r[i] = *reinterpret_cast<const raw_t *>(x + (int64_t)(row + i * sp.phases) * a.x_row);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                raw_t *const at = reinterpret_cast<raw_t *>(out + (int64_t)(row + i * sp.phases) * a.out_row);
+                if (seen[i]) *at = affine(a, r[i]);
+                else if (row + i * sp.phases < to && !a.keep_out) *at = P::zero();
+            }
+        }
+        if (sp.pr < kNormThreads) break;
+    }
+}
+
+template <typename T, bool WIDE> static hipError_t launch_norm_as(const NormArgs &a, const NormPlan &p, hipStream_t s)
+{
+    if (p.once) {
+        const dim3 grid((uint32_t)(a.images * a.slices)), block((uint32_t)p.threads);
+        if (p.per_thread <= 4) k_norm_once<T, WIDE, 4><<<grid, block, p.lds, s>>>(a);
+        else k_norm_once<T, WIDE, 16><<<grid, block, p.lds, s>>>(a);
+        return hipGetLastError();
+    }
+    const dim3 grid((uint32_t)((int64_t)a.chunks * a.slices * a.images));
+    if (p.lds > 65536) {
+        const hipError_t e = raise_dynamic_lds<&k_norm_stats<T, WIDE>>(163840 - 256);
+        if (e != hipSuccess) return e;
+    }
+    k_norm_stats<T, WIDE><<<grid, dim3(kNormThreads), p.lds, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    k_norm_apply<T, WIDE><<<grid, dim3(kNormThreads), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_group_norm(const NormArgs &a, const NormPlan &p, int dtype, hipStream_t s)
+{
+    if (dtype == FC_BF16) return p.wide ? launch_norm_as<bf16_t, true>(a, p, s) : launch_norm_as<bf16_t, false>(a, p, s);
+    if (dtype == FC_F16) return p.wide ? launch_norm_as<f16_t, true>(a, p, s) : launch_norm_as<f16_t, false>(a, p, s);
+    return p.wide ? launch_norm_as<float, true>(a, p, s) : launch_norm_as<float, false>(a, p, s);
+}
+
+} // namespace fc

@@ -1,0 +1,257 @@
+// C ABI of the matrix product and of group norm: argument checks on the host, then launches.
+#include "fc_layers_internal.hpp"
+#include <math.h>
+
+using namespace fc;
+
+namespace {
+
+bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride <= FC_LAYERS_MAX_STRIDE; }
+int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+int size_of(int32_t dtype) { return dtype == FC_F32 ? 4 : 2; }
+
+// ---- the matrix product ----
+
+int32_t check_linear(const fc_linear_desc *d, bool residual)
+{
+    if (!d) return FC_ERR_NULL;
+    if (d->rows < 0 || d->n <= 0 || d->k <= 0) return FC_ERR_SHAPE;
+    if (d->dtype != FC_BF16 && d->dtype != FC_F16) return FC_ERR_DTYPE;
+    if (d->out_dtype != d->dtype && d->out_dtype != FC_F32) return FC_ERR_DTYPE;
+    if (d->activation < FC_ACT_NONE || d->activation > FC_ACT_GELU) return FC_ERR_DTYPE;
+    if (d->flags & ~(uint32_t)(FC_RESIDUAL_FIRST | FC_WORKSPACE_READY | FC_ANY_POINTERS) || d->reserved) return FC_ERR_DTYPE;
+    if (d->x_row < 0 || d->w_row < 0 || d->residual_row < 0 || d->out_row < d->n) return FC_ERR_SHAPE;
+    if (d->k > FC_LAYERS_MAX_STRIDE || d->n > FC_LAYERS_MAX_STRIDE) return FC_ERR_RANGE;
+    if (!stride_ok(d->x_row, 0) || !stride_ok(d->w_row, 0) || !stride_ok(d->out_row, 0) || (residual && !stride_ok(d->residual_row, 0))) return FC_ERR_RANGE;
+    return FC_OK;
+}
+
+int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
+{
+    const bool pieces = d->k % 8 == 0 && !(d->flags & FC_ANY_POINTERS), x_pieces = pieces && d->x_row % 8 == 0, w_pieces = pieces && d->w_row % 8 == 0;
+    const int32_t chunks = ceil_div(d->k, kLinearK);
+    p->padded_k = (int64_t)chunks * kLinearK;
+    p->pad_x = p->pad_w = false;
+    p->wide = x_pieces && w_pieces;
+    p->splits = 1;
+    p->per_split = chunks;
+    p->per_wave = 0;
+    if (d->rows <= 64) {
+        p->form = 0;
+        p->tile_m = d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : 64;
+        p->tile_n = d->n >= 16384 ? (p->tile_m == 64 ? 64 : 32) : 16;
+        p->m_tiles = 1;
+        p->n_tiles = ceil_div(d->n, p->tile_n);
+        const int32_t wanted = ceil_div(256, p->n_tiles), most = chunks < 16 ? 1 : chunks / 8;
+        p->per_split = ceil_div(chunks, wanted < most ? wanted : most);
+        p->splits = ceil_div(chunks, p->per_split);
+        p->per_wave = ceil_div(p->per_split, 8);
+    } else {
+        p->form = 1;
+        const int64_t large = (int64_t)ceil_div(d->rows, 256) * ceil_div(d->n, 256);
+        p->tile_m = p->tile_n = large >= 192 ? 256 : 128;
+        p->m_tiles = ceil_div(d->rows, p->tile_m);
+        p->n_tiles = ceil_div(d->n, p->tile_n);
+        const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
+        if (p->tile_m == 128 && tiles < 256) {
+            const int32_t wanted = (int32_t)(512 / tiles), most = chunks < 8 ? 1 : chunks / 4;
+            p->per_split = ceil_div(chunks, wanted < most ? wanted : most);
+            p->splits = ceil_div(chunks, p->per_split);
+        }
+        p->pad_x = !x_pieces;
+        p->pad_w = !w_pieces;
+    }
+    const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
+    if (tiles * p->splits >= INT32_MAX / 1024) return FC_ERR_RANGE;     // (a dimension of a grid is counted in threads)
+    p->counters = p->splits == 1 ? 0 : align_up((size_t)tiles * sizeof(int32_t), 256);
+    p->at_x = p->counters;
+    p->at_w = p->at_x + (p->pad_x ? (size_t)d->rows * p->padded_k * 2 : 0);
+    p->at_part = align_up(p->at_w + (p->pad_w ? (size_t)d->n * p->padded_k * 2 : 0), 256);
+    p->workspace = p->splits == 1 ? p->at_part : p->at_part + (size_t)tiles * p->splits * p->tile_m * p->tile_n * sizeof(float);
+    return FC_OK;
+}
+
+// ---- group norm ----
+
+int32_t check_norm(const fc_group_norm_desc *d)
+{
+    if (!d) return FC_ERR_NULL;
+    if (d->images <= 0 || d->rows < 0 || d->max_rows < 0 || d->channels <= 0 || d->groups <= 0 || d->channels % d->groups) return FC_ERR_SHAPE;
+    if (d->dtype != FC_F32 && d->dtype != FC_BF16 && d->dtype != FC_F16) return FC_ERR_DTYPE;
+    if (d->activation < FC_ACT_NONE || d->activation > FC_ACT_GELU) return FC_ERR_DTYPE;
+    if (d->flags & ~(uint32_t)(FC_SKIP_ZERO_FILL | FC_WORKSPACE_READY | FC_ANY_POINTERS) || d->reserved) return FC_ERR_DTYPE;
+    if (!(d->eps >= 0.f) || !isfinite(d->eps) || d->x_row < 0 || d->out_row < d->channels) return FC_ERR_SHAPE;
+    if (d->channels > FC_LAYERS_MAX_STRIDE || d->channels / d->groups > FC_GROUP_MAX_CHANNELS) return FC_ERR_RANGE;
+    if (!stride_ok(d->x_row, 0) || !stride_ok(d->out_row, 0)) return FC_ERR_RANGE;
+    return FC_OK;
+}
+
+constexpr int kOnceGroups = 512;        // of a slice, at most
+
+int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
+{
+    const int32_t size = size_of(d->dtype), ve = 16 / size, per_group = d->channels / d->groups;
+    p->wide = !(d->flags & FC_ANY_POINTERS) && d->channels % ve == 0 && d->x_row % ve == 0 && d->out_row % ve == 0;
+    const int32_t e = p->wide ? ve : 1;         // elements of a piece
+    // the least slices: whole groups, whole pieces, 32 bytes
+    int32_t least = 1;
+    while (least < d->groups && (d->groups % least || least * per_group % e || least * per_group * size < 32)) ++least;
+    auto entries = [&](int32_t channels) { return per_group % e == 0 ? channels / e : channels; };
+    // an image's slice in the registers of a workgroup: up to 1024 threads with 16 pieces each
+    p->slice = least * per_group;
+    const int32_t pieces = p->slice / e;
+    p->once = false;
+    if (least <= kOnceGroups && pieces <= 1024) {
+        const int32_t threads[] = {256, 512, 1024};
+        for (int i = 0; i < 6 && !p->once; ++i) {
+            p->threads = threads[i % 3];
+            p->per_thread = i < 3 ? 4 : 16;
+            if (pieces > p->threads) continue;
+            const int32_t phases = p->threads / pieces;
+            p->lds = (size_t)phases * (entries(p->slice) * 8 + 4);
+            p->once = (int64_t)phases * p->per_thread >= d->max_rows && p->lds <= 60000;
+        }
+    }
+    p->chunks = p->chunk_rows = 1;
+    if (!p->once) {
+        // whole rows, or where they are longer than 4096 channels as many groups
+        int32_t of = d->groups;
+        while (of > least && ((int64_t)of * per_group > 4096 || d->groups % of || of * per_group % e)) --of;
+        p->slice = of * per_group;
+        const int32_t row_pieces = p->slice / e, phases = row_pieces < 256 ? 256 / row_pieces : 1;
+        p->lds = (size_t)phases * (entries(p->slice) * 8 + 4);
+        if (p->lds > 163840 - 256) return FC_ERR_RANGE;
+        const int64_t units = (int64_t)d->images * (d->channels / p->slice);
+        const int64_t wanted = (2048 + units - 1) / units, least_rows = (int64_t)phases * 8;
+        int64_t rows = (d->max_rows + wanted - 1) / wanted;
+        rows = (rows + least_rows - 1) / least_rows * least_rows;
+        p->chunk_rows = (int32_t)(rows < 1 ? 1 : rows);
+        p->chunks = ceil_div(d->max_rows, p->chunk_rows);
+        if (p->chunks < 1) p->chunks = 1;
+        p->threads = 256;
+    }
+    p->slices = d->channels / p->slice;
+    const int64_t units = (int64_t)d->images * p->slices;
+    if (units * p->chunks >= (1ll << 32) / 1024) return FC_ERR_RANGE;       // (a dimension of a grid is counted in threads)
+    p->counters = p->once ? 0 : align_up((size_t)units * sizeof(int32_t), 256);
+    p->at_stats = p->counters;
+    p->at_part = p->once ? 0 : align_up(p->at_stats + (size_t)d->images * d->groups * 8, 256);
+    p->workspace = p->once ? 0 : p->at_part + (size_t)d->images * p->chunks * d->groups * 12;
+    return FC_OK;
+}
+
+} // namespace
+
+extern "C" {
+
+int32_t fc_linear_workspace_bytes(const fc_linear_desc *d, size_t *bytes)
+{
+    if (!bytes) return FC_ERR_NULL;
+    int32_t rc = check_linear(d, true);
+    if (rc != FC_OK) return rc;
+    LinearPlan p;
+    rc = plan_linear(d, &p);
+    if (rc == FC_OK) *bytes = d->rows == 0 ? 0 : p.workspace;
+    return rc;
+}
+
+int32_t fc_group_norm_workspace_bytes(const fc_group_norm_desc *d, size_t *bytes)
+{
+    if (!bytes) return FC_ERR_NULL;
+    int32_t rc = check_norm(d);
+    if (rc != FC_OK) return rc;
+    NormPlan p;
+    rc = plan_norm(d, &p);
+    if (rc == FC_OK) *bytes = d->rows == 0 ? 0 : p.workspace;
+    return rc;
+}
+
+int32_t fc_linear(const fc_linear_desc *d, const void *x, const void *w, const float *bias, const void *residual, const int32_t *count,
+                  void *out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int32_t rc = check_linear(d, residual != nullptr);
+    if (rc != FC_OK) return rc;
+    const int size = size_of(d->out_dtype);
+    LinearPlan p;
+    rc = plan_linear(d, &p);
+    if (rc != FC_OK) return rc;
+    if (d->rows == 0) return FC_OK;
+    if (!x || !w || !out) return FC_ERR_NULL;
+    const uintptr_t least = d->flags & FC_ANY_POINTERS ? 2 : 16;
+    if (!aligned(x, least) || !aligned(w, least) || !aligned(out, size) || (residual && !aligned(residual, size)) || (bias && !aligned(bias, 16)) ||
+        (count && !aligned(count, 16)))
+        return FC_ERR_ALIGN;
+    if (p.workspace) {
+        if (!workspace || workspace_bytes < p.workspace) return FC_ERR_WORKSPACE;
+        if (!aligned(workspace, 16)) return FC_ERR_ALIGN;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t *const ws = static_cast<uint8_t *>(workspace);
+    LinearArgs a;
+    a.x = static_cast<const uint16_t *>(x);
+    a.w = static_cast<const uint16_t *>(w);
+    a.bias = bias;
+    a.residual = residual;
+    a.out = out;
+    a.count = count;
+    a.rows = d->rows; a.n = d->n; a.k = d->k; a.act = d->activation;
+    a.residual_first = (d->flags & FC_RESIDUAL_FIRST) != 0;
+    a.wide_out = d->n % 8 == 0 && aligned(out, 16) && d->out_row * size % 16 == 0 && (!residual || (aligned(residual, 16) && d->residual_row * size % 16 == 0));
+    a.x_row = d->x_row; a.w_row = d->w_row; a.residual_row = d->residual_row; a.out_row = d->out_row;
+    a.n_tiles = p.n_tiles; a.splits = p.splits; a.per_split = p.per_split; a.per_wave = p.per_wave;
+    a.part = reinterpret_cast<float *>(ws + p.at_part);
+    a.arrived = reinterpret_cast<int32_t *>(ws);
+    hipError_t e = hipSuccess;
+    if (p.counters && !(d->flags & FC_WORKSPACE_READY)) e = launch_zero_i32(a.arrived, p.m_tiles * p.n_tiles, s);
+    if (e == hipSuccess && (p.pad_x || p.pad_w)) {
+        uint16_t *const px = p.pad_x ? reinterpret_cast<uint16_t *>(ws + p.at_x) : nullptr, *const pw = p.pad_w ? reinterpret_cast<uint16_t *>(ws + p.at_w) : nullptr;
+        e = launch_linear_pad(a, p, px, pw, s);
+        if (px) a.x = px, a.x_row = p.padded_k;
+        if (pw) a.w = pw, a.w_row = p.padded_k;
+        if (px && pw) a.k = (int32_t)p.padded_k;
+    }
+    if (e == hipSuccess) e = p.form == 0 ? launch_linear_rows(a, p, d->dtype, d->out_dtype, s) : launch_linear_tile(a, p, d->dtype, d->out_dtype, s);
+    return e == hipSuccess ? FC_OK : FC_ERR_HIP;
+}
+
+int32_t fc_group_norm(const fc_group_norm_desc *d, const void *x, const float *weight, const float *bias, const uint8_t *mask,
+                      const int32_t *starts, void *out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int32_t rc = check_norm(d);
+    if (rc != FC_OK) return rc;
+    if (!starts && (int64_t)d->images * d->max_rows != d->rows) return FC_ERR_SHAPE;
+    NormPlan p;
+    rc = plan_norm(d, &p);
+    if (rc != FC_OK) return rc;
+    if (d->rows == 0 || d->max_rows == 0) return FC_OK;
+    if (!x || !out) return FC_ERR_NULL;
+    const uintptr_t least = d->flags & FC_ANY_POINTERS ? size_of(d->dtype) : 16;
+    if (!aligned(x, least) || !aligned(out, least) || (weight && !aligned(weight, 16)) || (bias && !aligned(bias, 16)) || (mask && !aligned(mask, 16)) ||
+        (starts && !aligned(starts, 16)))
+        return FC_ERR_ALIGN;
+    if (p.workspace) {
+        if (!workspace || workspace_bytes < p.workspace) return FC_ERR_WORKSPACE;
+        if (!aligned(workspace, 16)) return FC_ERR_ALIGN;
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t *const ws = static_cast<uint8_t *>(workspace);
+    NormArgs a;
+    a.x = x; a.out = out; a.weight = weight; a.bias = bias; a.mask = mask; a.starts = starts;
+    a.images = d->images; a.rows = d->rows; a.max_rows = d->max_rows; a.channels = d->channels; a.groups = d->groups;
+    a.per_group = d->channels / d->groups;
+    a.act = d->activation;
+    a.keep_out = (d->flags & FC_SKIP_ZERO_FILL) != 0;
+    a.eps = d->eps;
+    a.x_row = d->x_row; a.out_row = d->out_row;
+    a.slices = p.slices; a.slice = p.slice; a.chunks = p.chunks; a.chunk_rows = p.chunk_rows;
+    a.arrived = reinterpret_cast<int32_t *>(ws);
+    a.stats = reinterpret_cast<float2 *>(ws + p.at_stats);
+    a.part = reinterpret_cast<float *>(ws + p.at_part);
+    hipError_t e = hipSuccess;
+    if (p.counters && !(d->flags & FC_WORKSPACE_READY)) e = launch_zero_i32(a.arrived, d->images * p.slices, s);
+    if (e == hipSuccess) e = launch_group_norm(a, p, d->dtype, s);
+    return e == hipSuccess ? FC_OK : FC_ERR_HIP;
+}
+
+} // extern "C"

@@ -1,0 +1,172 @@
+"""Group norm of channels-last rows against its definition in 64 bits."""
+import pytest
+import torch
+
+from paper_2207_10741_amd import layers as L
+from tests import layers_oracle as O
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+ACTS = [None, "relu", "silu", "gelu"]
+
+
+def _normal(shape, dtype, seed, scale=1.0, shift=0.0):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).mul_(scale).add_(shift).to(dtype).to(DEV)
+
+
+def _check_images(x, got, groups, weight, bias, masks, activation, eps=1e-5):
+    """x, got: lists of an image's rows"""
+    for b, (rows, out) in enumerate(zip(x, got)):
+        want, error = O.group_norm(rows, groups, weight, bias, None if masks is None else masks[b], eps, activation)
+        O.check(out, want, error, "image %d" % b)
+
+
+# images of one row and of many, groups of one channel and of all, channels off the pieces of 16 bytes; the last ones do not fit a workgroup
+SIZES = [(1, 1, 8, 1), (2, 1, 64, 64), (1, 5, 3, 3), (3, 17, 32, 8), (2, 64, 60, 4), (1, 256, 512, 32), (2, 100, 515, 5), (4, 33, 96, 1), (1, 7, 1280, 32),
+         (2, 3, 4096, 1), (1, 2, 16384, 1), (1, 3, 9000, 1), (2, 2, 10002, 2), (1, 5000, 64, 32), (2, 9001, 128, 32), (1, 20000, 24, 3), (3, 4099, 60, 4), (1, 3000, 515, 5), (1, 40, 12288, 4),
+         (1, 2500, 40, 40), (1, 1100, 4098, 2), (1, 300, 16380, 3)]
+
+
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "%dx%dx%d-%d" % s)
+@pytest.mark.parametrize("dtype", [BF16, F16, F32], ids=["bf16", "f16", "f32"])
+def test_sizes(size, dtype):
+    images, rows, channels, groups = size
+    x = _normal((images, rows, channels), dtype, rows + channels, 1.5, 0.7)
+    weight = _normal((channels,), F32, 1, 0.3, 1.0) if channels % 2 else None
+    bias = _normal((channels,), F32, 2) if rows % 2 else None
+    act = ACTS[(rows + channels) % 4]
+    got = L.group_norm(x, groups, weight, bias, activation=act)
+    _check_images(x, got, groups, weight, bias, None, act)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,channels,groups", [(50, 64, 8), (50, 60, 4), (12000, 64, 8), (7000, 60, 4)])
+def test_masks(dtype, rows, channels, groups):
+    images = 5
+    x = _normal((images, rows, channels), dtype, 3)
+    gen = torch.Generator().manual_seed(4)
+    mask = torch.rand((images, rows), generator=gen) < 0.4
+    mask[1] = False                     # an image without a relevant row
+    mask[2] = False
+    mask[2, rows - 1] = True            # with one
+    mask[3] = True
+    dirty = x.clone()
+    dirty[~mask.to(DEV)] = float("nan")
+    byte = mask.to(torch.uint8).mul_(255).to(DEV)
+    weight, bias = _normal((channels,), F32, 1), _normal((channels,), F32, 2)
+    got = L.group_norm(dirty, groups, weight, bias, mask=byte, activation="gelu")
+    _check_images(x, got, groups, weight, bias, mask, "gelu")
+    assert not bool(got[~mask.to(DEV)].any()) and not bool(torch.signbit(got[~mask.to(DEV)]).any())
+    out = torch.full_like(x, 9.0)
+    L.group_norm(dirty, groups, weight, bias, mask=byte, activation="gelu", out=out, keep_out=True)
+    assert bool((out[~mask.to(DEV)] == 9).all()) and torch.equal(out[mask.to(DEV)], got[mask.to(DEV)])
+
+
+@pytest.mark.parametrize("channels,groups", [(64, 8), (60, 4)])
+@pytest.mark.parametrize("counts", [[5], [1, 0, 40, 3], [3000, 1, 0, 9000], [0, 0]])
+def test_images_of_different_sizes(channels, groups, counts):
+    ends = torch.tensor([2] + counts).cumsum(0)     # rows that belong to no image at both ends
+    x = _normal((int(ends[-1]) + 3, channels), F16, 5, 2.0, -1.0)
+    starts = ends.to(torch.int32).to(DEV)
+    for most in (None, max(max(counts), 1)):
+        out = torch.full_like(x, 4.0)
+        L.group_norm(x, groups, starts=starts, max_rows=most, activation="silu", out=out)
+        for b in range(len(counts)):
+            rows = slice(int(ends[b]), int(ends[b + 1]))
+            want, error = O.group_norm(x[rows], groups, activation="silu")
+            O.check(out[rows], want, error, "image %d" % b)
+        assert bool((out[:2] == 4).all()) and bool((out[int(ends[-1]):] == 4).all())
+
+
+def test_starts_beyond_the_bounds_are_cut_off():
+    x = _normal((30, 32), F32, 5)
+    out = torch.full_like(x, 4.0)
+    starts = torch.tensor([-5, 10, 2 ** 30, 7, 2 ** 31 - 1], dtype=torch.int32, device=DEV)     # 0 .. 10, 10 .. 30, nothing, 7 .. 30
+    L.group_norm(x, 4, starts=starts[:3], max_rows=8, out=out)
+    for rows in (slice(0, 8), slice(10, 18)):
+        want, error = O.group_norm(x[rows], 4)
+        O.check(out[rows], want, error)
+    assert bool((out[8:10] == 4).all()) and bool((out[18:] == 4).all())
+    L.group_norm(x, 4, starts=starts[2:].clone(), out=out)      # (a slice is not aligned to 16 bytes)
+    want, error = O.group_norm(x[7:], 4)
+    O.check(out[7:], want, error)
+
+
+@pytest.mark.parametrize("rows", [40, 9000])
+@pytest.mark.parametrize("dtype", [F32, F16], ids=["f32", "f16"])
+def test_a_mean_far_from_zero(rows, dtype):
+    x = _normal((2, rows, 32), dtype, 6, 0.5, 1000.0 if dtype == F32 else 100.0)
+    got = L.group_norm(x, 4)
+    _check_images(x, got, 4, None, None, None, None)
+
+
+@pytest.mark.parametrize("rows", [30, 9000])
+def test_equal_values_and_eps(rows):
+    x = torch.full((1, rows, 16), 3.25, dtype=F32, device=DEV)
+    bias = _normal((16,), F32, 1)
+    assert torch.equal(L.group_norm(x, 2, bias=bias)[0], bias.expand(rows, 16))
+    y = _normal((1, rows, 16), F32, 2, 1e-3)
+    got = L.group_norm(y, 2, eps=0.25)
+    _check_images(y, got, 2, None, None, None, None, 0.25)
+
+
+@pytest.mark.parametrize("rows", [30, 9000])
+def test_not_finite_values_stay_in_their_group(rows):
+    x = _normal((2, rows, 32), BF16, 3)
+    x[0, rows // 2, 9] = float("nan")
+    x[1, 1, 31] = float("inf")
+    got = L.group_norm(x, 4).float()
+    bad = torch.zeros((2, 4), dtype=torch.bool, device=DEV)
+    bad[0, 1] = bad[1, 3] = True
+    assert torch.equal(torch.isnan(got.view(2, rows, 4, 8)), bad[:, None, :, None].expand(2, rows, 4, 8))
+
+
+@pytest.mark.parametrize("rows", [20, 9000])
+@pytest.mark.parametrize("offset,extra", [(0, 8), (8, 8), (1, 7), (3, 0)])
+def test_strides(rows, offset, extra):
+    channels = 48
+    x = _normal((2, rows, offset + channels + extra), BF16, 3)[:, :, offset:offset + channels]
+    big = torch.full((2, rows, offset + channels + extra + 1), 7.0, dtype=BF16, device=DEV)
+    out = big[:, :, offset:offset + channels]
+    L.group_norm(x, 6, activation="relu", out=out)
+    _check_images(x, out, 6, None, None, None, "relu")
+    assert bool((big[:, :, :offset] == 7).all()) and bool((big[:, :, offset + channels:] == 7).all())
+
+
+@pytest.mark.parametrize("rows", [20, 9000])
+def test_in_place(rows):
+    x = _normal((2, rows, 64), F16, 3)
+    want = L.group_norm(x, 8, activation="silu")
+    assert L.group_norm(x, 8, activation="silu", out=x) is x and torch.equal(x, want)
+
+
+def test_four_dimensions_and_nothing():
+    x = _normal((2, 6, 9, 32), BF16, 3)
+    got = L.group_norm(x, 4)
+    assert got.shape == x.shape and torch.equal(got.view(2, 54, 32), L.group_norm(x.view(2, 54, 32), 4))
+    assert L.group_norm(x[:0], 4).shape == (0, 6, 9, 32)
+    assert L.group_norm(x[:, :0], 4).shape == (2, 0, 9, 32)
+
+
+@pytest.mark.parametrize("rows", [64, 20000])
+def test_captured_and_on_another_stream(rows):
+    x = _normal((2, rows, 64), BF16, 3)
+    call, other = L.PreparedGroupNorm(x, 8, activation="silu"), L.PreparedGroupNorm(x, 8)
+    eager, eager_other = call().clone(), other().clone()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        got = call()
+    for _ in range(4):
+        got.zero_()
+        graph.replay()
+        assert torch.equal(other(), eager_other)
+        torch.cuda.synchronize()
+        assert torch.equal(got, eager)
+        x.copy_(x.flip(2))
+        eager, eager_other = L.group_norm(x, 8, activation="silu").clone(), L.group_norm(x, 8).clone()
+    side.wait_stream(torch.cuda.current_stream())
+    out = L.group_norm(x, 8, activation="silu", stream=side)
+    side.synchronize()
+    assert torch.equal(out, eager)

@@ -76,6 +76,12 @@ template <typename T> __device__ __forceinline__ uint4 pack8(const float (&v)[8]
 {
     return make_uint4(pack2_of(T{}, v[0], v[1]), pack2_of(T{}, v[2], v[3]), pack2_of(T{}, v[4], v[5]), pack2_of(T{}, v[6], v[7]));
 }
+__device__ __forceinline__ f32x4_t load4_float(const float *p) { return *reinterpret_cast<const f32x4_t *>(p); }
+template <typename T> __device__ __forceinline__ f32x4_t load4_float(const T *p)
+{
+    const uint2 x = *reinterpret_cast<const uint2 *>(p);
+    return f32x4_t{to_float(T{(uint16_t)x.x}), to_float(T{(uint16_t)(x.x >> 16)}), to_float(T{(uint16_t)x.y}), to_float(T{(uint16_t)(x.y >> 16)})};
+}
 __device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
     *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
@@ -108,41 +114,29 @@ __device__ __forceinline__ int32_t rows_there(const LinearArgs &a)
     return a.count ? min(max(__builtin_amdgcn_readfirstlane(*a.count), 0), a.rows) : a.rows;
 }
 
-// N columns c .. of row r: bias, residual, activation, one rounding.  v: the sums.
-template <typename TO, int N> __device__ __forceinline__ void finish_columns(const LinearArgs &a, int64_t row, int c, float (&v)[N])
+// A column of a row: bias, residual, activation, one rounding.  v: the sum.
+template <typename TO> __device__ __forceinline__ void finish_one(const LinearArgs &a, int64_t row, int c, float v)
 {
-    TO *const to = static_cast<TO *>(a.out) + row * a.out_row + c;
-    const TO *const from = static_cast<const TO *>(a.residual) + row * a.residual_row + c;
-    if constexpr (N == 8) {
-        if (a.wide_out) {       // (whole pieces: c < n is c + 7 < n)
-            float more[8];
-            if (a.bias) {
-                load8_float(a.bias + c, more);
+    float y = v + (a.bias ? a.bias[c] : 0.f);
+    const float more = a.residual ? to_float(static_cast<const TO *>(a.residual)[row * a.residual_row + c]) : 0.f;
+    if (a.residual_first) y += more;
+    y = activate(y, a.act);
+    if (!a.residual_first) y += more;
+    from_float(y, static_cast<TO *>(a.out) + row * a.out_row + c);
+}
+// Eight columns of a row, before the rounding.  more: the residual's, where there is one.
+__device__ __forceinline__ void finish_eight(const LinearArgs &a, const float (&bias)[8], const float (&more)[8], float (&v)[8])
+{
+    const bool first = a.residual && a.residual_first, after = a.residual && !a.residual_first;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += more[i];
-            }
-            if (a.residual) load8_float(from, more);
-            if (a.residual && a.residual_first)
+    for (int i = 0; i < 8; ++i) v[i] += bias[i];
+    if (first)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += more[i];
-            activate_all(v, a.act);
-            if (a.residual && !a.residual_first)
+        for (int i = 0; i < 8; ++i) v[i] += more[i];
+    activate_all(v, a.act);
+    if (after)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += more[i];
-            store8(to, v);
-            return;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-        if (c + i < a.n) {
-            float y = v[i] + (a.bias ? a.bias[c + i] : 0.f);
-            const float more = a.residual ? to_float(from[i]) : 0.f;
-            if (a.residual_first) y += more;
-            y = activate(y, a.act);
-            if (!a.residual_first) y += more;
-            from_float(y, to + i);
-        }
+        for (int i = 0; i < 8; ++i) v[i] += more[i];
 }
 
 // Pieces of a tile that were written past the caches by workgroups of any XCD; the workgroup that comes last adds them in their order.

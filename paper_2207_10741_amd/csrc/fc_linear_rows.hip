@@ -128,8 +128,9 @@ void k_linear_rows(LinearArgs a)
     auto finish = [&](int item, f32x4_t v) __attribute__((always_inline)) {
         const int l = item & 63, block = item >> 6, row = r0 + block / NB * 16 + (l & 15), col = n0 + block % NB * 16 + (l >> 4) * 4;
         if (row >= rows || col >= a.n) return;
-        float y[4] = {v[0], v[1], v[2], v[3]};
-        finish_columns<TO, 4>(a, row, col, y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < a.n) finish_one<TO>(a, row, col + i, v[i]);
     };
     __amdgpu_buffer_rsrc_t part;
     if (a.splits > 1)

@@ -21,20 +21,20 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F &
     }
 }
 
-template <int WM, int WN, int PB> constexpr size_t kTileLds = (size_t)2 * (WM * PB * 32 + WN * 64) * 128 + 16;
+// three stages' rows of x, two stages' rows of w
+template <int WM, int WN, int PB, int CB> constexpr size_t kTileLds = (size_t)(3 * WM * PB + 2 * WN * CB) * 32 * 128;
 
-template <int DT, typename TO, int WM, int WN, int PB>
-__global__ __launch_bounds__(WM * WN * 64, 2)
+template <int DT, typename TO, int WM, int WN, int PB, int CB>
+__global__ __launch_bounds__(WM * WN * 64, CB == 4 ? 1 : 2)
 void k_linear_tile(LinearArgs a)
 {
-    constexpr int NT = WM * WN * 64, CB = 2, TM = WM * PB * 32, TN = WN * CB * 32;
+    constexpr int NT = WM * WN * 64, TM = WM * PB * 32, TN = WN * CB * 32;
     constexpr int RPL = NT / 8;                     // rows that the waves' loads cover side by side
     constexpr int XL = TM / RPL, WL = TN / RPL, KK = 4;
-    constexpr uint32_t XB = TM * 128u, SB = (TM + TN) * 128u;      // a stage: rows of x, then of w
+    constexpr uint32_t XB = TM * 128u, WB = TN * 128u, W0 = 3 * XB;     // a stage's rows of x, of w; where the latter begin
     static_assert(TM % RPL == 0 && TN % RPL == 0 && RPL % 16 == 0, "whole loads; the exchange is the same for all of a lane's rows");
 
     extern __shared__ __align__(16) unsigned char smem_raw[];
-    int32_t *const flag = reinterpret_cast<int32_t *>(smem_raw + 2 * SB);
     const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(smem_raw);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_m = wave % WM, wave_n = wave / WM;
@@ -70,24 +70,28 @@ void k_linear_tile(LinearArgs a)
     }
     const int k0 = split * a.per_split * kLinearK, stages = min(a.per_split, (a.k - k0 + kLinearK - 1) / kLinearK);
     const int k_end = min(a.k, k0 + stages * kLinearK);
-    // the next stage to be sent for (behind the last one: zeros)
-    int ld_k = k0;
-    uint32_t ld_s = 0;
-    bool ld_ok = false;
-    auto next_stage = [&]() __attribute__((always_inline)) {
-        ld_ok = ld_k + piece * 8 < k_end;
-        ld_s = ld_k < k_end ? (uint32_t)ld_k * 2u : 0u;
-        ld_k += kLinearK;
+    // the next stages to be sent for (behind the last one: zeros)
+    struct Next {
+        int k;
+        uint32_t s;
+        bool ok;
+    } nx = {k0, 0, false}, nw = {k0, 0, false};
+    auto advance = [&](Next &n) __attribute__((always_inline)) {
+        n.ok = n.k + piece * 8 < k_end;
+        n.s = n.k < k_end ? (uint32_t)n.k * 2u : 0u;
+        n.k += kLinearK;
     };
     const uint32_t lds_wave = lds0 + (uint32_t)wave * 1024u;
-    auto issue = [&](int j, uint32_t buf) __attribute__((always_inline)) {
-        if (j < XL) dma_load16_any(rsrc_x, ld_ok ? xo[j] : kOutOfRange, ld_s, lds_wave + buf * SB + (uint32_t)j * (RPL * 128u));
-        else dma_load16_any(rsrc_w, ld_ok ? wo[j - XL] : kOutOfRange, ld_s, lds_wave + buf * SB + XB + (uint32_t)(j - XL) * (RPL * 128u));
+    auto issue_x = [&](int j, uint32_t buf) __attribute__((always_inline)) {
+        dma_load16_any(rsrc_x, nx.ok ? xo[j] : kOutOfRange, nx.s, lds_wave + buf * XB + (uint32_t)j * (RPL * 128u));
+    };
+    auto issue_w = [&](int j, uint32_t buf) __attribute__((always_inline)) {
+        dma_load16_any(rsrc_w, nw.ok ? wo[j] : kOutOfRange, nw.s, lds_wave + W0 + buf * WB + (uint32_t)j * (RPL * 128u));
     };
 
     // where this lane's fragments are: row of the block, half of the k-step
     const uint32_t frow = (uint32_t)(lane & 31);
-    const uint32_t fx = (uint32_t)(wave_m * (PB * 32)) * 128u + frow * 128u, fw = XB + (uint32_t)(wave_n * (CB * 32)) * 128u + frow * 128u;
+    const uint32_t fx = (uint32_t)(wave_m * (PB * 32)) * 128u + frow * 128u, fw = W0 + (uint32_t)(wave_n * (CB * 32)) * 128u + frow * 128u;
     const uint32_t ft = (uint32_t)((lane >> 5) ^ FC_SWZ(frow)) * 16u;       // (blocks begin at multiples of 32 rows: the exchange is the row's in the block)
 
     f32x16_t acc[PB][CB];
@@ -98,67 +102,88 @@ void k_linear_tile(LinearArgs a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[p][b][i] = 0.f;
 
-    next_stage();
+    constexpr int NM = PB * CB, NR = PB + CB, NS = KK * NM;     // products and fragment reads of a k-step; products of a stage
+    constexpr int BAR = NM / 4, BARRIER = (KK - 1) * NM + BAR;  // the barrier of a stage stands before this product of its last k-step, of the stage
+    // From barrier to barrier the loads of the next stage's rows of w and then of the stage after next's rows of x go out at even distances: sent for in one
+    // go they wait for each other, and the products behind them for the loads.
+    constexpr int NL = XL + WL;
+    auto issue_at = [&](auto q_c, uint32_t xbuf, uint32_t wbuf) __attribute__((always_inline)) {
+        constexpr int q = decltype(q_c)::value, first = (q * NL + NS - 1) / NS, behind = ((q + 1) * NL + NS - 1) / NS;
+        each<behind - first>([&](auto e_c) __attribute__((always_inline)) {
+            constexpr int l = first + decltype(e_c)::value;
+            if constexpr (l < WL) issue_w(l, wbuf);
+            else issue_x(l - WL, xbuf);
+        });
+    };
+
+    advance(nx);
+    advance(nw);
 #pragma unroll
-    for (int j = 0; j < XL + WL; ++j) issue(j, 0);
-    next_stage();
+    for (int j = 0; j < XL; ++j) issue_x(j, 0);
 #pragma unroll
-    for (int j = 0; j < XL + WL; ++j) issue(j, 1);
-    wait_vmcnt<XL + WL>();
+    for (int j = 0; j < WL; ++j) issue_w(j, 0);
+    advance(nx);
+#pragma unroll
+    for (int j = 0; j < XL; ++j) issue_x(j, 1);
+    wait_vmcnt<XL>();
     __syncthreads();
+    advance(nx);
+    advance(nw);
+    each<NS - BARRIER>([&](auto q_c) __attribute__((always_inline)) { issue_at(q_c, 2, 1); });
 
     Frag<DT> wf[2][CB], xf[2][PB];
-    constexpr int NM = PB * CB, NR = PB + CB, NL = XL + WL;
     // fragment r of a k-step, in the order the products need them: w0, x0, w1, x1 ..
-    auto read_frag = [&](int r, int set, uint32_t buf, int kk) __attribute__((always_inline)) {
-        const uint32_t o = buf * SB + (((uint32_t)kk * 32u) ^ ft);
+    auto read_frag = [&](int r, int set, uint32_t xbuf, uint32_t wbuf, int kk) __attribute__((always_inline)) {
+        const uint32_t o = ((uint32_t)kk * 32u) ^ ft;
         if (r == 1 || r > CB) {
             const int p = r == 1 ? 0 : r - CB;
-            xf[set][p].load(smem_raw, o + fx + (uint32_t)p * 4096u);
+            xf[set][p].load(smem_raw, o + fx + xbuf * XB + (uint32_t)p * 4096u);
         } else {
             const int b = r == 0 ? 0 : r - 1;
-            wf[set][b].load(smem_raw, o + fw + (uint32_t)b * 4096u);
+            wf[set][b].load(smem_raw, o + fw + wbuf * WB + (uint32_t)b * 4096u);
         }
     };
 #pragma unroll
-    for (int r = 0; r < NR; ++r) read_frag(r, 0, 0, 0);
-    auto stage = [&](auto buf_c) __attribute__((always_inline)) {
-        constexpr uint32_t BUF = decltype(buf_c)::value;
+    for (int r = 0; r < NR; ++r) read_frag(r, 0, 0, 0, 0);
+    // stage N of six (three buffers of rows of x, two of w)
+    auto stage = [&](auto n_c) __attribute__((always_inline)) {
+        constexpr uint32_t N = decltype(n_c)::value, X = N % 3, W = N % 2;
         each<KK>([&](auto kk_c) __attribute__((always_inline)) {
             constexpr int kk = decltype(kk_c)::value;
             constexpr bool last = kk == KK - 1;
-            constexpr int BAR = NM / 4, from = last ? BAR : 0, gaps = NM - from, nl = last ? NL : 0;
+            constexpr int from = last ? BAR : 0, gaps = NM - from;
             each<NM>([&](auto i_c) __attribute__((always_inline)) {
-                constexpr int i = decltype(i_c)::value;
-                if constexpr (last && i == BAR) {       // the next stage has landed, everyone has read this one
+                constexpr int i = decltype(i_c)::value, t = kk * NM + i;
+                if constexpr (t == BARRIER) {       // the next stage has landed (its rows of x before the ones still on their way), everyone has read this one
                     lds_reads_done();
-                    wait_vmcnt<0>();
+                    wait_vmcnt<XL>();
                     __syncthreads();
-                    next_stage();
+                    advance(nx);
+                    advance(nw);
                 }
                 acc[i / CB][i % CB] = mfma32<DT>(wf[kk & 1][i % CB], xf[kk & 1][i / CB], acc[i / CB][i % CB]);
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (i >= from) {
-                    constexpr int j = i - from;         // this gap's share of the reads and loads
+                    constexpr int j = i - from;         // this gap's share of the reads
                     each<((j + 1) * NR + gaps - 1) / gaps - (j * NR + gaps - 1) / gaps>([&](auto e_c) __attribute__((always_inline)) {
                         constexpr int r = (j * NR + gaps - 1) / gaps + decltype(e_c)::value;
                         if constexpr (r < NR) {
-                            if constexpr (last) read_frag(r, 0, BUF ^ 1u, 0);
-                            else read_frag(r, (kk + 1) & 1, BUF, kk + 1);
+                            if constexpr (last) read_frag(r, 0, (X + 1) % 3, W ^ 1u, 0);
+                            else read_frag(r, (kk + 1) & 1, X, W, kk + 1);
                         }
                     });
-                    each<((j + 1) * nl) / gaps - (j * nl) / gaps>([&](auto e_c) __attribute__((always_inline)) {
-                        issue((j * nl) / gaps + decltype(e_c)::value, BUF);
-                    });
-                    __builtin_amdgcn_sched_barrier(0);
                 }
+                // (what goes out before the barrier belongs to the last one: stages one and two ahead of this)
+                if constexpr (t >= BARRIER) issue_at(std::integral_constant<int, t - BARRIER>{}, X, W);
+                else issue_at(std::integral_constant<int, t + NS - BARRIER>{}, (X + 2) % 3, W ^ 1u);
+                __builtin_amdgcn_sched_barrier(0);
             });
         });
     };
-    for (int s = 0; s < stages; s += 2) {
-        stage(std::integral_constant<uint32_t, 0>{});
-        if (s + 1 < stages) stage(std::integral_constant<uint32_t, 1>{});
-    }
+    for (int s = 0; s < stages; s += 6)
+        each<6>([&](auto n_c) __attribute__((always_inline)) {
+            if (s + decltype(n_c)::value < stages) stage(n_c);
+        });
     lds_reads_done();
     wait_vmcnt<0>();
     __syncthreads();
@@ -173,7 +198,8 @@ void k_linear_tile(LinearArgs a)
             const f32x4_t v = {s[q], s[q + 1], s[q + 2], s[q + 3]};
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), part, ((uint32_t)split * ITEMS + (uint32_t)i * NT + threadIdx.x) * 16u, 0, kPiecesPastCaches);
         });
-        if (!last_piece(a.arrived + tile, a.splits, flag)) return;
+        if (!last_piece(a.arrived + tile, a.splits, reinterpret_cast<int32_t *>(smem_raw))) return;
+        __syncthreads();
 #pragma unroll
         for (int p = 0; p < PB; ++p)
 #pragma unroll
@@ -189,30 +215,123 @@ void k_linear_tile(LinearArgs a)
             });
     }
 
-    // ---- epilogue: every wave turns its blocks of 32 rows x 64 columns through LDS of its own, so that a lane has eight columns next to each other ----
-    constexpr int OP = CB * 32 + 4;     // floats from row to row
-    static_assert((size_t)WM * WN * 32 * OP * 4 <= 2 * SB, "the waves' shares");
-    float *const os = reinterpret_cast<float *>(smem_raw) + wave * (32 * OP);
-    const int c8 = lane & 7, col = n0 + wave_n * (CB * 32) + c8 * 8;
+    // ---- epilogue: a wave's blocks of 32 rows go through LDS of its own ----
+    // (Sums of 256 registers are accumulators of the matrix instructions; left to itself the compiler copies all of them out at once and spills.  They stay
+    // until they are asked for.)
+    auto sums_of = [&](auto p_c, auto b_c) __attribute__((always_inline)) -> f32x16_t {
+        f32x16_t &s = acc[decltype(p_c)::value][decltype(b_c)::value];
+        if constexpr (CB == 4) __asm__ volatile("" : "+a"(s));
+        return s;
+    };
+    const int col0 = n0 + wave_n * (CB * 32), half = lane >> 5;
+    if (a.wide_out && a.act <= FC_ACT_RELU) {
+        // In the registers' order (a lane: a row, fours of columns): residuals come in and results go out in 16-byte pieces of rows.
+        constexpr int PPR = CB * 32 * (int)sizeof(TO) / 16, RPI = 64 / PPR, NI = 32 / RPI;    // pieces a row, rows a round, rounds
+        constexpr uint32_t OP = CB * 32 * sizeof(TO) + 16;
+        static_assert((size_t)WM * WN * 32 * OP <= kTileLds<WM, WN, PB, CB>, "the waves' shares");
+        unsigned char *const os = smem_raw + wave * (32 * OP), *const mine = os + (lane & 31) * OP + half * (4 * sizeof(TO));
+        constexpr int EPP = 16 / (int)sizeof(TO);
+        const int prow = lane / PPR, pcol = col0 + lane % PPR * EPP;
+        unsigned char *const piece_at = os + prow * OP + lane % PPR * 16;
+        f32x4_t bias[CB * 4];
+        each<CB * 4>([&](auto i_c) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_c)::value;
+            const int c = col0 + i * 8 + half * 4;
+            bias[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (a.bias && c < a.n) bias[i] = *reinterpret_cast<const f32x4_t *>(a.bias + c);
+        });
+        each<PB>([&](auto p_c) __attribute__((always_inline)) {
+            constexpr int p = decltype(p_c)::value;
+            const int row0 = r0 + (wave_m * PB + p) * 32 + prow;
+            if (a.residual) {
+                const TO *from = static_cast<const TO *>(a.residual) + pcol;
+                uint4 more[NI];
 #pragma unroll
-    for (int p = 0; p < PB; ++p) {
+                for (int i = 0; i < NI; ++i) {
+                    more[i] = make_uint4(0, 0, 0, 0);
+                    if (row0 + i * RPI < rows && pcol < a.n) more[i] = *reinterpret_cast<const uint4 *>(from + (int64_t)(row0 + i * RPI) * a.residual_row);
+                }
 #pragma unroll
-        for (int b = 0; b < CB; ++b)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4_t v = {acc[p][b][q * 4], acc[p][b][q * 4 + 1], acc[p][b][q * 4 + 2], acc[p][b][q * 4 + 3]};
-                *reinterpret_cast<f32x4_t *>(os + (lane & 31) * OP + b * 32 + q * 8 + (lane >> 5) * 4) = v;
+                for (int i = 0; i < NI; ++i) *reinterpret_cast<uint4 *>(piece_at + i * RPI * OP) = more[i];
+                wave_lds_order();
             }
-        wave_lds_order();
+            const bool relu_first = a.act == FC_ACT_RELU && !a.residual_first, relu_last = a.act == FC_ACT_RELU && a.residual_first;
+            each<CB * 4>([&](auto i_c) __attribute__((always_inline)) {
+                constexpr int i = decltype(i_c)::value, q = i % 4 * 4;
+                const f32x16_t s = sums_of(p_c, std::integral_constant<int, i / 4>{});
+                f32x4_t v = f32x4_t{s[q], s[q + 1], s[q + 2], s[q + 3]} + bias[i];
+                TO *const at = reinterpret_cast<TO *>(mine) + i * 8;
+                if (relu_first)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = i * 8 + (lane >> 3), row = r0 + (wave_m * PB + p) * 32 + r;
-            float v[8];
-            load8_float(os + r * OP + c8 * 8, v);
-            if (row < rows && col < a.n) finish_columns<TO, 8>(a, row, col, v);
+                    for (int j = 0; j < 4; ++j) v[j] = relu_keep_nan(v[j]);
+                if (a.residual) v += load4_float(at);
+                if (relu_last)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = relu_keep_nan(v[j]);
+                store4<DT, TO>(at, v[0], v[1], v[2], v[3]);
+                if constexpr (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (the compiler would copy all sums out of the accumulators first)
+            });
+            wave_lds_order();
+            uint4 done[NI];
+#pragma unroll
+            for (int i = 0; i < NI; ++i) done[i] = *reinterpret_cast<const uint4 *>(piece_at + i * RPI * OP);
+            TO *to = static_cast<TO *>(a.out) + pcol;
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+                if (row0 + i * RPI < rows && pcol < a.n) *reinterpret_cast<uint4 *>(to + (int64_t)(row0 + i * RPI) * a.out_row) = done[i];
+            wave_lds_order();
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        return;
+    }
+    // Activations with more arithmetic, and rows of any alignment: the sums go through LDS, and loops that are not unrolled finish them.
+    constexpr int LPR = CB * 4, RPI = 64 / LPR;      // lanes a row, rows a round, of eight columns
+    const int c8 = lane % LPR, col8 = col0 + c8 * 8;
+    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.wide_out && a.bias && col8 < a.n) load8_float(a.bias + col8, bias);
+    constexpr int OP = CB * 32 + 4;     // floats from row to row
+    static_assert((size_t)WM * WN * 32 * OP * 4 <= kTileLds<WM, WN, PB, CB>, "the waves' shares");
+    float *const os = reinterpret_cast<float *>(smem_raw) + wave * (32 * OP);
+    // (A loop over p that is not unrolled would put the sums into memory.)
+    each<PB>([&](auto p_c) __attribute__((always_inline)) {
+        constexpr int p = decltype(p_c)::value;
+        each<CB>([&](auto b_c) __attribute__((always_inline)) {
+            const f32x16_t s = sums_of(p_c, b_c);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4_t *>(os + (lane & 31) * OP + decltype(b_c)::value * 32 + q * 8 + half * 4) = f32x4_t{s[q * 4], s[q * 4 + 1], s[q * 4 + 2], s[q * 4 + 3]};
+        });
+        wave_lds_order();
+        const int row0 = r0 + (wave_m * PB + p) * 32, here = min(rows - row0, 32);
+        if (a.wide_out) {
+            // two rows' residuals are sent for together
+            constexpr int AT_ONCE = 2;
+#pragma unroll 1
+            for (int i = 0; i < 32 / RPI; i += AT_ONCE) {
+                float more[AT_ONCE][8];
+                if (a.residual)
+#pragma unroll
+                    for (int u = 0; u < AT_ONCE; ++u) {
+                        const int row = min(row0 + (i + u) * RPI + lane / LPR, rows - 1);
+                        load8_float(static_cast<const TO *>(a.residual) + row * a.residual_row + (col8 < a.n ? col8 : 0), more[u]);
+                    }
+#pragma unroll
+                for (int u = 0; u < AT_ONCE; ++u) {
+                    const int r = (i + u) * RPI + lane / LPR, row = row0 + r;
+                    float v[8];
+                    load8_float(os + r * OP + c8 * 8, v);
+                    finish_eight(a, bias, more[u], v);
+                    if (row < rows && col8 < a.n) store8(static_cast<TO *>(a.out) + row * a.out_row + col8, v);
+                }
+            }
+        } else {        // a lane a column
+#pragma unroll 1
+            for (int r = 0; r < here; ++r)
+                for (int c = lane; c < CB * 32; c += 64)
+                    if (col0 + c < a.n) finish_one<TO>(a, row0 + r, col0 + c, os[r * OP + c]);
         }
         wave_lds_order();
-    }
+    });
 }
 
 // Rows laid out anew: padded_k elements each, zeros behind k.
@@ -245,19 +364,19 @@ hipError_t launch_linear_pad(const LinearArgs &a, const LinearPlan &p, uint16_t 
     return hipGetLastError();
 }
 
-template <int DT, typename TO, int WM, int WN, int PB> static hipError_t launch_tile_of(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
+template <int DT, typename TO, int WM, int WN, int PB, int CB> static hipError_t launch_tile_of(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
-    constexpr size_t lds = kTileLds<WM, WN, PB>;
-    const hipError_t e = raise_dynamic_lds<&k_linear_tile<DT, TO, WM, WN, PB>>(lds);
+    constexpr size_t lds = kTileLds<WM, WN, PB, CB>;
+    const hipError_t e = raise_dynamic_lds<&k_linear_tile<DT, TO, WM, WN, PB, CB>>(lds);
     if (e != hipSuccess) return e;
     const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles * p.splits;
-    k_linear_tile<DT, TO, WM, WN, PB><<<dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, s>>>(a);
+    k_linear_tile<DT, TO, WM, WN, PB, CB><<<dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(WM * WN * 64), lds, s>>>(a);
     return hipGetLastError();
 }
 
 template <int DT, typename TO> static hipError_t launch_tile_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
-    return p.tile_m == 256 ? launch_tile_of<DT, TO, 2, 4, 4>(a, p, s) : launch_tile_of<DT, TO, 2, 2, 2>(a, p, s);
+    return p.tile_m == 256 ? launch_tile_of<DT, TO, 2, 2, 4, 4>(a, p, s) : launch_tile_of<DT, TO, 2, 2, 2, 2>(a, p, s);
 }
 
 hipError_t launch_linear_tile(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s)

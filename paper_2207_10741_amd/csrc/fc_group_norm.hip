@@ -18,17 +18,16 @@ struct Triple {
     float n, mean, s;
     __device__ __forceinline__ void join(float n2, float mean2, float s2)
     {
-        const float both = n + n2, part = both > 0.f ? n2 / both : 0.f, d = mean2 - mean;
+        const float both = n + n2, part = both > 0.f ? n2 * __builtin_amdgcn_rcpf(both) : 0.f, d = mean2 - mean;
         s += s2 + d * d * (n * part);
         mean += n2 > 0.f ? d * part : 0.f;
         n = both;
     }
 };
-// over the lanes of a wave, in a fixed order
-__device__ __forceinline__ Triple join_lanes(Triple t)
+// over `lanes` (a power of two) neighbouring lanes, in a fixed order
+__device__ __forceinline__ Triple join_lanes(Triple t, int lanes)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
+    for (int m = 1; m < lanes; m <<= 1) {
         const float n = __shfl_xor(t.n, m), mean = __shfl_xor(t.mean, m), s = __shfl_xor(t.s, m);
         // (both lanes of a pair join the same two in the same order)
         Triple lo = (threadIdx.x & m) ? Triple{n, mean, s} : t;
@@ -38,6 +37,13 @@ __device__ __forceinline__ Triple join_lanes(Triple t)
         t = lo;
     }
     return t;
+}
+// Lanes that take a group together: as many as there are threads for it.
+__device__ __forceinline__ int lanes_of(int groups)
+{
+    int lanes = 64;
+    while (lanes > 1 && lanes * groups > (int)blockDim.x) lanes >>= 1;
+    return lanes;
 }
 
 // A piece of a row: VE values, and the way back.
@@ -61,6 +67,11 @@ template <typename T, bool WIDE> struct Piece {
         } else if constexpr (sizeof(T) == 4) {
             return __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3]));
         } else return pack8<T>(v);
+    }
+    static __device__ __forceinline__ raw_t select(bool which, const raw_t &a, const raw_t &b)
+    {
+        if constexpr (WIDE) return make_uint4(which ? a.x : b.x, which ? a.y : b.y, which ? a.z : b.z, which ? a.w : b.w);
+        else return which ? a : b;
     }
     static __device__ __forceinline__ raw_t zero()
     {
@@ -116,30 +127,36 @@ template <typename P> struct Found {
     __device__ __forceinline__ void put(const Spread &sp, int p, float rows, const float (&pivot)[P::VE], const float (&s1)[P::VE], const float (&s2)[P::VE]) const
     {
         const float inverse = rows > 0.f ? 1.f / rows : 0.f;
-        if (whole) {
-            Triple t = {rows, pivot[0] + s1[0] * inverse, fmaxf(s2[0] - s1[0] * s1[0] * inverse, 0.f)};
-            if (s2[0] != s2[0]) t.s = s2[0];
+        float mean[P::VE], s[P::VE];
 #pragma unroll
-            for (int i = 1; i < P::VE; ++i) {
-                const float s = s2[i] - s1[i] * s1[i] * inverse;
-                t.join(rows, pivot[i] + s1[i] * inverse, s < 0.f ? 0.f : s);
-            }
-            entries[sp.phase * row + p] = make_float2(t.mean, t.s);
-        } else {
+        for (int i = 0; i < P::VE; ++i) {
+            mean[i] = pivot[i] + s1[i] * inverse;
+            s[i] = s2[i] - s1[i] * s1[i] * inverse;
+            s[i] = s[i] < 0.f ? 0.f : s[i];
+        }
+        if (whole) {        // (equal counts)
+            float m = 0.f, all = 0.f, off = 0.f;
+#pragma unroll
+            for (int i = 0; i < P::VE; ++i) m += mean[i] - mean[0];
+            m = mean[0] + m * (1.f / P::VE);
 #pragma unroll
             for (int i = 0; i < P::VE; ++i) {
-                const float s = s2[i] - s1[i] * s1[i] * inverse;
-                entries[sp.phase * row + p * P::VE + i] = make_float2(pivot[i] + s1[i] * inverse, s < 0.f ? 0.f : s);
+                all += s[i];
+                off = fmaf(mean[i] - m, mean[i] - m, off);
             }
+            entries[sp.phase * row + p] = make_float2(m, fmaf(rows, off, all));
+        } else {
+#pragma unroll
+            for (int i = 0; i < P::VE; ++i) entries[sp.phase * row + p * P::VE + i] = make_float2(mean[i], s[i]);
         }
         if (p == 0) counts[sp.phase] = rows;
     }
-    // group g of the slice, by a wave
-    __device__ __forceinline__ Triple group(const Spread &sp, int g) const
+    // group g of the slice, by `lanes` lanes
+    __device__ __forceinline__ Triple group(const Spread &sp, int g, int lanes) const
     {
-        const int lane = threadIdx.x & 63, items = per_group * sp.phases;
+        const int items = per_group * sp.phases;
         Triple t = {0.f, 0.f, 0.f};
-        for (int i = lane; i < items; i += 64) {
+        for (int i = (int)threadIdx.x & (lanes - 1); i < items; i += lanes) {
             const int phase = i / per_group, e = i - phase * per_group;
             const float n = counts[phase] * (float)per_entry;
             const float2 f = entries[phase * row + g * per_group + e];
@@ -148,7 +165,7 @@ template <typename P> struct Found {
                 else t.join(n, f.x, f.y);
             }
         }
-        return join_lanes(t);
+        return join_lanes(t, lanes);
     }
 };
 __device__ __forceinline__ float2 stats_of(const NormArgs &a, const Triple &t)
@@ -180,26 +197,36 @@ template <typename P> struct Affine {
     }
 };
 
+// A thread's sums about the first piece that it sees.  A piece that does not count is taken to be the pivot: it adds nothing.
 template <typename P> struct Sums {
+    typename P::raw_t first;
     float pivot[P::VE], s1[P::VE], s2[P::VE], rows;
     __device__ __forceinline__ Sums()
     {
         rows = 0.f;
+        first = P::zero();
 #pragma unroll
         for (int i = 0; i < P::VE; ++i) pivot[i] = s1[i] = s2[i] = 0.f;
     }
-    __device__ __forceinline__ void add(const typename P::raw_t &r)
+    template <int N> __device__ __forceinline__ void add(const typename P::raw_t (&r)[N], const bool (&seen)[N])
     {
-        float v[P::VE];
-        P::values(r, v);
+        if (rows == 0.f) {
 #pragma unroll
-        for (int i = 0; i < P::VE; ++i) {
-            pivot[i] = rows == 0.f ? v[i] : pivot[i];
-            const float d = v[i] - pivot[i];
-            s1[i] += d;
-            s2[i] = fmaf(d, d, s2[i]);
+            for (int i = N - 1; i >= 0; --i) first = P::select(seen[i], r[i], first);
+            P::values(first, pivot);
         }
-        rows += 1.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            float v[P::VE];
+            P::values(P::select(seen[n], r[n], first), v);
+#pragma unroll
+            for (int i = 0; i < P::VE; ++i) {
+                const float d = v[i] - pivot[i];
+                s1[i] += d;
+                s2[i] = fmaf(d, d, s2[i]);
+            }
+            rows += seen[n] ? 1.f : 0.f;
+        }
     }
 };
 
@@ -242,15 +269,13 @@ void k_norm_once(NormArgs a)
         if (seen[i]) r[i] = *reinterpret_cast<const raw_t *>(x + (int64_t)row * a.x_row);
     }
     Sums<P> sums;
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-        if (seen[i]) sums.add(r[i]);
+    sums.add(r, seen);
     if (sp.active) found.put(sp, sp.p, sums.rows, sums.pivot, sums.s1, sums.s2);
     __syncthreads();
-    const int groups = a.slice / a.per_group, waves = (int)blockDim.x / 64;
-    for (int g = threadIdx.x >> 6; g < groups; g += waves) {
-        const float2 s = stats_of(a, found.group(sp, g));
-        if ((threadIdx.x & 63) == 0) group_stats[g] = s;
+    const int groups = a.slice / a.per_group, lanes = lanes_of(groups);
+    for (int g = (int)threadIdx.x / lanes; g < groups; g += (int)blockDim.x / lanes) {
+        const float2 s = stats_of(a, found.group(sp, g, lanes));
+        if ((threadIdx.x & (lanes - 1)) == 0) group_stats[g] = s;
     }
     __syncthreads();
     if (!sp.active) return;
@@ -303,26 +328,28 @@ void k_norm_stats(NormArgs a)
                     r[i] = P::zero();
                     if (seen[i]) r[i] = *reinterpret_cast<const raw_t *>(x + (int64_t)(row + i * sp.phases) * a.x_row);
                 }
-#pragma unroll
-                for (int i = 0; i < kNormUnroll; ++i)
-                    if (seen[i]) sums.add(r[i]);
+                sums.add(r, seen);
             }
             found.put(sp, p, sums.rows, sums.pivot, sums.s1, sums.s2);
             if (sp.pr < kNormThreads) break;
         }
     __syncthreads();
-    const int groups = a.slice / a.per_group, lane = threadIdx.x & 63;
+    const int groups = a.slice / a.per_group, lanes = lanes_of(groups), lane = threadIdx.x & (lanes - 1);
     // [chunk][3][groups]: written and read past the caches
     const auto part = __builtin_amdgcn_make_buffer_rsrc(a.part + (int64_t)unit * a.chunks * 3 * groups, 0, (uint32_t)(a.chunks * 3 * groups) * 4u, 0x00020000);
-    for (int g = threadIdx.x >> 6; g < groups; g += kNormThreads / 64) {
-        const Triple t = found.group(sp, g);
-        const float v = lane == 0 ? t.n : lane == 1 ? t.mean : t.s;
-        if (lane < 3) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), part, (uint32_t)((chunk * 3 + lane) * groups + g) * 4u, 0, kPiecesPastCaches);
+    for (int g = (int)threadIdx.x / lanes; g < groups; g += kNormThreads / lanes) {
+        const Triple t = found.group(sp, g, lanes);
+        if (lane == 0) {
+            const float v[3] = {t.n, t.mean, t.s};
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), part, (uint32_t)((chunk * 3 + j) * groups + g) * 4u, 0, kPiecesPastCaches);
+        }
     }
     if (!last_piece(a.arrived + unit, a.chunks, &flag)) return;
-    for (int g = threadIdx.x >> 6; g < groups; g += kNormThreads / 64) {
+    for (int g = (int)threadIdx.x / lanes; g < groups; g += kNormThreads / lanes) {
         Triple t = {0.f, 0.f, 0.f};
-        for (int i = lane; i < a.chunks; i += 64) {
+        for (int i = lane; i < a.chunks; i += lanes) {
             float f[3];
 #pragma unroll
             for (int j = 0; j < 3; ++j) f[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(part, (uint32_t)((i * 3 + j) * groups + g) * 4u, 0, kPiecesPastCaches));
@@ -331,7 +358,7 @@ void k_norm_stats(NormArgs a)
                 else t.join(f[0], f[1], f[2]);
             }
         }
-        t = join_lanes(t);
+        t = join_lanes(t, lanes);
         if (lane == 0) a.stats[(int64_t)image * a.groups + slice * groups + g] = stats_of(a, t);
     }
 }

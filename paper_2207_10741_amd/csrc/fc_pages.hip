@@ -1,9 +1,10 @@
 // Pages of the key/value cache: giving blocks to sequences and back, forking, compacting, copying.
 //
 // Tables are small and blocks are large: what bounds the calls is launches where only tables change, and memory where blocks are copied.  A call that gives out
-// blocks is two launches.  The first goes over the sequences (a workgroup each, up to kMostWorkgroups at a time): blocks that are let go leave the counts of
-// users by atomics (sums of whole numbers: the order does not matter), and every sequence says how many blocks it wants.  Its last workgroup then has the
-// counts as they are after all of that, takes the lowest free blocks and deals them out in order.  The second launch copies blocks.
+// blocks is two launches.  The first goes over the sequences: blocks that are let go leave the counts of users by atomics (sums of whole numbers: the order
+// does not matter), and every sequence says how many blocks it wants.  Its last workgroup then has the counts as they are after all of that, adds up what is
+// wanted in order and lists the lowest free blocks.  The second launch writes the tables and copies blocks, every sequence for itself.  (Tables written by the
+// last workgroup of the first launch: 38 us for 256 sequences, its waves' round trips one after another.)
 //
 // What workgroups of other XCDs wrote in the same launch is read past the caches.
 #include "fc_attn_internal.hpp"
@@ -33,12 +34,12 @@ struct PagesArgs {
     const int32_t *parents;
     int32_t *missing;
     // workspace
-    int32_t *arrived;           // one counter
+    int32_t *arrived;           // one counter, of workgroups that are done; zero before and after every call
     int32_t *wanted;            // [batch]: blocks a sequence wants; its last one is to be a copy of own[b]
     int32_t *own;               // [batch]: -1, or the block that the sequence gets a copy of
     int32_t *offsets;           // [batch]
     int32_t *given;             // [blocks]: free blocks
-    int32_t *pairs;             // [0] how many, then (source, target)
+    int32_t *found;             // one: how many of them are listed
     int32_t *rows, *new_lengths;    // fork: the new table
 };
 
@@ -79,7 +80,7 @@ __device__ __forceinline__ Scanned scan(int32_t v, int32_t *lds)       // lds [k
     return {before + upto - v, all};
 }
 
-// The lowest free blocks, as many as `total` if there are so many: their numbers into given, how many there are returned.
+// The lowest free blocks, as many as `total` if there are so many: their numbers into given, their users 1; how many there are is returned.
 __device__ __forceinline__ int32_t find_free(const PagesArgs &a, int32_t total, int32_t *lds)
 {
     int32_t found = 0;
@@ -95,7 +96,11 @@ __device__ __forceinline__ int32_t find_free(const PagesArgs &a, int32_t total, 
         for (int i = 0; i < 16; ++i) free |= (u[i / 4][i % 4] == 0 && at + i < a.blocks ? 1u : 0u) << i;
         const Scanned s = scan(__popc(free), lds);
         int32_t rank = found + s.before;
-        for (uint32_t left = free; left && rank < total; left &= left - 1, ++rank) a.given[rank] = at + __ffs(left) - 1;
+        for (uint32_t left = free; left && rank < total; left &= left - 1, ++rank) {
+            const int32_t block = at + __ffs(left) - 1;
+            a.given[rank] = block;
+            a.users[block] = 1;
+        }
         found += s.all;
     }
     return min(found, total);
@@ -115,8 +120,8 @@ __device__ __forceinline__ bool last_workgroup(const PagesArgs &a, int32_t *flag
     return *flag;
 }
 
-// Offsets of what the sequences want, in order; the sum.
-__device__ __forceinline__ int32_t offsets_of(const PagesArgs &a, int32_t *lds)
+// The last workgroup's part: offsets of what the sequences want, in order, and the blocks they get.
+__device__ __forceinline__ void deal(const PagesArgs &a, int32_t *lds)
 {
     int32_t total = 0;
     for (int32_t first = 0; first < a.batch; first += kThreads) {
@@ -125,13 +130,16 @@ __device__ __forceinline__ int32_t offsets_of(const PagesArgs &a, int32_t *lds)
         if (b < a.batch) a.offsets[b] = total + s.before;
         total += s.all;
     }
-    __syncthreads();
-    return total;
+    const int32_t found = total ? find_free(a, total, lds) : 0;
+    if (threadIdx.x == 0) {
+        *a.found = found;
+        *a.missing = total - found;
+    }
 }
 
 __global__ __launch_bounds__(kThreads) void k_resize(PagesArgs a)
 {
-    __shared__ int32_t lds[kWaves], flag, pairs;
+    __shared__ int32_t lds[kWaves], flag;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // a wave a sequence: what lies behind its need goes back, what is not there is wanted
     for (int32_t b = (int32_t)blockIdx.x * kWaves + wave; b < a.batch; b += (int32_t)gridDim.x * kWaves) {
@@ -158,7 +166,6 @@ __global__ __launch_bounds__(kThreads) void k_resize(PagesArgs a)
     if (!last_workgroup(a, &flag)) return;
 
     // an unfinished last block that others hold as well: a copy
-    if (threadIdx.x == 0) pairs = 0;
     for (int32_t b = threadIdx.x; b < a.batch; b += kThreads) {
         int32_t source = -1;
         const int32_t length = a.lengths[b];
@@ -170,44 +177,12 @@ __global__ __launch_bounds__(kThreads) void k_resize(PagesArgs a)
         if (source >= 0) store_shared(a.wanted + b, load_shared(a.wanted + b) + 1);
     }
     __syncthreads();
-    const int32_t total = offsets_of(a, lds);
-    const int32_t found = total ? find_free(a, total, lds) : 0;
-    __syncthreads();
-    for (int32_t b = wave; b < a.batch; b += kWaves) {
-        if (load_shared(a.wanted + b) == 0) continue;
-        int32_t *const row = a.table + (int64_t)b * a.width;
-        const int32_t need = needed(a.lengths[b], a.width), source = a.own[b];
-        int32_t rank = a.offsets[b];
-        for (int32_t j0 = 0; j0 < need; j0 += 64) {
-            const int32_t j = j0 + lane, e = j < need ? row[j] : 0;
-            const bool copy = source >= 0 && j == need - 1, wants = j < need && ((uint32_t)e >= (uint32_t)a.blocks || copy);
-            const uint64_t all = __ballot(wants);
-            if (wants) {
-                const int32_t mine = rank + __popcll(all & ((1ull << lane) - 1)), block = mine < found ? a.given[mine] : -1;
-                row[j] = block;
-                if (block >= 0) count_users(a.users + block, 1);
-                if (copy) {
-                    count_users(a.users + source, -1);
-                    if (block >= 0) {
-                        const int32_t p = atomicAdd(&pairs, 1);     // (in any order: they do not touch each other)
-                        a.pairs[2 + 2 * p] = source;
-                        a.pairs[3 + 2 * p] = block;
-                    }
-                }
-            }
-            rank += __popcll(all);
-        }
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        a.pairs[0] = pairs;
-        *a.missing = total - found;
-    }
+    deal(a, lds);
 }
 
 __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a)
 {
-    __shared__ int32_t lds[kWaves], flag, pairs, lower;
+    __shared__ int32_t lds[kWaves], flag, lower;
     // a workgroup a slot
     for (int32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
         const int32_t p = a.parents[b];
@@ -252,27 +227,14 @@ __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a)
     }
     if (!last_workgroup(a, &flag)) return;
 
-    if (threadIdx.x == 0) pairs = 0;
-    const int32_t total = offsets_of(a, lds);
-    const int32_t found = total ? find_free(a, total, lds) : 0;
-    __syncthreads();
-    for (int32_t b = threadIdx.x; b < a.batch; b += kThreads) {
-        const int32_t source = load_shared(a.own + b), rank = a.offsets[b];
-        int32_t block = -1;
-        if (source >= 0 && rank < found) {
-            block = a.given[rank];
-            count_users(a.users + block, 1);
-            const int32_t p = atomicAdd(&pairs, 1);
-            a.pairs[2 + 2 * p] = source;
-            a.pairs[3 + 2 * p] = block;
-        }
-        a.offsets[b] = block;       // (what the next launch puts in the copy's place)
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        a.pairs[0] = pairs;
-        *a.missing = total - found;
-    }
+    deal(a, lds);
+}
+
+// The block that a sequence's last wanted place gets, -1: none.
+__device__ __forceinline__ int32_t last_given(const PagesArgs &a, int32_t b)
+{
+    const int32_t rank = a.offsets[b] + a.wanted[b] - 1;
+    return rank < *a.found ? a.given[rank] : -1;
 }
 
 // ---- copying ----
@@ -283,8 +245,7 @@ constexpr int kCopyThreads = 256, kCopyPieces = 8, kCopyBytes = kCopyThreads * k
 struct CopyArgs {
     CacheView from, to;
     int32_t blocks, blocks_to;
-    const int32_t *sources, *targets;   // item i: sources[i * stride], targets[i * stride]; targets NULL: block i
-    int32_t stride;
+    const int32_t *sources, *targets;   // targets NULL: block i
     const int32_t *count;               // how many there are, or NULL: all
     int32_t most;
     int32_t segments;                   // of a block's codes
@@ -298,50 +259,95 @@ template <typename V> __device__ __forceinline__ void copy_small(const Section &
     for (int32_t i = threadIdx.x; i < n; i += kCopyThreads) y[i] = x[i];
 }
 
-__device__ __forceinline__ void copy_blocks(const CopyArgs &c, int64_t first, int64_t step)
+// A segment of block s of one cache to block t of the other.
+__device__ __forceinline__ void copy_segment(const CopyArgs &c, int32_t s, int32_t t, int32_t segment)
 {
-    const int32_t count = c.count ? min(max(load_shared(c.count), 0), c.most) : c.most;
-    const int64_t items = (int64_t)count * c.segments;
-    for (int64_t i = first; i < items; i += step) {
-        const int32_t n = (int32_t)(i / c.segments), segment = (int32_t)(i - (int64_t)n * c.segments);
-        const int32_t s = c.sources[(int64_t)n * c.stride], t = c.targets ? c.targets[(int64_t)n * c.stride] : n;
-        if ((uint32_t)s >= (uint32_t)c.blocks || (uint32_t)t >= (uint32_t)c.blocks_to) continue;
-        const int64_t at = (int64_t)segment * kCopyBytes + threadIdx.x * 16, end = c.from.codes.block;
-        const uint8_t *const x = c.from.codes.base + s * end;
-        uint8_t *const y = c.to.codes.base + t * end;
-        u32x4_t v[kCopyPieces];
+    const int64_t at = (int64_t)segment * kCopyBytes + threadIdx.x * 16, end = c.from.codes.block;
+    const uint8_t *const x = c.from.codes.base + s * end;
+    uint8_t *const y = c.to.codes.base + t * end;
+    u32x4_t v[kCopyPieces];
 #pragma unroll
-        for (int j = 0; j < kCopyPieces; ++j) {
-            const int64_t o = at + j * (kCopyThreads * 16);
-            v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(x + (o < end ? o : 0)));
-        }
+    for (int j = 0; j < kCopyPieces; ++j) {
+        const int64_t o = at + j * (kCopyThreads * 16);
+        v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(x + (o < end ? o : 0)));
+    }
 #pragma unroll
-        for (int j = 0; j < kCopyPieces; ++j) {
-            const int64_t o = at + j * (kCopyThreads * 16);
-            if (o < end) *reinterpret_cast<u32x4_t *>(y + o) = v[j];
-        }
-        if (segment == 0) {
-            copy_small<float2>(c.from.scales, c.to.scales, s, t);
-            copy_small<float>(c.from.weights, c.to.weights, s, t);
-            copy_small<uint4>(c.from.sketches, c.to.sketches, s, t);
-        }
+    for (int j = 0; j < kCopyPieces; ++j) {
+        const int64_t o = at + j * (kCopyThreads * 16);
+        if (o < end) *reinterpret_cast<u32x4_t *>(y + o) = v[j];
+    }
+    if (segment == 0) {
+        copy_small<float2>(c.from.scales, c.to.scales, s, t);
+        copy_small<float>(c.from.weights, c.to.weights, s, t);
+        copy_small<uint4>(c.from.sketches, c.to.sketches, s, t);
     }
 }
 
-__global__ __launch_bounds__(kCopyThreads) void k_copy(CopyArgs c) { copy_blocks(c, blockIdx.x, gridDim.x); }
+__device__ __forceinline__ void copy_blocks(const CopyArgs &c)
+{
+    const int32_t count = c.count ? min(max(*c.count, 0), c.most) : c.most;
+    const int64_t items = (int64_t)count * c.segments;
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const int32_t n = (int32_t)(i / c.segments), segment = (int32_t)(i - (int64_t)n * c.segments);
+        const int32_t s = c.sources[n], t = c.targets ? c.targets[n] : n;
+        if ((uint32_t)s < (uint32_t)c.blocks && (uint32_t)t < (uint32_t)c.blocks_to) copy_segment(c, s, t, segment);
+    }
+}
 
-// The forked slots' rows and lengths; copies.
+__global__ __launch_bounds__(kCopyThreads) void k_copy(CopyArgs c) { copy_blocks(c); }
+
+// The copies that sequences get of blocks of their own: items of a sequence and a segment.
+__device__ __forceinline__ void copy_own(const PagesArgs &a, const CopyArgs &c)
+{
+    const int64_t items = (int64_t)a.batch * c.segments;
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const int32_t b = (int32_t)(i / c.segments), segment = (int32_t)(i - (int64_t)b * c.segments);
+        const int32_t source = a.own[b];
+        if (source < 0) continue;
+        const int32_t block = last_given(a, b);
+        if (block >= 0) copy_segment(c, source, block, segment);
+    }
+}
+
+// What the sequences wanted goes into their tables.
+__global__ __launch_bounds__(kCopyThreads) void k_resize_rows(PagesArgs a, CopyArgs c)
+{
+    const int lane = threadIdx.x & 63, waves = kCopyThreads / 64;
+    for (int32_t b = (int32_t)blockIdx.x * waves + (int32_t)(threadIdx.x >> 6); b < a.batch; b += (int32_t)gridDim.x * waves) {
+        if (a.wanted[b] == 0) continue;
+        int32_t *const row = a.table + (int64_t)b * a.width;
+        const int32_t need = needed(a.lengths[b], a.width), source = a.own[b], found = *a.found;
+        int32_t rank = a.offsets[b];
+        for (int32_t j0 = 0; j0 < need; j0 += 256) {
+            int32_t e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = j0 + i * 64 + lane < need ? row[j0 + i * 64 + lane] : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t j = j0 + i * 64 + lane;
+                const bool copy = source >= 0 && j == need - 1, wants = j < need && ((uint32_t)e[i] >= (uint32_t)a.blocks || copy);
+                const uint64_t all = __ballot(wants);
+                const int32_t mine = rank + __popcll(all & ((1ull << lane) - 1));
+                if (wants) row[j] = mine < found ? a.given[mine] : -1;
+                if (copy) count_users(a.users + source, -1);
+                rank += __popcll(all);
+            }
+        }
+    }
+    copy_own(a, c);
+}
+
 __global__ __launch_bounds__(kCopyThreads) void k_fork_rows(PagesArgs a, CopyArgs c)
 {
     for (int32_t b = blockIdx.x; b < a.batch; b += gridDim.x) {
         if (a.parents[b] == b) continue;
-        const int32_t length = a.new_lengths[b], own = a.own[b];
-        const int32_t last = own >= 0 ? needed(length, a.width) - 1 : -1, block = a.offsets[b];
+        const int32_t length = a.new_lengths[b];
+        const int32_t last = a.own[b] >= 0 ? needed(length, a.width) - 1 : -1, block = a.own[b] >= 0 ? last_given(a, b) : -1;
         for (int32_t j = threadIdx.x; j < a.width; j += kCopyThreads)
             a.table[(int64_t)b * a.width + j] = j == last ? block : a.rows[(int64_t)b * a.width + j];
         if (threadIdx.x == 0) a.lengths[b] = length;
     }
-    copy_blocks(c, blockIdx.x, gridDim.x);
+    copy_own(a, c);
 }
 
 // ---- compacting ----
@@ -403,7 +409,7 @@ __global__ __launch_bounds__(kCopyThreads) void k_compact(CompactArgs a, CopyArg
         a.table_to[i] = (uint32_t)e < (uint32_t)a.blocks ? a.numbers[e] : -1;
     }
     for (int64_t i = *a.count + thread; i < a.blocks_to; i += threads) a.users_to[i] = 0;
-    copy_blocks(c, blockIdx.x, gridDim.x);
+    copy_blocks(c);
 }
 
 // ---- the host side ----
@@ -443,7 +449,7 @@ int32_t check_to(const fc_pages_desc *d)
 
 // Workspace: offsets of its parts.
 struct Parts {
-    size_t wanted, own, offsets, given, pairs, rows, lengths, bytes;
+    size_t wanted, own, offsets, given, rows, lengths, bytes;
 };
 Parts parts_of(const fc_pages_desc *d, bool fork)
 {
@@ -453,8 +459,7 @@ Parts parts_of(const fc_pages_desc *d, bool fork)
     p.own = p.wanted + batch;
     p.offsets = p.own + batch;
     p.given = p.offsets + batch;
-    p.pairs = p.given + align_up((size_t)d->blocks * 4, 256);
-    p.rows = p.pairs + align_up((size_t)d->batch * 8 + 8, 256);
+    p.rows = p.given + align_up((size_t)d->blocks * 4, 256);
     p.lengths = p.rows + (fork ? align_up((size_t)d->batch * d->table_width * 4, 256) : 0);
     p.bytes = p.lengths + (fork ? batch : 0);
     return p;
@@ -467,7 +472,7 @@ PagesArgs args_of(const fc_pages_desc *d, int32_t *users, int32_t *table, int32_
     PagesArgs a;
     a.blocks = d->blocks; a.blocks_to = d->blocks; a.batch = d->batch; a.width = d->table_width;
     a.users = users; a.table = table; a.lengths = lengths; a.parents = parents; a.missing = missing;
-    a.arrived = at(0); a.wanted = at(p.wanted); a.own = at(p.own); a.offsets = at(p.offsets); a.given = at(p.given); a.pairs = at(p.pairs);
+    a.arrived = at(0); a.wanted = at(p.wanted); a.own = at(p.own); a.offsets = at(p.offsets); a.given = at(p.given); a.found = at(64);
     a.rows = at(p.rows); a.new_lengths = at(p.lengths);
     return a;
 }
@@ -479,18 +484,14 @@ CopyArgs copies(const fc_pages_desc *d, const void *from, const void *to, int32_
     c.to = view_of(to, blocks_to, d);
     c.blocks = d->blocks; c.blocks_to = blocks_to;
     c.sources = c.targets = nullptr;
-    c.stride = 1;
     c.count = nullptr;
     c.most = 0;
     c.segments = (int32_t)((c.from.codes.block + kCopyBytes - 1) / kCopyBytes);
     return c;
 }
-CopyArgs copies_of_pairs(const fc_pages_desc *d, const void *cache, const PagesArgs &a)
+CopyArgs copies_within(const fc_pages_desc *d, const void *cache)
 {
     CopyArgs c = copies(d, cache, cache, d->blocks);
-    c.sources = a.pairs + 2; c.targets = a.pairs + 3;
-    c.stride = 2;
-    c.count = a.pairs;
     c.most = d->batch;
     return c;
 }
@@ -565,8 +566,8 @@ int32_t fc_kv_resize(const fc_pages_desc *d, void *cache, int32_t *users, int32_
     const int32_t workgroups = (d->batch + kWaves - 1) / kWaves;
     k_resize<<<dim3((uint32_t)(workgroups < kMostWorkgroups ? workgroups : kMostWorkgroups)), dim3(kThreads), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return FC_ERR_HIP;
-    const CopyArgs c = copies_of_pairs(d, cache, a);
-    k_copy<<<dim3(workgroups_for(c, 1)), dim3(kCopyThreads), 0, s>>>(c);
+    const CopyArgs c = copies_within(d, cache);
+    k_resize_rows<<<dim3(workgroups_for(c, 1)), dim3(kCopyThreads), 0, s>>>(a, c);
     return hipGetLastError() == hipSuccess ? FC_OK : FC_ERR_HIP;
 }
 
@@ -584,7 +585,7 @@ int32_t fc_kv_fork(const fc_pages_desc *d, void *cache, int32_t *users, int32_t 
     if (!(d->flags & FC_WORKSPACE_READY) && launch_zero_i32(a.arrived, 1, s) != hipSuccess) return FC_ERR_HIP;
     k_fork<<<dim3((uint32_t)(d->batch < kMostWorkgroups ? d->batch : kMostWorkgroups)), dim3(kThreads), 0, s>>>(a);
     if (hipGetLastError() != hipSuccess) return FC_ERR_HIP;
-    const CopyArgs c = copies_of_pairs(d, cache, a);
+    const CopyArgs c = copies_within(d, cache);
     k_fork_rows<<<dim3(workgroups_for(c, d->batch)), dim3(kCopyThreads), 0, s>>>(a, c);
     return hipGetLastError() == hipSuccess ? FC_OK : FC_ERR_HIP;
 }

@@ -88,6 +88,7 @@ int32_t check_norm(const fc_group_norm_desc *d)
 }
 
 constexpr int kOnceGroups = 512;        // of a slice, at most
+constexpr int kNormGrid = 256;          // workgroups of the kernels with chunks
 
 int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
 {
@@ -98,7 +99,7 @@ int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
     int32_t least = 1;
     while (least < d->groups && (d->groups % least || least * per_group % e || least * per_group * size < 32)) ++least;
     auto entries = [&](int32_t channels) { return per_group % e == 0 ? channels / e : channels; };
-    // an image's slice in the registers of a workgroup: up to 1024 threads with 16 pieces each
+    // an image's slice in the registers of a workgroup: up to 1024 threads with 12 pieces each
     p->slice = least * per_group;
     const int32_t pieces = p->slice / e;
     p->once = false;
@@ -106,7 +107,7 @@ int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
         const int32_t threads[] = {256, 512, 1024};
         for (int i = 0; i < 6 && !p->once; ++i) {
             p->threads = threads[i % 3];
-            p->per_thread = i < 3 ? 4 : 16;
+            p->per_thread = i < 3 ? 4 : 12;
             if (pieces > p->threads) continue;
             const int32_t phases = p->threads / pieces;
             p->lds = (size_t)phases * (entries(p->slice) * 8 + 4);
@@ -115,29 +116,29 @@ int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
     }
     p->chunks = p->chunk_rows = 1;
     if (!p->once) {
-        // whole rows, or where they are longer than 4096 channels as many groups
+        // whole rows; shorter slices where rows are longer than 4096 channels, or have more than 64 groups and are longer than 512 bytes
         int32_t of = d->groups;
-        while (of > least && ((int64_t)of * per_group > 4096 || d->groups % of || of * per_group % e)) --of;
+        while (of > least && ((int64_t)of * per_group > 4096 || (of > 64 && (int64_t)of * per_group * size > 512) || d->groups % of || of * per_group % e)) --of;
         p->slice = of * per_group;
-        const int32_t row_pieces = p->slice / e, phases = row_pieces < 256 ? 256 / row_pieces : 1;
+        const int32_t row_pieces = p->slice / e, phases = row_pieces < 1024 ? 1024 / row_pieces : 1;
         p->lds = (size_t)phases * (entries(p->slice) * 8 + 4);
-        if (p->lds > 163840 - 256) return FC_ERR_RANGE;
-        const int64_t units = (int64_t)d->images * (d->channels / p->slice);
-        const int64_t wanted = (2048 + units - 1) / units, least_rows = (int64_t)phases * 8;
+        if (p->lds > 163840) return FC_ERR_RANGE;
+        // a workgroup a CU (two: outputs of 8 images of 16384 x 256 with a mask 26 -> 35 us); a chunk is no less than a round of a workgroup's loads, and an image's chunks leave no more than 128 KB to join
+        const int64_t units = (int64_t)d->images * (d->channels / p->slice), most = 8192 / of < 1 ? 1 : 8192 / of;
+        int64_t wanted = (kNormGrid + units - 1) / units;
+        if (wanted > most) wanted = most;
+        const int64_t least_rows = (int64_t)phases * 4;
         int64_t rows = (d->max_rows + wanted - 1) / wanted;
         rows = (rows + least_rows - 1) / least_rows * least_rows;
-        p->chunk_rows = (int32_t)(rows < 1 ? 1 : rows);
+        p->chunk_rows = (int32_t)(rows < 1 ? 1 : rows > INT32_MAX / 2 ? INT32_MAX / 2 : rows);
         p->chunks = ceil_div(d->max_rows, p->chunk_rows);
         if (p->chunks < 1) p->chunks = 1;
-        p->threads = 256;
+        p->threads = 1024;
     }
     p->slices = d->channels / p->slice;
     const int64_t units = (int64_t)d->images * p->slices;
     if (units * p->chunks >= (1ll << 32) / 1024) return FC_ERR_RANGE;       // (a dimension of a grid is counted in threads)
-    p->counters = p->once ? 0 : align_up((size_t)units * sizeof(int32_t), 256);
-    p->at_stats = p->counters;
-    p->at_part = p->once ? 0 : align_up(p->at_stats + (size_t)d->images * d->groups * 8, 256);
-    p->workspace = p->once ? 0 : p->at_part + (size_t)d->images * p->chunks * d->groups * 12;
+    p->workspace = p->once ? 0 : (size_t)d->images * p->chunks * d->groups * 16;
     return FC_OK;
 }
 
@@ -235,7 +236,6 @@ int32_t fc_group_norm(const fc_group_norm_desc *d, const void *x, const float *w
         if (!aligned(workspace, 16)) return FC_ERR_ALIGN;
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    uint8_t *const ws = static_cast<uint8_t *>(workspace);
     NormArgs a;
     a.x = x; a.out = out; a.weight = weight; a.bias = bias; a.mask = mask; a.starts = starts;
     a.images = d->images; a.rows = d->rows; a.max_rows = d->max_rows; a.channels = d->channels; a.groups = d->groups;
@@ -245,13 +245,8 @@ int32_t fc_group_norm(const fc_group_norm_desc *d, const void *x, const float *w
     a.eps = d->eps;
     a.x_row = d->x_row; a.out_row = d->out_row;
     a.slices = p.slices; a.slice = p.slice; a.chunks = p.chunks; a.chunk_rows = p.chunk_rows;
-    a.arrived = reinterpret_cast<int32_t *>(ws);
-    a.stats = reinterpret_cast<float2 *>(ws + p.at_stats);
-    a.part = reinterpret_cast<float *>(ws + p.at_part);
-    hipError_t e = hipSuccess;
-    if (p.counters && !(d->flags & FC_WORKSPACE_READY)) e = launch_zero_i32(a.arrived, d->images * p.slices, s);
-    if (e == hipSuccess) e = launch_group_norm(a, p, d->dtype, s);
-    return e == hipSuccess ? FC_OK : FC_ERR_HIP;
+    a.part = static_cast<float4 *>(workspace);
+    return launch_group_norm(a, p, d->dtype, s) == hipSuccess ? FC_OK : FC_ERR_HIP;
 }
 
 } // extern "C"

@@ -208,16 +208,14 @@ struct NormArgs {
     float eps;
     int64_t x_row, out_row;
     int32_t slices, slice, chunks, chunk_rows;      // channels of a slice (whole groups), rows of a chunk
-    float *part;                                    // [image][slice][chunk][3][groups of a slice]: counts, means, squared distances
-    float2 *stats;                                  // [image][group]: mean, 1 / sqrt(variance + eps)
-    int32_t *arrived;                               // [image][slice]
+    float4 *part;                                   // [image][slice][group of a slice][chunk]: count, mean, squared distances
 };
 
 struct NormPlan {
     bool once;                      // a workgroup holds an image's slice: read once
     bool wide;                      // pieces of 16 bytes, else elements
     int32_t threads, per_thread, slice, slices, chunks, chunk_rows;
-    size_t lds, counters, at_stats, at_part, workspace;
+    size_t lds, workspace;
 };
 
 hipError_t launch_group_norm(const NormArgs &a, const NormPlan &p, int dtype, hipStream_t s);

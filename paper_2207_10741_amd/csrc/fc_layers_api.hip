@@ -1,6 +1,7 @@
 // C ABI of the matrix product and of group norm: argument checks on the host, then launches.
 #include "fc_layers_internal.hpp"
 #include <math.h>
+#include <stdlib.h>
 
 using namespace fc;
 
@@ -9,6 +10,7 @@ namespace {
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride <= FC_LAYERS_MAX_STRIDE; }
 int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
+int32_t min_of(int32_t a, int32_t b) { return a < b ? a : b; }
 int size_of(int32_t dtype) { return dtype == FC_F32 ? 4 : 2; }
 
 // ---- the matrix product ----
@@ -29,6 +31,7 @@ int32_t check_linear(const fc_linear_desc *d, bool residual)
 
 int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
 {
+    const int32_t rows = d->rows < 1 ? 1 : d->rows;
     const bool pieces = d->k % 8 == 0 && !(d->flags & FC_ANY_POINTERS), x_pieces = pieces && d->x_row % 8 == 0, w_pieces = pieces && d->w_row % 8 == 0;
     const int32_t chunks = ceil_div(d->k, kLinearK);
     p->padded_k = (int64_t)chunks * kLinearK;
@@ -37,21 +40,38 @@ int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
     p->splits = 1;
     p->per_split = chunks;
     p->per_wave = 0;
-    if (d->rows <= 64) {
+    p->ring = false;
+    if (getenv("LF") ? rows <= atoi(getenv("LF")) : rows <= 64) {
         p->form = 0;
-        p->tile_m = d->rows <= 16 ? 16 : d->rows <= 32 ? 32 : 64;
-        p->tile_n = d->n >= 16384 ? (p->tile_m == 64 ? 64 : 32) : 16;
-        p->m_tiles = 1;
+        p->ring = p->wide && rows > (getenv("LR") ? atoi(getenv("LR")) : 0);
+        p->tile_m = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+        if (p->ring) p->tile_n = getenv("LN") ? atoi(getenv("LN")) : d->n >= 16384 && rows > 16 ? 64 : d->n >= 8192 ? 32 : 16;
+        else p->tile_n = d->n >= 16384 ? (p->tile_m == 64 ? 64 : 32) : 16;
+        p->m_tiles = ceil_div(rows, p->tile_m);
         p->n_tiles = ceil_div(d->n, p->tile_n);
-        const int32_t wanted = ceil_div(256, p->n_tiles), most = chunks < 16 ? 1 : chunks / 8;
+        const int32_t wanted = ceil_div(256, (int64_t)p->n_tiles * p->m_tiles), most = chunks < 16 ? 1 : chunks / 8;
         p->per_split = ceil_div(chunks, wanted < most ? wanted : most);
         p->splits = ceil_div(chunks, p->per_split);
-        p->per_wave = ceil_div(p->per_split, 8);
+        p->per_wave = ceil_div(p->per_split, p->ring && (p->tile_m == 64 || p->tile_n == 64) ? 4 : 8);
+    } else if (getenv("LS") ? rows <= atoi(getenv("LS")) : rows <= 128) {
+        p->form = 2;
+        p->tile_m = rows <= 64 ? 64 : 128;
+        p->tile_n = 128;
+        p->m_tiles = ceil_div(rows, p->tile_m);
+        p->n_tiles = ceil_div(d->n, p->tile_n);
+        const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
+        if (tiles < 256) {
+            const int32_t wanted = (int32_t)(256 / tiles), most = chunks < 8 ? 1 : chunks / 4;
+            p->per_split = ceil_div(chunks, min_of(wanted < 1 ? 1 : wanted < most ? wanted : most, getenv("LW") ? atoi(getenv("LW")) : 8));
+            p->splits = ceil_div(chunks, p->per_split);
+        }
+        p->pad_x = !x_pieces;
+        p->pad_w = !w_pieces;
     } else {
         p->form = 1;
-        const int64_t large = (int64_t)ceil_div(d->rows, 256) * ceil_div(d->n, 256);
+        const int64_t large = (int64_t)ceil_div(rows, 256) * ceil_div(d->n, 256);
         p->tile_m = p->tile_n = large >= 192 ? 256 : 128;
-        p->m_tiles = ceil_div(d->rows, p->tile_m);
+        p->m_tiles = ceil_div(rows, p->tile_m);
         p->n_tiles = ceil_div(d->n, p->tile_n);
         const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
         if (p->tile_m == 128 && tiles < 256) {
@@ -66,7 +86,7 @@ int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
     if (tiles * p->splits >= INT32_MAX / 1024) return FC_ERR_RANGE;     // (a dimension of a grid is counted in threads)
     p->counters = p->splits == 1 ? 0 : align_up((size_t)tiles * sizeof(int32_t), 256);
     p->at_x = p->counters;
-    p->at_w = p->at_x + (p->pad_x ? (size_t)d->rows * p->padded_k * 2 : 0);
+    p->at_w = p->at_x + (p->pad_x ? (size_t)rows * p->padded_k * 2 : 0);
     p->at_part = align_up(p->at_w + (p->pad_w ? (size_t)d->n * p->padded_k * 2 : 0), 256);
     p->workspace = p->splits == 1 ? p->at_part : p->at_part + (size_t)tiles * p->splits * p->tile_m * p->tile_n * sizeof(float);
     return FC_OK;
@@ -200,7 +220,7 @@ int32_t fc_linear(const fc_linear_desc *d, const void *x, const void *w, const f
     a.residual_first = (d->flags & FC_RESIDUAL_FIRST) != 0;
     a.wide_out = d->n % 8 == 0 && aligned(out, 16) && d->out_row * size % 16 == 0 && (!residual || (aligned(residual, 16) && d->residual_row * size % 16 == 0));
     a.x_row = d->x_row; a.w_row = d->w_row; a.residual_row = d->residual_row; a.out_row = d->out_row;
-    a.n_tiles = p.n_tiles; a.splits = p.splits; a.per_split = p.per_split; a.per_wave = p.per_wave;
+    a.m_tiles = p.m_tiles; a.n_tiles = p.n_tiles; a.splits = p.splits; a.per_split = p.per_split; a.per_wave = p.per_wave;
     a.part = reinterpret_cast<float *>(ws + p.at_part);
     a.arrived = reinterpret_cast<int32_t *>(ws);
     hipError_t e = hipSuccess;
@@ -212,7 +232,7 @@ int32_t fc_linear(const fc_linear_desc *d, const void *x, const void *w, const f
         if (pw) a.w = pw, a.w_row = p.padded_k;
         if (px && pw) a.k = (int32_t)p.padded_k;
     }
-    if (e == hipSuccess) e = p.form == 0 ? launch_linear_rows(a, p, d->dtype, d->out_dtype, s) : launch_linear_tile(a, p, d->dtype, d->out_dtype, s);
+    if (e == hipSuccess) e = p.form == 0 ? launch_linear_rows(a, p, d->dtype, d->out_dtype, s) : p.form == 2 ? launch_linear_stream(a, p, d->dtype, d->out_dtype, s) : launch_linear_tile(a, p, d->dtype, d->out_dtype, s);
     return e == hipSuccess ? FC_OK : FC_ERR_HIP;
 }
 

@@ -113,7 +113,7 @@ struct LinearArgs {
     int32_t wide_out;               // out's and residual's rows are pieces of 16 bytes, n of eight columns
     int64_t x_row, w_row, residual_row, out_row;
     // many rows: a grid of tiles, each in `splits` pieces of `per_split` stages of 64
-    int32_t n_tiles, splits, per_split;
+    int32_t m_tiles, n_tiles, splits, per_split;
     // few rows: pieces of `per_split` chunks of 64, a wave's share `per_wave`
     int32_t per_wave;
     float *part;                    // [tile][split][what a tile has], in the registers' order
@@ -183,9 +183,9 @@ constexpr int kLinearK = 64;        // columns of a stage, or chunk
 
 // How a product is cut.
 struct LinearPlan {
-    int32_t form;                   // 0: few rows (tile_m, tile_n rows and columns a workgroup), 1: many (likewise)
+    int32_t form;                   // 0: few rows, 1: many, 2: some dozens; tile_m, tile_n: rows and columns of a workgroup
     int32_t tile_m, tile_n, m_tiles, n_tiles, splits, per_split, per_wave;
-    bool wide;                      // x's and w's rows are whole 16-byte pieces (few rows)
+    bool wide, ring;                // x's and w's rows are whole 16-byte pieces (few rows); they go through LDS
     bool pad_x, pad_w;              // laid out anew (many rows)
     int64_t padded_k;
     size_t counters, at_x, at_w, at_part, workspace;
@@ -193,6 +193,7 @@ struct LinearPlan {
 
 hipError_t launch_linear_rows(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
 hipError_t launch_linear_tile(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
+hipError_t launch_linear_stream(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
 // Rows of x, of w, or of both, as rows of padded_k elements with zeros behind k.
 hipError_t launch_linear_pad(const LinearArgs &a, const LinearPlan &p, uint16_t *x, uint16_t *w, hipStream_t s);
 

@@ -7,19 +7,9 @@
 // the last k-step), a stage's loads after the barrier that frees their buffer.
 //
 // Bounds are explicit: a row or a piece that is not there has an offset out of every descriptor's range and comes back as zeros.
-#include "fc_layers_internal.hpp"
-#include <type_traits>
+#include "fc_linear_tile.hpp"
 
 namespace fc {
-
-// f(integral_constant 0) .. f(integral_constant N - 1)
-template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F &&f)
-{
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>{});
-        each<N, I + 1>(f);
-    }
-}
 
 // three stages' rows of x, two stages' rows of w
 template <int WM, int WN, int PB, int CB> constexpr size_t kTileLds = (size_t)(3 * WM * PB + 2 * WN * CB) * 32 * 128;
@@ -39,18 +29,10 @@ void k_linear_tile(LinearArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_m = wave % WM, wave_n = wave / WM;
 
-    // ---- which tile: an XCD (workgroups number 0 .. 7 in turn) takes a run of the tiles, which go down eight tiles of rows before the next columns ----
     const int rows = rows_there(a);
-    const int m_tiles = (rows + TM - 1) / TM, total = m_tiles * a.n_tiles * a.splits;
-    const int xcd = (int)blockIdx.x & 7, first = (int)(((int64_t)total * xcd) >> 3), behind = (int)(((int64_t)total * (xcd + 1)) >> 3);
-    const int number = first + ((int)blockIdx.x >> 3);
-    if (number >= behind) return;
-    const int split = number % a.splits, tile = number / a.splits;
-    constexpr int GROUP = 8;
-    const int group = tile / (GROUP * a.n_tiles), in_group = tile - group * GROUP * a.n_tiles;
-    const int high = min(GROUP, m_tiles - group * GROUP);
-    const int tile_m = group * GROUP + in_group % high, tile_n = in_group / high;
-    const int r0 = tile_m * TM, n0 = tile_n * TN;
+    const TileOf t = tile_of<TM>(a, rows);
+    if (!t.there) return;
+    const int split = t.split, r0 = t.tile_m * TM, n0 = t.tile_n * TN;
 
     const int here = min(rows - r0, TM), cols = min(a.n - n0, TN);
     const u32x4_t rsrc_x = make_rsrc_words(a.x + (int64_t)r0 * a.x_row, (uint32_t)((int64_t)(here - 1) * a.x_row + a.k) * 2u);
@@ -188,150 +170,7 @@ void k_linear_tile(LinearArgs a)
     wait_vmcnt<0>();
     __syncthreads();
 
-    // ---- pieces of the reduction (small tiles): written in the registers' order, added by the last workgroup in the pieces' order ----
-    if (TM == 128 && a.splits > 1) {
-        constexpr uint32_t ITEMS = (uint32_t)PB * CB * 4 * NT;     // of four sums
-        const auto part = __builtin_amdgcn_make_buffer_rsrc(a.part + (int64_t)tile * a.splits * (ITEMS * 4), 0, (uint32_t)a.splits * ITEMS * 16u, 0x00020000);
-        each<PB * CB * 4>([&](auto i_c) __attribute__((always_inline)) {
-            constexpr int i = decltype(i_c)::value, q = i % 4 * 4;
-            const f32x16_t &s = acc[i / 4 / CB][i / 4 % CB];
-            const f32x4_t v = {s[q], s[q + 1], s[q + 2], s[q + 3]};
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), part, ((uint32_t)split * ITEMS + (uint32_t)i * NT + threadIdx.x) * 16u, 0, kPiecesPastCaches);
-        });
-        if (!last_piece(a.arrived + tile, a.splits, reinterpret_cast<int32_t *>(smem_raw))) return;
-        __syncthreads();
-#pragma unroll
-        for (int p = 0; p < PB; ++p)
-#pragma unroll
-            for (int b = 0; b < CB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) acc[p][b][i] = 0.f;
-        for (int n = 0; n < a.splits; ++n)
-            each<PB * CB * 4>([&](auto i_c) __attribute__((always_inline)) {
-                constexpr int i = decltype(i_c)::value, q = i % 4 * 4;
-                const f32x4_t v = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(part, ((uint32_t)n * ITEMS + (uint32_t)i * NT + threadIdx.x) * 16u, 0, kPiecesPastCaches));
-                f32x16_t &s = acc[i / 4 / CB][i / 4 % CB];
-                s[q] += v[0], s[q + 1] += v[1], s[q + 2] += v[2], s[q + 3] += v[3];
-            });
-    }
-
-    // ---- epilogue: a wave's blocks of 32 rows go through LDS of its own ----
-    // (Sums of 256 registers are accumulators of the matrix instructions; left to itself the compiler copies all of them out at once and spills.  They stay
-    // until they are asked for.)
-    auto sums_of = [&](auto p_c, auto b_c) __attribute__((always_inline)) -> f32x16_t {
-        f32x16_t &s = acc[decltype(p_c)::value][decltype(b_c)::value];
-        if constexpr (CB == 4) __asm__ volatile("" : "+a"(s));
-        return s;
-    };
-    const int col0 = n0 + wave_n * (CB * 32), half = lane >> 5;
-    if (a.wide_out && a.act <= FC_ACT_RELU) {
-        // In the registers' order (a lane: a row, fours of columns): residuals come in and results go out in 16-byte pieces of rows.
-        constexpr int PPR = CB * 32 * (int)sizeof(TO) / 16, RPI = 64 / PPR, NI = 32 / RPI;    // pieces a row, rows a round, rounds
-        constexpr uint32_t OP = CB * 32 * sizeof(TO) + 16;
-        static_assert((size_t)WM * WN * 32 * OP <= kTileLds<WM, WN, PB, CB>, "the waves' shares");
-        unsigned char *const os = smem_raw + wave * (32 * OP), *const mine = os + (lane & 31) * OP + half * (4 * sizeof(TO));
-        constexpr int EPP = 16 / (int)sizeof(TO);
-        const int prow = lane / PPR, pcol = col0 + lane % PPR * EPP;
-        unsigned char *const piece_at = os + prow * OP + lane % PPR * 16;
-        f32x4_t bias[CB * 4];
-        each<CB * 4>([&](auto i_c) __attribute__((always_inline)) {
-            constexpr int i = decltype(i_c)::value;
-            const int c = col0 + i * 8 + half * 4;
-            bias[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            if (a.bias && c < a.n) bias[i] = *reinterpret_cast<const f32x4_t *>(a.bias + c);
-        });
-        each<PB>([&](auto p_c) __attribute__((always_inline)) {
-            constexpr int p = decltype(p_c)::value;
-            const int row0 = r0 + (wave_m * PB + p) * 32 + prow;
-            if (a.residual) {
-                const TO *from = static_cast<const TO *>(a.residual) + pcol;
-                uint4 more[NI];
-#pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    more[i] = make_uint4(0, 0, 0, 0);
-                    if (row0 + i * RPI < rows && pcol < a.n) more[i] = *reinterpret_cast<const uint4 *>(from + (int64_t)(row0 + i * RPI) * a.residual_row);
-                }
-#pragma unroll
-                for (int i = 0; i < NI; ++i) *reinterpret_cast<uint4 *>(piece_at + i * RPI * OP) = more[i];
-                wave_lds_order();
-            }
-            const bool relu_first = a.act == FC_ACT_RELU && !a.residual_first, relu_last = a.act == FC_ACT_RELU && a.residual_first;
-            each<CB * 4>([&](auto i_c) __attribute__((always_inline)) {
-                constexpr int i = decltype(i_c)::value, q = i % 4 * 4;
-                const f32x16_t s = sums_of(p_c, std::integral_constant<int, i / 4>{});
-                f32x4_t v = f32x4_t{s[q], s[q + 1], s[q + 2], s[q + 3]} + bias[i];
-                TO *const at = reinterpret_cast<TO *>(mine) + i * 8;
-                if (relu_first)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = relu_keep_nan(v[j]);
-                if (a.residual) v += load4_float(at);
-                if (relu_last)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = relu_keep_nan(v[j]);
-                store4<DT, TO>(at, v[0], v[1], v[2], v[3]);
-                if constexpr (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (the compiler would copy all sums out of the accumulators first)
-            });
-            wave_lds_order();
-            uint4 done[NI];
-#pragma unroll
-            for (int i = 0; i < NI; ++i) done[i] = *reinterpret_cast<const uint4 *>(piece_at + i * RPI * OP);
-            TO *to = static_cast<TO *>(a.out) + pcol;
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-                if (row0 + i * RPI < rows && pcol < a.n) *reinterpret_cast<uint4 *>(to + (int64_t)(row0 + i * RPI) * a.out_row) = done[i];
-            wave_lds_order();
-            __builtin_amdgcn_sched_barrier(0);
-        });
-        return;
-    }
-    // Activations with more arithmetic, and rows of any alignment: the sums go through LDS, and loops that are not unrolled finish them.
-    constexpr int LPR = CB * 4, RPI = 64 / LPR;      // lanes a row, rows a round, of eight columns
-    const int c8 = lane % LPR, col8 = col0 + c8 * 8;
-    float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (a.wide_out && a.bias && col8 < a.n) load8_float(a.bias + col8, bias);
-    constexpr int OP = CB * 32 + 4;     // floats from row to row
-    static_assert((size_t)WM * WN * 32 * OP * 4 <= kTileLds<WM, WN, PB, CB>, "the waves' shares");
-    float *const os = reinterpret_cast<float *>(smem_raw) + wave * (32 * OP);
-    // (A loop over p that is not unrolled would put the sums into memory.)
-    each<PB>([&](auto p_c) __attribute__((always_inline)) {
-        constexpr int p = decltype(p_c)::value;
-        each<CB>([&](auto b_c) __attribute__((always_inline)) {
-            const f32x16_t s = sums_of(p_c, b_c);
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<f32x4_t *>(os + (lane & 31) * OP + decltype(b_c)::value * 32 + q * 8 + half * 4) = f32x4_t{s[q * 4], s[q * 4 + 1], s[q * 4 + 2], s[q * 4 + 3]};
-        });
-        wave_lds_order();
-        const int row0 = r0 + (wave_m * PB + p) * 32, here = min(rows - row0, 32);
-        if (a.wide_out) {
-            // two rows' residuals are sent for together
-            constexpr int AT_ONCE = 2;
-#pragma unroll 1
-            for (int i = 0; i < 32 / RPI; i += AT_ONCE) {
-                float more[AT_ONCE][8];
-                if (a.residual)
-#pragma unroll
-                    for (int u = 0; u < AT_ONCE; ++u) {
-                        const int row = min(row0 + (i + u) * RPI + lane / LPR, rows - 1);
-                        load8_float(static_cast<const TO *>(a.residual) + row * a.residual_row + (col8 < a.n ? col8 : 0), more[u]);
-                    }
-#pragma unroll
-                for (int u = 0; u < AT_ONCE; ++u) {
-                    const int r = (i + u) * RPI + lane / LPR, row = row0 + r;
-                    float v[8];
-                    load8_float(os + r * OP + c8 * 8, v);
-                    finish_eight(a, bias, more[u], v);
-                    if (row < rows && col8 < a.n) store8(static_cast<TO *>(a.out) + row * a.out_row + col8, v);
-                }
-            }
-        } else {        // a lane a column
-#pragma unroll 1
-            for (int r = 0; r < here; ++r)
-                for (int c = lane; c < CB * 32; c += 64)
-                    if (col0 + c < a.n) finish_one<TO>(a, row0 + r, col0 + c, os[r * OP + c]);
-        }
-        wave_lds_order();
-    });
+    finish_tile<DT, TO, WM, WN, PB, CB, TM == 128, kTileLds<WM, WN, PB, CB>>(a, acc, smem_raw, t, rows, wave, wave_m, wave_n);
 }
 
 // Rows laid out anew: padded_k elements each, zeros behind k.

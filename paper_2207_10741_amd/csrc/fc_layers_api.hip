@@ -1,7 +1,6 @@
 // C ABI of the matrix product and of group norm: argument checks on the host, then launches.
 #include "fc_layers_internal.hpp"
 #include <math.h>
-#include <stdlib.h>
 
 using namespace fc;
 
@@ -10,7 +9,6 @@ namespace {
 bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 bool stride_ok(int64_t stride, int64_t least) { return stride >= least && stride <= FC_LAYERS_MAX_STRIDE; }
 int32_t ceil_div(int64_t a, int64_t b) { return (int32_t)((a + b - 1) / b); }
-int32_t min_of(int32_t a, int32_t b) { return a < b ? a : b; }
 int size_of(int32_t dtype) { return dtype == FC_F32 ? 4 : 2; }
 
 // ---- the matrix product ----
@@ -29,59 +27,88 @@ int32_t check_linear(const fc_linear_desc *d, bool residual)
     return FC_OK;
 }
 
+// What a cut of the product takes, in microseconds: beginning and ending a launch, its rounds of stages of 64, the weights' bytes where the kernel waits for
+// them, and joining pieces.  From times of every form on 41 products (64 .. 4096 rows, 256 .. 8192 columns of x, 1024 .. 16384 of out), which it gives to within a fifth or
+// so; what it is for is the order of the forms.  Measured there, rows x k x n (rings / shared stages / tiles of 128 / of 256):
+//   64 x 4096 x 4096 14.7 / 15.0 in four pieces      128 x 1024 x 1024 6.0 / 10.8 / 11.3         256 x 4096 x 4096 30.6 / 23.1 in four / 25.1 in four
+//   512 x 4096 x 4096 59.5 / 30.1 in two / 35.3      1024 x 4096 x 4096 121 / 43.6 / 52.4 / 80.8   2048 x 4096 x 4096 - / - / 71.2 / 82.5
+//   4096 x 4096 x 4096 - / - / 141 / 109             2048 x 8192 x 1024 - / - / 51.6 in four, 87.4 in one / 146
+struct Cut {
+    double us;
+    int32_t form, tile_m, tile_n, splits;
+    bool ring;
+};
+double rounds_of(int64_t units) { return (double)((units + 255) / 256); }
+// tiles of 128 columns; rows of a tile over 128
+double join_us(int64_t units, int32_t splits, double rows) { return splits > 1 ? 2.5 + 0.03 * (double)units * rows : 0.; }
+
+Cut best_cut(int32_t rows, int32_t n, int32_t k)
+{
+    const int32_t chunks = ceil_div(k, kLinearK);
+    const double weights = 2e-6 * (double)n * (double)k / 6.;
+    Cut best = {1e30, 0, 0, 0, 1, false};
+    auto take = [&](const Cut &c) {
+        if (c.us < best.us) best = c;
+    };
+    // rings: a wave's steps; of 64, 32 or 16 rows and 16, 32 or 64 columns
+    const int32_t ring_m = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    static const double step_us[3][3] = {{0.2, 0.3, 0.}, {0.25, 0.33, 0.45}, {0.36, 0.5, 0.67}};
+    for (int32_t i = 0; i < (ring_m == 16 ? 2 : 3); ++i) {
+        const int64_t units = (int64_t)ceil_div(rows, ring_m) * ceil_div(n, 16 << i);
+        const double steps = ceil_div(chunks, ring_m == 64 || i == 2 ? 4 : 8);
+        // (several tiles of rows: the weights come from the L2, and the steps wait for it as the chip fills)
+        const double full = rows > ring_m ? 1. + 0.6 * (double)(units < 256 ? units : 256) / 256. : 1.;
+        take({1.2 + rounds_of(units) * (2. + steps * step_us[ring_m / 32][i] * full) + weights, 0, ring_m, 16 << i, 1, true});
+    }
+    for (int32_t splits = 1; splits <= 16; splits *= 2) {
+        if (splits > 1 && chunks / splits < 2) break;
+        const int32_t stages = ceil_div(chunks, splits);
+        // shared stages
+        const int32_t m = rows <= 64 ? 64 : 128;
+        const int64_t units = (int64_t)ceil_div(rows, m) * ceil_div(n, 128) * splits;
+        take({1. + rounds_of(units) * (2.5 + stages * (m == 64 ? 0.31 : units < 256 ? 0.45 : 0.5)) + (m == 64 ? 0.85 : 0.7) * weights + join_us(units, splits, m / 128.), 2, m, 128, splits, false});
+        // tiles of 128: two on a CU
+        if (rows > 64 && splits <= 8) {
+            const int64_t u = (int64_t)ceil_div(rows, 128) * ceil_div(n, 128) * splits;
+            take({3.5 + stages * (u <= 256 ? 0.8 : 1.1 * (double)((u + 511) / 512)) + join_us(u, splits, 1.), 1, 128, 128, splits, false});
+        }
+    }
+    const int64_t large = (int64_t)ceil_div(rows, 256) * ceil_div(n, 256);
+    take({3.5 + rounds_of(large) * (5. + chunks * (1.25 + 0.35 * (large < 256 ? large : 256) / 256.)), 1, 256, 256, 1, false});
+    return best;
+}
+
 int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
 {
-    const int32_t rows = d->rows < 1 ? 1 : d->rows;
+    const int32_t rows = d->rows < 1 ? 1 : d->rows, chunks = ceil_div(d->k, kLinearK);
     const bool pieces = d->k % 8 == 0 && !(d->flags & FC_ANY_POINTERS), x_pieces = pieces && d->x_row % 8 == 0, w_pieces = pieces && d->w_row % 8 == 0;
-    const int32_t chunks = ceil_div(d->k, kLinearK);
     p->padded_k = (int64_t)chunks * kLinearK;
     p->pad_x = p->pad_w = false;
     p->wide = x_pieces && w_pieces;
-    p->splits = 1;
-    p->per_split = chunks;
     p->per_wave = 0;
-    p->ring = false;
-    if (getenv("LF") ? rows <= atoi(getenv("LF")) : rows <= 64) {
+    if (rows <= 64 && !p->wide) {
+        // straight into fragments: laying the weights out anew takes as long as the product (33 MB: 20 us)
         p->form = 0;
-        p->ring = p->wide && rows > (getenv("LR") ? atoi(getenv("LR")) : 0);
+        p->ring = false;
         p->tile_m = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-        if (p->ring) p->tile_n = getenv("LN") ? atoi(getenv("LN")) : d->n >= 16384 && rows > 16 ? 64 : d->n >= 8192 ? 32 : 16;
-        else p->tile_n = d->n >= 16384 ? (p->tile_m == 64 ? 64 : 32) : 16;
-        p->m_tiles = ceil_div(rows, p->tile_m);
-        p->n_tiles = ceil_div(d->n, p->tile_n);
-        const int32_t wanted = ceil_div(256, (int64_t)p->n_tiles * p->m_tiles), most = chunks < 16 ? 1 : chunks / 8;
-        p->per_split = ceil_div(chunks, wanted < most ? wanted : most);
-        p->splits = ceil_div(chunks, p->per_split);
-        p->per_wave = ceil_div(p->per_split, p->ring && (p->tile_m == 64 || p->tile_n == 64) ? 4 : 8);
-    } else if (getenv("LS") ? rows <= atoi(getenv("LS")) : rows <= 128) {
-        p->form = 2;
-        p->tile_m = rows <= 64 ? 64 : 128;
-        p->tile_n = 128;
-        p->m_tiles = ceil_div(rows, p->tile_m);
-        p->n_tiles = ceil_div(d->n, p->tile_n);
-        const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
-        if (tiles < 256) {
-            const int32_t wanted = (int32_t)(256 / tiles), most = chunks < 8 ? 1 : chunks / 4;
-            p->per_split = ceil_div(chunks, min_of(wanted < 1 ? 1 : wanted < most ? wanted : most, getenv("LW") ? atoi(getenv("LW")) : 8));
-            p->splits = ceil_div(chunks, p->per_split);
-        }
-        p->pad_x = !x_pieces;
-        p->pad_w = !w_pieces;
+        p->tile_n = d->n >= 16384 ? (p->tile_m == 64 ? 64 : 32) : 16;
+        const int32_t wanted = ceil_div(256, ceil_div(d->n, p->tile_n)), most = chunks < 16 ? 1 : chunks / 8;
+        p->splits = wanted < most ? wanted : most;
     } else {
-        p->form = 1;
-        const int64_t large = (int64_t)ceil_div(rows, 256) * ceil_div(d->n, 256);
-        p->tile_m = p->tile_n = large >= 192 ? 256 : 128;
-        p->m_tiles = ceil_div(rows, p->tile_m);
-        p->n_tiles = ceil_div(d->n, p->tile_n);
-        const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
-        if (p->tile_m == 128 && tiles < 256) {
-            const int32_t wanted = (int32_t)(512 / tiles), most = chunks < 8 ? 1 : chunks / 4;
-            p->per_split = ceil_div(chunks, wanted < most ? wanted : most);
-            p->splits = ceil_div(chunks, p->per_split);
-        }
+        const Cut c = best_cut(rows, d->n, d->k);
+        p->form = c.form;
+        p->ring = c.ring;
+        p->tile_m = c.tile_m;
+        p->tile_n = c.tile_n;
+        p->splits = c.splits;
         p->pad_x = !x_pieces;
         p->pad_w = !w_pieces;
     }
+    p->m_tiles = ceil_div(rows, p->tile_m);
+    p->n_tiles = ceil_div(d->n, p->tile_n);
+    p->per_split = ceil_div(chunks, p->splits);
+    p->splits = ceil_div(chunks, p->per_split);
+    if (p->form == 0) p->per_wave = ceil_div(p->per_split, p->ring && (p->tile_m == 64 || p->tile_n == 64) ? 4 : 8);
     const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
     if (tiles * p->splits >= INT32_MAX / 1024) return FC_ERR_RANGE;     // (a dimension of a grid is counted in threads)
     p->counters = p->splits == 1 ? 0 : align_up((size_t)tiles * sizeof(int32_t), 256);

@@ -1,13 +1,14 @@
 // Matrix product of few rows (one user's next token, a batch's next tokens): out = act(x w^T + bias) + residual.
 //
-// Every weight is needed once, so the weights' bytes bound it: they go straight from memory to the registers that the 16x16x32 matrix
-// instructions read, with no LDS and no barrier between.  A workgroup of eight waves has 16 NB columns of the output (rows of w) and 16 RB rows of x; its
-// waves divide the reduction among them, so that a launch of few columns still has all of its loads under way at once, and add their sums through LDS in
-// order.  Where columns are fewer than the chip wants workgroups, workgroups divide the reduction as well (pieces, joined by the last in order).
+// Every weight is needed once, so the weights' bytes bound it.  A workgroup has 16 NB columns of the output (rows of w) and 16 RB rows of x; its waves divide the
+// reduction among them, so that a launch of few columns still has all of its loads under way at once, and add their sums through LDS in order.
+//   k_linear_ring   rows of whole 16-byte pieces: both operands come in lines of 128 bytes through a ring in LDS of each wave's own.  1 x 4096 x 4096 9.9 us (33 MB: 6.4 at
+//                   the rate of a copy, and a launch), 1 x 4096 x 16384 30.8 (4.4 TB/s), 64 x 4096 x 16384 36
+//   k_linear_rows   rows of any alignment: straight from memory to the registers that the matrix instructions read, with no LDS and no barrier between.  Where columns are
+//                   fewer than the chip wants workgroups, workgroups divide the reduction as well (pieces, joined by the last in order)
 //
-// A lane of an operand holds eight consecutive elements of one row: lanes 0 .. 15 the rows, quarter = lane / 16 the eighths of 32 elements.
+// A lane of an operand of the 16x16x32 instructions holds eight consecutive elements of one row: lanes 0 .. 15 the rows, quarter = lane / 16 the eighths of 32 elements.
 #include "fc_layers_internal.hpp"
-#include <stdlib.h>
 
 namespace fc {
 
@@ -28,26 +29,19 @@ __device__ __forceinline__ RowsTile rows_tile(const LinearArgs &a)
     return t;
 }
 
-// Eight elements c .. of a row.  FULL: all are inside k; else those behind are zero.  WIDE: the row's pieces are aligned to 16 bytes.
-template <bool WIDE, bool FULL> __device__ __forceinline__ uint4 row_piece(const uint16_t *__restrict__ row, int c, int k)
+// Eight elements c .. of a row of any alignment.  FULL: all are inside k; else those behind are zero.
+template <bool FULL> __device__ __forceinline__ uint4 row_piece(const uint16_t *__restrict__ row, int c, int k)
 {
+    uint4 v;
     if constexpr (FULL) {
-        if constexpr (WIDE) return *reinterpret_cast<const uint4 *>(row + c);
-        uint4 v;
         __builtin_memcpy(&v, row + c, 16);
-        return v;
-    } else if constexpr (WIDE) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(row + (c < k ? c : 0));
-        return c < k ? v : make_uint4(0, 0, 0, 0);
     } else {
-        uint32_t v[4];
+        uint16_t e[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = c + 2 * j < k ? row[c + 2 * j] : 0, hi = c + 2 * j + 1 < k ? row[c + 2 * j + 1] : 0;
-            v[j] = lo | hi << 16;
-        }
-        return make_uint4(v[0], v[1], v[2], v[3]);
+        for (int j = 0; j < 8; ++j) e[j] = c + j < k ? row[c + j] : 0;
+        __builtin_memcpy(&v, e, 16);
     }
+    return v;
 }
 
 template <int DT> __device__ __forceinline__ f32x4_t mfma16_of(const uint4 &a, const uint4 &b, const f32x4_t &c)
@@ -103,7 +97,7 @@ __device__ __forceinline__ void finish_rows(const LinearArgs &a, const f32x4_t (
 }
 
 // RB, NB: blocks of 16 rows and of 16 columns; U: chunks of 64 whose loads are sent for together.
-template <int DT, typename TO, int RB, int NB, int U, bool WIDE>
+template <int DT, typename TO, int RB, int NB, int U>
 __global__ __launch_bounds__(kRowsThreads, 2)
 void k_linear_rows(LinearArgs a)
 {
@@ -140,9 +134,9 @@ void k_linear_rows(LinearArgs a)
         for (int h = 0; h < 2; ++h) {
             const int c = chunk * kLinearK + h * 32 + at;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) wf[u][b][h] = row_piece<WIDE, FULL>(wp[b], c, a.k);
+            for (int b = 0; b < NB; ++b) wf[u][b][h] = row_piece<FULL>(wp[b], c, a.k);
 #pragma unroll
-            for (int b = 0; b < RB; ++b) xf[u][b][h] = row_piece<WIDE, FULL>(xp[b], c, a.k);
+            for (int b = 0; b < RB; ++b) xf[u][b][h] = row_piece<FULL>(xp[b], c, a.k);
         }
     };
     auto multiply = [&](int u) __attribute__((always_inline)) {
@@ -182,30 +176,26 @@ void k_linear_rows(LinearArgs a)
     finish_rows<TO, RB, NB, kRowsWaves>(a, acc, sums, &flag, rows, r0, n0, tile, split);
 }
 
-template <int DT, typename TO, int RB, int NB, int U, bool WIDE> static hipError_t launch_rows_of(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
+template <int DT, typename TO, int RB, int NB, int U> static hipError_t launch_rows_of(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
     constexpr size_t lds = (size_t)kRowsWaves * RB * NB * 1024;
     if (lds > 65536) {
-        const hipError_t e = raise_dynamic_lds<&k_linear_rows<DT, TO, RB, NB, U, WIDE>>(lds);
+        const hipError_t e = raise_dynamic_lds<&k_linear_rows<DT, TO, RB, NB, U>>(lds);
         if (e != hipSuccess) return e;
     }
-    k_linear_rows<DT, TO, RB, NB, U, WIDE><<<dim3((uint32_t)((p.n_tiles + 7) / 8 * 8 * p.m_tiles * p.splits)), dim3(kRowsThreads), lds, s>>>(a);
+    k_linear_rows<DT, TO, RB, NB, U><<<dim3((uint32_t)((p.n_tiles + 7) / 8 * 8 * p.m_tiles * p.splits)), dim3(kRowsThreads), lds, s>>>(a);
     return hipGetLastError();
 }
 
 template <int DT, typename TO> static hipError_t launch_rows_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
-    auto form = [&](auto wide) {
-        constexpr bool W = decltype(wide)::value;
-        if (p.tile_m == 16) return p.tile_n == 16 ? launch_rows_of<DT, TO, 1, 1, 6, W>(a, p, s) : launch_rows_of<DT, TO, 1, 2, 4, W>(a, p, s);
-        if (p.tile_m == 32) return p.tile_n == 16 ? launch_rows_of<DT, TO, 2, 1, 4, W>(a, p, s) : launch_rows_of<DT, TO, 2, 2, 3, W>(a, p, s);
-        return p.tile_n == 16 ? launch_rows_of<DT, TO, 4, 1, 3, W>(a, p, s) : launch_rows_of<DT, TO, 4, 4, 2, W>(a, p, s);
-    };
-    return p.wide ? form(std::true_type{}) : form(std::false_type{});
+    if (p.tile_m == 16) return p.tile_n == 16 ? launch_rows_of<DT, TO, 1, 1, 6>(a, p, s) : launch_rows_of<DT, TO, 1, 2, 4>(a, p, s);
+    if (p.tile_m == 32) return p.tile_n == 16 ? launch_rows_of<DT, TO, 2, 1, 4>(a, p, s) : launch_rows_of<DT, TO, 2, 2, 3>(a, p, s);
+    return p.tile_n == 16 ? launch_rows_of<DT, TO, 4, 1, 3>(a, p, s) : launch_rows_of<DT, TO, 4, 4, 2>(a, p, s);
 }
 
-// The same with both operands through LDS.  Loads of 16 rows of 64 bytes come at 18 bytes a clock and CU, whole lines of 128 bytes at 64: with 17 rows and more, whose x is
-// as many bytes as the weights that a workgroup reads, that is slower than memory (64 x 4096 x 16384: 44 us).  A wave has a ring of D chunks of its own and no one to
+// Both operands through LDS.  Loads of 16 rows of 64 bytes come at 18 bytes a clock and CU, whole lines of 128 bytes at 64: with some dozens of rows, whose x is
+// as many bytes as the weights that a workgroup reads, the first is slower than memory (64 x 4096 x 16384 straight into registers 44 us, so 36).  A wave has a ring of D chunks of its own and no one to
 // wait for: its loads are D - 1 chunks ahead, and the barrier comes when the sums are added.
 template <int RB, int NB, int WAVES, int D> constexpr size_t kRingLds = (size_t)WAVES * D * (RB + NB) * 2048;
 
@@ -304,11 +294,8 @@ template <int DT, typename TO, int RB, int NB, int WAVES, int D> static hipError
 
 template <int DT, typename TO> static hipError_t launch_ring_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
-    const int v = getenv("LV") ? atoi(getenv("LV")) : 0;
     if (p.tile_m == 16) return p.tile_n == 16 ? launch_ring_of<DT, TO, 1, 1, 8, 4>(a, p, s) : launch_ring_of<DT, TO, 1, 2, 8, 3>(a, p, s);
     if (p.tile_m == 32) return p.tile_n == 16 ? launch_ring_of<DT, TO, 2, 1, 8, 3>(a, p, s) : p.tile_n == 32 ? launch_ring_of<DT, TO, 2, 2, 8, 2>(a, p, s) : launch_ring_of<DT, TO, 2, 4, 4, 3>(a, p, s);
-    if (v == 1) return p.tile_n == 16 ? launch_ring_of<DT, TO, 4, 1, 8, 2>(a, p, s) : launch_ring_of<DT, TO, 4, 2, 4, 3>(a, p, s);
-    if (v == 2) return p.tile_n == 16 ? launch_ring_of<DT, TO, 4, 1, 4, 3>(a, p, s) : launch_ring_of<DT, TO, 4, 2, 4, 2>(a, p, s);
     return p.tile_n == 16 ? launch_ring_of<DT, TO, 4, 1, 4, 4>(a, p, s) : p.tile_n == 32 ? launch_ring_of<DT, TO, 4, 2, 4, 3>(a, p, s) : launch_ring_of<DT, TO, 4, 4, 4, 2>(a, p, s);
 }
 

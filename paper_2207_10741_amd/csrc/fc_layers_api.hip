@@ -74,7 +74,7 @@ Cut best_cut(int32_t rows, int32_t n, int32_t k)
         }
     }
     const int64_t large = (int64_t)ceil_div(rows, 256) * ceil_div(n, 256);
-    take({3.5 + rounds_of(large) * (5. + chunks * (1.25 + 0.35 * (large < 256 ? large : 256) / 256.)), 1, 256, 256, 1, false});
+    take({3.5 + rounds_of(large) * (5. + chunks * (1.25 + 0.35 * (large < 256 ? large : 256) / 256.)), 3, 256, 256, 1, false});
     return best;
 }
 
@@ -259,7 +259,9 @@ int32_t fc_linear(const fc_linear_desc *d, const void *x, const void *w, const f
         if (pw) a.w = pw, a.w_row = p.padded_k;
         if (px && pw) a.k = (int32_t)p.padded_k;
     }
-    if (e == hipSuccess) e = p.form == 0 ? launch_linear_rows(a, p, d->dtype, d->out_dtype, s) : p.form == 2 ? launch_linear_stream(a, p, d->dtype, d->out_dtype, s) : launch_linear_tile(a, p, d->dtype, d->out_dtype, s);
+    if (e == hipSuccess)
+        e = p.form == 0 ? launch_linear_rows(a, p, d->dtype, d->out_dtype, s) : p.form == 1 ? launch_linear_tile(a, p, d->dtype, d->out_dtype, s)
+            : p.form == 2 ? launch_linear_stream(a, p, d->dtype, d->out_dtype, s) : launch_linear_large(a, p, d->dtype, d->out_dtype, s);
     return e == hipSuccess ? FC_OK : FC_ERR_HIP;
 }
 

@@ -183,7 +183,7 @@ constexpr int kLinearK = 64;        // columns of a stage, or chunk
 
 // How a product is cut.
 struct LinearPlan {
-    int32_t form;                   // 0: few rows, 1: many, 2: some dozens; tile_m, tile_n: rows and columns of a workgroup
+    int32_t form;                   // 0: few rows, 2: some dozens, 1: many in tiles of 128, 3: of 256; tile_m, tile_n: rows and columns of a workgroup
     int32_t tile_m, tile_n, m_tiles, n_tiles, splits, per_split, per_wave;
     bool wide, ring;                // x's and w's rows are whole 16-byte pieces (few rows); they go through LDS
     bool pad_x, pad_w;              // laid out anew (many rows)
@@ -194,6 +194,7 @@ struct LinearPlan {
 hipError_t launch_linear_rows(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
 hipError_t launch_linear_tile(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
 hipError_t launch_linear_stream(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
+hipError_t launch_linear_large(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
 // Rows of x, of w, or of both, as rows of padded_k elements with zeros behind k.
 hipError_t launch_linear_pad(const LinearArgs &a, const LinearPlan &p, uint16_t *x, uint16_t *w, hipStream_t s);
 

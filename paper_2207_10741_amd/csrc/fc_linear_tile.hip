@@ -15,7 +15,7 @@ namespace fc {
 template <int WM, int WN, int PB, int CB> constexpr size_t kTileLds = (size_t)(3 * WM * PB + 2 * WN * CB) * 32 * 128;
 
 template <int DT, typename TO, int WM, int WN, int PB, int CB>
-__global__ __launch_bounds__(WM * WN * 64, CB == 4 ? 1 : 2)
+__global__ __launch_bounds__(WM * WN * 64, 2)
 void k_linear_tile(LinearArgs a)
 {
     constexpr int NT = WM * WN * 64, TM = WM * PB * 32, TN = WN * CB * 32;
@@ -52,23 +52,30 @@ void k_linear_tile(LinearArgs a)
     }
     const int k0 = split * a.per_split * kLinearK, stages = min(a.per_split, (a.k - k0 + kLinearK - 1) / kLinearK);
     const int k_end = min(a.k, k0 + stages * kLinearK);
-    // the next stages to be sent for (behind the last one: zeros)
-    struct Next {
-        int k;
-        uint32_t s;
-        bool ok;
-    } nx = {k0, 0, false}, nw = {k0, 0, false};
-    auto advance = [&](Next &n) __attribute__((always_inline)) {
-        n.ok = n.k + piece * 8 < k_end;
-        n.s = n.k < k_end ? (uint32_t)n.k * 2u : 0u;
-        n.k += kLinearK;
+    // The next stages to be sent for.  From the stage on that the reduction ends in, pieces behind its end come from out of range (zeros): there is no stage
+    // after it that would want them back.
+    int nx_k = k0, nw_k = k0;
+    uint32_t nx_s = 0, nw_s = 0;
+    auto advance_x = [&]() __attribute__((always_inline)) {
+        if (nx_k + kLinearK > k_end)
+#pragma unroll
+            for (int j = 0; j < XL; ++j) xo[j] = nx_k + piece * 8 < k_end ? xo[j] : kOutOfRange;
+        nx_s = nx_k < k_end ? (uint32_t)nx_k * 2u : 0u;
+        nx_k += kLinearK;
+    };
+    auto advance_w = [&]() __attribute__((always_inline)) {
+        if (nw_k + kLinearK > k_end)
+#pragma unroll
+            for (int j = 0; j < WL; ++j) wo[j] = nw_k + piece * 8 < k_end ? wo[j] : kOutOfRange;
+        nw_s = nw_k < k_end ? (uint32_t)nw_k * 2u : 0u;
+        nw_k += kLinearK;
     };
     const uint32_t lds_wave = lds0 + (uint32_t)wave * 1024u;
     auto issue_x = [&](int j, uint32_t buf) __attribute__((always_inline)) {
-        dma_load16_any(rsrc_x, nx.ok ? xo[j] : kOutOfRange, nx.s, lds_wave + buf * XB + (uint32_t)j * (RPL * 128u));
+        dma_load16_any(rsrc_x, xo[j], nx_s, lds_wave + buf * XB + (uint32_t)j * (RPL * 128u));
     };
     auto issue_w = [&](int j, uint32_t buf) __attribute__((always_inline)) {
-        dma_load16_any(rsrc_w, nw.ok ? wo[j] : kOutOfRange, nw.s, lds_wave + W0 + buf * WB + (uint32_t)j * (RPL * 128u));
+        dma_load16_any(rsrc_w, wo[j], nw_s, lds_wave + W0 + buf * WB + (uint32_t)j * (RPL * 128u));
     };
 
     // where this lane's fragments are: row of the block, half of the k-step
@@ -98,19 +105,19 @@ void k_linear_tile(LinearArgs a)
         });
     };
 
-    advance(nx);
-    advance(nw);
+    advance_x();
+    advance_w();
 #pragma unroll
     for (int j = 0; j < XL; ++j) issue_x(j, 0);
 #pragma unroll
     for (int j = 0; j < WL; ++j) issue_w(j, 0);
-    advance(nx);
+    advance_x();
 #pragma unroll
     for (int j = 0; j < XL; ++j) issue_x(j, 1);
     wait_vmcnt<XL>();
     __syncthreads();
-    advance(nx);
-    advance(nw);
+    advance_x();
+    advance_w();
     each<NS - BARRIER>([&](auto q_c) __attribute__((always_inline)) { issue_at(q_c, 2, 1); });
 
     Frag<DT> wf[2][CB], xf[2][PB];
@@ -140,8 +147,8 @@ void k_linear_tile(LinearArgs a)
                     lds_reads_done();
                     wait_vmcnt<XL>();
                     __syncthreads();
-                    advance(nx);
-                    advance(nw);
+                    advance_x();
+                    advance_w();
                 }
                 acc[i / CB][i % CB] = mfma32<DT>(wf[kk & 1][i % CB], xf[kk & 1][i / CB], acc[i / CB][i % CB]);
                 __builtin_amdgcn_sched_barrier(0);
@@ -170,7 +177,7 @@ void k_linear_tile(LinearArgs a)
     wait_vmcnt<0>();
     __syncthreads();
 
-    finish_tile<DT, TO, WM, WN, PB, CB, TM == 128, kTileLds<WM, WN, PB, CB>>(a, acc, smem_raw, t, rows, wave, wave_m, wave_n);
+    finish_tile<DT, TO, WM, WN, PB, CB, true, kTileLds<WM, WN, PB, CB>>(a, acc, smem_raw, t, rows, wave, wave_m, wave_n);
 }
 
 // Rows laid out anew: padded_k elements each, zeros behind k.
@@ -213,10 +220,7 @@ template <int DT, typename TO, int WM, int WN, int PB, int CB> static hipError_t
     return hipGetLastError();
 }
 
-template <int DT, typename TO> static hipError_t launch_tile_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
-{
-    return p.tile_m == 256 ? launch_tile_of<DT, TO, 2, 2, 4, 4>(a, p, s) : launch_tile_of<DT, TO, 2, 2, 2, 2>(a, p, s);
-}
+template <int DT, typename TO> static hipError_t launch_tile_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s) { return launch_tile_of<DT, TO, 2, 2, 2, 2>(a, p, s); }
 
 hipError_t launch_linear_tile(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s)
 {

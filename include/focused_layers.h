@@ -46,7 +46,8 @@ enum { FC_ACT_NONE = 0, FC_ACT_RELU = 1, FC_ACT_SILU = 2, FC_ACT_GELU = 3 };
 
 enum {
     FC_RESIDUAL_FIRST = 128u, /* fc_linear: the residual is added before the activation */
-    FC_ANY_POINTERS = 256u    /* x and w (fc_linear), x and out (fc_group_norm) are aligned to their element only; without it to 16 bytes */
+    FC_ANY_POINTERS = 256u,   /* x and w (fc_linear), x and out (fc_group_norm) are aligned to their element only; without it to 16 bytes */
+    FC_COUNTED = 512u         /* fc_linear: the work is laid out for half of the rows, as a count leaves them that a mask makes (results are the same) */
 };
 
 enum { FC_LAYERS_MAX_STRIDE = 4194304 };    /* elements between rows, and sizes of rows */

@@ -20,7 +20,7 @@ int32_t check_linear(const fc_linear_desc *d, bool residual)
     if (d->dtype != FC_BF16 && d->dtype != FC_F16) return FC_ERR_DTYPE;
     if (d->out_dtype != d->dtype && d->out_dtype != FC_F32) return FC_ERR_DTYPE;
     if (d->activation < FC_ACT_NONE || d->activation > FC_ACT_GELU) return FC_ERR_DTYPE;
-    if (d->flags & ~(uint32_t)(FC_RESIDUAL_FIRST | FC_WORKSPACE_READY | FC_ANY_POINTERS) || d->reserved) return FC_ERR_DTYPE;
+    if (d->flags & ~(uint32_t)(FC_RESIDUAL_FIRST | FC_WORKSPACE_READY | FC_ANY_POINTERS | FC_COUNTED) || d->reserved) return FC_ERR_DTYPE;
     if (d->x_row < 0 || d->w_row < 0 || d->residual_row < 0 || d->out_row < d->n) return FC_ERR_SHAPE;
     if (d->k > FC_LAYERS_MAX_STRIDE || d->n > FC_LAYERS_MAX_STRIDE) return FC_ERR_RANGE;
     if (!stride_ok(d->x_row, 0) || !stride_ok(d->w_row, 0) || !stride_ok(d->out_row, 0) || (residual && !stride_ok(d->residual_row, 0))) return FC_ERR_RANGE;
@@ -32,7 +32,9 @@ int32_t check_linear(const fc_linear_desc *d, bool residual)
 // so; what it is for is the order of the forms.  Measured there, rows x k x n (rings / shared stages / tiles of 128 / of 256):
 //   64 x 4096 x 4096 14.7 / 15.0 in four pieces      128 x 1024 x 1024 6.0 / 10.8 / 11.3         256 x 4096 x 4096 30.6 / 23.1 in four / 25.1 in four
 //   512 x 4096 x 4096 59.5 / 30.1 in two / 35.3      1024 x 4096 x 4096 121 / 43.6 / 52.4 / 80.8   2048 x 4096 x 4096 - / - / 71.2 / 82.5
-//   4096 x 4096 x 4096 - / - / 141 / 109             2048 x 8192 x 1024 - / - / 51.6 in four, 87.4 in one / 146
+//   4096 x 4096 x 4096 - / - / 141 / 100             2048 x 8192 x 1024 - / - / 51.6 in four, 87.4 in one / 146
+// Rows of any alignment (through registers / laid out anew for tiles of 128 / of 256): 128 x 4097 x 4095 26 in eight / 37 in four / -, 512 x 4097 x 4095 44 in two / 54 / 111,
+// 2048 x 4097 x 4095 127 / 87 / 117, 2048 x 4097 x 16383 493 / 329 / 292.
 struct Cut {
     double us;
     int32_t form, tile_m, tile_n, splits;
@@ -42,7 +44,7 @@ double rounds_of(int64_t units) { return (double)((units + 255) / 256); }
 // tiles of 128 columns; rows of a tile over 128
 double join_us(int64_t units, int32_t splits, double rows) { return splits > 1 ? 2.5 + 0.03 * (double)units * rows : 0.; }
 
-Cut best_cut(int32_t rows, int32_t n, int32_t k)
+Cut best_cut(int32_t rows, int32_t n, int32_t k, bool wide)
 {
     const int32_t chunks = ceil_div(k, kLinearK);
     const double weights = 2e-6 * (double)n * (double)k / 6.;
@@ -53,28 +55,37 @@ Cut best_cut(int32_t rows, int32_t n, int32_t k)
     // rings: a wave's steps; of 64, 32 or 16 rows and 16, 32 or 64 columns
     const int32_t ring_m = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
     static const double step_us[3][3] = {{0.2, 0.3, 0.}, {0.25, 0.33, 0.45}, {0.36, 0.5, 0.67}};
-    for (int32_t i = 0; i < (ring_m == 16 ? 2 : 3); ++i) {
+    for (int32_t i = 0; i < (!wide ? 0 : ring_m == 16 ? 2 : 3); ++i) {
         const int64_t units = (int64_t)ceil_div(rows, ring_m) * ceil_div(n, 16 << i);
         const double steps = ceil_div(chunks, ring_m == 64 || i == 2 ? 4 : 8);
         // (several tiles of rows: the weights come from the L2, and the steps wait for it as the chip fills)
         const double full = rows > ring_m ? 1. + 0.6 * (double)(units < 256 ? units : 256) / 256. : 1.;
         take({1.2 + rounds_of(units) * (2. + steps * step_us[ring_m / 32][i] * full) + weights, 0, ring_m, 16 << i, 1, true});
     }
+    // rows of any alignment straight into fragments (us, so / through LDS: 1 x 1001 x 4095 5.8 / 9.1, 1 x 8191 x 1023 11.7 / 15.6, 32 x 1001 x 4095 9.8 / 10.4; 16 x 4097 x 4095
+    // 28.4 / 17.4, 1 x 4097 x 16383 60 / 37)
+    if (!wide && rows <= 32 && (double)n * (double)k * (1. + rows / 16.) <= 16777216.) {
+        const int32_t units = ceil_div(n, 16), wanted = ceil_div(256, units), most = chunks < 16 ? 1 : chunks / 8;
+        return {0., 0, ring_m, 16, wanted < most ? wanted : most, false};
+    }
+    // laying both operands out anew
+    const double pad = wide ? 0. : 4. + 4e-6 / 8. * ((double)rows + (double)n) * (double)k;
     for (int32_t splits = 1; splits <= 16; splits *= 2) {
         if (splits > 1 && chunks / splits < 2) break;
         const int32_t stages = ceil_div(chunks, splits);
         // shared stages
         const int32_t m = rows <= 64 ? 64 : 128;
         const int64_t units = (int64_t)ceil_div(rows, m) * ceil_div(n, 128) * splits;
-        take({1. + rounds_of(units) * (2.5 + stages * (m == 64 ? 0.31 : units < 256 ? 0.45 : 0.5)) + (m == 64 ? 0.85 : 0.7) * weights + join_us(units, splits, m / 128.), 2, m, 128, splits, false});
+        const double stage_us = wide ? (m == 64 ? 0.31 : units < 256 ? 0.45 : 0.5) : m == 64 ? 0.8 : 1.05;
+        take({(wide ? 1. : 3.) + rounds_of(units) * (2.5 + stages * stage_us) + (wide ? (m == 64 ? 0.85 : 0.7) * weights : 0.) + join_us(units, splits, wide || units > 256 ? m / 128. : m / 384.), 2, m, 128, splits, false});
         // tiles of 128: two on a CU
         if (rows > 64 && splits <= 8) {
             const int64_t u = (int64_t)ceil_div(rows, 128) * ceil_div(n, 128) * splits;
-            take({3.5 + stages * (u <= 256 ? 0.8 : 1.1 * (double)((u + 511) / 512)) + join_us(u, splits, 1.), 1, 128, 128, splits, false});
+            take({3.5 + pad + stages * (u <= 256 ? 0.8 : 1.1 * (double)((u + 511) / 512)) + join_us(u, splits, 1.), 1, 128, 128, splits, false});
         }
     }
     const int64_t large = (int64_t)ceil_div(rows, 256) * ceil_div(n, 256);
-    take({3.5 + rounds_of(large) * (5. + chunks * (1.25 + 0.35 * (large < 256 ? large : 256) / 256.)), 3, 256, 256, 1, false});
+    take({3.5 + pad + rounds_of(large) * (5. + chunks * (1.2 + 0.2 * (large < 256 ? large : 256) / 256.)), 3, 256, 256, 1, false});
     return best;
 }
 
@@ -86,21 +97,14 @@ int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
     p->pad_x = p->pad_w = false;
     p->wide = x_pieces && w_pieces;
     p->per_wave = 0;
-    if (rows <= 64 && !p->wide) {
-        // straight into fragments: laying the weights out anew takes as long as the product (33 MB: 20 us)
-        p->form = 0;
-        p->ring = false;
-        p->tile_m = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-        p->tile_n = d->n >= 16384 ? (p->tile_m == 64 ? 64 : 32) : 16;
-        const int32_t wanted = ceil_div(256, ceil_div(d->n, p->tile_n)), most = chunks < 16 ? 1 : chunks / 8;
-        p->splits = wanted < most ? wanted : most;
-    } else {
-        const Cut c = best_cut(rows, d->n, d->k);
-        p->form = c.form;
-        p->ring = c.ring;
-        p->tile_m = c.tile_m;
-        p->tile_n = c.tile_n;
-        p->splits = c.splits;
+    // (half of the rows: 1924 of 4811 rows of 1001 with 515 columns in two pieces)
+    const Cut c = best_cut(d->flags & FC_COUNTED ? (rows + 1) / 2 : rows, d->n, d->k, p->wide);
+    p->form = c.form;
+    p->ring = c.ring;
+    p->tile_m = c.tile_m;
+    p->tile_n = c.tile_n;
+    p->splits = c.splits;
+    if (p->form == 1 || p->form == 3) {
         p->pad_x = !x_pieces;
         p->pad_w = !w_pieces;
     }

@@ -181,6 +181,31 @@ template <auto KERNEL> hipError_t raise_dynamic_lds(size_t bytes)
 
 constexpr int kLinearK = 64;        // columns of a stage, or chunk
 
+// Eight elements c .. of a row of k elements and any alignment, zeros behind its end.  Without a branch between loads, which would wait for each of them: 16 bytes that end
+// where the row does, shifted; of rows shorter than that every element by itself.
+__device__ __forceinline__ uint4 row_end(const uint16_t *__restrict__ row, int c, int k)
+{
+    if (k >= 8) {
+        const int at = min(c, k - 8), by = c - at;
+        uint64_t v[2];
+        __builtin_memcpy(v, row + at, 16);
+        uint64_t lo = by >= 4 ? v[1] : v[0], hi = by >= 4 ? 0 : v[1];
+        const int bits = (by & 3) * 16;
+        lo = bits ? lo >> bits | hi << (64 - bits) : lo;
+        hi >>= bits;
+        lo = by >= 8 ? 0 : lo;
+        hi = by >= 8 ? 0 : hi;
+        return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+    }
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = row[min(c + i, k - 1)];
+    loaded_together(e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = c + i < k ? e[i] : 0;
+    return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+}
+
 // How a product is cut.
 struct LinearPlan {
     int32_t form;                   // 0: few rows, 2: some dozens, 1: many in tiles of 128, 3: of 256; tile_m, tile_n: rows and columns of a workgroup

@@ -32,15 +32,9 @@ __device__ __forceinline__ RowsTile rows_tile(const LinearArgs &a)
 // Eight elements c .. of a row of any alignment.  FULL: all are inside k; else those behind are zero.
 template <bool FULL> __device__ __forceinline__ uint4 row_piece(const uint16_t *__restrict__ row, int c, int k)
 {
+    if constexpr (!FULL) return row_end(row, c, k);
     uint4 v;
-    if constexpr (FULL) {
-        __builtin_memcpy(&v, row + c, 16);
-    } else {
-        uint16_t e[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = c + j < k ? row[c + j] : 0;
-        __builtin_memcpy(&v, e, 16);
-    }
+    __builtin_memcpy(&v, row + c, 16);
     return v;
 }
 
@@ -189,9 +183,7 @@ template <int DT, typename TO, int RB, int NB, int U> static hipError_t launch_r
 
 template <int DT, typename TO> static hipError_t launch_rows_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
-    if (p.tile_m == 16) return p.tile_n == 16 ? launch_rows_of<DT, TO, 1, 1, 6>(a, p, s) : launch_rows_of<DT, TO, 1, 2, 4>(a, p, s);
-    if (p.tile_m == 32) return p.tile_n == 16 ? launch_rows_of<DT, TO, 2, 1, 4>(a, p, s) : launch_rows_of<DT, TO, 2, 2, 3>(a, p, s);
-    return p.tile_n == 16 ? launch_rows_of<DT, TO, 4, 1, 3>(a, p, s) : launch_rows_of<DT, TO, 4, 4, 2>(a, p, s);
+    return p.tile_m == 16 ? launch_rows_of<DT, TO, 1, 1, 6>(a, p, s) : launch_rows_of<DT, TO, 2, 1, 4>(a, p, s);
 }
 
 // Both operands through LDS.  Loads of 16 rows of 64 bytes come at 18 bytes a clock and CU, whole lines of 128 bytes at 64: with some dozens of rows, whose x is

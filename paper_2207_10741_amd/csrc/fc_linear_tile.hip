@@ -190,15 +190,7 @@ __global__ __launch_bounds__(256) void k_linear_pad(LinearArgs a, int32_t padded
         const int64_t at = of_x ? i : i - x_items, row = at / per_row;
         const int c = (int)(at - row * per_row) * 8;
         const uint16_t *const from = of_x ? a.x + row * a.x_row : a.w + row * a.w_row;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (c + 8 <= a.k) {
-            __builtin_memcpy(&v, from + c, 16);
-        } else {
-            uint16_t e[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = c + j < a.k ? from[c + j] : 0;
-            __builtin_memcpy(&v, e, 16);
-        }
+        const uint4 v = row_end(from, c, a.k);
         *reinterpret_cast<uint4 *>((of_x ? x : w) + row * padded_k + c) = v;
     }
 }

@@ -194,8 +194,8 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, V (&acc)[PB][CB
                 }
             }
         } else {
-            // a lane a column (of fewer than 64 columns: of several rows), eight rows' residuals sent for together
-            constexpr int COLS = CW < 64 ? CW : 64, ROWS = 64 / COLS, AT_ONCE = 8;
+            // a lane a column (of fewer than 64 columns: of several rows), many rows' residuals sent for together
+            constexpr int COLS = CW < 64 ? CW : 64, ROWS = 64 / COLS, AT_ONCE = BS / ROWS < 16 ? BS / ROWS : 16;
 #pragma unroll 1
             for (int c0 = 0; c0 < CW; c0 += COLS) {
                 const int c = c0 + lane % COLS, col = col0 + c;

@@ -17,7 +17,7 @@ from . import binding as B
 from .attention import _Prepared, _made
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
-RESIDUAL_FIRST, ANY_POINTERS = 128, 256
+RESIDUAL_FIRST, ANY_POINTERS, COUNTED = 128, 256, 512
 MAX_STRIDE = 4194304
 GROUP_MAX_CHANNELS = 16384
 
@@ -145,8 +145,7 @@ class PreparedLinear(_PreparedLayer):
             desc.residual_row = _matrix(residual, "residual", device)
             if tuple(residual.shape) != shape or residual.dtype != out.dtype:
                 raise ValueError("residual must be like out")
-        if not _aligned(x, w):
-            desc.flags |= ANY_POINTERS
+        desc.flags |= (0 if _aligned(x, w) else ANY_POINTERS) | (0 if count is None else COUNTED)
         self._finish(desc, (x.data_ptr(), w.data_ptr(), B._ptr(bias), B._ptr(residual), B._ptr(count), out.data_ptr()),
                      (x, w, bias, residual, count, out), workspace, device, stream, out)
 

@@ -34,7 +34,7 @@ def test_descriptors_and_constants_mirror_the_headers():
     assert _fields(layers, "fc_linear_desc") == [n for n, _ in L.LinearDesc._fields_]
     assert _fields(layers, "fc_group_norm_desc") == [n for n, _ in L.GroupNormDesc._fields_]
     assert _fields(pages, "fc_pages_desc") == [n for n, _ in P.PagesDesc._fields_]
-    for name, value in (("FC_RESIDUAL_FIRST", L.RESIDUAL_FIRST), ("FC_ANY_POINTERS", L.ANY_POINTERS), ("FC_LAYERS_MAX_STRIDE", L.MAX_STRIDE),
+    for name, value in (("FC_RESIDUAL_FIRST", L.RESIDUAL_FIRST), ("FC_ANY_POINTERS", L.ANY_POINTERS), ("FC_COUNTED", L.COUNTED), ("FC_LAYERS_MAX_STRIDE", L.MAX_STRIDE),
                         ("FC_GROUP_MAX_CHANNELS", L.GROUP_MAX_CHANNELS), ("FC_ACT_RELU", L.ACTIVATIONS["relu"]), ("FC_ACT_SILU", L.ACTIVATIONS["silu"]),
                         ("FC_ACT_GELU", L.ACTIVATIONS["gelu"])):
         assert value == int(re.search(name + r"\s*=\s*(\d+)", layers).group(1))
@@ -75,7 +75,7 @@ def test_linear_refuses():
     for bad in (dict(rows=-1), dict(n=0), dict(k=0), dict(n=-4), dict(x_row=-1), dict(w_row=-1), dict(residual_row=-1), dict(out_row=63)):
         assert _linear(_linear_desc(**bad)) == SHAPE and _bytes(L, "fc_linear", _linear_desc(**bad)) == SHAPE
     for bad in (dict(dtype=B.F32), dict(dtype=B.FP8), dict(dtype=7), dict(out_dtype=B.F16), dict(out_dtype=B.FP8), dict(activation=4), dict(activation=-1),
-                dict(flags=1), dict(flags=512), dict(reserved=1)):
+                dict(flags=1), dict(flags=1024), dict(reserved=1)):
         assert _linear(_linear_desc(**bad)) == DTYPE
     most = L.MAX_STRIDE
     for bad in (dict(k=most + 1), dict(n=most + 1, out_row=most + 1), dict(x_row=most + 1), dict(w_row=most + 1), dict(out_row=most + 1),
@@ -96,9 +96,12 @@ def test_linear_workspace():
     assert need > 100 * 64 * 4
     assert _linear(long, ws=None) == WORKSPACE and _linear(long, ws_bytes=need - 1) == WORKSPACE and _linear(long, ws=ctypes.c_void_p(24)) == ALIGN
     assert _bytes(L, "fc_linear", _linear_desc(rows=0)) == 0
-    plain, odd = _linear_desc(rows=300, k=128), _linear_desc(rows=300, k=127)
-    assert _bytes(L, "fc_linear", odd) >= _bytes(L, "fc_linear", plain) + (300 + 64) * 128 * 2
-    assert _bytes(L, "fc_linear", _linear_desc(rows=300, flags=L.ANY_POINTERS)) >= _bytes(L, "fc_linear", plain) + (300 + 64) * 128 * 2
+    # many rows of any alignment are laid out anew
+    sizes = dict(rows=4096, n=4096, out_row=4096, residual_row=4096, x_row=4096, w_row=4096)
+    plain, odd = _linear_desc(k=4096, **sizes), _linear_desc(k=4095, **sizes)
+    room = 2 * 4096 * 4096 * 2
+    assert _bytes(L, "fc_linear", odd) >= _bytes(L, "fc_linear", plain) + room
+    assert _bytes(L, "fc_linear", _linear_desc(k=4096, flags=L.ANY_POINTERS, **sizes)) >= _bytes(L, "fc_linear", plain) + room
     b = ctypes.c_size_t()
     assert L.lib().fc_linear_workspace_bytes(None, ctypes.byref(b)) == NULL and L.lib().fc_linear_workspace_bytes(ctypes.byref(plain), None) == NULL
 

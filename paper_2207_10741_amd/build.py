@@ -25,7 +25,7 @@ HIPCC_FLAGS = [
 ]
 
 # sources that hold many kernel instances are compiled as several units (-D<macro>=p), side by side with the others
-PARTS = {"fc_conv_mfma.hip": ("FC_MFMA_PART", 6), "fc_conv_wide.hip": ("FC_WIDE_PART", 9)}
+PARTS = {"fc_conv_mfma.hip": ("FC_MFMA_PART", 6), "fc_conv_wide.hip": ("FC_WIDE_PART", 9), "fc_linear_large.hip": ("FC_LARGE_PART", 4)}
 
 
 def _run(cmd, verbose):

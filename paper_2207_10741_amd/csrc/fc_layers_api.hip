@@ -123,6 +123,12 @@ int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
     return FC_OK;
 }
 
+hipError_t launch_linear_large(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s)
+{
+    if (dtype == FC_BF16) return out_dtype == FC_F32 ? launch_large_as<FC_BF16, float>(a, p, s) : launch_large_as<FC_BF16, bf16_t>(a, p, s);
+    return out_dtype == FC_F32 ? launch_large_as<FC_F16, float>(a, p, s) : launch_large_as<FC_F16, f16_t>(a, p, s);
+}
+
 // ---- group norm ----
 
 int32_t check_norm(const fc_group_norm_desc *d)

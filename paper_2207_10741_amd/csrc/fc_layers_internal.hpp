@@ -219,7 +219,8 @@ struct LinearPlan {
 hipError_t launch_linear_rows(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
 hipError_t launch_linear_tile(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
 hipError_t launch_linear_stream(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
-hipError_t launch_linear_large(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s);
+// (DT, TO: storage type, carrier of the output)
+template <int DT, typename TO> hipError_t launch_large_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s);
 // Rows of x, of w, or of both, as rows of padded_k elements with zeros behind k.
 hipError_t launch_linear_pad(const LinearArgs &a, const LinearPlan &p, uint16_t *x, uint16_t *w, hipStream_t s);
 

@@ -188,7 +188,7 @@ void k_linear_large(LinearArgs a)
     finish_tile<DT, TO, WM, 2, PB, CB, false, kLargeLds>(a, acc, smem_raw, t, rows, wave, wave_m, wave_n);
 }
 
-template <int DT, typename TO> static hipError_t launch_large_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
+template <int DT, typename TO> hipError_t launch_large_as(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
     const hipError_t e = raise_dynamic_lds<&k_linear_large<DT, TO>>(kLargeLds);
     if (e != hipSuccess) return e;
@@ -197,10 +197,18 @@ template <int DT, typename TO> static hipError_t launch_large_as(const LinearArg
     return hipGetLastError();
 }
 
-hipError_t launch_linear_large(const LinearArgs &a, const LinearPlan &p, int dtype, int out_dtype, hipStream_t s)
-{
-    if (dtype == FC_BF16) return out_dtype == FC_F32 ? launch_large_as<FC_BF16, float>(a, p, s) : launch_large_as<FC_BF16, bf16_t>(a, p, s);
-    return out_dtype == FC_F32 ? launch_large_as<FC_F16, float>(a, p, s) : launch_large_as<FC_F16, f16_t>(a, p, s);
-}
+// (compiled as several units, one instance each)
+#if !defined(FC_LARGE_PART) || FC_LARGE_PART == 0
+template hipError_t launch_large_as<FC_BF16, bf16_t>(const LinearArgs &, const LinearPlan &, hipStream_t);
+#endif
+#if !defined(FC_LARGE_PART) || FC_LARGE_PART == 1
+template hipError_t launch_large_as<FC_BF16, float>(const LinearArgs &, const LinearPlan &, hipStream_t);
+#endif
+#if !defined(FC_LARGE_PART) || FC_LARGE_PART == 2
+template hipError_t launch_large_as<FC_F16, f16_t>(const LinearArgs &, const LinearPlan &, hipStream_t);
+#endif
+#if !defined(FC_LARGE_PART) || FC_LARGE_PART == 3
+template hipError_t launch_large_as<FC_F16, float>(const LinearArgs &, const LinearPlan &, hipStream_t);
+#endif
 
 } // namespace fc

@@ -27,6 +27,8 @@
  *
  * Activations: y < 0 ? 0 : y; y / (1 + exp(-y)); y (1 + erf(y / sqrt(2))) / 2, in 32 bits, NaN where the formula says so (-infinity of the last two).
  *
+ * Sizes beyond the limits below, and more work than a launch holds (2^31 threads), give FC_ERR_RANGE.
+ *
  * Conventions are those of focused_conv.h: device pointers, a stream, nothing allocated and no waiting, argument errors found before
  * anything is launched, launches only (calls can be captured after one eager call).  bias, weight, count, starts, mask and workspaces are
  * aligned to 16 bytes.  With FC_WORKSPACE_READY (4) in flags the caller vouches that the workspace's counters are zero, as a workspace that was zeroed
@@ -52,6 +54,7 @@ enum {
 
 enum { FC_LAYERS_MAX_STRIDE = 4194304 };    /* elements between rows, and sizes of rows */
 enum { FC_GROUP_MAX_CHANNELS = 16384 };      /* channels of a group */
+enum { FC_NORM_MAX_ROWS = 1073741824 };      /* rows of an image */
 
 typedef struct {
     int32_t rows, n, k;                                   /* rows of x and out, columns of out, columns of x and w */

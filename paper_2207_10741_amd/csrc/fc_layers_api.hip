@@ -114,7 +114,7 @@ int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
     p->splits = ceil_div(chunks, p->per_split);
     if (p->form == 0) p->per_wave = ceil_div(p->per_split, p->ring && (p->tile_m == 64 || p->tile_n == 64) ? 4 : 8);
     const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles;
-    if (tiles * p->splits >= INT32_MAX / 1024) return FC_ERR_RANGE;     // (a dimension of a grid is counted in threads)
+    if (tiles * p->splits >= INT32_MAX / 512) return FC_ERR_RANGE;      // (a dimension of a grid is counted in threads)
     p->counters = p->splits == 1 ? 0 : align_up((size_t)tiles * sizeof(int32_t), 256);
     p->at_x = p->counters;
     p->at_w = p->at_x + (p->pad_x ? (size_t)rows * p->padded_k * 2 : 0);
@@ -140,6 +140,7 @@ int32_t check_norm(const fc_group_norm_desc *d)
     if (d->flags & ~(uint32_t)(FC_SKIP_ZERO_FILL | FC_WORKSPACE_READY | FC_ANY_POINTERS) || d->reserved) return FC_ERR_DTYPE;
     if (!(d->eps >= 0.f) || !isfinite(d->eps) || d->x_row < 0 || d->out_row < d->channels) return FC_ERR_SHAPE;
     if (d->channels > FC_LAYERS_MAX_STRIDE || d->channels / d->groups > FC_GROUP_MAX_CHANNELS) return FC_ERR_RANGE;
+    if (d->max_rows > FC_NORM_MAX_ROWS) return FC_ERR_RANGE;
     if (!stride_ok(d->x_row, 0) || !stride_ok(d->out_row, 0)) return FC_ERR_RANGE;
     return FC_OK;
 }
@@ -152,9 +153,14 @@ int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
     const int32_t size = size_of(d->dtype), ve = 16 / size, per_group = d->channels / d->groups;
     p->wide = !(d->flags & FC_ANY_POINTERS) && d->channels % ve == 0 && d->x_row % ve == 0 && d->out_row % ve == 0;
     const int32_t e = p->wide ? ve : 1;         // elements of a piece
-    // the least slices: whole groups, whole pieces, 32 bytes
+    // the least slices: whole groups, whole pieces, and 32 bytes where the groups divide so that they are not long
     int32_t least = 1;
-    while (least < d->groups && (d->groups % least || least * per_group % e || least * per_group * size < 32)) ++least;
+    while (least < d->groups && (d->groups % least || least * per_group % e)) ++least;
+    for (int32_t of = least; of <= d->groups && of * per_group <= 4096; ++of)
+        if (d->groups % of == 0 && of * per_group % e == 0 && of * per_group * size >= 32) {
+            least = of;
+            break;
+        }
     auto entries = [&](int32_t channels) { return per_group % e == 0 ? channels / e : channels; };
     // an image's slice in the registers of a workgroup: up to 1024 threads with 12 pieces each
     p->slice = least * per_group;

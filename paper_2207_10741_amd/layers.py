@@ -14,12 +14,14 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from .attention import _Prepared, _made
+from .attention import _made
+from .pages import _OnDevice
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 RESIDUAL_FIRST, ANY_POINTERS, COUNTED = 128, 256, 512
 MAX_STRIDE = 4194304
 GROUP_MAX_CHANNELS = 16384
+NORM_MAX_ROWS = 1073741824
 
 FUNCTIONS = ("fc_linear_workspace_bytes", "fc_group_norm_workspace_bytes", "fc_linear", "fc_group_norm")
 
@@ -89,7 +91,7 @@ def _aligned(*tensors):
     return all(t.data_ptr() % 16 == 0 for t in tensors)
 
 
-class _PreparedLayer(_Prepared):
+class _PreparedLayer(_OnDevice):
     def _bytes(self, desc):
         b = ctypes.c_size_t()
         name = self._name + "_workspace_bytes"
@@ -111,7 +113,7 @@ class _PreparedLayer(_Prepared):
         B._require_cuda(workspace)
         if workspace is None and need:
             workspace = self._workspace(need, device, stream, desc)
-        self._keep = (desc, workspace) + keep
+        self._keep, self._device = (desc, workspace) + keep, device.index
         self._fn = getattr(lib(), self._name)
         self._args = (ctypes.byref(desc),) + pointers + (B._ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
         self._result = result

@@ -81,7 +81,17 @@ def _other(cache, to):
         raise ValueError("both caches must have the same heads, channels and device")
 
 
-class _PreparedPages(_Prepared):
+class _OnDevice(_Prepared):
+    """A call whose tensors are on device `_device`, which the stream has to be of."""
+
+    def __call__(self, stream=None):
+        device = B._torch()._C._cuda_getDevice() if stream is None else stream.device_index
+        if device != self._device:
+            raise ValueError("the tensors are on cuda:%d, the stream on cuda:%d" % (self._device, device))
+        return super().__call__(stream)
+
+
+class _PreparedPages(_OnDevice):
     def _finish(self, name, desc, cache, pointers, keep, missing, workspace, stream):
         """pointers: what lies between the descriptor and missing"""
         torch = B._torch()
@@ -92,7 +102,7 @@ class _PreparedPages(_Prepared):
         B._require_cuda(workspace)
         if workspace is None:
             workspace = self._workspace(need.value, cache.device, stream, desc)
-        self._keep = (desc, cache.data, missing, workspace) + keep
+        self._keep, self._device = (desc, cache.data, missing, workspace) + keep, cache.device.index
         self._fn = getattr(lib(), name)
         self._args = (ctypes.byref(desc),) + pointers + (missing.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size())
         self._result = missing
@@ -141,7 +151,7 @@ class PreparedCompact(_PreparedPages):
                      (users, table, cache_to.data, users_to, table_to), missing, workspace, stream)
 
 
-class PreparedCopy(_Prepared):
+class PreparedCopy(_OnDevice):
     """kv_copy with its arguments marshalled once."""
 
     def __init__(self, cache, sources, cache_to, targets):
@@ -152,7 +162,7 @@ class PreparedCopy(_Prepared):
         for t, what in ((sources, "sources"), (targets, "targets")):
             _int32(t, tuple(sources.shape), cache.device, what)
         desc = PagesDesc(blocks=cache.blocks, kv_heads=cache.kv_heads, head_dim=cache.head_dim, blocks_to=cache_to.blocks, pairs=sources.shape[0])
-        self._keep = (desc, cache.data, sources, cache_to.data, targets)
+        self._keep, self._device = (desc, cache.data, sources, cache_to.data, targets), cache.device.index
         self._fn = lib().fc_kv_copy
         self._args = (ctypes.byref(desc), cache.data.data_ptr(), sources.data_ptr(), cache_to.data.data_ptr(), targets.data_ptr())
         self._result = cache_to

@@ -25,7 +25,7 @@ def _check_images(x, got, groups, weight, bias, masks, activation, eps=1e-5):
 # images of one row and of many, groups of one channel and of all, channels off the pieces of 16 bytes; the last ones do not fit a workgroup
 SIZES = [(1, 1, 8, 1), (2, 1, 64, 64), (1, 5, 3, 3), (3, 17, 32, 8), (2, 64, 60, 4), (1, 256, 512, 32), (2, 100, 515, 5), (4, 33, 96, 1), (1, 7, 1280, 32),
          (2, 3, 4096, 1), (1, 2, 16384, 1), (1, 3, 9000, 1), (2, 2, 10002, 2), (1, 5000, 64, 32), (2, 9001, 128, 32), (1, 20000, 24, 3), (3, 4099, 60, 4), (1, 3000, 515, 5), (1, 40, 12288, 4),
-         (1, 2500, 40, 40), (1, 1100, 4098, 2), (1, 300, 16380, 3)]
+         (1, 2500, 40, 40), (1, 1100, 4098, 2), (1, 300, 16380, 3), (1, 30, 4099, 4099), (2, 3, 1031, 1031), (1, 5, 8248, 1031)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: "%dx%dx%d-%d" % s)

@@ -34,7 +34,7 @@ def test_descriptors_and_constants_mirror_the_headers():
     assert _fields(layers, "fc_linear_desc") == [n for n, _ in L.LinearDesc._fields_]
     assert _fields(layers, "fc_group_norm_desc") == [n for n, _ in L.GroupNormDesc._fields_]
     assert _fields(pages, "fc_pages_desc") == [n for n, _ in P.PagesDesc._fields_]
-    for name, value in (("FC_RESIDUAL_FIRST", L.RESIDUAL_FIRST), ("FC_ANY_POINTERS", L.ANY_POINTERS), ("FC_COUNTED", L.COUNTED), ("FC_LAYERS_MAX_STRIDE", L.MAX_STRIDE),
+    for name, value in (("FC_RESIDUAL_FIRST", L.RESIDUAL_FIRST), ("FC_ANY_POINTERS", L.ANY_POINTERS), ("FC_COUNTED", L.COUNTED), ("FC_NORM_MAX_ROWS", L.NORM_MAX_ROWS), ("FC_LAYERS_MAX_STRIDE", L.MAX_STRIDE),
                         ("FC_GROUP_MAX_CHANNELS", L.GROUP_MAX_CHANNELS), ("FC_ACT_RELU", L.ACTIVATIONS["relu"]), ("FC_ACT_SILU", L.ACTIVATIONS["silu"]),
                         ("FC_ACT_GELU", L.ACTIVATIONS["gelu"])):
         assert value == int(re.search(name + r"\s*=\s*(\d+)", layers).group(1))
@@ -116,7 +116,7 @@ def test_group_norm_refuses():
         assert _norm(_norm_desc(**bad)) == DTYPE
     most = L.MAX_STRIDE
     for bad in (dict(channels=L.GROUP_MAX_CHANNELS + 1, groups=1, out_row=most), dict(x_row=most + 1), dict(out_row=most + 1),
-                dict(images=2 ** 30, max_rows=1, rows=2 ** 30, channels=512, groups=512, out_row=512)):
+                dict(images=1, max_rows=2 ** 30 + 1, rows=2 ** 30 + 1), dict(images=2 ** 30, max_rows=1, rows=2 ** 30, channels=512, groups=512, out_row=512)):
         assert _norm(_norm_desc(**bad)) == RANGE
     assert _norm(_norm_desc(), x=None) == NULL and _norm(_norm_desc(), out=None) == NULL
     for name in ("x", "out", "weight", "bias", "mask", "starts"):
@@ -194,3 +194,27 @@ def test_the_binding_refuses_tensors_it_cannot_take():
         P.kv_resize(cache, P.kv_users(cache), table, table[:, 0].contiguous())
     with pytest.raises(ValueError, match="device"):
         P.kv_copy(cache, table[0], cache, table[0])
+
+
+def test_group_norm_takes_groups_that_do_not_divide():
+    """A prime number of groups is no reason to refuse: slices of one group then."""
+    for groups, per_group, dtype in ((65537, 1, B.BF16), (65537, 8, B.BF16), (65537, 16, B.F32), (4099, 5, B.F16), (7, 16384, B.F32)):
+        channels = groups * per_group
+        rows = 10000
+        d = _norm_desc(images=1, rows=rows, max_rows=rows, channels=channels, groups=groups, dtype=dtype, x_row=channels, out_row=channels)
+        assert _bytes(L, "fc_group_norm", d) >= 0
+
+
+class _Stream:
+    device_index, cuda_stream = 1, 0
+
+
+def test_a_stream_of_another_device_is_refused():
+    call = L.PreparedLinear.__new__(L.PreparedLinear)
+    call._device = 0
+    with pytest.raises(ValueError, match="cuda:0, the stream on cuda:1"):
+        call(_Stream())
+    call = P.PreparedFork.__new__(P.PreparedFork)
+    call._device = 0
+    with pytest.raises(ValueError, match="cuda:0, the stream on cuda:1"):
+        call(_Stream())

@@ -259,8 +259,9 @@ template <typename V> __device__ __forceinline__ void copy_small(const Section &
     for (int32_t i = threadIdx.x; i < n; i += kCopyThreads) y[i] = x[i];
 }
 
-// A segment of block s of one cache to block t of the other.
-__device__ __forceinline__ void copy_segment(const CopyArgs &c, int32_t s, int32_t t, int32_t segment)
+// A segment of block s of one cache to block t of the other.  MANY: its loads leave the caches to others.  (Whole caches move in 89 us so and in 112 without, 330 MB; a fork's
+// few blocks are read again by whoever goes on with them: 256 sequences forked and their last tokens read 44 us so, 37 without.)
+template <bool MANY> __device__ __forceinline__ void copy_segment(const CopyArgs &c, int32_t s, int32_t t, int32_t segment)
 {
     const int64_t at = (int64_t)segment * kCopyBytes + threadIdx.x * 16, end = c.from.codes.block;
     const uint8_t *const x = c.from.codes.base + s * end;
@@ -269,7 +270,9 @@ __device__ __forceinline__ void copy_segment(const CopyArgs &c, int32_t s, int32
 #pragma unroll
     for (int j = 0; j < kCopyPieces; ++j) {
         const int64_t o = at + j * (kCopyThreads * 16);
-        v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(x + (o < end ? o : 0)));
+        const u32x4_t *const p = reinterpret_cast<const u32x4_t *>(x + (o < end ? o : 0));
+        if constexpr (MANY) v[j] = __builtin_nontemporal_load(p);
+        else v[j] = *p;
     }
 #pragma unroll
     for (int j = 0; j < kCopyPieces; ++j) {
@@ -290,7 +293,7 @@ __device__ __forceinline__ void copy_blocks(const CopyArgs &c)
     for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
         const int32_t n = (int32_t)(i / c.segments), segment = (int32_t)(i - (int64_t)n * c.segments);
         const int32_t s = c.sources[n], t = c.targets ? c.targets[n] : n;
-        if ((uint32_t)s < (uint32_t)c.blocks && (uint32_t)t < (uint32_t)c.blocks_to) copy_segment(c, s, t, segment);
+        if ((uint32_t)s < (uint32_t)c.blocks && (uint32_t)t < (uint32_t)c.blocks_to) copy_segment<true>(c, s, t, segment);
     }
 }
 
@@ -305,7 +308,7 @@ __device__ __forceinline__ void copy_own(const PagesArgs &a, const CopyArgs &c)
         const int32_t source = a.own[b];
         if (source < 0) continue;
         const int32_t block = last_given(a, b);
-        if (block >= 0) copy_segment(c, source, block, segment);
+        if (block >= 0) copy_segment<false>(c, source, block, segment);
     }
 }
 

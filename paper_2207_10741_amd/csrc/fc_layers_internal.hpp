@@ -65,6 +65,7 @@ __device__ __forceinline__ void load8_float(const float *p, float (&v)[8])
 }
 template <typename T> __device__ __forceinline__ void unpack8(const uint4 &x, float (&v)[8])
 {
+    static_assert(sizeof(T) == 2, "16-bit values");
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {

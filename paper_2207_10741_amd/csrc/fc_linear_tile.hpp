@@ -93,14 +93,27 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, V (&acc)[PB][CB
         return s;
     };
     const int col0 = n0 + wave_n * CW, lrow = lane % BS, part4 = lane / BS * 4;
+    // Residuals come in 16-byte pieces of rows, those of all blocks together where there are registers for them (block after block each waits for memory: 8192 x 64 x 8192
+    // 82 us, so 78).
+    constexpr int PPR = CW * (int)sizeof(TO) / 16, RPP = 64 / PPR, NI = BS / RPP;    // pieces a row, rows a round, rounds
+    constexpr bool AHEAD = PB * NI <= 32;
+    const int prow = lane / PPR, pcol = col0 + lane % PPR * (16 / (int)sizeof(TO));
+    auto residual_piece = [&](int p, int i) __attribute__((always_inline)) {
+        const int row = r0 + (wave_m * PB + p) * BS + prow + i * RPP;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < rows && pcol < a.n) v = *reinterpret_cast<const uint4 *>(static_cast<const TO *>(a.residual) + (int64_t)row * a.residual_row + pcol);
+        return v;
+    };
+    uint4 ahead[AHEAD ? PB : 1][NI];
+    if (AHEAD && a.wide_out && a.residual)
+        each<AHEAD ? PB : 0>([&](auto p_c) __attribute__((always_inline)) {
+            each<NI>([&](auto i_c) __attribute__((always_inline)) { ahead[decltype(p_c)::value][decltype(i_c)::value] = residual_piece(decltype(p_c)::value, decltype(i_c)::value); });
+        });
     if (a.wide_out && a.act <= FC_ACT_RELU) {
-        // In the registers' order (a lane: a row, fours of columns): residuals come in and results go out in 16-byte pieces of rows.
-        constexpr int PPR = CW * (int)sizeof(TO) / 16, RPI = 64 / PPR, NI = BS / RPI;    // pieces a row, rows a round, rounds
+        // In the registers' order (a lane: a row, fours of columns): residuals come in and results go out through LDS.
         constexpr uint32_t OP = CW * sizeof(TO) + 16;
         static_assert((size_t)WM * WN * BS * OP <= LDS, "the waves' shares");
         unsigned char *const os = smem_raw + wave * (BS * OP), *const mine = os + lrow * OP + part4 * sizeof(TO);
-        constexpr int EPP = 16 / (int)sizeof(TO);
-        const int prow = lane / PPR, pcol = col0 + lane % PPR * EPP;
         unsigned char *const piece_at = os + prow * OP + lane % PPR * 16;
         f32x4_t bias[NF];
         each<NF>([&](auto i_c) __attribute__((always_inline)) {
@@ -113,15 +126,14 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, V (&acc)[PB][CB
             constexpr int p = decltype(p_c)::value;
             const int row0 = r0 + (wave_m * PB + p) * BS + prow;
             if (a.residual) {
-                const TO *from = static_cast<const TO *>(a.residual) + pcol;
                 uint4 more[NI];
+                each<NI>([&](auto i_c) __attribute__((always_inline)) {
+                    constexpr int i = decltype(i_c)::value;
+                    if constexpr (AHEAD) more[i] = ahead[p][i];
+                    else more[i] = residual_piece(p, i);
+                });
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    more[i] = make_uint4(0, 0, 0, 0);
-                    if (row0 + i * RPI < rows && pcol < a.n) more[i] = *reinterpret_cast<const uint4 *>(from + (int64_t)(row0 + i * RPI) * a.residual_row);
-                }
-#pragma unroll
-                for (int i = 0; i < NI; ++i) *reinterpret_cast<uint4 *>(piece_at + i * RPI * OP) = more[i];
+                for (int i = 0; i < NI; ++i) *reinterpret_cast<uint4 *>(piece_at + i * RPP * OP) = more[i];
                 wave_lds_order();
             }
             const bool relu_first = a.act == FC_ACT_RELU && !a.residual_first, relu_last = a.act == FC_ACT_RELU && a.residual_first;
@@ -143,11 +155,11 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, V (&acc)[PB][CB
             wave_lds_order();
             uint4 done[NI];
 #pragma unroll
-            for (int i = 0; i < NI; ++i) done[i] = *reinterpret_cast<const uint4 *>(piece_at + i * RPI * OP);
+            for (int i = 0; i < NI; ++i) done[i] = *reinterpret_cast<const uint4 *>(piece_at + i * RPP * OP);
             TO *to = static_cast<TO *>(a.out) + pcol;
 #pragma unroll
             for (int i = 0; i < NI; ++i)
-                if (row0 + i * RPI < rows && pcol < a.n) *reinterpret_cast<uint4 *>(to + (int64_t)(row0 + i * RPI) * a.out_row) = done[i];
+                if (row0 + i * RPP < rows && pcol < a.n) *reinterpret_cast<uint4 *>(to + (int64_t)(row0 + i * RPP) * a.out_row) = done[i];
             wave_lds_order();
             __builtin_amdgcn_sched_barrier(0);
         });
@@ -173,12 +185,18 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, V (&acc)[PB][CB
         wave_lds_order();
         const int row0 = r0 + (wave_m * PB + p) * BS, here = min(rows - row0, BS);
         if (a.wide_out) {
-            // two rows' residuals are sent for together
+            // (a lane's eight columns are a piece of 16-bit values; by way of LDS, as the loop is not unrolled)
             constexpr int AT_ONCE = 2;
+            constexpr bool PIECES = AHEAD && sizeof(TO) == 2 && (size_t)WM * WN * (BS * OP * 4 + NI * 1024) <= LDS;
+            unsigned char *const pieces = smem_raw + WM * WN * BS * OP * 4 + wave * (NI * 1024) + lane * 16;
+            if constexpr (PIECES) {
+                if (a.residual) each<NI>([&](auto i_c) __attribute__((always_inline)) { *reinterpret_cast<uint4 *>(pieces + decltype(i_c)::value * 1024) = ahead[p][decltype(i_c)::value]; });
+                wave_lds_order();
+            }
 #pragma unroll 1
             for (int i = 0; i < BS / RPI; i += AT_ONCE) {
                 float more[AT_ONCE][8];
-                if (a.residual)
+                if (!PIECES && a.residual)
 #pragma unroll
                     for (int u = 0; u < AT_ONCE; ++u) {
                         const int row = min(row0 + (i + u) * RPI + lane / LPR, rows - 1);
@@ -189,6 +207,8 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, V (&acc)[PB][CB
                     const int r = (i + u) * RPI + lane / LPR, row = row0 + r;
                     float v[8];
                     load8_float(os + r * OP + c8 * 8, v);
+                    if constexpr (PIECES)
+                        if (a.residual) unpack8<TO>(*reinterpret_cast<const uint4 *>(pieces + (i + u) * 1024), more[u]);
                     finish_eight(a, bias, more[u], v);
                     if (row < rows && col8 < a.n) store8(static_cast<TO *>(a.out) + row * a.out_row + col8, v);
                 }

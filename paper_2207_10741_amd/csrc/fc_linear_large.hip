@@ -88,7 +88,7 @@ void k_linear_large(LinearArgs a)
         nw_k += kLinearK;
     };
     const uint32_t lds_wave = lds0 + (uint32_t)wave * 1024u;
-    // A load in two pieces, a product between them: where it goes (M0, which nothing else here writes), and the load.
+    // A load in two pieces, a product between them, which is the wait state that M0 wants: where it goes (M0, which nothing else here writes), and the load.
     auto aim_x = [&](int j, uint32_t buf) __attribute__((always_inline)) { aim(lds_wave + buf * XB + (uint32_t)j * (RPL * 128u)); };
     auto aim_w = [&](int j, uint32_t buf) __attribute__((always_inline)) { aim(lds_wave + W0 + buf * WB + (uint32_t)j * (RPL * 128u)); };
     auto issue_x = [&](int j, uint32_t buf) __attribute__((always_inline)) {
@@ -138,7 +138,15 @@ void k_linear_large(LinearArgs a)
     __syncthreads();
     advance_x();
     advance_w();
-    each<NS - BARRIER>([&](auto q_c) __attribute__((always_inline)) { issue_at(q_c, 2, 1); });
+    // (those before the first stage's barrier: no product stands between M0's write and a load, which have to be a wait state apart)
+    static_assert((NS - BARRIER) % EVERY != kLoadShift, "a load and its place on the same side");
+    each<NS - BARRIER>([&](auto q_c) __attribute__((always_inline)) {
+        constexpr int q = decltype(q_c)::value, l = q / EVERY;
+        if constexpr (q % EVERY == kLoadShift) {
+            if constexpr (l < WL) issue_w(l, 1);
+            else issue_x(l - WL, 2);
+        }
+    });
 
     uint4 wf[2][CB], xf[2][PB];
     // fragment r of a k-step, in the order the products need them: w0, x0, w1 .. w7, x1 ..

@@ -79,6 +79,17 @@ typedef struct {
 int32_t fc_linear_workspace_bytes(const fc_linear_desc *d, size_t *bytes);
 int32_t fc_group_norm_workspace_bytes(const fc_group_norm_desc *d, size_t *bytes);
 
+/* How a product is cut, for measurements and tests; what a caller has to know of it is the workspace's size alone.  A reduction in several pieces is shared by as many
+ * workgroups, and joined in the pieces' order. */
+enum { FC_LINEAR_RINGS = 0, FC_LINEAR_ROWS = 1, FC_LINEAR_STAGES = 2, FC_LINEAR_STAGES_ANY = 3, FC_LINEAR_TILES = 4, FC_LINEAR_LARGE = 5 };
+typedef struct {
+    int32_t kernel;                                       /* FC_LINEAR_... */
+    int32_t tile_rows, tile_columns;                      /* of a workgroup */
+    int32_t pieces;                                       /* of the reduction */
+    int32_t anew_x, anew_w;                               /* 1: the operand is laid out anew in the workspace first */
+} fc_linear_cut;
+int32_t fc_linear_cut_of(const fc_linear_desc *d, fc_linear_cut *cut);
+
 /* x [rows][k], w [n][k], bias [n] float32 or NULL, residual [rows][n] or NULL, count one int32 or NULL, out [rows][n]. */
 int32_t fc_linear(const fc_linear_desc *d, const void *x, const void *w, const float *bias, const void *residual, const int32_t *count,
                   void *out, void *workspace, size_t workspace_bytes, void *stream);

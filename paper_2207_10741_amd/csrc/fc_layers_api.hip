@@ -220,6 +220,24 @@ int32_t fc_linear_workspace_bytes(const fc_linear_desc *d, size_t *bytes)
     return rc;
 }
 
+int32_t fc_linear_cut_of(const fc_linear_desc *d, fc_linear_cut *cut)
+{
+    if (!cut) return FC_ERR_NULL;
+    int32_t rc = check_linear(d, true);
+    if (rc != FC_OK) return rc;
+    LinearPlan p;
+    rc = plan_linear(d, &p);
+    if (rc != FC_OK) return rc;
+    cut->kernel = p.form == 0 ? (p.ring ? FC_LINEAR_RINGS : FC_LINEAR_ROWS) : p.form == 1 ? FC_LINEAR_TILES : p.form == 3 ? FC_LINEAR_LARGE
+                  : p.wide ? FC_LINEAR_STAGES : FC_LINEAR_STAGES_ANY;
+    cut->tile_rows = p.tile_m;
+    cut->tile_columns = p.tile_n;
+    cut->pieces = p.splits;
+    cut->anew_x = p.pad_x;
+    cut->anew_w = p.pad_w;
+    return FC_OK;
+}
+
 int32_t fc_group_norm_workspace_bytes(const fc_group_norm_desc *d, size_t *bytes)
 {
     if (!bytes) return FC_ERR_NULL;

@@ -23,13 +23,20 @@ MAX_STRIDE = 4194304
 GROUP_MAX_CHANNELS = 16384
 NORM_MAX_ROWS = 1073741824
 
-FUNCTIONS = ("fc_linear_workspace_bytes", "fc_group_norm_workspace_bytes", "fc_linear", "fc_group_norm")
+LINEAR_KERNELS = ("rings", "rows", "stages", "stages_any", "tiles", "large")
+
+FUNCTIONS = ("fc_linear_workspace_bytes", "fc_group_norm_workspace_bytes", "fc_linear_cut_of", "fc_linear", "fc_group_norm")
 
 
 class LinearDesc(ctypes.Structure):
     """Mirror of fc_linear_desc."""
     _fields_ = ([(k, ctypes.c_int32) for k in ("rows", "n", "k", "dtype", "out_dtype", "activation")] + [("flags", ctypes.c_uint32)] +
                 [("reserved", ctypes.c_int32)] + [(k, ctypes.c_int64) for k in ("x_row", "w_row", "residual_row", "out_row")])
+
+
+class LinearCut(ctypes.Structure):
+    """Mirror of fc_linear_cut."""
+    _fields_ = [(k, ctypes.c_int32) for k in ("kernel", "tile_rows", "tile_columns", "pieces", "anew_x", "anew_w")]
 
 
 class GroupNormDesc(ctypes.Structure):
@@ -51,6 +58,7 @@ def lib():
         linear, norm = ctypes.POINTER(LinearDesc), ctypes.POINTER(GroupNormDesc)
         for name, args in (("fc_linear_workspace_bytes", [linear, ctypes.POINTER(size)]),
                            ("fc_group_norm_workspace_bytes", [norm, ctypes.POINTER(size)]),
+                           ("fc_linear_cut_of", [linear, ctypes.POINTER(LinearCut)]),
                            ("fc_linear", [linear] + [vp] * 7 + [size, vp]),
                            ("fc_group_norm", [norm] + [vp] * 7 + [size, vp])):
             f = getattr(L, name)
@@ -91,6 +99,13 @@ def _aligned(*tensors):
     return all(t.data_ptr() % 16 == 0 for t in tensors)
 
 
+def linear_cut(desc):
+    """fc_linear_cut_of: how a product (LinearDesc) is cut."""
+    cut = LinearCut()
+    B._check(lib().fc_linear_cut_of(ctypes.byref(desc), ctypes.byref(cut)), "fc_linear_cut_of")
+    return cut
+
+
 class _PreparedLayer(_OnDevice):
     def _bytes(self, desc):
         b = ctypes.c_size_t()
@@ -122,6 +137,11 @@ class _PreparedLayer(_OnDevice):
 class PreparedLinear(_PreparedLayer):
     """linear with its arguments marshalled once."""
     _name = "fc_linear"
+
+    @property
+    def cut(self):
+        """How the product is cut (LinearCut)."""
+        return linear_cut(self._keep[0])
 
     def __init__(self, x, w, bias=None, residual=None, activation=None, residual_first=False, count=None, out=None, out_dtype=None,
                  workspace=None, stream=None):

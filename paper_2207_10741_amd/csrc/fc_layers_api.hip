@@ -148,10 +148,11 @@ int32_t check_norm(const fc_group_norm_desc *d)
 constexpr int kOnceGroups = 512;        // of a slice, at most
 constexpr int kNormGrid = 256;          // workgroups of the kernels with chunks
 
-int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
+// (wide: in pieces of 16 bytes, which the rows have to be made of)
+int32_t plan_norm_as(const fc_group_norm_desc *d, bool wide, NormPlan *p)
 {
     const int32_t size = size_of(d->dtype), ve = 16 / size, per_group = d->channels / d->groups;
-    p->wide = !(d->flags & FC_ANY_POINTERS) && d->channels % ve == 0 && d->x_row % ve == 0 && d->out_row % ve == 0;
+    p->wide = wide;
     const int32_t e = p->wide ? ve : 1;         // elements of a piece
     // the least slices: whole groups, whole pieces, and 32 bytes where the groups divide so that they are not long
     int32_t least = 1;
@@ -203,6 +204,15 @@ int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
     if (units * p->chunks >= (1ll << 32) / 1024) return FC_ERR_RANGE;       // (a dimension of a grid is counted in threads)
     p->workspace = p->once ? 0 : (size_t)d->images * p->chunks * d->groups * 16;
     return FC_OK;
+}
+
+int32_t plan_norm(const fc_group_norm_desc *d, NormPlan *p)
+{
+    const int32_t ve = 16 / size_of(d->dtype);
+    const bool wide = !(d->flags & FC_ANY_POINTERS) && d->channels % ve == 0 && d->x_row % ve == 0 && d->out_row % ve == 0;
+    const int32_t rc = plan_norm_as(d, wide, p);
+    // (long groups that are not whole pieces: several of them that are together may have more entries than LDS holds; one of them by elements never has)
+    return wide && rc == FC_ERR_RANGE ? plan_norm_as(d, false, p) : rc;
 }
 
 } // namespace

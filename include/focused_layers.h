@@ -27,7 +27,7 @@
  *
  * Activations: y < 0 ? 0 : y; y / (1 + exp(-y)); y (1 + erf(y / sqrt(2))) / 2, in 32 bits, NaN where the formula says so (-infinity of the last two).
  *
- * Sizes beyond the limits below, and more work than a launch holds (2^31 threads), give FC_ERR_RANGE.
+ * Sizes beyond the limits below, and more work than a launch holds (2^31 threads; of fc_group_norm 2^32), give FC_ERR_RANGE.
  *
  * Conventions are those of focused_conv.h: device pointers, a stream, nothing allocated and no waiting, argument errors found before
  * anything is launched, launches only (calls can be captured after one eager call).  bias, weight, count, starts, mask and workspaces are

@@ -18,6 +18,8 @@
  *                  sequence), entries before it that are no block get one (nothing is written into it).  Before fc_kv_append with lengths that
  *                  have grown; after lengths were cut.  A cut that ends within a block that others hold too gives the sequence a copy
  *                  of its own of that block, in its place of the order above.  Blocks given back count as free in the same call, but for those that are copied from.
+ *                  Where there are too few blocks for all that, a block that nobody holds but sequences that are cut within it stays with the lowest of them, and the
+ *                  others alone want copies: what is cached there is not lost for all.
  *   fc_kv_fork     slot b becomes what slot parents[b] was before the call: the beams of a search, the samples of a prompt, a reordered batch.
  *                  parents[b] = b: it stays as it is; outside [0, batch): it is freed, its length becomes zero.  A slot that does
  *                  not stay gives its blocks back first and holds the blocks that the parent's length needs: full ones with it, an unfinished last one

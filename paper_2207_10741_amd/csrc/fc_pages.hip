@@ -120,8 +120,8 @@ __device__ __forceinline__ bool last_workgroup(const PagesArgs &a, int32_t *flag
     return *flag;
 }
 
-// The last workgroup's part: offsets of what the sequences want, in order, and the blocks they get.
-__device__ __forceinline__ void deal(const PagesArgs &a, int32_t *lds)
+// The last workgroup's part: offsets of what the sequences want, in order (all of it is returned), and the blocks they get.
+__device__ __forceinline__ int32_t order_wanted(const PagesArgs &a, int32_t *lds)
 {
     int32_t total = 0;
     for (int32_t first = 0; first < a.batch; first += kThreads) {
@@ -130,11 +130,50 @@ __device__ __forceinline__ void deal(const PagesArgs &a, int32_t *lds)
         if (b < a.batch) a.offsets[b] = total + s.before;
         total += s.all;
     }
-    const int32_t found = total ? find_free(a, total, lds) : 0;
+    return total;
+}
+__device__ __forceinline__ void dealt(const PagesArgs &a, int32_t total, int32_t found)
+{
     if (threadIdx.x == 0) {
         *a.found = found;
         *a.missing = total - found;
     }
+}
+
+// Everything that this workgroup has written is there for all of it.
+__device__ __forceinline__ void written()
+{
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
+// Too few blocks for all that is wanted: a block that nobody holds but sequences that are cut within it stays with the lowest of them, which wants no copy then.
+// The blocks' users themselves say who that is: less those sequences none are left, and the lowest sequence leaves the least mark below zero.
+__device__ __forceinline__ void keep_where_all_are_cut(const PagesArgs &a)
+{
+    constexpr int32_t MARKS = 65536;        // (sequences number below)
+    for (int32_t b = threadIdx.x; b < a.batch; b += kThreads)
+        if (a.own[b] >= 0) count_users(a.users + a.own[b], -1);
+    written();
+    for (int32_t b = threadIdx.x; b < a.batch; b += kThreads)
+        if (a.own[b] >= 0 && load_shared(a.users + a.own[b]) <= 0) __hip_atomic_fetch_min(a.users + a.own[b], b - MARKS, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    written();
+    // (a keeper's block is -2 - own until the counts are as they were)
+    for (int32_t b = threadIdx.x; b < a.batch; b += kThreads)
+        if (a.own[b] >= 0 && load_shared(a.users + a.own[b]) == b - MARKS) {
+            a.own[b] = -2 - a.own[b];
+            store_shared(a.wanted + b, load_shared(a.wanted + b) - 1);
+        }
+    written();
+    for (int32_t b = threadIdx.x; b < a.batch; b += kThreads) {
+        const int32_t own = a.own[b];
+        if (own >= 0) count_users(a.users + own, 1);
+        if (own < -1) {
+            count_users(a.users + (-2 - own), 1 + MARKS - b);
+            a.own[b] = -1;
+        }
+    }
+    written();
 }
 
 __global__ __launch_bounds__(kThreads) void k_resize(PagesArgs a)
@@ -177,7 +216,16 @@ __global__ __launch_bounds__(kThreads) void k_resize(PagesArgs a)
         if (source >= 0) store_shared(a.wanted + b, load_shared(a.wanted + b) + 1);
     }
     __syncthreads();
-    deal(a, lds);
+    int32_t total = order_wanted(a, lds);
+    int32_t found = total ? find_free(a, total, lds) : 0;
+    if (found < total) {
+        written();
+        keep_where_all_are_cut(a);
+        total = order_wanted(a, lds);
+        for (int32_t i = total + (int32_t)threadIdx.x; i < found; i += kThreads) a.users[a.given[i]] = 0;      // (more than are wanted now)
+        found = min(found, total);
+    }
+    dealt(a, total, found);
 }
 
 __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a)
@@ -227,7 +275,8 @@ __global__ __launch_bounds__(kThreads) void k_fork(PagesArgs a)
     }
     if (!last_workgroup(a, &flag)) return;
 
-    deal(a, lds);
+    const int32_t total = order_wanted(a, lds);
+    dealt(a, total, total ? find_free(a, total, lds) : 0);
 }
 
 // The block that a sequence's last wanted place gets, -1: none.

@@ -53,6 +53,13 @@ class Pages:
                     places.append((b, j, None))
                 elif j == need - 1 and _unfinished(length, width) and shared[e]:
                     places.append((b, j, e))
+        if len(places) > sum(n == 0 for n in self.users):
+            cut = {}
+            for place in places:
+                cut.setdefault(place[2], []).append(place)
+            for e, held in cut.items():
+                if e is not None and len(held) >= self.users[e]:
+                    places.remove(held[0])
         return self._deal(places)
 
     def fork(self, parents):

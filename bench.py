@@ -41,16 +41,20 @@ TRAFFIC_PROFILE = os.path.join(ROOT, "profiles", "k_conv_resnet50_3x3_b16_48pct.
 HBM_PEAK_GBPS = 8000.0
 
 
-def kernel_source_hash():
-    """sha256 (first 16 hex digits) over the sources of the library's kernels but for attention's, of which nothing is
-    run or included by what is timed here, in name order."""
+def kernel_sources():
+    """The sources of the library's kernels in name order, but for those of attention, of the layers around it and of the
+    cache's pages, of which nothing is run or included by what is timed here."""
     import glob
+    base = os.path.join(ROOT, "paper_2207_10741_amd", "csrc")
+    others = ("fc_attn_", "fc_kv_", "fc_linear_", "fc_layers_", "fc_group_norm", "fc_pages")
+    return [f for f in sorted(glob.glob(os.path.join(base, "*.hip")) + glob.glob(os.path.join(base, "*.hpp"))) if not os.path.basename(f).startswith(others)]
+
+
+def kernel_source_hash():
+    """sha256 (first 16 hex digits) over kernel_sources()."""
     import hashlib
     h = hashlib.sha256()
-    base = os.path.join(ROOT, "paper_2207_10741_amd", "csrc")
-    for f in sorted(glob.glob(os.path.join(base, "*.hip")) + glob.glob(os.path.join(base, "*.hpp"))):
-        if os.path.basename(f).startswith(("fc_attn_", "fc_kv_")):
-            continue
+    for f in kernel_sources():
         h.update(os.path.basename(f).encode())
         h.update(open(f, "rb").read())
     return h.hexdigest()[:16]

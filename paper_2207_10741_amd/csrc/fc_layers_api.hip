@@ -29,7 +29,7 @@ int32_t check_linear(const fc_linear_desc *d, bool residual)
 
 // What a cut of the product takes, in microseconds: beginning and ending a launch, its rounds of stages of 64, the weights' bytes where the kernel waits for
 // them, and joining pieces.  From times of every form on 41 products (64 .. 4096 rows, 256 .. 8192 columns of x, 1024 .. 16384 of out), which it gives to within a fifth or
-// so; what it is for is the order of the forms.  Measured there, rows x k x n (rings / shared stages / tiles of 128 / of 256):
+// so; what it is for is the order of the forms.  Measured there, rows x k x n (rings, which have become 0.2 to 0.5 us shorter since / shared stages / tiles of 128 / of 256):
 //   64 x 4096 x 4096 14.7 / 15.0 in four pieces      128 x 1024 x 1024 6.0 / 10.8 / 11.3         256 x 4096 x 4096 30.6 / 23.1 in four / 25.1 in four
 //   512 x 4096 x 4096 59.5 / 30.1 in two / 35.3      1024 x 4096 x 4096 121 / 43.6 / 52.4 / 80.8   2048 x 4096 x 4096 - / - / 71.2 / 82.5
 //   4096 x 4096 x 4096 - / - / 141 / 100             2048 x 8192 x 1024 - / - / 51.6 in four, 87.4 in one / 146
@@ -97,7 +97,7 @@ int32_t plan_linear(const fc_linear_desc *d, LinearPlan *p)
     p->pad_x = p->pad_w = false;
     p->wide = x_pieces && w_pieces;
     p->per_wave = 0;
-    // (half of the rows: 1924 of 4811 rows of 1001 with 515 columns in two pieces)
+    // (half of the rows, as a mask that keeps about half leaves them: 1924 of 4811 rows of 1001 with 515 columns in two pieces, a plan for all of them in one.  It is a guess: the count is the device's)
     const Cut c = best_cut(d->flags & FC_COUNTED ? (rows + 1) / 2 : rows, d->n, d->k, p->wide);
     p->form = c.form;
     p->ring = c.ring;

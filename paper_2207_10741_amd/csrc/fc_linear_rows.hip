@@ -2,8 +2,8 @@
 //
 // Every weight is needed once, so the weights' bytes bound it.  A workgroup has 16 NB columns of the output (rows of w) and 16 RB rows of x; its waves divide the
 // reduction among them, so that a launch of few columns still has all of its loads under way at once, and add their sums through LDS in order.
-//   k_linear_ring   rows of whole 16-byte pieces: both operands come in lines of 128 bytes through a ring in LDS of each wave's own.  1 x 4096 x 4096 9.9 us (33 MB: 6.4 at
-//                   the rate of a copy, and a launch), 1 x 4096 x 16384 30.8 (4.4 TB/s), 64 x 4096 x 16384 36
+//   k_linear_ring   rows of whole 16-byte pieces: both operands come in lines of 128 bytes through a ring in LDS of each wave's own.  Weights that are not in a cache:
+//                   1 x 4096 x 4096 9.5 us (33 MB: 6.4 at the rate of a copy, and a launch), 1 x 4096 x 16384 30.1 (4.5 TB/s), 64 x 4096 x 16384 36.7
 //   k_linear_rows   rows of any alignment: straight from memory to the registers that the matrix instructions read, with no LDS and no barrier between.  Where columns are
 //                   fewer than the chip wants workgroups, workgroups divide the reduction as well (pieces, joined by the last in order)
 //
@@ -18,9 +18,9 @@ constexpr int kRowsWaves = 8, kRowsThreads = kRowsWaves * 64;
 struct RowsTile {
     int tile, split, m, n;
 };
-__device__ __forceinline__ RowsTile rows_tile(const LinearArgs &a)
+template <bool SPLIT> __device__ __forceinline__ RowsTile rows_tile(const LinearArgs &a)
 {
-    const int slot = (int)blockIdx.x >> 3, split = slot % a.splits, pair = slot / a.splits;
+    const int slot = (int)blockIdx.x >> 3, split = SPLIT ? slot % a.splits : 0, pair = SPLIT ? slot / a.splits : slot;
     RowsTile t;
     t.split = split;
     t.m = pair % a.m_tiles;
@@ -46,8 +46,8 @@ template <int DT> __device__ __forceinline__ f32x4_t mfma16_of(const uint4 &a, c
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
 }
 
-// From the waves' sums to the output: added in the waves' order, in pieces' order where workgroups share the reduction.  sums: LDS for all of them.
-template <typename TO, int RB, int NB, int WAVES>
+// From the waves' sums to the output: added in the waves' order, and with SPLIT in pieces' order where workgroups share the reduction.  sums: LDS for all of them.
+template <typename TO, int RB, int NB, int WAVES, bool SPLIT>
 __device__ __forceinline__ void finish_rows(const LinearArgs &a, const f32x4_t (&acc)[RB][NB], f32x4_t *sums, int32_t *flag, int rows, int r0, int n0, int tile, int split)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -64,29 +64,34 @@ __device__ __forceinline__ void finish_rows(const LinearArgs &a, const f32x4_t (
         for (int i = 0; i < 4; ++i)
             if (col + i < a.n) finish_one<TO>(a, row, col + i, v[i]);
     };
-    __amdgpu_buffer_rsrc_t part;
-    if (a.splits > 1)
-        part = __builtin_amdgcn_make_buffer_rsrc(a.part + (int64_t)tile * a.splits * (ITEMS * 4), 0, (uint32_t)a.splits * ITEMS * 16u, 0x00020000);
-    for (int item = threadIdx.x; item < ITEMS; item += (WAVES * 64)) {
+    auto sum_of = [&](int item) __attribute__((always_inline)) {
         f32x4_t v = sums[item];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v += sums[w * ITEMS + item];
-        if (a.splits == 1) finish(item, v);
-        else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), part, (uint32_t)(split * ITEMS + item) * 16u, 0, kPiecesPastCaches);
+        return v;
+    };
+    if (!SPLIT || a.splits == 1) {
+        for (int item = threadIdx.x; item < ITEMS; item += (WAVES * 64)) finish(item, sum_of(item));
+        return;
     }
-    if (a.splits == 1 || !last_piece(a.arrived + tile, a.splits, flag)) return;
-    for (int item = threadIdx.x; item < ITEMS; item += (WAVES * 64)) {
-        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < a.splits; i += 4) {
-            f32x4_t p[4];
+    if constexpr (SPLIT) {
+        const auto part = __builtin_amdgcn_make_buffer_rsrc(a.part + (int64_t)tile * a.splits * (ITEMS * 4), 0, (uint32_t)a.splits * ITEMS * 16u, 0x00020000);
+        for (int item = threadIdx.x; item < ITEMS; item += (WAVES * 64))
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, sum_of(item)), part, (uint32_t)(split * ITEMS + item) * 16u, 0, kPiecesPastCaches);
+        if (!last_piece(a.arrived + tile, a.splits, flag)) return;
+        for (int item = threadIdx.x; item < ITEMS; item += (WAVES * 64)) {
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < a.splits; i += 4) {
+                f32x4_t p[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                p[u] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(part, (uint32_t)(min(i + u, a.splits - 1) * ITEMS + item) * 16u, 0, kPiecesPastCaches));
+                for (int u = 0; u < 4; ++u)
+                    p[u] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(part, (uint32_t)(min(i + u, a.splits - 1) * ITEMS + item) * 16u, 0, kPiecesPastCaches));
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (i + u < a.splits) v += p[u];
+                for (int u = 0; u < 4; ++u)
+                    if (i + u < a.splits) v += p[u];
+            }
+            finish(item, v);
         }
-        finish(item, v);
     }
 }
 
@@ -99,7 +104,7 @@ void k_linear_rows(LinearArgs a)
     f32x4_t *const sums = reinterpret_cast<f32x4_t *>(smem_raw);       // [wave][block][lane]
     __shared__ int32_t flag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowsTile t = rows_tile(a);
+    const RowsTile t = rows_tile<true>(a);
     const int split = t.split, tile = t.tile, n0 = t.n * (16 * NB), r0 = t.m * (16 * RB);
     const int rows = rows_there(a);
     if (t.n >= a.n_tiles || r0 >= rows) return;
@@ -167,7 +172,7 @@ void k_linear_rows(LinearArgs a)
         multiply(0);
     }
 
-    finish_rows<TO, RB, NB, kRowsWaves>(a, acc, sums, &flag, rows, r0, n0, tile, split);
+    finish_rows<TO, RB, NB, kRowsWaves, true>(a, acc, sums, &flag, rows, r0, n0, tile, split);
 }
 
 template <int DT, typename TO, int RB, int NB, int U> static hipError_t launch_rows_of(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
@@ -187,8 +192,9 @@ template <int DT, typename TO> static hipError_t launch_rows_as(const LinearArgs
 }
 
 // Both operands through LDS.  Loads of 16 rows of 64 bytes come at 18 bytes a clock and CU, whole lines of 128 bytes at 64: with some dozens of rows, whose x is
-// as many bytes as the weights that a workgroup reads, the first is slower than memory (64 x 4096 x 16384 straight into registers 44 us, so 36).  A wave has a ring of D chunks of its own and no one to
-// wait for: its loads are D - 1 chunks ahead, and the barrier comes when the sums are added.
+// as many bytes as the weights that a workgroup reads, the first is slower than memory (64 x 4096 x 16384 straight into registers 44 us, so 37).  A wave has a ring of D chunks of its own and no one to
+// wait for: its loads are D - 1 chunks ahead, and the barrier comes when the sums are added.  The reduction is not divided among workgroups: with the arithmetic and the
+// branches for that, which no product wanted, 1 x 1024 x 1024 took 3.86 us and 64 x 1024 x 1024 6.35, so 3.67 and 5.91.
 template <int RB, int NB, int WAVES, int D> constexpr size_t kRingLds = (size_t)WAVES * D * (RB + NB) * 2048;
 
 template <int DT, typename TO, int RB, int NB, int WAVES, int D>
@@ -199,8 +205,8 @@ void k_linear_ring(LinearArgs a)
     constexpr int NL = 2 * (RB + NB);
     extern __shared__ __align__(16) unsigned char smem_raw[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const RowsTile t = rows_tile(a);
-    const int split = t.split, tile = t.tile, n0 = t.n * (16 * NB), r0 = t.m * (16 * RB);
+    const RowsTile t = rows_tile<false>(a);
+    const int n0 = t.n * (16 * NB), r0 = t.m * (16 * RB);
     const int rows = rows_there(a);
     if (t.n >= a.n_tiles || r0 >= rows) return;
     const int here = min(rows - r0, 16 * RB), cols = min(a.n - n0, 16 * NB);
@@ -221,8 +227,7 @@ void k_linear_ring(LinearArgs a)
     }
     // this wave's chunks
     const int chunks = (a.k + kLinearK - 1) / kLinearK;
-    const int from = split * a.per_split + wave * a.per_wave;
-    const int to = min(min(from + a.per_wave, (split + 1) * a.per_split), chunks), k_end = min(to * kLinearK, a.k);
+    const int from = wave * a.per_wave, to = min(from + a.per_wave, chunks), k_end = min(to * kLinearK, a.k);
     unsigned char *const ring = smem_raw + (uint32_t)wave * (D * CHUNK);
     const uint32_t ring0 = (uint32_t)reinterpret_cast<uintptr_t>(smem_raw) + (uint32_t)wave * (D * CHUNK);
     int ld_k = from * kLinearK;
@@ -271,16 +276,16 @@ void k_linear_ring(LinearArgs a)
     lds_reads_done();
     wait_vmcnt<0>();
     __syncthreads();
-    finish_rows<TO, RB, NB, WAVES>(a, acc, reinterpret_cast<f32x4_t *>(smem_raw), reinterpret_cast<int32_t *>(smem_raw + WAVES * RB * NB * 1024), rows, r0, n0, tile, split);
+    finish_rows<TO, RB, NB, WAVES, false>(a, acc, reinterpret_cast<f32x4_t *>(smem_raw), nullptr, rows, r0, n0, 0, 0);
 }
 
 template <int DT, typename TO, int RB, int NB, int WAVES, int D> static hipError_t launch_ring_of(const LinearArgs &a, const LinearPlan &p, hipStream_t s)
 {
     constexpr size_t lds = kRingLds<RB, NB, WAVES, D>;
-    static_assert(lds > (size_t)WAVES * RB * NB * 1024, "room for the sums and a flag");
+    static_assert(lds >= (size_t)WAVES * RB * NB * 1024, "room for the sums");
     const hipError_t e = raise_dynamic_lds<&k_linear_ring<DT, TO, RB, NB, WAVES, D>>(lds);
     if (e != hipSuccess) return e;
-    k_linear_ring<DT, TO, RB, NB, WAVES, D><<<dim3((uint32_t)((p.n_tiles + 7) / 8 * 8 * p.m_tiles * p.splits)), dim3(WAVES * 64), lds, s>>>(a);
+    k_linear_ring<DT, TO, RB, NB, WAVES, D><<<dim3((uint32_t)((p.n_tiles + 7) / 8 * 8 * p.m_tiles)), dim3(WAVES * 64), lds, s>>>(a);
     return hipGetLastError();
 }
 

@@ -49,7 +49,8 @@ enum { FC_ACT_NONE = 0, FC_ACT_RELU = 1, FC_ACT_SILU = 2, FC_ACT_GELU = 3 };
 enum {
     FC_RESIDUAL_FIRST = 128u, /* fc_linear: the residual is added before the activation */
     FC_ANY_POINTERS = 256u,   /* x and w (fc_linear), x and out (fc_group_norm) are aligned to their element only; without it to 16 bytes */
-    FC_COUNTED = 512u         /* fc_linear: the work is laid out for half of the rows, as a count leaves them that a mask makes (results are the same) */
+    FC_COUNTED = 512u         /* fc_linear: the work is laid out for half of the rows, as a count leaves them that a mask makes.  Any count goes with it; the order of sums is
+                                 that of a product of half the rows, so results are those without the flag but for the roundings of 32-bit sums */
 };
 
 enum { FC_LAYERS_MAX_STRIDE = 4194304 };    /* elements between rows, and sizes of rows */
@@ -60,7 +61,7 @@ typedef struct {
     int32_t rows, n, k;                                   /* rows of x and out, columns of out, columns of x and w */
     int32_t dtype, out_dtype;                             /* of x and w; of out and residual */
     int32_t activation;                                   /* FC_ACT_... */
-    uint32_t flags;                                       /* FC_RESIDUAL_FIRST, FC_WORKSPACE_READY */
+    uint32_t flags;                                       /* FC_RESIDUAL_FIRST, FC_ANY_POINTERS, FC_COUNTED, FC_WORKSPACE_READY */
     int32_t reserved;                                     /* zero */
     int64_t x_row, w_row, residual_row, out_row;          /* strides in elements; out_row >= n */
 } fc_linear_desc;
@@ -69,7 +70,7 @@ typedef struct {
     int32_t images, rows, max_rows, channels, groups;     /* max_rows: of an image (without starts rows / images) */
     int32_t dtype;                                        /* of x and out */
     int32_t activation;                                   /* FC_ACT_... */
-    uint32_t flags;                                       /* FC_SKIP_ZERO_FILL, FC_WORKSPACE_READY */
+    uint32_t flags;                                       /* FC_SKIP_ZERO_FILL, FC_ANY_POINTERS, FC_WORKSPACE_READY */
     float eps;                                            /* >= 0, finite */
     int32_t reserved;                                     /* zero */
     int64_t x_row, out_row;                               /* strides in elements; out_row >= channels */

@@ -232,7 +232,8 @@ class _GroupNorm(PreparedGroupNorm):
 def linear(x, w, bias=None, residual=None, activation=None, residual_first=False, count=None, out=None, out_dtype=None, workspace=None,
            stream=None):
     """fc_linear.  x [rows, k], w [n, k], bfloat16 or float16, any stride of rows; bias float32 [n]; residual [rows, n] of out's type;
-    activation None, "relu", "silu" or "gelu"; count int32 [1]: the rows that there are.  Returns out [rows, n] of residual's type, or x's."""
+    activation None, "relu", "silu" or "gelu"; count int32 [1]: the rows that there are, known on the device (the work is laid out for half of
+    them, which changes the order of sums).  Returns out [rows, n] of residual's type, or x's."""
     return _Linear(x, w, bias, residual, activation, residual_first, count, out, out_dtype, workspace, stream)(stream)
 
 

@@ -99,6 +99,18 @@ def _aligned(*tensors):
     return all(t.data_ptr() % 16 == 0 for t in tensors)
 
 
+def _in_order(mask, rows):
+    """Does a mask of this shape go over rows of that shape in their order?  Dimensions of one, and neighbouring dimensions as one, make no difference."""
+    def lengths(shape):
+        found, n = set(), 1
+        for d in reversed(shape):
+            n *= d
+            found.add(n)
+        return found - {1}
+    a, b = lengths(mask), lengths(rows)
+    return a <= b or b <= a
+
+
 def linear_cut(desc):
     """fc_linear_cut_of: how a product (LinearDesc) is cut."""
     cut = LinearCut()
@@ -211,6 +223,8 @@ class PreparedGroupNorm(_PreparedLayer):
         if mask is not None:
             if mask.numel() != rows or not mask.is_cuda or mask.device != device or not mask.is_contiguous() or mask.element_size() != 1:
                 raise ValueError("mask is a byte a row, contiguous, on the same device")
+            if rows and not _in_order(mask.shape, x.shape[:-1]):
+                raise ValueError("mask %s does not go over the rows %s in their order" % (list(mask.shape), list(x.shape[:-1])))
         if not _aligned(x, out):
             desc.flags |= ANY_POINTERS
         self._finish(desc, (x.data_ptr(), B._ptr(weight), B._ptr(bias), B._ptr(mask), B._ptr(starts), out.data_ptr()),

@@ -184,6 +184,19 @@ class PreparedRead(_Prepared):
         self._result = (k, v)
 
 
+def _ready_workspace(need, device, stream, desc):
+    """A workspace of a prepared call's own, cleared here once: the calls leave its counters zero.  One that is made during a capture is not: the clearing would be the
+    graph's, and a call before its first replay would find anything; such calls clear the counters by themselves."""
+    torch = B._torch()
+    with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty((need,), dtype=torch.uint8, device=device)
+        desc.flags |= B.WORKSPACE_READY
+        workspace = torch.zeros((need,), dtype=torch.uint8, device=device)
+        torch.cuda.current_stream(device).synchronize()     # (a call may come on any stream)
+    return workspace
+
+
 class _PreparedAttend(_Prepared):
     def _prepare(self, name, desc, cache, q, table, lengths, starts, scale, out, lse, selected, workspace, stream):
         torch = B._torch()
@@ -208,14 +221,7 @@ class _PreparedAttend(_Prepared):
         self._result = out if selected is None else (out, selected)
 
     def _workspace(self, need, device, stream, desc):
-        """A workspace of the call's own, cleared here once: the calls leave its counters zero."""
-        torch = B._torch()
-        desc.flags |= B.WORKSPACE_READY
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
-            workspace = torch.zeros((need,), dtype=torch.uint8, device=device)
-            if not torch.cuda.is_current_stream_capturing():
-                torch.cuda.current_stream(device).synchronize()     # (a call may come on any stream)
-        return workspace
+        return _ready_workspace(need, device, stream, desc)
 
 
 class PreparedAttention(_PreparedAttend):

@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from .attention import _made
+from .attention import _kept_workspace, _made, _ready_workspace
 from .pages import _OnDevice
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
@@ -126,14 +126,7 @@ class _PreparedLayer(_OnDevice):
         return b.value
 
     def _workspace(self, need, device, stream, desc):
-        """A workspace of the call's own, cleared here once: the calls leave its counters zero."""
-        torch = B._torch()
-        desc.flags |= B.WORKSPACE_READY
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
-            workspace = torch.zeros((need,), dtype=torch.uint8, device=device)
-            if not torch.cuda.is_current_stream_capturing():
-                torch.cuda.current_stream(device).synchronize()     # (a call may come on any stream)
-        return workspace
+        return _ready_workspace(need, device, stream, desc)
 
     def _finish(self, desc, pointers, keep, workspace, device, stream, result):
         need = self._bytes(desc)
@@ -229,10 +222,6 @@ class PreparedGroupNorm(_PreparedLayer):
             desc.flags |= ANY_POINTERS
         self._finish(desc, (x.data_ptr(), B._ptr(weight), B._ptr(bias), B._ptr(mask), B._ptr(starts), out.data_ptr()),
                      (x, weight, bias, mask, starts, out), workspace, device, stream, out)
-
-
-def _kept_workspace(self, need, device, stream, desc):
-    return B._own_workspace(need, device, B._stream(stream), stream)
 
 
 class _Linear(PreparedLinear):

@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from .attention import _Prepared, _made
+from .attention import _Prepared, _kept_workspace, _made, _ready_workspace
 
 FUNCTIONS = ("fc_kv_resize_workspace_bytes", "fc_kv_fork_workspace_bytes", "fc_kv_compact_workspace_bytes", "fc_kv_resize", "fc_kv_fork",
              "fc_kv_compact", "fc_kv_copy")
@@ -108,14 +108,7 @@ class _PreparedPages(_OnDevice):
         self._result = missing
 
     def _workspace(self, need, device, stream, desc):
-        """A workspace of the call's own, cleared here once: the calls leave its counters zero."""
-        torch = B._torch()
-        desc.flags |= B.WORKSPACE_READY
-        with torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(device)):
-            workspace = torch.zeros((need,), dtype=torch.uint8, device=device)
-            if not torch.cuda.is_current_stream_capturing():
-                torch.cuda.current_stream(device).synchronize()     # (a call may come on any stream)
-        return workspace
+        return _ready_workspace(need, device, stream, desc)
 
 
 class PreparedResize(_PreparedPages):
@@ -166,10 +159,6 @@ class PreparedCopy(_OnDevice):
         self._fn = lib().fc_kv_copy
         self._args = (ctypes.byref(desc), cache.data.data_ptr(), sources.data_ptr(), cache_to.data.data_ptr(), targets.data_ptr())
         self._result = cache_to
-
-
-def _kept_workspace(self, need, device, stream, desc):
-    return B._own_workspace(need, device, B._stream(stream), stream)
 
 
 class _Resize(PreparedResize):

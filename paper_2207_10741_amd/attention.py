@@ -184,6 +184,12 @@ class PreparedRead(_Prepared):
         self._result = (k, v)
 
 
+def _check_workspace(workspace, device):
+    B._require_cuda(workspace)
+    if workspace is not None and workspace.device != device:
+        raise ValueError("the workspace must be on the same device")
+
+
 def _ready_workspace(need, device, stream, desc):
     """A workspace of a prepared call's own, cleared here once: the calls leave its counters zero.  One that is made during a capture is not: the clearing would be the
     graph's, and a call before its first replay would find anything; such calls clear the counters by themselves."""
@@ -203,7 +209,8 @@ class _PreparedAttend(_Prepared):
         desc.dtype, desc.heads = _dtype(q), q.shape[1]
         desc.q_row, desc.q_head = _rows(q, cache, None, "q")
         desc.scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else scale
-        B._require_cuda(out, lse, selected, workspace)
+        B._require_cuda(out, lse, selected)
+        _check_workspace(workspace, q.device)
         if out is None:
             out = _made(tuple(q.shape), q.dtype, q.device, stream)
         elif out.shape != q.shape or out.dtype != q.dtype or out.device != q.device:

@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from .attention import _kept_workspace, _made, _ready_workspace
+from .attention import _check_workspace, _kept_workspace, _made, _ready_workspace
 from .pages import _OnDevice
 
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
@@ -130,7 +130,7 @@ class _PreparedLayer(_OnDevice):
 
     def _finish(self, desc, pointers, keep, workspace, device, stream, result):
         need = self._bytes(desc)
-        B._require_cuda(workspace)
+        _check_workspace(workspace, device)
         if workspace is None and need:
             workspace = self._workspace(need, device, stream, desc)
         self._keep, self._device = (desc, workspace) + keep, device.index

@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding as B
-from .attention import _Prepared, _kept_workspace, _made, _ready_workspace
+from .attention import _Prepared, _check_workspace, _kept_workspace, _made, _ready_workspace
 
 FUNCTIONS = ("fc_kv_resize_workspace_bytes", "fc_kv_fork_workspace_bytes", "fc_kv_compact_workspace_bytes", "fc_kv_resize", "fc_kv_fork",
              "fc_kv_compact", "fc_kv_copy")
@@ -99,7 +99,7 @@ class _PreparedPages(_OnDevice):
             missing = _made((1,), torch.int32, cache.device, stream)
         need = ctypes.c_size_t()
         B._check(getattr(lib(), name + "_workspace_bytes")(ctypes.byref(desc), ctypes.byref(need)), name + "_workspace_bytes")
-        B._require_cuda(workspace)
+        _check_workspace(workspace, cache.device)
         if workspace is None:
             workspace = self._workspace(need.value, cache.device, stream, desc)
         self._keep, self._device = (desc, cache.data, missing, workspace) + keep, cache.device.index

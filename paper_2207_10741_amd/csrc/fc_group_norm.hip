@@ -74,7 +74,7 @@ template <typename T, bool WIDE> struct Piece {
         if constexpr (WIDE) return make_uint4(which ? a.x : b.x, which ? a.y : b.y, which ? a.z : b.z, which ? a.w : b.w);
         else return which ? a : b;
     }
-    // (past the caches: x is still in them for the next call's or launch's reads; 268 MB of bf16, statistics 80 -> 67 us, outputs 99 -> 106)
+    // (past the caches: x is still in them for the next call's or launch's reads; 268 MB of bf16, statistics 73 -> 52 us, outputs 100 -> 104; a mask that keeps half of 67 MB 15.6 -> 14.1 and 26.9 -> 25.4)
     static __device__ __forceinline__ void store(raw_t *p, const raw_t &v)
     {
         if constexpr (WIDE) __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_t *>(p));

@@ -207,6 +207,15 @@ __device__ __forceinline__ uint4 row_end(const uint16_t *__restrict__ row, int c
     return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
 }
 
+// The sums of a block of 16 x 16 with the products of 32 more columns of both operands.
+template <int DT> __device__ __forceinline__ f32x4_t mfma16_of(const uint4 &a, const uint4 &b, const f32x4_t &c)
+{
+    if constexpr (DT == FC_BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
 // How a product is cut.
 struct LinearPlan {
     int32_t form;                   // 0: few rows, 2: some dozens, 1: many in tiles of 128, 3: of 256; tile_m, tile_n: rows and columns of a workgroup

@@ -13,14 +13,6 @@
 
 namespace fc {
 
-template <int DT> __device__ __forceinline__ f32x4_t mfma16_of(const uint4 &a, const uint4 &b, const f32x4_t &c)
-{
-    if constexpr (DT == FC_BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-}
-
 __device__ __forceinline__ void aim(uint32_t lds_addr) { __asm__ volatile("s_mov_b32 m0, %0" : : "s"(lds_addr) : "memory"); }
 __device__ __forceinline__ void load_aimed(const u32x4_t &rsrc, uint32_t byte_offset, uint32_t scalar_offset)
 {

@@ -38,14 +38,6 @@ template <bool FULL> __device__ __forceinline__ uint4 row_piece(const uint16_t *
     return v;
 }
 
-template <int DT> __device__ __forceinline__ f32x4_t mfma16_of(const uint4 &a, const uint4 &b, const f32x4_t &c)
-{
-    if constexpr (DT == FC_BF16)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-    else
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
-}
-
 // From the waves' sums to the output: added in the waves' order, and with SPLIT in pieces' order where workgroups share the reduction.  sums: LDS for all of them.
 template <typename TO, int RB, int NB, int WAVES, bool SPLIT>
 __device__ __forceinline__ void finish_rows(const LinearArgs &a, const f32x4_t (&acc)[RB][NB], f32x4_t *sums, int32_t *flag, int rows, int r0, int n0, int tile, int split)

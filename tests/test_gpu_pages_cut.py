@@ -93,7 +93,7 @@ def test_random_cuts_in_small_pools(seed):
         s.resize([min(int(n), rng.randint(1, width * 64)) for n in s.lengths.tolist()])
 
 
-@pytest.mark.parametrize("batch,width,blocks", [(3000, 3, 1100), (5000, 2, 600), (1025, 5, 900)])
+@pytest.mark.parametrize("batch,width,blocks", [(3000, 3, 1100), (5000, 2, 600), (1025, 5, 900), (20000, 2, 1500), (65535, 1, 300)])
 def test_many_sequences(batch, width, blocks):
     """More sequences than threads, blocks that hundreds hold."""
     rng = random.Random(batch)

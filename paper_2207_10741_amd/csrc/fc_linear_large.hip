@@ -7,8 +7,8 @@
 // The reduction goes in stages of 64, rows of x three stages deep in LDS and rows of w two.  Everything that is not a product goes out between two of them, one
 // piece at a time: fragments a k-step ahead, across the stage's border too (its barrier stands inside the last k-step), a stage's loads at even distances from
 // barrier to barrier.  8192 cubed with 32x32x16 instructions: loads in one go behind the barrier, eight waves, 862 us; spread 815; four waves 794.  With 16x16x32
-// instructions 749, and with M0 set a product before its load, so that no gap of 16 clocks holds three instructions, 732 (1.50 PFLOP/s; the library's product on the
-// same values 706): 2315 clocks a stage of which the products take 2048.
+// instructions 749, and with M0 set a product before its load, so that no gap of 16 clocks holds three instructions, 732; with the epilogue of
+// today 715 - 720 (1.53 PFLOP/s; the library's product on the same values 688 - 695): 2315 clocks a stage of which the products take 2048.
 #include "fc_linear_tile.hpp"
 
 namespace fc {

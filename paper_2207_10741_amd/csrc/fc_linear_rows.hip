@@ -3,7 +3,7 @@
 // Every weight is needed once, so the weights' bytes bound it.  A workgroup has 16 NB columns of the output (rows of w) and 16 RB rows of x; its waves divide the
 // reduction among them, so that a launch of few columns still has all of its loads under way at once, and add their sums through LDS in order.
 //   k_linear_ring   rows of whole 16-byte pieces: both operands come in lines of 128 bytes through a ring in LDS of each wave's own.  Weights that are not in a cache:
-//                   1 x 4096 x 4096 9.5 us (33 MB: 6.4 at the rate of a copy, and a launch), 1 x 4096 x 16384 30.1 (4.5 TB/s), 64 x 4096 x 16384 36.7
+//                   1 x 4096 x 4096 9.2 us (33 MB: 6.4 at the rate of a copy, and a launch), 1 x 4096 x 16384 29.4 (4.6 TB/s), 64 x 4096 x 16384 33.8 (with bias and GELU 36.6)
 //   k_linear_rows   rows of any alignment: straight from memory to the registers that the matrix instructions read, with no LDS and no barrier between.  Where columns are
 //                   fewer than the chip wants workgroups, workgroups divide the reduction as well (pieces, joined by the last in order)
 //
@@ -184,7 +184,7 @@ template <int DT, typename TO> static hipError_t launch_rows_as(const LinearArgs
 }
 
 // Both operands through LDS.  Loads of 16 rows of 64 bytes come at 18 bytes a clock and CU, whole lines of 128 bytes at 64: with some dozens of rows, whose x is
-// as many bytes as the weights that a workgroup reads, the first is slower than memory (64 x 4096 x 16384 straight into registers 44 us, so 37).  A wave has a ring of D chunks of its own and no one to
+// as many bytes as the weights that a workgroup reads, the first is slower than memory (64 x 4096 x 16384 straight into registers 44 us, so 36 when both were built).  A wave has a ring of D chunks of its own and no one to
 // wait for: its loads are D - 1 chunks ahead, and the barrier comes when the sums are added.  The reduction is not divided among workgroups: with the arithmetic and the
 // branches for that, which no product wanted, 1 x 1024 x 1024 took 3.86 us and 64 x 1024 x 1024 6.35, so 3.67 and 5.91.
 template <int RB, int NB, int WAVES, int D> constexpr size_t kRingLds = (size_t)WAVES * D * (RB + NB) * 2048;
